@@ -272,6 +272,62 @@ int rnnlm_sort_segments(rnnlm_t *h, const int32_t *x, int32_t T, int32_t *perm, 
 int rnnlm_sort_segments_static(const int32_t *x, int32_t T, int32_t B, int32_t V, int32_t *perm, int32_t *seg_start,
                                int32_t *nseg, int32_t *range_flag, void *stream);
 
+/* ---- Logits -----------------------------------------------------------------------------------------------
+ * Operators on arrays of logits, next to the criteria above: a teacher's list of likely words, the criterion that teaches a
+ * student from such lists, and the verification of words that a small model drafted for a large one.  They need no handle.
+ * A row holds the V logits of one position; rows lie ld elements apart (ld >= V, any alignment of their element type) and
+ * are ordered like a window's positions (row t*B + s).  All rows, lists and outputs are device arrays.  The calls allocate
+ * nothing, run on the CURRENT device, which must be the stream's, keep nothing between calls, and may be captured into a
+ * graph; calls that overlap in time need workspaces of their own.  V <= 2^20; tau in [0.001, 1000]. */
+typedef enum { RNNLM_DTYPE_FP32 = 0, RNNLM_DTYPE_BF16 = 1 } rnnlm_dtype;
+
+/* The K greatest logits of every row in descending order (equal ones: the lower id first) and lse = ln sum_v exp(z[v]/tau)
+ * over the whole row.  -inf marks masked words: they come last, in the order of their ids, and a row of nothing else has
+ * lse = -inf.  A NaN ranks as -inf (and is given as such); lse is then NaN, as it is with +inf.
+ * ids: dev int32[rows][K]; vals: dev float[rows][K]; lse: dev float[rows] or NULL; 1 <= K <= min(V, 256); workspace: dev,
+ * 256-byte aligned, at least rnnlm_top_logits_workspace_bytes (0: sizes out of range), larger ones are fine. */
+size_t rnnlm_top_logits_workspace_bytes(int64_t rows, int32_t V, int32_t K, int32_t dtype);
+int rnnlm_top_logits(const void *logits, int32_t dtype, int64_t rows, int32_t V, int64_t ld, int32_t K, float tau,
+                     int32_t *ids, float *vals, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Distillation: loss of a student's rows against a teacher's lists (rnnlm_top_logits of the teacher's rows), and its
+ * gradient.  With p_k = exp(vals[k]/tau - n), pi = sum_k p_k, q_tau = softmax(z/tau):
+ *     loss = weight * (alpha tau^2 sum_k p_k (ln p_k - ln q_tau(ids[k])) - (1 - alpha) ln q_1(y))
+ *     dlogits[v] = scale * weight * (alpha tau (pi q_tau(v) - sum_{k: ids[k] = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
+ * lse given (the teacher's, at the same tau): n = lse, the list keeps the share pi it has of the teacher's distribution;
+ * lse NULL: n = ln sum_k exp(vals[k]/tau), the list is taken for the whole of it.  A negative id is an absent entry and a
+ * negative y a missing label (their terms are left out); ids and labels >= V count as absent and raise *range_flag.  A word
+ * that a list holds twice has both probabilities.  Positions of weight 0 have loss 0 and a gradient of zeros whatever their
+ * row holds.  scale is the factor of the mean (1 / (B*T) as in rnnlm_train_chunk); the losses are without it.
+ * A student's -inf logit (masked word) has no gradient beyond -p_k; the loss is +inf where the list gives it mass.
+ * ids: dev int32[rows][K], vals: dev float[rows][K], 1 <= K <= 1024; lse: dev float[rows] or NULL; y: dev int32[rows], may be
+ * NULL where alpha = 1; weight: dev float[rows] or NULL (all 1); 0 <= alpha <= 1; loss: dev float[rows]; sum_loss: dev double
+ * or NULL; dlogits: dev, of the logits' type, rows ld_dlogits apart, or NULL (loss only); it may be the logits themselves
+ * (same ld), else the two must not overlap; range_flag: dev int32 or NULL: set to 1 by such ids, never cleared. */
+int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t V, int64_t ld, const int32_t *ids,
+                       const float *vals, int32_t K, const float *lse, const int32_t *y, const float *weight, float tau,
+                       float alpha, float scale, float *loss, double *sum_loss, void *dlogits, int64_t ld_dlogits,
+                       int32_t *range_flag, void *stream);
+
+/* Verification of drafted words: for each of B texts, K words that a draft model proposed one after the other are checked
+ * against the target model's distributions, from given random numbers, so that the words that come out are distributed as if
+ * the target had drawn them all.  p_i = softmax(target row i / tau), q_i = softmax(draft row i / tau_draft):
+ * draft i is accepted iff u[i] q_i(d_i) < p_i(d_i); at the first that is not, n, a word is drawn from max(p_n - q_n, 0);
+ * where all of a text's drafts are accepted, from the row behind them.  draft NULL: drafts without probabilities (q_i has
+ * all its mass on d_i).  The drawn word is the first v whose sum of weights over words <= v exceeds u[K] times the whole
+ * sum (in 64 bits); weights that are all zero: p_n itself.  -inf marks masked words.  A row with no probability (all masked,
+ * a NaN or +inf) accepts no draft and draws the word -1.  Drafts outside [0, V) are rejected and raise *range_flag.
+ * K = 0 (draft and drafts NULL) draws one word of each row.
+ * target: dev [K+1][B] rows, draft: dev [K][B] rows, both of dtype; drafts: dev int32[K][B]; lengths: dev int32[B], a text's
+ * own number of drafts (clamped to [0, K]; rows behind it are not read), or NULL: K; u: dev float[K+1][B], in [0, 1);
+ * accepted: dev int32[B] = n; tokens: dev int32[K+1][B]: the n accepted drafts, the drawn word, then -1.
+ * 0 <= K <= 1024, B <= 2^20; workspace as above, rnnlm_verify_workspace_bytes; range_flag as above. */
+size_t rnnlm_verify_workspace_bytes(int32_t K, int32_t B, int32_t V);
+int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft, int64_t ld_draft, int32_t dtype, int32_t K,
+                        int32_t B, int32_t V, const int32_t *drafts, const int32_t *lengths, const float *u, float tau,
+                        float tau_draft, int32_t *accepted, int32_t *tokens, int32_t *range_flag, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
 /* Number of polls, of about 4 us each (or as many shorter ones as take that time), a wait of the persistent
  * recurrent kernels makes before it gives up, raises the flag that rnnlm_check reports as RNNLM_ERR_TIMEOUT and
  * lets the kernel run to its end (default 2^18, about a second).  A wait lasts longer than a step's few

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(HERE, "librnnlm_hip.so")
 
 RNNLM_FP32 = 0
 RNNLM_BF16_FP32MASTER = 1
+RNNLM_DTYPE_FP32, RNNLM_DTYPE_BF16 = 0, 1
 RNNLM_EXCHANGE_AUTO, RNNLM_EXCHANGE_CHIP_WIDE, RNNLM_EXCHANGE_XCD_LOCAL = 0, 1, 2
 
 SYMBOLS = [
@@ -26,7 +27,10 @@ SYMBOLS = [
     "rnnlm_train_chunk_rmsprop", "rnnlm_nce_train_chunk_rmsprop",
     "rnnlm_grad_chunk_compressed", "rnnlm_quantize_weights", "rnnlm_forward_score_shortlist",
     "rnnlm_set_recurrent_exchange", "rnnlm_sort_segments_static",
+    "rnnlm_top_logits_workspace_bytes", "rnnlm_top_logits", "rnnlm_distill_loss", "rnnlm_verify_workspace_bytes",
+    "rnnlm_verify_drafts",
 ]
+SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes"]  # return bytes
 
 STAGES = ["prep", "rnn_fwd", "out_fwd", "stats", "softmax_grad", "out_bwd_h", "rnn_bwd", "out_bwd_w", "rec_w", "emb", "reduce",
           "nce_score", "nce_grad", "nce_bwd_h", "nce_bwd_w", "nce_update", "rmsprop", "proj"]
@@ -71,7 +75,6 @@ def load():
                           "(there is no fallback path)")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
-    lib.rnnlm_workspace_bytes.restype = C.c_size_t
     lib.rnnlm_workspace_bytes.argtypes = [C.POINTER(rnnlm_config)]
     lib.rnnlm_init.argtypes = [C.POINTER(rnnlm_config), C.POINTER(rnnlm_buffers), C.POINTER(vp)]
     lib.rnnlm_free.argtypes = [vp]
@@ -99,12 +102,19 @@ def load():
     lib.rnnlm_forward_score_shortlist.argtypes = [vp, vp, vp, i32, i32, f32, vp, vp]
     lib.rnnlm_grad_chunk_compressed.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
     lib.rnnlm_quantize_weights.argtypes = [vp, C.POINTER(rnnlm_quantized), vp]
+    lib.rnnlm_top_logits_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.rnnlm_top_logits.argtypes = [vp, i32, i64, i32, i64, i32, f32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.rnnlm_distill_loss.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, vp]
+    lib.rnnlm_verify_workspace_bytes.argtypes = [i32, i32, i32]
+    lib.rnnlm_verify_drafts.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, f32, f32, vp, vp, vp, vp, C.c_size_t, vp]
+    for name in SIZES:
+        getattr(lib, name).restype = C.c_size_t
     lib.rnnlm_profile_enable.argtypes = [vp, C.c_uint32]
     lib.rnnlm_profile_read.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(i64)]
     lib.rnnlm_status_string.argtypes = [C.c_int]
     lib.rnnlm_status_string.restype = C.c_char_p
     for name in SYMBOLS:
-        if name not in ("rnnlm_workspace_bytes", "rnnlm_free", "rnnlm_status_string"):
+        if name not in SIZES + ["rnnlm_free", "rnnlm_status_string"]:
             getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib
@@ -138,6 +148,146 @@ def rnnlm_sort_segments_static(x, V: int, perm, seg_start, nseg, range_flag=None
     """The handle-free call: x int32[T][B] and the three outputs are device tensors the caller allocated."""
     _ok(load().rnnlm_sort_segments_static(_ptr(x), x.shape[0], x.shape[1], V, _ptr(perm), _ptr(seg_start), _ptr(nseg),
                                           _ptr(range_flag), _stream(stream)), "rnnlm_sort_segments_static")
+
+
+# -- operators on arrays of logits: device tensors, no handle ------------------------------------------------
+def _need(ok, call: str, what: str):
+    if not ok:
+        raise RnnlmError(-1, f"{call}: {what}")
+
+
+def _rows(call, name, t, device=None, dtype=None):
+    """(rows, V, elements from row to row, dtype) of a tensor [..., V] whose rows are evenly spaced and dense in V."""
+    import torch
+    _need(t.dim() >= 2 and t.shape[-1] >= 1 and t.is_cuda, call, f"{name}: rows of logits on a GPU are wanted")
+    _need(t.dtype in (torch.float32, torch.bfloat16), call, f"{name}: float32 or bfloat16 is wanted")
+    _need(device is None or t.device == device, call, f"{name}: on another device")
+    _need(dtype is None or t.dtype == dtype, call, f"{name}: of another type")
+    V, rows, ld = t.shape[-1], 1, None
+    _need(V == 1 or t.stride(-1) == 1, call, f"{name}: a row's elements have to be neighbours")
+    for n, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n != 1:
+            ld = step if ld is None else ld
+            _need(step == ld * rows, call, f"{name}: rows have to be evenly spaced")
+        rows *= n
+    ld = V if ld is None else ld
+    _need(ld >= V or rows == 0, call, f"{name}: rows overlap")
+    return rows, V, max(ld, V), RNNLM_DTYPE_FP32 if t.dtype == torch.float32 else RNNLM_DTYPE_BF16
+
+
+def _dense(call, name, t, dtype, shape, device):
+    """A contiguous tensor of that many elements (its last dimension as given), or None."""
+    if t is None:
+        return
+    n = 1
+    for s in shape:
+        n *= s
+    _need(t.dtype == dtype and t.device == device and t.is_contiguous() and t.numel() == n and
+          (len(shape) < 2 or t.shape[-1] == shape[-1]), call, f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is wanted")
+
+
+def _scratch(call, t, nbytes, device):
+    import torch
+    if t is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _need(t.device == device and t.is_contiguous(), call, "workspace: a contiguous tensor on the logits' device is wanted")
+    return t
+
+
+def _on(device, stream):
+    """(guard that makes the device current, the stream)"""
+    import torch
+    return torch.cuda.device(device), C.c_void_p((torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+
+
+def rnnlm_top_logits_workspace_bytes(rows: int, V: int, K: int, dtype: int) -> int:
+    return int(load().rnnlm_top_logits_workspace_bytes(rows, V, K, dtype))
+
+
+def rnnlm_top_logits(logits, K: int, tau: float = 1.0, ids=None, vals=None, lse=None, workspace=None, stream=None):
+    """logits: float32 or bfloat16 [..., V], rows evenly spaced.  Returns (ids int32 [..., K], vals float32 [..., K],
+    lse float32 [...]); tensors given for them, and a workspace, are used."""
+    import torch
+    call = "rnnlm_top_logits"
+    rows, V, ld, dt = _rows(call, "logits", logits)
+    dev, lead = logits.device, logits.shape[:-1]
+    nbytes = rnnlm_top_logits_workspace_bytes(rows, V, K, dt)
+    _need(nbytes > 0, call, f"K = {K} of V = {V}, {rows} rows")
+    ids = torch.empty(*lead, K, dtype=torch.int32, device=dev) if ids is None else ids
+    vals = torch.empty(*lead, K, dtype=torch.float32, device=dev) if vals is None else vals
+    lse = torch.empty(lead, dtype=torch.float32, device=dev) if lse is None else lse
+    _dense(call, "ids", ids, torch.int32, (rows, K), dev)
+    _dense(call, "vals", vals, torch.float32, (rows, K), dev)
+    _dense(call, "lse", lse, torch.float32, (rows,), dev)
+    workspace = _scratch(call, workspace, nbytes, dev)
+    guard, st = _on(dev, stream)
+    with guard:
+        _ok(load().rnnlm_top_logits(_ptr(logits), dt, rows, V, ld, K, tau, _ptr(ids), _ptr(vals), _ptr(lse), _ptr(workspace),
+                                    workspace.nbytes, st), call)
+    return ids, vals, lse
+
+
+def rnnlm_distill_loss(logits, ids, vals, lse=None, y=None, weight=None, tau: float = 1.0, alpha: float = 1.0,
+                       scale: float = 1.0, loss=None, dlogits=None, sum_loss=None, range_flag=None, stream=None):
+    """logits: float32 or bfloat16 [..., V]; ids, vals [..., K]: the teacher's lists; lse [...]: the teacher's, or None.
+    Returns loss float32 [...].  dlogits (a tensor like logits, or logits itself) receives the gradient; sum_loss float64 [1]."""
+    import torch
+    call = "rnnlm_distill_loss"
+    rows, V, ld, dt = _rows(call, "logits", logits)
+    dev, K = logits.device, ids.shape[-1]
+    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev) if loss is None else loss
+    for name, t, dtype, shape in (("ids", ids, torch.int32, (rows, K)), ("vals", vals, torch.float32, (rows, K)),
+                                  ("lse", lse, torch.float32, (rows,)), ("y", y, torch.int32, (rows,)),
+                                  ("weight", weight, torch.float32, (rows,)), ("loss", loss, torch.float32, (rows,)),
+                                  ("sum_loss", sum_loss, torch.float64, (1,)), ("range_flag", range_flag, torch.int32, (1,))):
+        _dense(call, name, t, dtype, shape, dev)
+    ldd = 0
+    if dlogits is not None:
+        _need(dlogits.shape == logits.shape, call, "dlogits: the logits' shape is wanted")
+        ldd = _rows(call, "dlogits", dlogits, dev, logits.dtype)[2]
+        if dlogits.data_ptr() == logits.data_ptr():  # in place (one row has no distance to the next)
+            ldd = ld if rows <= 1 else ldd
+    guard, st = _on(dev, stream)
+    with guard:
+        _ok(load().rnnlm_distill_loss(_ptr(logits), dt, rows, V, ld, _ptr(ids), _ptr(vals), K, _ptr(lse), _ptr(y), _ptr(weight),
+                                      tau, alpha, scale, _ptr(loss), _ptr(sum_loss), _ptr(dlogits), ldd, _ptr(range_flag), st),
+            call)
+    return loss
+
+
+def rnnlm_verify_workspace_bytes(K: int, B: int, V: int) -> int:
+    return int(load().rnnlm_verify_workspace_bytes(K, B, V))
+
+
+def rnnlm_verify_drafts(target, drafts, u, draft=None, lengths=None, tau: float = 1.0, tau_draft: float = 1.0, accepted=None,
+                        tokens=None, workspace=None, range_flag=None, stream=None):
+    """target: float32 or bfloat16 [K+1][B][V]; drafts int32 [K][B] (K = 0: None); u float32 [K+1][B]; draft [K][B][V] or None:
+    drafts without probabilities; lengths int32 [B] or None.  Returns (accepted int32 [B], tokens int32 [K+1][B])."""
+    import torch
+    call = "rnnlm_verify_drafts"
+    _need(target.dim() == 3, call, "target: [K+1][B][V] is wanted")
+    rows, V, ld, dt = _rows(call, "target", target)
+    K, B, dev = target.shape[0] - 1, target.shape[1], target.device
+    nbytes = rnnlm_verify_workspace_bytes(K, B, V)
+    _need(nbytes > 0, call, f"K = {K}, B = {B}, V = {V}")
+    ldd = 0
+    if draft is not None and K > 0:
+        _need(tuple(draft.shape) == (K, B, V), call, f"draft: [{K}][{B}][{V}] is wanted")
+        ldd = _rows(call, "draft", draft, dev, target.dtype)[2]
+    _need(drafts is not None or K == 0, call, "drafts are wanted")
+    accepted = torch.empty(B, dtype=torch.int32, device=dev) if accepted is None else accepted
+    tokens = torch.empty(K + 1, B, dtype=torch.int32, device=dev) if tokens is None else tokens
+    for name, t, dtype, shape in (("drafts", drafts, torch.int32, (K, B)), ("u", u, torch.float32, (K + 1, B)),
+                                  ("lengths", lengths, torch.int32, (B,)), ("accepted", accepted, torch.int32, (B,)),
+                                  ("tokens", tokens, torch.int32, (K + 1, B)), ("range_flag", range_flag, torch.int32, (1,))):
+        _dense(call, name, t, dtype, shape, dev)
+    workspace = _scratch(call, workspace, nbytes, dev)
+    guard, st = _on(dev, stream)
+    with guard:
+        _ok(load().rnnlm_verify_drafts(_ptr(target), ld, _ptr(draft) if K > 0 else None, ldd, dt, K, B, V, _ptr(drafts),
+                                       _ptr(lengths), _ptr(u), tau, tau_draft, _ptr(accepted), _ptr(tokens), _ptr(range_flag),
+                                       _ptr(workspace), workspace.nbytes, st), call)
+    return accepted, tokens
 
 
 class Rnnlm:

@@ -1,0 +1,287 @@
+// Host side of the operators on arrays of logits (include/rnnlm.h, "Logits"): checks of arguments, choice of kernel, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/rnnlm.h"
+#include "distill.h"
+#include "top_logits.h"
+#include "verify.h"
+
+using namespace rnnlm_dev;
+
+namespace {
+
+#define LAUNCHED()                                             \
+  do {                                                         \
+    if (hipGetLastError() != hipSuccess) return RNNLM_ERR_HIP; \
+  } while (0)
+
+constexpr int64_t GRID_MAX = (int64_t(1) << 31) - 1;
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+size_t elem_bytes(int32_t dtype) { return dtype == RNNLM_DTYPE_FP32 ? 4 : 2; }
+// 16-byte slots of a row, the last of them possibly not whole
+int slots_of(int32_t V, int32_t dtype) { return (int)(((int64_t)V * (int64_t)elem_bytes(dtype) + 15) / 16); }
+bool tau_ok(float tau) { return std::isfinite(tau) && tau >= 1e-3f && tau <= 1e3f; }
+
+// rows of V elements, ld apart: addresses stay within what 64 bits and the kernels' 32-bit element counts reach
+bool rows_ok(const void *p, int32_t dtype, int64_t rows, int32_t V, int64_t ld) {
+  if ((!p && rows != 0) || (dtype != RNNLM_DTYPE_FP32 && dtype != RNNLM_DTYPE_BF16) || !aligned(p, elem_bytes(dtype))) return false;
+  return rows >= 0 && V >= 1 && V <= TOP_V_MAX && ld >= V && ld <= (int64_t(1) << 40) && rows <= GRID_MAX &&
+         (rows == 0 || ld <= (int64_t(1) << 60) / rows);
+}
+
+struct Span {
+  uintptr_t at, end;
+};
+Span span(const void *p, size_t bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  return {a, p ? a + bytes : a};
+}
+bool meet(Span a, Span b) { return a.at < b.end && b.at < a.end; }
+
+// ---- top logits ----
+struct TopPlan {
+  int chunks, per, nv;
+};
+constexpr int TOP_NV_MAX = 16;
+// One chunk a row as long as it fits the registers and the rows alone fill the chip, else shorter ones.
+TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
+  const int slots = slots_of(V, dtype);
+  int nv = TOP_NV_MAX;
+  auto chunks = [&](int n) { return (slots + n * TOP_THREADS - 1) / (n * TOP_THREADS); };
+  while (nv > 2 && rows * chunks(nv) < 512 && chunks(nv / 2) * K <= TOP_MERGE_LDS) nv /= 2;
+  TopPlan p;
+  p.chunks = chunks(nv);
+  p.per = (slots + p.chunks - 1) / p.chunks;
+  p.chunks = (slots + p.per - 1) / p.per;
+  p.nv = nv;
+  return p;
+}
+size_t top_bytes(const TopPlan &p, int64_t rows, int32_t K) {
+  if (p.chunks == 1) return 0;
+  return align256((size_t)rows * p.chunks * K * 8) + align256((size_t)rows * p.chunks * 8);
+}
+bool top_sizes_ok(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
+  return rows >= 0 && rows <= GRID_MAX / 1024 && V >= 1 && V <= TOP_V_MAX && K >= 1 && K <= std::min(V, TOP_K_MAX) &&
+         (dtype == RNNLM_DTYPE_FP32 || dtype == RNNLM_DTYPE_BF16);
+}
+template <typename T>
+void launch_top(const TopArgs &a, int64_t rows, int nv, hipStream_t st) {
+  const dim3 grid((unsigned)(rows * a.chunks)), threads(TOP_THREADS);
+  if (nv == 2) hipLaunchKernelGGL((top_chunk_kernel<T, 2>), grid, threads, 0, st, a);
+  else if (nv == 4) hipLaunchKernelGGL((top_chunk_kernel<T, 4>), grid, threads, 0, st, a);
+  else if (nv == 8) hipLaunchKernelGGL((top_chunk_kernel<T, 8>), grid, threads, 0, st, a);
+  else hipLaunchKernelGGL((top_chunk_kernel<T, 16>), grid, threads, 0, st, a);
+}
+
+// ---- distillation ----
+template <typename T, int THREADS, int NV, bool TWO>
+void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
+  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, TWO>), dim3((unsigned)rows), dim3(THREADS),
+                     (a.K + 1) * sizeof(DistillEntry), st, a);
+}
+template <typename T, bool TWO>
+void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
+  const int slots = (a.V + SlotOf<T>::N - 1) / SlotOf<T>::N;
+  if (!a.dz || slots > 1024 * 26) {
+    hipLaunchKernelGGL((distill_stream_kernel<T, 512, TWO>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
+                       st, a);
+  } else if (slots <= 256) {
+    launch_distill_row<T, 256, 1, TWO>(a, rows, st);
+  } else if (slots <= 256 * 4) {
+    launch_distill_row<T, 256, 4, TWO>(a, rows, st);
+  } else if (slots <= 256 * 8) {
+    launch_distill_row<T, 256, 8, TWO>(a, rows, st);
+  } else if (slots <= 512 * 8) {
+    launch_distill_row<T, 512, 8, TWO>(a, rows, st);
+  } else if (slots <= 512 * 16) {
+    launch_distill_row<T, 512, 16, TWO>(a, rows, st);
+  } else if (slots <= 512 * 26) {
+    launch_distill_row<T, 512, 26, TWO>(a, rows, st);
+  } else {
+    launch_distill_row<T, 1024, 26, TWO>(a, rows, st);
+  }
+}
+template <typename T>
+int distill_call(DistillArgs<T> a, int64_t rows, hipStream_t st) {
+  if (a.y && a.alpha < 1.0f && a.tau != 1.0f) launch_distill<T, true>(a, rows, st);
+  else launch_distill<T, false>(a, rows, st);
+  LAUNCHED();
+  return RNNLM_OK;
+}
+
+// ---- verification ----
+struct VerifyPlan {
+  int parts, per;
+  size_t stat, sums, rest, seq, total;
+};
+VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
+  VerifyPlan p;
+  const int slots = slots_of(V, RNNLM_DTYPE_BF16);  // (fp32 rows have twice as many: parts of twice the slots)
+  const int64_t rows = (int64_t)(2 * K + 1) * B;
+  int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, std::min<int64_t>(rows, 2048)));
+  want = std::max<int64_t>(want, std::max<int64_t>(1, 1024 / B));
+  p.parts = (int)std::min<int64_t>({want, VERIFY_PARTS, (slots + VERIFY_THREADS - 1) / VERIFY_THREADS});
+  size_t o = 0;
+  auto take = [&](size_t n) {
+    const size_t at = o;
+    o = align256(o + n);
+    return at;
+  };
+  p.stat = take((size_t)rows * p.parts * 8);
+  p.sums = take((size_t)B * p.parts * 16);
+  p.rest = take((size_t)B * p.parts * 8);
+  p.seq = take((size_t)B * sizeof(VerifySeq));
+  p.total = o;
+  return p;
+}
+bool verify_sizes_ok(int32_t K, int32_t B, int32_t V) {
+  return K >= 0 && K <= 1024 && B >= 1 && B <= (1 << 20) && V >= 1 && V <= TOP_V_MAX &&
+         (int64_t)(2 * K + 1) * B <= GRID_MAX / VERIFY_PARTS;
+}
+template <typename T>
+int verify_call(const VerifyArgs &a, hipStream_t st) {
+  const dim3 threads(VERIFY_THREADS);
+  const int64_t rows = (int64_t)(a.draft ? 2 * a.K + 1 : a.K + 1) * a.B;
+  hipLaunchKernelGGL(verify_stats_kernel<T>, dim3((unsigned)(rows * a.parts)), threads, 0, st, a);
+  hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.parts)), threads, 0, st, a);
+  hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.parts)), threads, 0, st, a);
+  hipLaunchKernelGGL(verify_draw_kernel<T>, dim3((unsigned)a.B), threads, 0, st, a);
+  LAUNCHED();
+  return RNNLM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t rnnlm_top_logits_workspace_bytes(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
+  return top_sizes_ok(rows, V, K, dtype) ? std::max<size_t>(256, top_bytes(top_plan(rows, V, K, dtype), rows, K)) : 0;
+}
+
+int rnnlm_top_logits(const void *logits, int32_t dtype, int64_t rows, int32_t V, int64_t ld, int32_t K, float tau,
+                     int32_t *ids, float *vals, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!top_sizes_ok(rows, V, K, dtype) || !rows_ok(logits, dtype, rows, V, ld) || !tau_ok(tau) || (rows > 0 && (!ids || !vals)))
+    return RNNLM_ERR_ARG;
+  if (!aligned(ids, 4) || !aligned(vals, 4) || !aligned(lse, 4)) return RNNLM_ERR_ARG;
+  const TopPlan p = top_plan(rows, V, K, dtype);
+  const size_t need = top_bytes(p, rows, K);
+  if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return RNNLM_ERR_ARG;
+  if (rows == 0) return RNNLM_OK;
+  TopArgs a = {};
+  a.z = logits;
+  a.ld = ld;
+  a.V = V;
+  a.K = K;
+  a.chunks = p.chunks;
+  a.per = p.per;
+  a.tau = tau;
+  a.ids = ids;
+  a.vals = vals;
+  a.lse = lse;
+  if (need) {
+    a.part = static_cast<unsigned long long *>(workspace);
+    a.stat = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + align256((size_t)rows * p.chunks * K * 8));
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if (dtype == RNNLM_DTYPE_FP32) launch_top<float>(a, rows, p.nv, st);
+  else launch_top<bf16_t>(a, rows, p.nv, st);
+  LAUNCHED();
+  if (p.chunks > 1) {
+    hipLaunchKernelGGL(top_merge_kernel, dim3((unsigned)rows), dim3(TOP_THREADS), 0, st, a);
+    LAUNCHED();
+  }
+  return RNNLM_OK;
+}
+
+int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t V, int64_t ld, const int32_t *ids,
+                       const float *vals, int32_t K, const float *lse, const int32_t *y, const float *weight, float tau,
+                       float alpha, float scale, float *loss, double *sum_loss, void *dlogits, int64_t ld_dlogits,
+                       int32_t *range_flag, void *stream) {
+  if (!rows_ok(logits, dtype, rows, V, ld) || (rows > 0 && (!ids || !vals || !loss || (alpha < 1.0f && !y))) || K < 1 || K > 1024 || !tau_ok(tau) ||
+      !(alpha >= 0.0f && alpha <= 1.0f) || !std::isfinite(scale))
+    return RNNLM_ERR_ARG;
+  if (!aligned(ids, 4) || !aligned(vals, 4) || !aligned(lse, 4) || !aligned(y, 4) || !aligned(weight, 4) ||
+      !aligned(loss, 4) || !aligned(sum_loss, 8) || !aligned(range_flag, 4))
+    return RNNLM_ERR_ARG;
+  const size_t es = elem_bytes(dtype);
+  if (dlogits) {
+    if (!rows_ok(dlogits, dtype, rows, V, ld_dlogits)) return RNNLM_ERR_ARG;
+    // in place row by row, or apart
+    if (dlogits == logits ? ld != ld_dlogits
+                          : rows > 0 && meet(span(logits, ((size_t)(rows - 1) * ld + V) * es),
+                                             span(dlogits, ((size_t)(rows - 1) * ld_dlogits + V) * es)))
+      return RNNLM_ERR_ARG;
+  }
+  hipStream_t st = (hipStream_t)stream;
+  if (rows > 0) {
+    int rc;
+    if (dtype == RNNLM_DTYPE_FP32) {
+      rc = distill_call(DistillArgs<float>{static_cast<const float *>(logits), ld, static_cast<float *>(dlogits), ld_dlogits, ids, y,
+                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K},
+                        rows, st);
+    } else {
+      rc = distill_call(DistillArgs<bf16_t>{static_cast<const bf16_t *>(logits), ld, static_cast<bf16_t *>(dlogits), ld_dlogits,
+                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K},
+                        rows, st);
+    }
+    if (rc) return rc;
+  }
+  if (sum_loss) {
+    hipLaunchKernelGGL(sum_losses_kernel, dim3(1), dim3(1024), 0, st, loss, (long)rows, sum_loss);
+    LAUNCHED();
+  }
+  return RNNLM_OK;
+}
+
+size_t rnnlm_verify_workspace_bytes(int32_t K, int32_t B, int32_t V) {
+  return verify_sizes_ok(K, B, V) ? verify_plan(K, B, V).total : 0;
+}
+
+int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft, int64_t ld_draft, int32_t dtype, int32_t K,
+                        int32_t B, int32_t V, const int32_t *drafts, const int32_t *lengths, const float *u, float tau,
+                        float tau_draft, int32_t *accepted, int32_t *tokens, int32_t *range_flag, void *workspace,
+                        size_t workspace_bytes, void *stream) {
+  if (!verify_sizes_ok(K, B, V) || !rows_ok(target, dtype, (int64_t)(K + 1) * B, V, ld_target) || !u || !accepted || !tokens ||
+      (K > 0 && !drafts) || !tau_ok(tau) || !tau_ok(tau_draft))
+    return RNNLM_ERR_ARG;
+  if (K == 0) draft = nullptr;
+  if (draft && !rows_ok(draft, dtype, (int64_t)K * B, V, ld_draft)) return RNNLM_ERR_ARG;
+  if (!aligned(drafts, 4) || !aligned(lengths, 4) || !aligned(u, 4) || !aligned(accepted, 4) || !aligned(tokens, 4) ||
+      !aligned(range_flag, 4))
+    return RNNLM_ERR_ARG;
+  const VerifyPlan p = verify_plan(K, B, V);
+  if (!workspace || !aligned(workspace, 256) || workspace_bytes < p.total) return RNNLM_ERR_ARG;
+  char *ws = static_cast<char *>(workspace);
+  VerifyArgs a = {};
+  a.target = target;
+  a.draft = draft;
+  a.ldt = ld_target;
+  a.ldd = ld_draft;
+  a.drafts = drafts;
+  a.lengths = lengths;
+  a.u = u;
+  a.V = V;
+  a.B = B;
+  a.K = K;
+  a.parts = p.parts;
+  a.per = (slots_of(V, dtype) + p.parts - 1) / p.parts;
+  a.tau = tau;
+  a.tau_d = tau_draft;
+  a.accepted = accepted;
+  a.tokens = tokens;
+  a.range_flag = range_flag;
+  a.stat = reinterpret_cast<float2 *>(ws + p.stat);
+  a.sums = reinterpret_cast<double *>(ws + p.sums);
+  a.rest = reinterpret_cast<double *>(ws + p.rest);
+  a.seq = reinterpret_cast<VerifySeq *>(ws + p.seq);
+  hipStream_t st = (hipStream_t)stream;
+  return dtype == RNNLM_DTYPE_FP32 ? verify_call<float>(a, st) : verify_call<bf16_t>(a, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,120 @@
+// Rows of logits as the operators on arrays of logits read them (logit_ops.hip): 16-byte slots of a row that may start at
+// any element, and reductions over a workgroup.
+#pragma once
+#include "common.h"
+
+namespace rnnlm_dev {
+
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr double LOG2E_64 = 1.44269504088896340736, LN2_64 = 0.693147180559945309417;
+
+// A row starts where the one before ends, at any element: its slots are read and written at the elements' alignment.
+typedef u32x4_t slot_t;
+typedef u32x4_t slot_bf16_t __attribute__((aligned(2)));
+typedef u32x4_t slot_fp32_t __attribute__((aligned(4)));
+template <typename T>
+struct SlotOf;
+template <>
+struct SlotOf<float> {
+  typedef slot_fp32_t type;
+  static constexpr int N = 4;
+};
+template <>
+struct SlotOf<bf16_t> {
+  typedef slot_bf16_t type;
+  static constexpr int N = 8;
+};
+
+// Element e of a slot.
+template <typename T>
+__device__ inline float slot_elem(const slot_t &s, int e);
+template <>
+__device__ inline float slot_elem<float>(const slot_t &s, int e) {
+  const unsigned w = s[e];
+  return __builtin_bit_cast(float, w);
+}
+template <>
+__device__ inline float slot_elem<bf16_t>(const slot_t &s, int e) {
+  const unsigned w = s[e >> 1];
+  return __builtin_bit_cast(float, e & 1 ? w & 0xffff0000u : w << 16);
+}
+
+template <typename T>
+__device__ inline slot_t empty_slot() {  // -inf in every element
+  const unsigned w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  return slot_t{w, w, w, w};
+}
+
+// Whole slot j of a row.  The elements behind a row's last whole slot are taken one by one (tail_elem).
+template <typename T>
+__device__ inline slot_t load_slot(const T *row, int j) {
+  return *reinterpret_cast<const typename SlotOf<T>::type *>(row + j * SlotOf<T>::N);
+}
+template <typename T>
+__device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N]) {
+  constexpr int N = SlotOf<T>::N;
+  union {
+    slot_t s;
+    T t[N];
+  } o;
+#pragma unroll
+  for (int e = 0; e < N; ++e) o.t[e] = from_f32<T>(v[e]);
+  *reinterpret_cast<typename SlotOf<T>::type *>(row + j * N) = o.s;
+}
+// Element of the row behind its whole slots that thread tid takes; -inf for the others.
+template <typename T>
+__device__ inline float tail_elem(const T *row, int tid, int V) {
+  const int at = V / SlotOf<T>::N * SlotOf<T>::N + tid;
+  return at < V ? to_f32(row[at]) : -INFINITY;
+}
+// Slot j of a row, whole or not: elements behind the row are -inf.
+template <typename T>
+__device__ inline slot_t load_any_slot(const T *row, int j, int V) {
+  constexpr int N = SlotOf<T>::N;
+  if (j * N + N <= V) return load_slot(row, j);
+  union {
+    slot_t s;
+    T t[N];
+  } o;
+  o.s = empty_slot<T>();
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (j * N + e < V) o.t[e] = row[j * N + e];
+  return o.s;
+}
+// Makes the compiler unpack a slot anew where it is used again: elements of a bf16 slot kept unpacked take twice its
+// registers (a row that fits them spilled 280 of them).
+__device__ inline void keep_packed(slot_t &s) { asm volatile("" : "+v"(s)); }
+
+// The greatest of three numbers (NaNs lose).  (fmaxf of values from memory costs an instruction more for each of them, which
+// makes signalling NaNs quiet: two and a half instructions for two elements instead of one.)
+__device__ inline float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// The greatest of m and the elements of a slot.
+template <typename T>
+__device__ inline float slot_max(float m, const slot_t &s) {
+#pragma unroll
+  for (int e = 0; e < SlotOf<T>::N; e += 2) m = max3(m, slot_elem<T>(s, e), slot_elem<T>(s, e + 1));
+  return m;
+}
+
+__device__ inline float exp2_32(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <typename X, class Op>
+__device__ inline X wave_reduce(X v, Op &&op) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ inline float wave_max(float v) {
+  return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <typename X>
+__device__ inline X wave_sum(X v) {
+  return wave_reduce(v, [](X a, X b) { return a + b; });
+}
+
+}  // namespace rnnlm_dev

@@ -1,0 +1,255 @@
+// The K greatest logits of a row, in descending order (equal ones: the lower id first), and ln sum_v exp(z_v / tau).
+// A row is cut into chunks that fit a workgroup's registers, so it is read once.  A word is ranked by one 64-bit key, the
+// logit's bits in an order that integers have, above the complement of the id: keys differ, so the order is total and a result
+// does not depend on which wave arrives first.  (A NaN ranks with the masked words, -inf; -0 ranks with +0.)
+//   1. maxima of groups of elements (two groups a thread), maximum and sum of exponentials of the chunk
+//   2. a threshold that at least K of the maxima reach, so at least K elements do: bisection over the maxima by one wave
+//   3. elements that reach it into LDS (K to about 1.5 K of them for rows without structure)
+//   4. their ranks among each other by counting
+// Where step 3 finds more than LDS holds, or fewer than K elements are numbers, the exact K-th key is found by bisection over
+// the bits of logit and id with a count of the whole chunk for each: 32 + 20 counts, right for every input.
+#pragma once
+#include "rows.h"
+
+namespace rnnlm_dev {
+
+constexpr int TOP_K_MAX = 256;
+constexpr int TOP_THREADS = 256, TOP_CAP = 1024, TOP_MERGE_LDS = 2048;
+constexpr int TOP_V_MAX = 1 << 20;  // ids fit 20 bits
+constexpr unsigned TOP_MASKED = 0x007fffffu;  // order of -inf
+
+// The order of a logit as an unsigned integer, and back.
+__device__ inline unsigned logit_order(float z) {
+  z = fmaxf(z, -INFINITY) + 0.0f;
+  const unsigned u = __builtin_bit_cast(unsigned, z);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ inline float order_logit(unsigned k) {
+  return __builtin_bit_cast(float, k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ inline unsigned long long top_key(unsigned order, int id) {
+  return (unsigned long long)order << 32 | (unsigned)~id;
+}
+
+struct TopArgs {
+  const void *z;
+  long ld;
+  int V, K, chunks, per;  // per: slots of a chunk
+  float tau;
+  int32_t *ids;
+  float *vals, *lse;
+  unsigned long long *part;  // [row][chunk][K], descending; 0 behind a chunk's last element
+  float2 *stat;              // [row][chunk]: maximum, sum of exponentials at tau relative to it
+};
+
+__device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned long long key) {
+  a.ids[row * a.K + rank] = (int)~(unsigned)key;
+  a.vals[row * a.K + rank] = order_logit((unsigned)(key >> 32));
+}
+
+__device__ inline float row_lse(float m, float s, float tau) {
+  return s == 0.0f ? -INFINITY : (float)((double)m / (double)tau + log((double)s));
+}
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(TOP_THREADS, 4) top_chunk_kernel(const TopArgs a) {
+  constexpr int N = SlotOf<T>::N, WAVES = TOP_THREADS / 64;
+  __shared__ float sh_m[WAVES], sh_s[WAVES];
+  __shared__ unsigned group[2 * TOP_THREADS];
+  __shared__ unsigned long long cand[TOP_CAP];
+  __shared__ unsigned sh_t, sh_n, sh_count[2][WAVES];
+  const long row = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x % a.chunks, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const T *z = static_cast<const T *>(a.z) + row * a.ld;
+  const int full = a.V / N, first = chunk * a.per, slots = min(a.per, full - first), K = a.K;
+  slot_t raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int j = i * TOP_THREADS + tid;
+    raw[i] = j < slots ? load_slot(z, first + j) : empty_slot<T>();
+  }
+  const int tail = chunk == a.chunks - 1 ? full * N + tid : a.V;  // the last chunk has the row's last elements, one a thread
+  const float zt = tail < a.V ? to_f32(z[tail]) : -INFINITY;
+  if (tid == 0) sh_n = 0;
+  // 1.
+  float top[NV], half[2] = {zt, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    top[i] = slot_max<T>(-INFINITY, raw[i]);
+    half[i & 1] = fmaxf(half[i & 1], top[i]);
+    keep_packed(raw[i]);
+  }
+  group[tid] = logit_order(half[0]);
+  group[TOP_THREADS + tid] = logit_order(half[1]);
+  float mx = wave_max(fmaxf(half[0], half[1]));
+  if (lane == 0) sh_m[wave] = mx;
+  __syncthreads();
+  mx = sh_m[0];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) mx = fmaxf(mx, sh_m[i]);
+  // 2.
+  if (wave == 0) {
+    unsigned g[2 * WAVES], low = 0xffffffffu;
+#pragma unroll
+    for (int i = 0; i < 2 * WAVES; ++i) {
+      g[i] = group[i * 64 + lane];
+      low = min(low, g[i]);
+    }
+    low = wave_reduce(low, [](unsigned p, unsigned q) { return min(p, q); });
+    // at least K of the maxima reach lo (0: all of them do), fewer reach hi; a little more than K will do
+    unsigned lo = K <= 2 * TOP_THREADS ? low : 0, hi = logit_order(mx) + 1;
+    while (hi - lo > 1) {
+      const unsigned mid = lo + (hi - lo) / 2;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < 2 * WAVES; ++i) n += __popcll(__ballot(g[i] >= mid));
+      if (n >= K) {
+        lo = mid;
+        if (n <= K + K / 8) break;
+      } else {
+        hi = mid;
+      }
+    }
+    if (lane == 0) sh_t = lo;
+  }
+  const float base = mx == -INFINITY ? 0.0f : mx, c = LOG2E / a.tau, b = -base * c;
+  float s = exp2_32(fmaf(zt, c, b));
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if (i * TOP_THREADS + wave * 64 >= slots) break;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(raw[i], e), c, b));
+    keep_packed(raw[i]);
+  }
+  s = wave_sum(s);
+  if (lane == 0) sh_s[wave] = s;
+  __syncthreads();
+  // 3.
+  const unsigned thr = sh_t;
+  const bool few = thr <= TOP_MASKED;  // some of the K are masked, or no element at all
+  if (!few) {
+    const float t = order_logit(thr);
+    auto take = [&](float v, int id) {
+      if (v >= t) {
+        const unsigned at = atomicAdd(&sh_n, 1u);
+        if (at < TOP_CAP) cand[at] = top_key(logit_order(v), id);
+      }
+    };
+    take(zt, tail);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (top[i] >= t) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) take(slot_elem<T>(raw[i], e), (first + i * TOP_THREADS + tid) * N + e);
+      }
+    __syncthreads();
+  }
+  int n = (int)sh_n;
+  if (few || n > TOP_CAP) {
+    // exact: the order of the K-th element, then the id up to which elements of that order belong
+    int turn = 0;
+    auto each = [&](auto &&element) {
+      if (tail < a.V) element(logit_order(zt), tail);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int j = i * TOP_THREADS + tid;
+        if (j >= slots) break;
+#pragma unroll
+        for (int e = 0; e < N; ++e) element(logit_order(slot_elem<T>(raw[i], e)), (first + j) * N + e);
+        keep_packed(raw[i]);
+      }
+    };
+    auto count = [&](auto &&reaches) {
+      int mine = 0;
+      each([&](unsigned k, int id) { mine += reaches(k, id); });
+      mine = wave_sum(mine);
+      if (lane == 0) sh_count[turn][wave] = mine;
+      __syncthreads();
+      int all = 0;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) all += sh_count[turn][i];
+      turn ^= 1;  // the next count writes the other copy, so nobody waits for this one's readers
+      return all;
+    };
+    unsigned kth = 0;
+    for (unsigned bit = 1u << 31; bit; bit >>= 1)
+      if (count([&](unsigned k, int) { return k >= (kth | bit); }) >= K) kth |= bit;
+    const int above = count([&](unsigned k, int) { return k > kth; });
+    int bound = 0;  // greatest id below which fewer than the missing elements are found
+    for (int bit = TOP_V_MAX >> 1; bit; bit >>= 1)
+      if (count([&](unsigned k, int id) { return k == kth && id < (bound | bit); }) < K - above) bound |= bit;
+    if (tid == 0) sh_n = 0;
+    __syncthreads();
+    each([&](unsigned k, int id) {
+      if (k > kth || (k == kth && id <= bound)) cand[atomicAdd(&sh_n, 1u)] = top_key(k, id);
+    });
+    __syncthreads();
+    n = (int)sh_n;
+  }
+  // 4.
+  for (int i = tid; i < n; i += TOP_THREADS) {
+    const unsigned long long key = cand[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += cand[j] > key;
+    if (rank < K) {
+      if (a.chunks == 1)
+        top_store(a, row, rank, key);
+      else
+        a.part[(long)blockIdx.x * K + rank] = key;
+    }
+  }
+  if (a.chunks > 1)
+    for (int i = n + tid; i < K; i += TOP_THREADS) a.part[(long)blockIdx.x * K + i] = 0;
+  if (tid == 0) {
+    s = sh_s[0];
+    for (int i = 1; i < WAVES; ++i) s += sh_s[i];
+    if (a.chunks > 1) a.stat[blockIdx.x] = make_float2(mx, s);
+    else if (a.lse) a.lse[row] = row_lse(mx, s, a.tau);
+  }
+}
+
+// Joins the chunks of a row.  A key's rank: its place in its own chunk's list, and how many keys of the other lists are above
+// it (each by bisection).
+__global__ void __launch_bounds__(TOP_THREADS) top_merge_kernel(const TopArgs a) {
+  __shared__ unsigned long long lds[TOP_MERGE_LDS];
+  const long row = blockIdx.x;
+  const int n = a.chunks * a.K, K = a.K;
+  const unsigned long long *key = a.part + row * n;
+  if (n <= TOP_MERGE_LDS) {  // (more: the widest vocabularies with the longest lists)
+    for (int i = threadIdx.x; i < n; i += TOP_THREADS) lds[i] = key[i];
+    __syncthreads();
+    key = lds;
+  }
+  for (int i = threadIdx.x; i < n; i += TOP_THREADS) {
+    const unsigned long long k = key[i];
+    if (k == 0) continue;
+    const int mine = i / K;
+    int rank = i - mine * K;
+    for (int l = 0; l < a.chunks && rank < K; ++l) {
+      if (l == mine) continue;
+      int lo = 0, hi = K;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (key[l * K + mid] > k) lo = mid + 1;
+        else hi = mid;
+      }
+      rank += lo;
+    }
+    if (rank < K) top_store(a, row, rank, k);
+  }
+  if (threadIdx.x < 64 && a.lse) {
+    const float c = LOG2E / a.tau;
+    float m = -INFINITY, s = 0.0f;
+    for (int l = threadIdx.x; l < a.chunks; l += 64) {
+      const float2 q = a.stat[row * a.chunks + l];
+      const float top = fmaxf(m, q.x), base = top == -INFINITY ? 0.0f : top;
+      s = s * exp2_32((m - base) * c) + q.y * exp2_32((q.x - base) * c);
+      m = top;
+    }
+    const float top = wave_max(m), base = top == -INFINITY ? 0.0f : top;
+    s = wave_sum(s * exp2_32((m - base) * c));
+    if (threadIdx.x == 0) a.lse[row] = row_lse(top, s, a.tau);
+  }
+}
+
+}  // namespace rnnlm_dev
