@@ -328,6 +328,59 @@ int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft
                         float tau_draft, int32_t *accepted, int32_t *tokens, int32_t *range_flag, void *workspace,
                         size_t workspace_bytes, void *stream);
 
+/* The operators above on a handle's own windows (both architectures).  Rows of logits are of the handle's compute type
+ * (RNNLM_FP32: float, RNNLM_BF16_FP32MASTER: bf16), [T][B] rows ld elements apart, in the caller's memory.
+ *
+ * rnnlm_forward_logits: the logits Wo h + b of every position of the window x: dev int32[T][B], starting from h_state,
+ * which is advanced: what rnnlm_top_logits makes a teacher's lists of and rnnlm_verify_drafts decides by. */
+int rnnlm_forward_logits(rnnlm_t *h, const int32_t *x, int32_t T, void *logits, int64_t ld, void *stream);
+
+/* A window's teacher, as in rnnlm_distill_loss; all arrays [T][B].  logits: scratch of [T][B] rows (afterwards: the gradient
+ * of the window's loss with respect to the logits). */
+typedef struct {
+  const int32_t *ids;  /* dev int32[T][B][K] */
+  const float *vals;   /* dev float[T][B][K] */
+  const float *lse;    /* dev float[T][B] or NULL */
+  const float *weight; /* dev float[T][B] or NULL */
+  int32_t K;
+  float tau, alpha;
+  void *logits;
+  int64_t ld;
+} rnnlm_distill;
+
+/* rnnlm_train_chunk with the criterion of rnnlm_distill_loss in place of the normalised cross-entropy: forward pass, gradients
+ * of the mean over the window's B*T positions (weights and all), back-propagation and the same plain SGD step.
+ * y: dev int32[T][B], may be NULL where alpha = 1; negative labels are missing ones; loss: dev float[T][B] or NULL; sum_loss:
+ * dev double or NULL.  A sum that is not finite and ids out of range are reported by rnnlm_check. */
+int rnnlm_distill_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float lr,
+                              float *loss, double *sum_loss, void *stream);
+
+/* Its gradients into caller buffers, as rnnlm_grad_chunk and rnnlm_grad_chunk_compressed give theirs. */
+int rnnlm_distill_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE,
+                             float *dU, float *dWo, float *db, float *loss, void *stream);
+int rnnlm_distill_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d,
+                                        float *dE, float *dA, float *dU, float *dC, float *db, float *loss, void *stream);
+
+/* A verification by the handle's model, as in rnnlm_verify_drafts (target rows: the model's own logits). */
+typedef struct {
+  const void *draft;  /* dev [K][B] rows of the draft model's logits, or NULL */
+  int64_t ld_draft;
+  const int32_t *lengths; /* dev int32[B] or NULL */
+  const float *u;     /* dev float[K+1][B] */
+  float tau, tau_draft;
+  void *logits;       /* scratch: [K+1][B] rows (afterwards: the model's logits) */
+  int64_t ld;
+  void *workspace;    /* as rnnlm_verify_drafts */
+  size_t workspace_bytes;
+} rnnlm_verify;
+
+/* One step of drafting and verifying: x: dev int32[K+1][B]: row 0 the last word of every text that the model has not read
+ * yet, rows 1..K the drafts, 0 <= K < T_max.  Runs the model over them from h_state, verifies, and leaves in h_state the state
+ * after row 0 and the accepted drafts of each text (bf16: as the recurrence carries it, rounded to bf16), so that the drawn
+ * words are row 0 of the next call.  accepted, tokens: as rnnlm_verify_drafts. */
+int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,
+                       void *stream);
+
 /* Number of polls, of about 4 us each (or as many shorter ones as take that time), a wait of the persistent
  * recurrent kernels makes before it gives up, raises the flag that rnnlm_check reports as RNNLM_ERR_TIMEOUT and
  * lets the kernel run to its end (default 2^18, about a second).  A wait lasts longer than a step's few

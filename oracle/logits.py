@@ -35,8 +35,8 @@ def distill(z, ids, vals, n=None, y=-1, weight=1.0, tau=1.0, alpha=1.0, scale=1.
     if n is None:
         n = lse([t for _, t in there]) if there else 0.0
     q, q1 = softmax(z, tau), softmax(z)
-    ln_q, ln_q1 = np.asarray(z, np.float64) / tau - lse(z, tau), np.asarray(z, np.float64) - lse(z)
-    empty = np.isneginf(np.max(z))
+    empty = np.isneginf(np.max(z))  # (no logarithm of its softmax is asked for)
+    ln_q, ln_q1 = (np.asarray(z, np.float64) / t - (0.0 if empty else lse(z, t)) for t in (tau, 1.0))
     kd = mass = 0.0
     for i, t in there:
         p = np.exp(t - n)

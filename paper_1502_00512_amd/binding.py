@@ -28,7 +28,8 @@ SYMBOLS = [
     "rnnlm_grad_chunk_compressed", "rnnlm_quantize_weights", "rnnlm_forward_score_shortlist",
     "rnnlm_set_recurrent_exchange", "rnnlm_sort_segments_static",
     "rnnlm_top_logits_workspace_bytes", "rnnlm_top_logits", "rnnlm_distill_loss", "rnnlm_verify_workspace_bytes",
-    "rnnlm_verify_drafts",
+    "rnnlm_verify_drafts", "rnnlm_forward_logits", "rnnlm_distill_train_chunk", "rnnlm_distill_grad_chunk",
+    "rnnlm_distill_grad_chunk_compressed", "rnnlm_verify_chunk",
 ]
 SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes"]  # return bytes
 
@@ -55,6 +56,17 @@ class rnnlm_buffers(C.Structure):
 class rnnlm_quantized(C.Structure):
     _fields_ = [("qE", C.c_void_p), ("sE", C.c_void_p), ("qA", C.c_void_p), ("sA", C.c_void_p),
                 ("qU", C.c_void_p), ("sU", C.c_void_p), ("qC", C.c_void_p), ("sC", C.c_void_p)]
+
+
+class rnnlm_distill(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("vals", C.c_void_p), ("lse", C.c_void_p), ("weight", C.c_void_p), ("K", C.c_int32),
+                ("tau", C.c_float), ("alpha", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64)]
+
+
+class rnnlm_verify(C.Structure):
+    _fields_ = [("draft", C.c_void_p), ("ld_draft", C.c_int64), ("lengths", C.c_void_p), ("u", C.c_void_p), ("tau", C.c_float),
+                ("tau_draft", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class RnnlmError(RuntimeError):
@@ -107,6 +119,11 @@ def load():
     lib.rnnlm_distill_loss.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, vp]
     lib.rnnlm_verify_workspace_bytes.argtypes = [i32, i32, i32]
     lib.rnnlm_verify_drafts.argtypes = [vp, i64, vp, i64, i32, i32, i32, i32, vp, vp, vp, f32, f32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.rnnlm_forward_logits.argtypes = [vp, vp, i32, vp, i64, vp]
+    lib.rnnlm_distill_train_chunk.argtypes = [vp, vp, vp, i32, C.POINTER(rnnlm_distill), f32, vp, vp, vp]
+    lib.rnnlm_distill_grad_chunk.argtypes = [vp, vp, vp, i32, C.POINTER(rnnlm_distill), vp, vp, vp, vp, vp, vp]
+    lib.rnnlm_distill_grad_chunk_compressed.argtypes = [vp, vp, vp, i32, C.POINTER(rnnlm_distill), vp, vp, vp, vp, vp, vp, vp]
+    lib.rnnlm_verify_chunk.argtypes = [vp, vp, i32, C.POINTER(rnnlm_verify), vp, vp, vp]
     for name in SIZES:
         getattr(lib, name).restype = C.c_size_t
     lib.rnnlm_profile_enable.argtypes = [vp, C.c_uint32]
@@ -460,6 +477,85 @@ class Rnnlm:
                                           _ptr(lnq), lnZ, _ptr(dE), _ptr(dU), _ptr(dWo), _ptr(db), _ptr(J),
                                           _stream(stream)), "rnnlm_nce_grad_chunk")
         return dict(gE=dE, gU=dU, gWo=dWo, gb=db, J=J)
+
+    # -- windows whose logits are the caller's -----------------------------------------------------
+    def _logit_rows(self, call, T, logits):
+        """A tensor [T][B][V] of the compute type (allocated if None) and the distance of its rows."""
+        import torch
+        dtype = torch.float32 if self.precision == RNNLM_FP32 else torch.bfloat16
+        if logits is None:
+            return torch.empty(T, self.B, self.V, dtype=dtype, device=self.device), self.V
+        _need(tuple(logits.shape) == (T, self.B, self.V), call, f"logits: [{T}][{self.B}][{self.V}] is wanted")
+        return logits, _rows(call, "logits", logits, self.device, dtype)[2]
+
+    def _window(self, call, x):
+        import torch
+        _need(x.dim() == 2 and x.shape[1] == self.B, call, f"x: [T][{self.B}] is wanted")
+        _dense(call, "x", x, torch.int32, tuple(x.shape), self.device)
+        return x.shape[0]
+
+    def rnnlm_forward_logits(self, x, logits=None, stream=None):
+        T = self._window("rnnlm_forward_logits", x)
+        logits, ld = self._logit_rows("rnnlm_forward_logits", T, logits)
+        _ok(self.lib.rnnlm_forward_logits(self.handle, _ptr(x), T, _ptr(logits), ld, _stream(stream)), "rnnlm_forward_logits")
+        return logits
+
+    def _distill(self, call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss):
+        import torch
+        T = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        n, K = T * self.B, ids.shape[-1]
+        for name, t, dtype, shape in (("y", y, torch.int32, (n,)), ("ids", ids, torch.int32, (n, K)), ("vals", vals, torch.float32, (n, K)),
+                                      ("lse", lse, torch.float32, (n,)), ("weight", weight, torch.float32, (n,)),
+                                      ("loss", loss, torch.float32, (n,)), ("sum_loss", sum_loss, torch.float64, (1,))):
+            _dense(call, name, t, dtype, shape, self.device)
+        at = lambda t: None if t is None else t.data_ptr()
+        return rnnlm_distill(at(ids), at(vals), at(lse), at(weight), K, tau, alpha, logits.data_ptr(), ld), logits, T
+
+    def rnnlm_distill_train_chunk(self, x, y, ids, vals, lr: float, lse=None, weight=None, tau: float = 1.0, alpha: float = 1.0,
+                                  logits=None, loss=None, sum_loss=None, stream=None):
+        """ids, vals [T][B][K], lse [T][B] or None: the teacher's (rnnlm_top_logits of its rnnlm_forward_logits at the same tau)."""
+        call = "rnnlm_distill_train_chunk"
+        d, _keep, T = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss)
+        _ok(self.lib.rnnlm_distill_train_chunk(self.handle, _ptr(x), _ptr(y), T, C.byref(d), lr, _ptr(loss), _ptr(sum_loss),
+                                               _stream(stream)), call)
+
+    def rnnlm_distill_grad_chunk(self, x, y, ids, vals, lse=None, weight=None, tau: float = 1.0, alpha: float = 1.0, logits=None,
+                                 stream=None):
+        import torch
+        call = "rnnlm_distill_grad_chunk" + ("_compressed" if self.P else "")
+        z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
+        loss = z(x.shape[0], self.B)
+        d, _keep, T = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, None)
+        if self.P:
+            g = dict(gE=z(self.V, self.P), gA=z(self.H, self.P), gU=z(self.H, self.H), gC=z(self.P, self.H), gb=z(self.V))
+        else:
+            g = dict(gE=z(self.V, self.H), gU=z(self.H, self.H), gWo=z(self.V, self.H), gb=z(self.V))
+        _ok(getattr(self.lib, call)(self.handle, _ptr(x), _ptr(y), T, C.byref(d), *map(_ptr, g.values()), _ptr(loss), _stream(stream)),
+            call)
+        return dict(loss=loss, **g)
+
+    def rnnlm_verify_chunk(self, x, u, draft=None, lengths=None, tau: float = 1.0, tau_draft: float = 1.0, logits=None, accepted=None,
+                           tokens=None, workspace=None, stream=None):
+        """x int32 [K+1][B]: the word not read yet, then the drafts.  Returns (accepted [B], tokens [K+1][B])."""
+        import torch
+        call = "rnnlm_verify_chunk"
+        K = self._window(call, x) - 1
+        logits, ld = self._logit_rows(call, K + 1, logits)
+        ldd = 0
+        if draft is not None and K > 0:
+            ldd = self._logit_rows(call, K, draft)[1]
+        nbytes = rnnlm_verify_workspace_bytes(K, self.B, self.V)
+        accepted = torch.empty(self.B, dtype=torch.int32, device=self.device) if accepted is None else accepted
+        tokens = torch.empty(K + 1, self.B, dtype=torch.int32, device=self.device) if tokens is None else tokens
+        for name, t, dtype, shape in (("u", u, torch.float32, (K + 1, self.B)), ("lengths", lengths, torch.int32, (self.B,)),
+                                      ("accepted", accepted, torch.int32, (self.B,)), ("tokens", tokens, torch.int32, (K + 1, self.B))):
+            _dense(call, name, t, dtype, shape, self.device)
+        workspace = _scratch(call, workspace, nbytes, self.device)
+        v = rnnlm_verify(draft.data_ptr() if ldd else None, ldd, None if lengths is None else lengths.data_ptr(), u.data_ptr(), tau,
+                         tau_draft, logits.data_ptr(), ld, workspace.data_ptr(), workspace.nbytes)
+        _ok(self.lib.rnnlm_verify_chunk(self.handle, _ptr(x), K, C.byref(v), _ptr(accepted), _ptr(tokens), _stream(stream)), call)
+        return accepted, tokens
 
     def rnnlm_reset_state(self, stream=None):
         _ok(self.lib.rnnlm_reset_state(self.handle, _stream(stream)), "rnnlm_reset_state")

@@ -92,7 +92,7 @@ __device__ inline DistillRow distill_finish(const DistillArgs<T> &a, long m, flo
   const float inv_tau = 1.0f / a.tau, g = w * a.scale;
   const bool label = ent[a.K].id >= 0;
   const double n = a.lse ? (double)a.lse[m] : (double)tmax + log(S);
-  const double pi = S > 0.0 ? (a.lse ? exp((double)tmax - n) * S : 1.0) : 0.0;
+  const double pi = S == 0.0 ? 0.0 : a.lse ? exp((double)tmax - n) * S : S / S;  // (a NaN in the list stays one)
   const float s1 = TWO ? r.s1 : r.s;
   DistillRow o;
   const float base = r.m == -INFINITY ? 0.0f : r.m;  // no finite logit: every exponential below is 0
@@ -114,10 +114,10 @@ __device__ inline DistillRow distill_finish(const DistillArgs<T> &a, long m, flo
   if (threadIdx.x == 0) {
     double loss = 0.0;
     if (r.s == 0.0f) {
-      if ((a.alpha > 0.0f && pi > 0.0) || (label && a.alpha < 1.0f)) loss = INFINITY;
+      if ((a.alpha > 0.0f && pi != 0.0) || (label && a.alpha < 1.0f)) loss = INFINITY;
     } else {
       const double top = (double)r.m * (double)inv_tau;
-      if (a.alpha > 0.0f && pi > 0.0) loss = (double)(a.alpha * a.tau) * (double)a.tau * pi * (A / S + top + log((double)r.s) - n);
+      if (a.alpha > 0.0f && pi != 0.0) loss = (double)(a.alpha * a.tau) * (double)a.tau * pi * (A / S + top + log((double)r.s) - n);
       if (label && a.alpha < 1.0f)
         loss += (double)(1.0f - a.alpha) * ((double)r.m - (double)ent[a.K].z + log((double)s1));
     }

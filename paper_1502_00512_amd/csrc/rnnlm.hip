@@ -20,6 +20,7 @@
 #include "gemm_ring64.h"
 #include "gemm_split.h"
 #include "gemm_tail.h"
+#include "logit_window.h"
 #include "rnn_persistent.h"
 #include "rnn_resident.h"
 #include "rnn_step.h"
@@ -905,12 +906,12 @@ bool short_output_update(rnnlm_t *h, int Tn) {
   return 2.0 * n * window_plan(h, (long)Tn * h->Bp).Mp / rate + 8.0 * n / 4e6 < 15.0;
 }
 
-// train: a backward pass follows.  sort_inputs: its embedding update wants the input ids sorted: started on the side
+// train: a backward pass follows.  logits_only: the window ends with its logits, no statistics are formed.  sort_inputs: its embedding update wants the input ids sorted: started on the side
 // stream as soon as the padded ids exist (the update runs on that stream too).
 template <typename T>
 int forward_window(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float *logp_out, bool advance_state,
                    bool with_output, hipStream_t st, bool train = false, bool sort_inputs = false, bool need_feat = false,
-                   const WindowSum *wsum = nullptr) {
+                   const WindowSum *wsum = nullptr, bool logits_only = false) {
   const rnnlm_config &c = h->cfg;
   const int Hp = h->Hp, Bp = h->Bp, Vp = h->Vp;
   const int Mrows = Tn * Bp;
@@ -1050,7 +1051,7 @@ int forward_window(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float
     StageTimer tm(h, RNNLM_STAGE_OUT_FWD, st);
     EpiOutFwd<T> epi;
     epi.b = h->buf.b;
-    epi.ZT = train ? at<T>(h, h->L.ZT) : nullptr;  // evaluation wants the statistics only
+    epi.ZT = train || logits_only ? at<T>(h, h->L.ZT) : nullptr;  // evaluation wants the statistics only
     epi.part = at<float2>(h, h->L.stat);
     epi.yp = yp;
     epi.zy = zy;
@@ -1084,7 +1085,7 @@ int forward_window(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float
       HIP_TRY((f32_gemm<ROWK, ROWK>(st, at<T>(h, h->L.Wo_c), h->Dp, feat, h->Dp, Vp, Mp, round_up(h->D, 32), plan, epi, 8)));
     }
   }
-  if (train && merged_in_pass(h, window_plan(h, Mrows))) return RNNLM_OK;
+  if (logits_only || (train && merged_in_pass(h, window_plan(h, Mrows)))) return RNNLM_OK;
   StageTimer tm(h, RNNLM_STAGE_STATS, st);
   hipLaunchKernelGGL(merge_stats_kernel, dim3(blocks_for(Mrows, MERGE_M)), dim3(1024), 0, st, at<float2>(h, h->L.stat),
                      window_plan(h, Mrows).parts, Mp, Tn, c.B, Bp, zy, lse, at<float>(h, h->L.logp_int), logp_out,
@@ -1105,6 +1106,47 @@ int sort_segments(rnnlm_t *h, int Tn, int32_t *perm, int32_t *seg, int32_t *nseg
 }
 
 // One call of the noise-contrastive criterion (Sec. 4.2): K noise words shared by the window.
+// ---- windows whose logits are the caller's (criteria and decisions on arrays of logits) ----
+template <typename T>
+constexpr int32_t logit_dtype() {
+  return sizeof(T) == 4 ? RNNLM_DTYPE_FP32 : RNNLM_DTYPE_BF16;
+}
+LogitWindow logit_window(rnnlm_t *h, int Tn, int64_t ld) {
+  return {Tn, h->cfg.B, h->Bp, h->cfg.V, (long)h->MpMax, (long)ld};
+}
+// The logits of the window's positions as rows t*B + s.
+template <typename T>
+int logits_to_rows(rnnlm_t *h, int Tn, void *logits, int64_t ld, hipStream_t st) {
+  hipLaunchKernelGGL(logits_to_rows_kernel<T>, dim3(blocks_for(h->cfg.V, LW_TILE), blocks_for((long)Tn * h->Bp, LW_TILE)), dim3(256), 0,
+                     st, at<T>(h, h->L.ZT), static_cast<T *>(logits), logit_window(h, Tn, ld));
+  HIP_TRY(hipGetLastError());
+  return RNNLM_OK;
+}
+struct DistillCall {
+  const rnnlm_distill *d;
+  const int32_t *y;
+  float *loss;  // may be nullptr
+};
+// The place of the softmax gradient in a distilled window: the criterion on rows of logits, its sum, and the gradient of
+// the logits back in the output layer's order with the bias update.
+template <typename T>
+int distill_gradient(rnnlm_t *h, int Tn, int Mp, const DistillCall &c, const WindowSum &ws, const float *b, float *b_out, float alpha,
+                     float lr, hipStream_t st) {
+  const rnnlm_distill &d = *c.d;
+  const int n = Tn * h->cfg.B;
+  float *loss = c.loss ? c.loss : at<float>(h, h->L.logp_int);
+  int rc = logits_to_rows<T>(h, Tn, d.logits, d.ld, st);
+  if (rc) return rc;
+  rc = rnnlm_distill_loss(d.logits, logit_dtype<T>(), n, h->cfg.V, d.ld, d.ids, d.vals, d.K, d.lse, c.y, d.weight, d.tau, d.alpha,
+                          1.0f / (float)n, loss, nullptr, d.logits, d.ld, p_flags(h), st);
+  if (rc) return rc;
+  hipLaunchKernelGGL(losses_sum_kernel, dim3(1), dim3(1024), 0, st, loss, n, ws);
+  hipLaunchKernelGGL(rows_to_logits_kernel<T>, dim3(h->Vp / LW_TILE), dim3(256), 0, st, static_cast<const T *>(d.logits),
+                     at<T>(h, h->L.ZT), Mp, b, b_out, alpha, lr, logit_window(h, Tn, d.ld));
+  HIP_TRY(hipGetLastError());
+  return RNNLM_OK;
+}
+
 struct NceCall {
   const int32_t *noise;
   int K;
@@ -1305,7 +1347,7 @@ int launch_window_update(rnnlm_t *h, WindowUpdate<T> &w, int tile, int Mrows, hi
 // other stream is not.
 template <typename T>
 int backward_window(rnnlm_t *h, int Tn, const UpdateTargets &u, const NceCall *nce, hipStream_t st, hipStream_t *rec_stream,
-                    float *logp_out, const WindowSum &wsum) {
+                    float *logp_out, const WindowSum &wsum, const DistillCall *distill = nullptr) {
   const rnnlm_config &c = h->cfg;
   const int Hp = h->Hp, Bp = h->Bp, Vp = h->Vp;
   const int Mrows = Tn * Bp;
@@ -1328,7 +1370,11 @@ int backward_window(rnnlm_t *h, int Tn, const UpdateTargets &u, const NceCall *n
     if (rc) return rc;
   } else {
   // fused softmax gradient + bias update, in place on the vocabulary-major logits
-  {
+  if (distill) {
+    StageTimer tm(h, RNNLM_STAGE_SOFTMAX_GRAD, st);
+    int rc = distill_gradient<T>(h, Tn, Mp, *distill, wsum, h->buf.b, u.b, u.alpha, u.lr, st);
+    if (rc) return rc;
+  } else {
     StageTimer tm(h, RNNLM_STAGE_SOFTMAX_GRAD, st);
     const WindowPlan &wp = window_plan(h, Mrows);
     const StatsMerge merge = {at<float2>(h, h->L.stat), wp.parts, Tn, c.B, Bp, at<float>(h, h->L.zy), at<float>(h, h->L.logp_int),
@@ -1692,6 +1738,34 @@ int window_call(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float *l
   }
   if (u) rc = backward_window<T>(h, Tn, *u, nce, st, rec_stream, logp, ws);
   return rc;
+}
+
+template <typename T>
+int distill_window_call(rnnlm_t *h, const int32_t *x, int Tn, const DistillCall &c, double *sum_loss, const UpdateTargets &u,
+                        bool advance_state, hipStream_t st) {
+  const WindowSum ws = {sum_loss ? sum_loss : p_sum(h), nullptr, p_flags(h), p_counter(h)};
+  int rc = forward_window<T>(h, x, nullptr, Tn, nullptr, advance_state, true, st, true, !scan_ids(h, Tn, u), false, nullptr, true);
+  if (rc) return rc;
+  return backward_window<T>(h, Tn, u, nullptr, st, nullptr, nullptr, ws, &c);
+}
+
+template <typename T>
+int logits_call(rnnlm_t *h, const int32_t *x, int Tn, void *logits, int64_t ld, bool advance_state, hipStream_t st) {
+  int rc = forward_window<T>(h, x, nullptr, Tn, nullptr, advance_state, true, st, false, false, false, nullptr, true);
+  return rc ? rc : logits_to_rows<T>(h, Tn, logits, ld, st);
+}
+
+template <typename T>
+int verify_call(rnnlm_t *h, const int32_t *x, int K, const rnnlm_verify &v, int32_t *accepted, int32_t *tokens, hipStream_t st) {
+  const rnnlm_config &c = h->cfg;
+  int rc = logits_call<T>(h, x, K + 1, v.logits, v.ld, false, st);
+  if (rc) return rc;
+  rc = rnnlm_verify_drafts(v.logits, v.ld, v.draft, v.ld_draft, logit_dtype<T>(), K, c.B, c.V, K > 0 ? x + c.B : nullptr, v.lengths, v.u,
+                           v.tau, v.tau_draft, accepted, tokens, p_flags(h), v.workspace, v.workspace_bytes, st);
+  if (rc) return rc;
+  hipLaunchKernelGGL(keep_states_kernel<T>, dim3(c.B), dim3(256), 0, st, at<T>(h, h->L.Hs_c), accepted, c.H, h->Hp, h->Bp, h->buf.h_state);
+  HIP_TRY(hipGetLastError());
+  return RNNLM_OK;
 }
 
 template <typename T>
@@ -2086,6 +2160,84 @@ int rnnlm_forward_score_shortlist(rnnlm_t *h, const int32_t *x, const int32_t *c
   hipStream_t st = (hipStream_t)stream;
   return (h->cfg.precision == RNNLM_FP32) ? shortlist_call<float>(h, x, cand, C, T, lnZ, score, st)
                                           : shortlist_call<bf16_t>(h, x, cand, C, T, lnZ, score, st);
+}
+
+namespace {
+// Arguments of the calls on rows of logits that their own checks would refuse after the window has started.
+bool logit_rows_ok(const rnnlm_t *h, const void *p, int64_t ld) {
+  const uintptr_t es = h->cfg.precision == RNNLM_FP32 ? 4 : 2;
+  return p && reinterpret_cast<uintptr_t>(p) % es == 0 && ld >= h->cfg.V && ld <= (int64_t(1) << 31) && h->cfg.V <= (1 << 20);
+}
+bool tau_in_range(float tau) { return tau >= 1e-3f && tau <= 1e3f; }
+bool distill_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d) {
+  if (!h || !x || !d || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, d->logits, d->ld)) return false;
+  if (!d->ids || !d->vals || d->K < 1 || d->K > 1024 || !tau_in_range(d->tau) || !(d->alpha >= 0.0f && d->alpha <= 1.0f)) return false;
+  if (d->alpha < 1.0f && !y) return false;
+  return ((reinterpret_cast<uintptr_t>(d->ids) | reinterpret_cast<uintptr_t>(d->vals) | reinterpret_cast<uintptr_t>(d->lse) |
+           reinterpret_cast<uintptr_t>(d->weight) | reinterpret_cast<uintptr_t>(y)) & 3) == 0;
+}
+int distill_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, const UpdateTargets &u,
+                  float *loss, double *sum_loss, bool advance_state, hipStream_t st) {
+  const DistillCall c = {d, y, loss};
+  return (h->cfg.precision == RNNLM_FP32) ? distill_window_call<float>(h, x, T, c, sum_loss, u, advance_state, st)
+                                          : distill_window_call<bf16_t>(h, x, T, c, sum_loss, u, advance_state, st);
+}
+}  // namespace
+
+int rnnlm_forward_logits(rnnlm_t *h, const int32_t *x, int32_t T, void *logits, int64_t ld, void *stream) {
+  if (!h || !x || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, logits, ld)) return RNNLM_ERR_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  return (h->cfg.precision == RNNLM_FP32) ? logits_call<float>(h, x, T, logits, ld, true, st)
+                                          : logits_call<bf16_t>(h, x, T, logits, ld, true, st);
+}
+
+int rnnlm_distill_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float lr,
+                              float *loss, double *sum_loss, void *stream) {
+  if (!distill_args_ok(h, x, y, T, d) || !(lr == lr)) return RNNLM_ERR_ARG;
+  UpdateTargets u{h->buf.E, h->buf.U, h->buf.Wo, h->buf.b, 1.0f, lr, true, true};
+  u.A = h->buf.A;
+  u.C = h->buf.C;
+  return distill_chunk(h, x, y, T, d, u, loss, sum_loss, true, (hipStream_t)stream);
+}
+
+int rnnlm_distill_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE, float *dU,
+                             float *dWo, float *db, float *loss, void *stream) {
+  if (!distill_args_ok(h, x, y, T, d) || !dE || !dU || !dWo || !db || h->cfg.P > 0) return RNNLM_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dU) | reinterpret_cast<uintptr_t>(dWo) |
+       reinterpret_cast<uintptr_t>(db)) & 15)
+    return RNNLM_ERR_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  const long nE = (long)h->cfg.V * h->cfg.H;
+  hipLaunchKernelGGL(fill_kernel<float>, dim3(std::min<long>(blocks_for(nE, 256), 65535)), dim3(256), 0, st, dE, nE, 0.0f);
+  HIP_TRY(hipGetLastError());
+  return distill_chunk(h, x, y, T, d, UpdateTargets{dE, dU, dWo, db, 0.0f, -1.0f, false, false}, loss, nullptr, false, st);
+}
+
+int rnnlm_distill_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE,
+                                        float *dA, float *dU, float *dC, float *db, float *loss, void *stream) {
+  if (!distill_args_ok(h, x, y, T, d) || !dE || !dA || !dU || !dC || !db || h->cfg.P <= 0) return RNNLM_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dA) | reinterpret_cast<uintptr_t>(dU) |
+       reinterpret_cast<uintptr_t>(dC) | reinterpret_cast<uintptr_t>(db)) & 15)
+    return RNNLM_ERR_ARG;
+  UpdateTargets u{dE, dU, nullptr, db, 0.0f, -1.0f, false, false};
+  u.A = dA;
+  u.C = dC;
+  return distill_chunk(h, x, y, T, d, u, loss, nullptr, false, (hipStream_t)stream);
+}
+
+int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,
+                       void *stream) {
+  if (!h || !x || !v || K < 0 || K >= h->cfg.T_max || !logit_rows_ok(h, v->logits, v->ld) || !v->u || !accepted || !tokens ||
+      !tau_in_range(v->tau) || !tau_in_range(v->tau_draft) || (v->draft && K > 0 && !logit_rows_ok(h, v->draft, v->ld_draft)))
+    return RNNLM_ERR_ARG;
+  const size_t need = rnnlm_verify_workspace_bytes(K, h->cfg.B, h->cfg.V);
+  if (need == 0 || !v->workspace || (reinterpret_cast<uintptr_t>(v->workspace) & 255) || v->workspace_bytes < need ||
+      ((reinterpret_cast<uintptr_t>(v->lengths) | reinterpret_cast<uintptr_t>(v->u) | reinterpret_cast<uintptr_t>(accepted) |
+        reinterpret_cast<uintptr_t>(tokens)) & 3))
+    return RNNLM_ERR_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  return (h->cfg.precision == RNNLM_FP32) ? verify_call<float>(h, x, K, *v, accepted, tokens, st)
+                                          : verify_call<bf16_t>(h, x, K, *v, accepted, tokens, st);
 }
 
 namespace {

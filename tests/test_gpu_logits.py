@@ -234,6 +234,18 @@ def test_distill_a_nan_stays_in_its_row():
     assert bool(torch.isfinite(out[0]).all()) and bool(torch.isfinite(out[2]).all()) and bool(torch.isnan(out[1]).all())
 
 
+def test_distill_a_nan_in_a_list_stays_in_its_row():
+    z, (ids, vals, y, w) = patterns("normal", 3, 500, 1), lists(3, 500, 6, 2, False)
+    vals[1, 4] = np.nan
+    vals[2, 4], ids[2, 4] = np.nan, -1  # of an absent entry: nobody's
+    d, _ = place(z, "fp32")
+    out = torch.empty_like(d)
+    for n in (None, torch.full((3,), 9.0, device="cuda")):
+        loss = binding.rnnlm_distill_loss(d, torch.as_tensor(ids).cuda(), torch.as_tensor(vals).cuda(), n, torch.as_tensor(y).cuda(), None, 1.0, 0.5, dlogits=out)
+        assert torch.isnan(loss).tolist() == [False, True, False]
+        assert bool(torch.isfinite(out[0]).all()) and bool(torch.isfinite(out[2]).all()) and bool(torch.isnan(out[1]).all())
+
+
 def test_distill_gradient_is_the_loss_difference():
     """Against differences of the call's own losses: fp32 losses of about 4 to 2^-22, steps of 2^-5, third derivatives below 1."""
     rng = np.random.default_rng(2)
