@@ -3,8 +3,8 @@
 //   loss  = w (alpha tau^2 sum_k p_k (ln p_k - ln q_tau(id_k)) - (1 - alpha) ln q_1(y)),   q_tau = softmax(z / tau)
 //   dz[v] = w g (alpha tau (pi q_tau(v) - sum_{k: id_k = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
 // The sum over the list is pi (A / S + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (t_k - z_k / tau):
-// a pass over the row needs the maximum and the sum of exponentials only, and the listed words are read one by one.
-// The list's sums are formed in 64 bits (a few hundred terms a row): the loss is a difference of numbers ten times its size.
+// a pass over the row needs a sum of exponentials only, and the listed words are read one by one.
+// A sum is taken relative to a reference m: sum_v e^{(z_v - m) / tau}.  Any m will do that leaves it finite and far from 0.
 #pragma once
 #include "rows.h"
 
@@ -24,25 +24,81 @@ struct DistillArgs {
   int V, K;
 };
 
+// Exponentials of an element.  ONE: a single temperature (tau = 1, or no labels).  SQUARE: tau = 2 and labels, whose
+// exponential at 1 is the square of the one at 2 (a multiplication in place of 5 instructions' time; tau = 2 is the usual
+// temperature).  TWO: any other tau, and labels.
+enum DistillMode { DISTILL_ONE, DISTILL_SQUARE, DISTILL_TWO };
+
 struct DistillEntry {  // a word of the list, or (last) the label
   int id;              // -1: absent
-  float t, z, coef;    // teacher's logit / tau, student's logit, what the word's gradient has taken off
+  float t, z, p;       // teacher's logit / tau, student's logit, e^{t - t_max}
 };
 
-// What a row's softmax is made of: maximum, and the sums of exponentials relative to it at tau and at 1.
+// What a row's softmax is made of: a reference, and the sums of exponentials relative to it at tau and at 1.
 struct RowSums {
   float m, s, s1;
 };
 
+template <int MODE>
+struct DistillExp {
+  float c, b, b1;
+  __device__ DistillExp(float m, float tau) : c(LOG2E / tau), b(-m * c), b1(-m * LOG2E) {}
+  __device__ void add(float z, float &s, float &s1) const {
+    const float e = exp2_32(fmaf(z, c, b));
+    s += e;
+    if (MODE == DISTILL_SQUARE) s1 = fmaf(e, e, s1);
+    if (MODE == DISTILL_TWO) s1 += exp2_32(fmaf(z, LOG2E, b1));
+  }
+  // The sums, from reference m to this one.
+  __device__ void move(float m, float &s, float &s1) const {
+    const float e = exp2_32(fmaf(m, c, b));
+    s *= e;
+    if (MODE == DISTILL_SQUARE) s1 *= e * e;
+    if (MODE == DISTILL_TWO) s1 *= exp2_32(fmaf(m, LOG2E, b1));
+  }
+};
+
+// The dense part of a row's gradient: pi g alpha tau q_tau(v) + g (1 - alpha) q_1(v).  The factors (of one sign) go into the
+// exponents, or (SQUARE) d = e (a + a1 e).
+template <int MODE>
+struct DistillDense {
+  float c, b, a, a1;
+  unsigned sign;
+  __device__ DistillDense(const RowSums &r, float tau, float soft, float hard) {
+    c = LOG2E / tau;
+    const float s1 = MODE == DISTILL_ONE ? r.s : r.s1;
+    b = -r.m * c;
+    sign = 0u;
+    if (MODE == DISTILL_SQUARE) {
+      a = r.s == 0.0f ? 0.0f : soft / r.s;
+      a1 = s1 == 0.0f ? 0.0f : hard / s1;
+    } else {  // (sums may be as large as fp32 goes: no quotients)
+      a = MODE == DISTILL_ONE ? soft + hard : soft;
+      if (a < 0.0f || hard < 0.0f) sign = 0x80000000u;
+      b += r.s == 0.0f ? -INFINITY : __log2f(fabsf(a)) - __log2f(r.s);
+      a1 = -r.m * LOG2E + (s1 == 0.0f ? -INFINITY : __log2f(fabsf(hard)) - __log2f(s1));
+    }
+  }
+  __device__ float bare(float z) const {
+    const float e = exp2_32(fmaf(z, c, b));
+    if (MODE == DISTILL_SQUARE) return e * fmaf(a1, e, a);
+    return MODE == DISTILL_TWO ? e + exp2_32(fmaf(z, LOG2E, a1)) : e;
+  }
+  __device__ float operator()(float z) const { return sign ? -bare(z) : bare(z); }
+  template <typename T>
+  __device__ unsigned flip() const { return sizeof(T) == 4 ? sign : sign | sign >> 16; }
+};
+
 // Reads the list of row m: this thread's entries e = tid, tid + THREADS, ...  Returns the greatest t among them.
 template <typename T, int THREADS>
-__device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T *row, bool label, DistillEntry *ent) {
+__device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T *row, DistillEntry *ent) {
   float tmax = -INFINITY;
   const float inv_tau = 1.0f / a.tau;
+  const bool label = a.y && a.alpha < 1.0f;
   for (int e = threadIdx.x; e <= a.K; e += THREADS) {
     DistillEntry d;
     d.t = -INFINITY;
-    d.z = d.coef = 0.0f;
+    d.z = d.p = 0.0f;
     if (e < a.K) {
       d.id = a.ids[m * a.K + e];
       d.t = a.vals[m * a.K + e] * inv_tau;
@@ -62,84 +118,97 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
   return tmax;
 }
 
-// The list's sums S and A of this thread's entries.
+// The list's sums S and A over this thread's entries.  (A in 64 bits: masked words may be on the list, at the type's lowest
+// value.)
 template <int THREADS>
-__device__ inline void distill_list_sums(const DistillEntry *ent, int K, float inv_tau, float tmax, double &S, double &A) {
-  S = A = 0.0;
+__device__ inline void distill_list_sums(DistillEntry *ent, int K, float inv_tau, float tmax, float &S, double &A) {
   for (int e = threadIdx.x; e < K; e += THREADS) {
     const DistillEntry d = ent[e];
     if (d.t == -INFINITY) continue;  // absent, or a probability of zero: no term
-    const double p = exp((double)d.t - (double)tmax);
-    if (p == 0.0) continue;
+    const float p = exp2_32((d.t - tmax) * LOG2E);
+    ent[e].p = p;
+    if (p == 0.0f) continue;
     S += p;
-    A += p * ((double)d.t - (double)d.z * (double)inv_tau);
+    A += (double)p * ((double)d.t - (double)d.z * (double)inv_tau);
   }
 }
 
-// What the gradient of a row is made of: dz = a exp2(z c + b) + a1 exp2(z log2 e + b1) - coefficients of the listed words.
-struct DistillRow {
-  float c, b, a, b1, a1, hard;
-  __device__ float dense(float z, bool two) const {
-    const float d = a * exp2_32(fmaf(z, c, b));
-    return two ? fmaf(a1, exp2_32(fmaf(z, LOG2E, b1)), d) : d;
-  }
+// Sums over the workgroup's waves, by way of LDS.
+template <int WAVES>
+struct DistillShared {
+  float m[WAVES], t[WAVES], s[WAVES], s1[WAVES], S[WAVES], again[WAVES];
+  double A[WAVES];
 };
 
-// Loss of the row (thread 0 writes it), the coefficients of the listed words, and the dense part's constants.
-template <typename T, int THREADS, bool TWO>
-__device__ inline DistillRow distill_finish(const DistillArgs<T> &a, long m, float w, RowSums r, float tmax, double S, double A,
-                                            DistillEntry *ent) {
-  const float inv_tau = 1.0f / a.tau, g = w * a.scale;
-  const bool label = ent[a.K].id >= 0;
-  const double n = a.lse ? (double)a.lse[m] : (double)tmax + log(S);
-  const double pi = S == 0.0 ? 0.0 : a.lse ? exp((double)tmax - n) * S : S / S;  // (a NaN in the list stays one)
-  const float s1 = TWO ? r.s1 : r.s;
-  DistillRow o;
-  const float base = r.m == -INFINITY ? 0.0f : r.m;  // no finite logit: every exponential below is 0
-  o.c = LOG2E * inv_tau;
-  o.b = -base * o.c;
-  o.b1 = -base * LOG2E;
-  o.hard = label ? g * (1.0f - a.alpha) : 0.0f;
-  const float soft = (float)((double)(g * a.alpha * a.tau) * pi);
-  o.a = r.s == 0.0f ? 0.0f : soft / r.s;
-  o.a1 = s1 == 0.0f ? 0.0f : o.hard / s1;
-  if (!TWO) o.a += o.a1;  // tau = 1, or no label anywhere
-  for (int e = threadIdx.x; e <= a.K; e += THREADS) {
-    const DistillEntry d = ent[e];
-    float coef = 0.0f;
-    if (e == a.K) coef = o.hard;
-    else if (d.t != -INFINITY) coef = (float)((double)(g * a.alpha * a.tau) * exp((double)d.t - n));
-    ent[e].coef = coef;
+struct DistillList {
+  float tmax, S, factor, pi;  // p_k = factor e^{t_k - t_max}
+};
+
+// The list's sums (the barrier in between also publishes the waves' sums of the row): all threads take part.
+template <typename T, int THREADS>
+__device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, DistillEntry *ent, DistillShared<THREADS / 64> &sh) {
+  constexpr int WAVES = THREADS / 64;
+  DistillList l;
+  l.tmax = waves_max<WAVES>(sh.t);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float S = 0.0f;
+  double A = 0.0;
+  if (wave * 64 < a.K) {
+    distill_list_sums<THREADS>(ent, a.K, 1.0f / a.tau, l.tmax, S, A);
+    S = wave_sum(S);
+    A = wave_sum(A);
   }
-  if (threadIdx.x == 0) {
-    double loss = 0.0;
-    if (r.s == 0.0f) {
-      if ((a.alpha > 0.0f && pi != 0.0) || (label && a.alpha < 1.0f)) loss = INFINITY;
-    } else {
-      const double top = (double)r.m * (double)inv_tau;
-      if (a.alpha > 0.0f && pi != 0.0) loss = (double)(a.alpha * a.tau) * (double)a.tau * pi * (A / S + top + log((double)r.s) - n);
-      if (label && a.alpha < 1.0f)
-        loss += (double)(1.0f - a.alpha) * ((double)r.m - (double)ent[a.K].z + log((double)s1));
+  if ((threadIdx.x & 63) == 0) {
+    sh.S[wave] = S;
+    sh.A[wave] = A;
+  }
+  __syncthreads();
+  l.S = waves_sum<WAVES>(sh.S);
+  // (a NaN in the list stays one)
+  l.factor = l.S == 0.0f ? 0.0f : a.lse ? exp2_32((l.tmax - a.lse[m]) * LOG2E) : 1.0f / l.S;
+  l.pi = l.S == 0.0f ? 0.0f : a.lse ? l.factor * l.S : l.S / l.S;
+  return l;
+}
+
+// The row's loss, by one thread.  (In 64 bits: it is a difference of numbers ten times its size.)
+template <typename T, int MODE>
+__device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, const RowSums &r, const DistillList &l,
+                                    const DistillEntry &label, const double *A_of_wave, int waves) {
+  const bool hard = label.id >= 0;
+  double loss = 0.0;
+  if (r.s == 0.0f) {  // no word left
+    if ((a.alpha > 0.0f && l.pi != 0.0f) || hard) loss = INFINITY;
+  } else {
+    const double tau = a.tau;
+    if (a.alpha > 0.0f && l.pi != 0.0f) {
+      double A = 0.0;
+      for (int i = 0; i < waves; ++i) A += A_of_wave[i];
+      const double n = a.lse ? (double)a.lse[m] : (double)l.tmax + log((double)l.S);
+      loss = (double)a.alpha * tau * tau * (double)l.pi * (A / (double)l.S + (double)r.m / tau + log((double)r.s) - n);
     }
-    a.loss[m] = (float)((double)w * loss);
+    if (hard) loss += (double)(1.0f - a.alpha) * ((double)r.m - (double)label.z + log((double)(MODE == DISTILL_ONE ? r.s : r.s1)));
   }
-  return o;
+  a.loss[m] = (float)((double)w * loss);
 }
 
 // The listed words' gradients, behind the dense pass: each word is written once, with everything that the list takes off it.
-template <typename T, int THREADS, bool TWO>
-__device__ inline void distill_listed(const DistillArgs<T> &a, const DistillRow &o, const DistillEntry *ent, T *drow) {
+template <typename T, int THREADS, int MODE>
+__device__ inline void distill_listed(const DistillArgs<T> &a, const DistillDense<MODE> &dense, float coef, float hard,
+                                      const DistillEntry *ent, T *drow) {
   for (int e = threadIdx.x; e <= a.K; e += THREADS) {
     const int id = ent[e].id;
     if (id < 0) continue;
-    float off = 0.0f;
+    float p = 0.0f;
     bool first = true;
-    for (int j = 0; j <= a.K; ++j)
+    for (int j = 0; j < a.K; ++j)
       if (ent[j].id == id) {
-        off += ent[j].coef;
+        p += ent[j].p;
         first = first && j >= e;
       }
-    if (first) drow[id] = from_f32<T>(o.dense(ent[e].z, TWO) - off);
+    if (!first) continue;
+    float off = coef * p;
+    if (ent[a.K].id == id) off += hard;
+    drow[id] = from_f32<T>(dense(ent[e].z) - off);
   }
 }
 
@@ -154,119 +223,42 @@ __device__ inline void distill_without_weight(const DistillArgs<T> &a, long m) {
   if (at < a.V) drow[at] = from_f32<T>(0.0f);
 }
 
-// A workgroup's row stays in registers between the sums and the gradient: the row is read once and its gradient written once,
-// which is all that bounds the call (HBM).  NV: slots of a thread.  TWO: tau != 1 and labels (two exponentials an element).
-template <typename T, int THREADS, int NV, bool TWO>
-__global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillArgs<T> a) {
-  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
-  extern __shared__ __align__(16) unsigned char lds[];
-  DistillEntry *ent = reinterpret_cast<DistillEntry *>(lds);
-  __shared__ float sh_m[WAVES], sh_t[WAVES], sh_s[WAVES], sh_s1[WAVES];
-  __shared__ double sh_S[WAVES], sh_A[WAVES];
-  const long m = blockIdx.x;
-  const float w = a.weight ? a.weight[m] : 1.0f;
-  if (w == 0.0f) return distill_without_weight<T, THREADS>(a, m);
-  const T *row = a.z + m * a.ldz;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
-  slot_t raw[NV];
+// The waves' sums joined: references may differ.
+template <int THREADS, int MODE>
+__device__ inline RowSums distill_join(const DistillShared<THREADS / 64> &sh, float tau) {
+  constexpr int WAVES = THREADS / 64;
+  RowSums r = {waves_max<WAVES>(sh.m), 0.0f, 0.0f};
+  if (r.m == -INFINITY) r.m = 0.0f;
+  const int wave = threadIdx.x & (WAVES - 1);
+  r.s = sh.s[wave];
+  r.s1 = MODE == DISTILL_ONE ? 0.0f : sh.s1[wave];
+  DistillExp<MODE>(r.m, tau).move(sh.m[wave], r.s, r.s1);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int j = i * THREADS + tid;
-    raw[i] = j < full ? load_slot(row, j) : empty_slot<T>();
+  for (int o = WAVES / 2; o > 0; o >>= 1) {
+    r.s += __shfl_xor(r.s, o, 64);
+    if (MODE != DISTILL_ONE) r.s1 += __shfl_xor(r.s1, o, 64);
   }
-  const float zt = tail_elem(row, tid, a.V);
-  const float te = distill_entries<T, THREADS>(a, m, row, a.y && a.alpha < 1.0f, ent);
-  float mx = zt;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    mx = slot_max<T>(mx, raw[i]);
-    keep_packed(raw[i]);
-  }
-  mx = wave_max(mx);
-  const float tw = wave_max(te);
-  if (lane == 0) {
-    sh_m[wave] = mx;
-    sh_t[wave] = tw;
-  }
-  __syncthreads();
-  float tmax = sh_t[0];
-  mx = sh_m[0];
-#pragma unroll
-  for (int i = 1; i < WAVES; ++i) {
-    mx = fmaxf(mx, sh_m[i]);
-    tmax = fmaxf(tmax, sh_t[i]);
-  }
-  const float base = mx == -INFINITY ? 0.0f : mx, c = LOG2E / a.tau, b = -base * c, b1 = -base * LOG2E;
-  float s = exp2_32(fmaf(zt, c, b)), s1 = TWO ? exp2_32(fmaf(zt, LOG2E, b1)) : 0.0f;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (i * THREADS + wave * 64 >= full) break;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float z = slot_elem<T>(raw[i], e);
-      s += exp2_32(fmaf(z, c, b));
-      if (TWO) s1 += exp2_32(fmaf(z, LOG2E, b1));
-    }
-    keep_packed(raw[i]);
-  }
-  double S, A;
-  distill_list_sums<THREADS>(ent, a.K, 1.0f / a.tau, tmax, S, A);
-  s = wave_sum(s);
-  if (TWO) s1 = wave_sum(s1);
-  if (wave * 64 < a.K) {
-    S = wave_sum(S);
-    A = wave_sum(A);
-  }
-  if (lane == 0) {
-    sh_s[wave] = s;
-    if (TWO) sh_s1[wave] = s1;
-    sh_S[wave] = S;
-    sh_A[wave] = A;
-  }
-  __syncthreads();
-  RowSums r = {mx, 0.0f, 0.0f};
-  S = A = 0.0;
-#pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    r.s += sh_s[i];
-    if (TWO) r.s1 += sh_s1[i];
-    S += sh_S[i];
-    A += sh_A[i];
-  }
-  const DistillRow o = distill_finish<T, THREADS, TWO>(a, m, w, r, tmax, S, A, ent);
-  if (!a.dz) return;
-  T *drow = a.dz + m * a.ldd;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int j = i * THREADS + tid;
-    if (j >= full) break;
-    float d[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) d[e] = o.dense(slot_elem<T>(raw[i], e), TWO);
-    store_slot(drow, j, d);
-  }
-  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(o.dense(zt, TWO));
-  __syncthreads();  // the dense pass first, then the listed words on top of it
-  distill_listed<T, THREADS, TWO>(a, o, ent, drow);
+  return r;
 }
 
-// Rows that do not fit the registers, and calls without a gradient: one pass with a running maximum and sum of each thread,
-// then (with a gradient) a second one.
-template <typename T, int THREADS, bool TWO>
-__global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillArgs<T> a) {
-  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64, FLIGHT = 4;
-  extern __shared__ __align__(16) unsigned char lds[];
-  DistillEntry *ent = reinterpret_cast<DistillEntry *>(lds);
-  __shared__ float sh_m[WAVES], sh_t[WAVES], sh_s[WAVES], sh_s1[WAVES];
-  __shared__ double sh_S[WAVES], sh_A[WAVES];
-  const long m = blockIdx.x;
-  const float w = a.weight ? a.weight[m] : 1.0f;
-  if (w == 0.0f) return distill_without_weight<T, THREADS>(a, m);
-  const T *row = a.z + m * a.ldz;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
-  const float c = LOG2E / a.tau;
-  const float te = distill_entries<T, THREADS>(a, m, row, a.y && a.alpha < 1.0f, ent);
-  const float zt = tail_elem(row, tid, a.V);
+// A wave's sums and their reference, for the workgroup.
+template <int MODE, int WAVES>
+__device__ inline void distill_publish(DistillShared<WAVES> &sh, float ref, float s, float s1) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  s = wave_sum(s);
+  if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
+  if ((threadIdx.x & 63) == 0) {
+    sh.m[wave] = ref;
+    sh.s[wave] = s;
+    sh.s1[wave] = s1;
+  }
+}
+
+// The row's sums in one pass with a running maximum and sum of each thread (zt: its element behind the whole slots).
+template <typename T, int THREADS, int MODE, int FLIGHT>
+__device__ inline void distill_stream(const DistillArgs<T> &a, const T *row, float zt, DistillShared<THREADS / 64> &sh) {
+  constexpr int N = SlotOf<T>::N;
+  const int tid = threadIdx.x, full = a.V / N;
   float mx = zt, s = zt == -INFINITY ? 0.0f : 1.0f, s1 = s;
   for (int j0 = tid; j0 < full; j0 += FLIGHT * THREADS) {
     slot_t raw[FLIGHT];
@@ -278,76 +270,121 @@ __global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillAr
     float top = mx;
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i) top = slot_max<T>(top, raw[i]);
-    const float base = top == -INFINITY ? 0.0f : top, b = -base * c, b1 = -base * LOG2E;
+    const DistillExp<MODE> ex(top == -INFINITY ? 0.0f : top, a.tau);
     if (top > mx) {  // (mx = -inf: the sums are 0, and so is the factor)
-      s *= exp2_32(fmaf(mx, c, b));
-      if (TWO) s1 *= exp2_32(fmaf(mx, LOG2E, b1));
+      ex.move(mx, s, s1);
       mx = top;
     }
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float z = slot_elem<T>(raw[i], e);
-        s += exp2_32(fmaf(z, c, b));
-        if (TWO) s1 += exp2_32(fmaf(z, LOG2E, b1));
-      }
+      for (int e = 0; e < N; ++e) ex.add(slot_elem<T>(raw[i], e), s, s1);
   }
-  const float own = mx;
-  mx = wave_max(mx);
-  const float tw = wave_max(te);
+  const float top = wave_max(mx);
+  DistillExp<MODE>(top == -INFINITY ? 0.0f : top, a.tau).move(mx, s, s1);
+  distill_publish<MODE>(sh, top, s, s1);
+}
+
+// A workgroup's row stays in registers between the sums and the gradient: the row is read once and its gradient written once,
+// which is all that bounds the call (HBM, with the exponentials' instructions not far behind).  NV: slots of a thread.
+// The sums run while the row arrives: a wave's reference is the greatest element of its first slots, so a later element of
+// it can only overflow by being e^88 times greater, and the sum cannot vanish.  Where a sum is no number after all, or a wave's
+// first slots are masked throughout, the row's maximum is formed and the sums are repeated.
+template <typename T, int THREADS, int NV, int MODE>
+__global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillArgs<T> a) {
+  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
+  extern __shared__ __align__(16) unsigned char lds[];
+  DistillEntry *ent = reinterpret_cast<DistillEntry *>(lds);
+  __shared__ DistillShared<WAVES> sh;
+  const long m = blockIdx.x;
+  const float w = a.weight ? a.weight[m] : 1.0f;
+  if (w == 0.0f) return distill_without_weight<T, THREADS>(a, m);
+  const T *row = a.z + m * a.ldz;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
+  slot_t raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    raw[i] = i * THREADS + tid < full ? load_slot(row + i * THREADS * N, tid) : empty_slot<T>();
+  }
+  const float zt = tail_elem(row, tid, a.V);
+  const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
+  const float ref = wave_max(slot_max<T>(zt, raw[0]));
+  const DistillExp<MODE> ex(ref == -INFINITY ? 0.0f : ref, a.tau);
+  float s = 0.0f, s1 = 0.0f;
+  ex.add(zt, s, s1);
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < N; ++e) ex.add(slot_elem<T>(raw[i], e), s, s1);
+  distill_publish<MODE>(sh, ref, s, s1);
+  const float sum = s + s1;
+  const bool again = __any(!(sum - sum == 0.0f)) || (ref == -INFINITY && wave * 64 < full);
   if (lane == 0) {
-    sh_m[wave] = mx;
-    sh_t[wave] = tw;
+    sh.t[wave] = tw;
+    sh.again[wave] = again ? 1.0f : 0.0f;
   }
   __syncthreads();
-  float tmax = sh_t[0];
-  mx = sh_m[0];
+  if (waves_max<WAVES>(sh.again) != 0.0f) {
+    __syncthreads();
+    distill_stream<T, THREADS, MODE, 1>(a, row, zt, sh);
+    __syncthreads();
+  }
+  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);
+  const RowSums r = distill_join<THREADS, MODE>(sh, a.tau);
+  const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
+  const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
+  T *drow = a.dz + m * a.ldd;
 #pragma unroll
-  for (int i = 1; i < WAVES; ++i) {
-    mx = fmaxf(mx, sh_m[i]);
-    tmax = fmaxf(tmax, sh_t[i]);
+  for (int i = 0; i < NV; ++i) {
+    keep_packed(raw[i]);
+    if (i * THREADS + tid < full) {
+      float d[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) d[e] = dense.bare(slot_elem<T>(raw[i], e));
+      store_slot(drow + i * THREADS * N, tid, d, dense.template flip<T>());
+    }
   }
-  const float base = mx == -INFINITY ? 0.0f : mx;
-  s *= exp2_32(fmaf(own, c, -base * c));
-  if (TWO) s1 *= exp2_32(fmaf(own, LOG2E, -base * LOG2E));
-  double S, A;
-  distill_list_sums<THREADS>(ent, a.K, 1.0f / a.tau, tmax, S, A);
-  s = wave_sum(s);
-  if (TWO) s1 = wave_sum(s1);
-  if (wave * 64 < a.K) {
-    S = wave_sum(S);
-    A = wave_sum(A);
-  }
-  if (lane == 0) {
-    sh_s[wave] = s;
-    if (TWO) sh_s1[wave] = s1;
-    sh_S[wave] = S;
-    sh_A[wave] = A;
-  }
+  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense(zt));
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
+  __syncthreads();  // the dense pass first, then the listed words on top of it
+  distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
+}
+
+// Rows that do not fit the registers, and calls without a gradient: one pass with a running maximum and sum of each thread,
+// then (with a gradient) a second one.
+template <typename T, int THREADS, int MODE>
+__global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillArgs<T> a) {
+  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
+  extern __shared__ __align__(16) unsigned char lds[];
+  DistillEntry *ent = reinterpret_cast<DistillEntry *>(lds);
+  __shared__ DistillShared<WAVES> sh;
+  const long m = blockIdx.x;
+  const float w = a.weight ? a.weight[m] : 1.0f;
+  if (w == 0.0f) return distill_without_weight<T, THREADS>(a, m);
+  const T *row = a.z + m * a.ldz;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
+  const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
+  const float zt = tail_elem(row, tid, a.V);
+  distill_stream<T, THREADS, MODE, 4>(a, row, zt, sh);
+  if (lane == 0) sh.t[wave] = tw;
   __syncthreads();
-  RowSums r = {mx, 0.0f, 0.0f};
-  S = A = 0.0;
-#pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    r.s += sh_s[i];
-    if (TWO) r.s1 += sh_s1[i];
-    S += sh_S[i];
-    A += sh_A[i];
-  }
-  const DistillRow o = distill_finish<T, THREADS, TWO>(a, m, w, r, tmax, S, A, ent);
+  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);
+  const RowSums r = distill_join<THREADS, MODE>(sh, a.tau);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
   if (!a.dz) return;
+  const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
+  const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
   T *drow = a.dz + m * a.ldd;
   for (int j = tid; j < full; j += THREADS) {
     const slot_t raw = load_slot(row, j);
     float d[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) d[e] = o.dense(slot_elem<T>(raw, e), TWO);
-    store_slot(drow, j, d);
+    for (int e = 0; e < N; ++e) d[e] = dense.bare(slot_elem<T>(raw, e));
+    store_slot(drow, j, d, dense.template flip<T>());
   }
-  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(o.dense(zt, TWO));
+  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense(zt));
   __syncthreads();
-  distill_listed<T, THREADS, TWO>(a, o, ent, drow);
+  distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
 }
 
 // Sum of n losses in 64 bits, in a fixed order, by one workgroup.

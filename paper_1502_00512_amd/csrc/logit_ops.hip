@@ -80,37 +80,38 @@ void launch_top(const TopArgs &a, int64_t rows, int nv, hipStream_t st) {
 }
 
 // ---- distillation ----
-template <typename T, int THREADS, int NV, bool TWO>
+template <typename T, int THREADS, int NV, int MODE>
 void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
-  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, TWO>), dim3((unsigned)rows), dim3(THREADS),
+  hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, MODE>), dim3((unsigned)rows), dim3(THREADS),
                      (a.K + 1) * sizeof(DistillEntry), st, a);
 }
-template <typename T, bool TWO>
+template <typename T, int MODE>
 void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   const int slots = (a.V + SlotOf<T>::N - 1) / SlotOf<T>::N;
   if (!a.dz || slots > 1024 * 26) {
-    hipLaunchKernelGGL((distill_stream_kernel<T, 512, TWO>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
+    hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
                        st, a);
   } else if (slots <= 256) {
-    launch_distill_row<T, 256, 1, TWO>(a, rows, st);
+    launch_distill_row<T, 256, 1, MODE>(a, rows, st);
   } else if (slots <= 256 * 4) {
-    launch_distill_row<T, 256, 4, TWO>(a, rows, st);
+    launch_distill_row<T, 256, 4, MODE>(a, rows, st);
   } else if (slots <= 256 * 8) {
-    launch_distill_row<T, 256, 8, TWO>(a, rows, st);
+    launch_distill_row<T, 256, 8, MODE>(a, rows, st);
   } else if (slots <= 512 * 8) {
-    launch_distill_row<T, 512, 8, TWO>(a, rows, st);
+    launch_distill_row<T, 512, 8, MODE>(a, rows, st);
   } else if (slots <= 512 * 16) {
-    launch_distill_row<T, 512, 16, TWO>(a, rows, st);
+    launch_distill_row<T, 512, 16, MODE>(a, rows, st);
   } else if (slots <= 512 * 26) {
-    launch_distill_row<T, 512, 26, TWO>(a, rows, st);
+    launch_distill_row<T, 512, 26, MODE>(a, rows, st);
   } else {
-    launch_distill_row<T, 1024, 26, TWO>(a, rows, st);
+    launch_distill_row<T, 1024, 26, MODE>(a, rows, st);
   }
 }
 template <typename T>
 int distill_call(DistillArgs<T> a, int64_t rows, hipStream_t st) {
-  if (a.y && a.alpha < 1.0f && a.tau != 1.0f) launch_distill<T, true>(a, rows, st);
-  else launch_distill<T, false>(a, rows, st);
+  if (!a.y || a.alpha == 1.0f || a.tau == 1.0f) launch_distill<T, DISTILL_ONE>(a, rows, st);
+  else if (a.tau == 2.0f) launch_distill<T, DISTILL_SQUARE>(a, rows, st);
+  else launch_distill<T, DISTILL_TWO>(a, rows, st);
   LAUNCHED();
   return RNNLM_OK;
 }

@@ -45,13 +45,14 @@ __device__ inline slot_t empty_slot() {  // -inf in every element
   return slot_t{w, w, w, w};
 }
 
-// Whole slot j of a row.  The elements behind a row's last whole slot are taken one by one (tail_elem).
+// Whole slot j of a row (store_slot: flip is laid over each 32 bits, the sign bits of a gradient with a negative factor).  The elements behind a row's last whole slot are taken one by one (tail_elem).
 template <typename T>
 __device__ inline slot_t load_slot(const T *row, int j) {
-  return *reinterpret_cast<const typename SlotOf<T>::type *>(row + j * SlotOf<T>::N);
+  // (an unsigned 32-bit offset from a row that all lanes share: no 64-bit address in registers)
+  return *reinterpret_cast<const typename SlotOf<T>::type *>(reinterpret_cast<const char *>(row) + (unsigned)j * 16u);
 }
 template <typename T>
-__device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N]) {
+__device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N], unsigned flip = 0) {
   constexpr int N = SlotOf<T>::N;
   union {
     slot_t s;
@@ -59,7 +60,9 @@ __device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N])
   } o;
 #pragma unroll
   for (int e = 0; e < N; ++e) o.t[e] = from_f32<T>(v[e]);
-  *reinterpret_cast<typename SlotOf<T>::type *>(row + j * N) = o.s;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o.s[e] ^= flip;
+  *reinterpret_cast<typename SlotOf<T>::type *>(reinterpret_cast<char *>(row) + (unsigned)j * 16u) = o.s;
 }
 // Element of the row behind its whole slots that thread tid takes; -inf for the others.
 template <typename T>
@@ -108,6 +111,23 @@ __device__ inline X wave_reduce(X v, Op &&op) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
   return v;
+}
+// The same over WAVES numbers of LDS (a power of two, one a wave of the workgroup), for every lane: each group of WAVES lanes
+// reads them all.  (Unrolled over registers instead, 16 waves' numbers took 16 registers for each sum.)
+template <int WAVES, class Op>
+__device__ inline float waves_reduce(const float *of_wave, Op &&op) {
+  float v = of_wave[threadIdx.x & (WAVES - 1)];
+#pragma unroll
+  for (int o = WAVES / 2; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
+  return v;
+}
+template <int WAVES>
+__device__ inline float waves_max(const float *of_wave) {
+  return waves_reduce<WAVES>(of_wave, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int WAVES>
+__device__ inline float waves_sum(const float *of_wave) {
+  return waves_reduce<WAVES>(of_wave, [](float a, float b) { return a + b; });
 }
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });

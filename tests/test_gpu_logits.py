@@ -56,6 +56,8 @@ def patterns(kind, rows, V, seed):
         z[:, V // 2] = np.inf
     elif kind == "clustered":  # all the large ones next to each other
         z[:, : min(V, 300)] += 40.0
+    elif kind == "steep":  # far apart: later words dwarf the earlier ones
+        z = np.linspace(-200.0, 250.0, V)[None] + z
     elif kind == "lowest":  # masks of the type's lowest value
         z[rng.random((rows, V)) < 0.9] = -3e38
     return z
@@ -136,6 +138,8 @@ def check_distill(z, ids, vals, y, w, dtype, pad=0, tau=1.0, alpha=0.5, scale=0.
         yr = -1 if y is None else int(y[r])
         nr = None if n is None else float(n[r])
         l, gr = L.distill(ref[r], ids[r], vals[r], nr, yr, float(w_[r]), tau, alpha, scale)
+        if abs(l) > float(torch.finfo(torch.float32).max):  # a label's or a listed word's logit at the type's lowest value
+            l = np.inf
         there = (ids[r] >= 0) & (ids[r] < V) & np.isfinite(vals[r])
         t = vals[r][there].astype(np.float64) / tau
         norm = nr if nr is not None else (L.lse(t) if len(t) else 0.0)
@@ -175,6 +179,22 @@ def check_distill(z, ids, vals, y, w, dtype, pad=0, tau=1.0, alpha=0.5, scale=0.
                                           (1, 300001, 16, 0)])
 def test_distill_sizes(rows, V, K, pad, dtype):
     check_distill(patterns("normal", rows, V, V), *lists(rows, V, K, V + 1, False), dtype, pad, tau=2.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+@pytest.mark.parametrize("kind", ["equal", "steep", "falling", "clustered", "lowest", "late"])
+@pytest.mark.parametrize("V", [1203, 9001, 70001])
+def test_distill_patterns(V, kind, tau, dtype):
+    z = patterns("normal" if kind == "late" else kind, 2, V, 5)
+    ids, vals, y, w = lists(2, V, 9, 4, False)
+    if kind == "falling":
+        z *= 60.0
+    if kind == "late":  # only the last words are left, far below zero
+        z[:, : V - 300] = -np.inf
+        z[:, V - 300:] -= 500.0
+        ids, y = V - 1 - ids % 300, V - 1 - y % 300
+    check_distill(z, ids.astype(np.int32), vals, y.astype(np.int32), w, dtype, tau=tau)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
