@@ -22,6 +22,7 @@ struct DistillArgs {
   int32_t *range_flag;
   float tau, alpha, scale;
   int V, K;
+  bool once;  // read past the caches
 };
 
 // Exponentials of an element.  ONE: a single temperature (tau = 1, or no labels).  SQUARE: tau = 2 and labels, whose
@@ -255,7 +256,7 @@ __device__ inline void distill_publish(DistillShared<WAVES> &sh, float ref, floa
 }
 
 // The row's sums in one pass with a running maximum and sum of each thread (zt: its element behind the whole slots).
-template <typename T, int THREADS, int MODE, int FLIGHT>
+template <typename T, int THREADS, int MODE, int FLIGHT, bool ONCE = false>
 __device__ inline void distill_stream(const DistillArgs<T> &a, const T *row, float zt, DistillShared<THREADS / 64> &sh) {
   constexpr int N = SlotOf<T>::N;
   const int tid = threadIdx.x, full = a.V / N;
@@ -265,7 +266,7 @@ __device__ inline void distill_stream(const DistillArgs<T> &a, const T *row, flo
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i) {
       const int j = j0 + i * THREADS;
-      raw[i] = j < full ? load_slot(row, j) : empty_slot<T>();
+      raw[i] = j < full ? load_slot<T, ONCE>(row, j) : empty_slot<T>();
     }
     float top = mx;
 #pragma unroll
@@ -302,9 +303,12 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
   const T *row = a.z + m * a.ldz;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
   slot_t raw[NV];
+  if (a.once) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    raw[i] = i * THREADS + tid < full ? load_slot(row + i * THREADS * N, tid) : empty_slot<T>();
+    for (int i = 0; i < NV; ++i) raw[i] = i * THREADS + tid < full ? load_slot<T, true>(row + i * THREADS * N, tid) : empty_slot<T>();
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = i * THREADS + tid < full ? load_slot(row + i * THREADS * N, tid) : empty_slot<T>();
   }
   const float zt = tail_elem(row, tid, a.V);
   const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
@@ -365,7 +369,8 @@ __global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillAr
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
   const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
   const float zt = tail_elem(row, tid, a.V);
-  distill_stream<T, THREADS, MODE, 4>(a, row, zt, sh);
+  if (a.once && !a.dz) distill_stream<T, THREADS, MODE, 4, true>(a, row, zt, sh);
+  else distill_stream<T, THREADS, MODE, 4>(a, row, zt, sh);
   if (lane == 0) sh.t[wave] = tw;
   __syncthreads();
   const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);

@@ -26,6 +26,7 @@ bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 size_t elem_bytes(int32_t dtype) { return dtype == RNNLM_DTYPE_FP32 ? 4 : 2; }
 // 16-byte slots of a row, the last of them possibly not whole
 int slots_of(int32_t V, int32_t dtype) { return (int)(((int64_t)V * (int64_t)elem_bytes(dtype) + 15) / 16); }
+bool read_once(int64_t rows, int32_t V, int32_t dtype) { return (double)rows * V * (double)elem_bytes(dtype) > (double)READ_ONCE_BYTES; }
 bool tau_ok(float tau) { return std::isfinite(tau) && tau >= 1e-3f && tau <= 1e3f; }
 
 // rows of V elements, ld apart: addresses stay within what 64 bits and the kernels' 32-bit element counts reach
@@ -46,20 +47,25 @@ bool meet(Span a, Span b) { return a.at < b.end && b.at < a.end; }
 
 // ---- top logits ----
 struct TopPlan {
-  int chunks, per, nv;
+  int chunks, per, threads, nv;
 };
-constexpr int TOP_NV_MAX = 16;
-// One chunk a row as long as it fits the registers and the rows alone fill the chip, else shorter ones.
+// Whole rows in a workgroup's registers where they fit (no second launch), else chunks, shorter ones where the rows are few.
 TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   const int slots = slots_of(V, dtype);
-  int nv = TOP_NV_MAX;
-  auto chunks = [&](int n) { return (slots + n * TOP_THREADS - 1) / (n * TOP_THREADS); };
-  while (nv > 2 && rows * chunks(nv) < 512 && chunks(nv / 2) * K <= TOP_MERGE_LDS) nv /= 2;
   TopPlan p;
-  p.chunks = chunks(nv);
+  p.threads = 256;
+  p.nv = 16;
+  auto chunks = [&]() { return (slots + p.nv * p.threads - 1) / (p.nv * p.threads); };
+  if (chunks() == 1) {
+    while (p.nv > 2 && p.nv / 2 * p.threads >= slots) p.nv /= 2;
+  } else if (slots <= TOP_WIDE * 16 && rows >= 512) {
+    p.threads = TOP_WIDE;
+  } else {
+    while (p.nv > 2 && rows * chunks() < 512 && 2 * chunks() * K <= TOP_MERGE_LDS) p.nv /= 2;
+  }
+  p.chunks = chunks();
   p.per = (slots + p.chunks - 1) / p.chunks;
   p.chunks = (slots + p.per - 1) / p.per;
-  p.nv = nv;
   return p;
 }
 size_t top_bytes(const TopPlan &p, int64_t rows, int32_t K) {
@@ -70,13 +76,17 @@ bool top_sizes_ok(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   return rows >= 0 && rows <= GRID_MAX / 1024 && V >= 1 && V <= TOP_V_MAX && K >= 1 && K <= std::min(V, TOP_K_MAX) &&
          (dtype == RNNLM_DTYPE_FP32 || dtype == RNNLM_DTYPE_BF16);
 }
+template <typename T, int THREADS, int NV>
+void launch_top_chunks(const TopArgs &a, int64_t rows, hipStream_t st) {
+  hipLaunchKernelGGL((top_chunk_kernel<T, THREADS, NV>), dim3((unsigned)(rows * a.chunks)), dim3(THREADS), 0, st, a);
+}
 template <typename T>
-void launch_top(const TopArgs &a, int64_t rows, int nv, hipStream_t st) {
-  const dim3 grid((unsigned)(rows * a.chunks)), threads(TOP_THREADS);
-  if (nv == 2) hipLaunchKernelGGL((top_chunk_kernel<T, 2>), grid, threads, 0, st, a);
-  else if (nv == 4) hipLaunchKernelGGL((top_chunk_kernel<T, 4>), grid, threads, 0, st, a);
-  else if (nv == 8) hipLaunchKernelGGL((top_chunk_kernel<T, 8>), grid, threads, 0, st, a);
-  else hipLaunchKernelGGL((top_chunk_kernel<T, 16>), grid, threads, 0, st, a);
+void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st) {
+  if (p.threads == TOP_WIDE) launch_top_chunks<T, TOP_WIDE, 16>(a, rows, st);
+  else if (p.nv == 2) launch_top_chunks<T, 256, 2>(a, rows, st);
+  else if (p.nv == 4) launch_top_chunks<T, 256, 4>(a, rows, st);
+  else if (p.nv == 8) launch_top_chunks<T, 256, 8>(a, rows, st);
+  else launch_top_chunks<T, 256, 16>(a, rows, st);
 }
 
 // ---- distillation ----
@@ -87,24 +97,36 @@ void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
 }
 template <typename T, int MODE>
 void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
-  const int slots = (a.V + SlotOf<T>::N - 1) / SlotOf<T>::N;
-  if (!a.dz || slots > 1024 * 26) {
+  const int slots = a.V / SlotOf<T>::N;  // whole ones: what a thread's registers hold
+  if (!a.dz || slots > 1024 * 25) {
     hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
                        st, a);
   } else if (slots <= 256) {
     launch_distill_row<T, 256, 1, MODE>(a, rows, st);
+  } else if (slots <= 256 * 2) {
+    launch_distill_row<T, 256, 2, MODE>(a, rows, st);
   } else if (slots <= 256 * 4) {
     launch_distill_row<T, 256, 4, MODE>(a, rows, st);
+  } else if (slots <= 256 * 6) {
+    launch_distill_row<T, 256, 6, MODE>(a, rows, st);
   } else if (slots <= 256 * 8) {
     launch_distill_row<T, 256, 8, MODE>(a, rows, st);
+  } else if (slots <= 512 * 6) {
+    launch_distill_row<T, 512, 6, MODE>(a, rows, st);
   } else if (slots <= 512 * 8) {
     launch_distill_row<T, 512, 8, MODE>(a, rows, st);
+  } else if (slots <= 512 * 12) {
+    launch_distill_row<T, 512, 12, MODE>(a, rows, st);
   } else if (slots <= 512 * 16) {
     launch_distill_row<T, 512, 16, MODE>(a, rows, st);
-  } else if (slots <= 512 * 26) {
-    launch_distill_row<T, 512, 26, MODE>(a, rows, st);
+  } else if (slots <= 512 * 20) {
+    launch_distill_row<T, 512, 20, MODE>(a, rows, st);
+  } else if (slots <= 512 * 25) {
+    launch_distill_row<T, 512, 25, MODE>(a, rows, st);
+  } else if (slots <= 1024 * 18) {
+    launch_distill_row<T, 1024, 18, MODE>(a, rows, st);
   } else {
-    launch_distill_row<T, 1024, 26, MODE>(a, rows, st);
+    launch_distill_row<T, 1024, 25, MODE>(a, rows, st);
   }
 }
 template <typename T>
@@ -185,16 +207,17 @@ int rnnlm_top_logits(const void *logits, int32_t dtype, int64_t rows, int32_t V,
   a.ids = ids;
   a.vals = vals;
   a.lse = lse;
+  a.once = read_once(rows, V, dtype);
   if (need) {
     a.part = static_cast<unsigned long long *>(workspace);
     a.stat = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + align256((size_t)rows * p.chunks * K * 8));
   }
   hipStream_t st = (hipStream_t)stream;
-  if (dtype == RNNLM_DTYPE_FP32) launch_top<float>(a, rows, p.nv, st);
-  else launch_top<bf16_t>(a, rows, p.nv, st);
+  if (dtype == RNNLM_DTYPE_FP32) launch_top<float>(a, rows, p, st);
+  else launch_top<bf16_t>(a, rows, p, st);
   LAUNCHED();
   if (p.chunks > 1) {
-    hipLaunchKernelGGL(top_merge_kernel, dim3((unsigned)rows), dim3(TOP_THREADS), 0, st, a);
+    hipLaunchKernelGGL(top_merge_kernel, dim3((unsigned)rows), dim3(TOP_MERGE_THREADS), 0, st, a);
     LAUNCHED();
   }
   return RNNLM_OK;
@@ -211,6 +234,7 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
       !aligned(loss, 4) || !aligned(sum_loss, 8) || !aligned(range_flag, 4))
     return RNNLM_ERR_ARG;
   const size_t es = elem_bytes(dtype);
+  const bool once = read_once(rows, V, dtype);
   if (dlogits) {
     if (!rows_ok(dlogits, dtype, rows, V, ld_dlogits)) return RNNLM_ERR_ARG;
     // in place row by row, or apart
@@ -224,11 +248,11 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
     int rc;
     if (dtype == RNNLM_DTYPE_FP32) {
       rc = distill_call(DistillArgs<float>{static_cast<const float *>(logits), ld, static_cast<float *>(dlogits), ld_dlogits, ids, y,
-                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K},
+                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once},
                         rows, st);
     } else {
       rc = distill_call(DistillArgs<bf16_t>{static_cast<const bf16_t *>(logits), ld, static_cast<bf16_t *>(dlogits), ld_dlogits,
-                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K},
+                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once},
                         rows, st);
     }
     if (rc) return rc;

@@ -5,6 +5,11 @@
 
 namespace rnnlm_dev {
 
+// Rows of more bytes than this in a call are read past the caches: more than half of the memory-side cache's 256 MB, so little
+// of them is still there from whoever wrote them.  Read so and ordinarily: 164 MB (loss only) 30.4 and 33.4 us, 328 MB (with
+// gradient) 132 and 138, but 51 MB 27.8 and 24.5, 120 MB 58.3 and 54.5.
+constexpr long READ_ONCE_BYTES = 128L << 20;
+
 constexpr float LOG2E = 1.44269504088896340736f;
 constexpr double LOG2E_64 = 1.44269504088896340736, LN2_64 = 0.693147180559945309417;
 
@@ -46,11 +51,17 @@ __device__ inline slot_t empty_slot() {  // -inf in every element
 }
 
 // Whole slot j of a row (store_slot: flip is laid over each 32 bits, the sign bits of a gradient with a negative factor).  The elements behind a row's last whole slot are taken one by one (tail_elem).
-template <typename T>
+// once: nobody reads it again soon, it need not displace anything in the caches.
+template <typename T, bool ONCE = false>
 __device__ inline slot_t load_slot(const T *row, int j) {
   // (an unsigned 32-bit offset from a row that all lanes share: no 64-bit address in registers)
-  return *reinterpret_cast<const typename SlotOf<T>::type *>(reinterpret_cast<const char *>(row) + (unsigned)j * 16u);
+  const auto *p = reinterpret_cast<const typename SlotOf<T>::type *>(reinterpret_cast<const char *>(row) + (unsigned)j * 16u);
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  return *p;
 }
+// Gradients are written past the caches: they are as large as the logits, and with ordinary stores the rows that other
+// workgroups are about to read were displaced (2560 rows of 10000 bf16 words 30.2 -> 24.5 us, of 64000 149 -> 138; 8192 of
+// 100000 733 -> 691).
 template <typename T>
 __device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N], unsigned flip = 0) {
   constexpr int N = SlotOf<T>::N;
@@ -62,7 +73,7 @@ __device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N],
   for (int e = 0; e < N; ++e) o.t[e] = from_f32<T>(v[e]);
 #pragma unroll
   for (int e = 0; e < 4; ++e) o.s[e] ^= flip;
-  *reinterpret_cast<typename SlotOf<T>::type *>(reinterpret_cast<char *>(row) + (unsigned)j * 16u) = o.s;
+  __builtin_nontemporal_store(o.s, reinterpret_cast<typename SlotOf<T>::type *>(reinterpret_cast<char *>(row) + (unsigned)j * 16u));
 }
 // Element of the row behind its whole slots that thread tid takes; -inf for the others.
 template <typename T>
@@ -88,6 +99,9 @@ __device__ inline slot_t load_any_slot(const T *row, int j, int V) {
 // Makes the compiler unpack a slot anew where it is used again: elements of a bf16 slot kept unpacked take twice its
 // registers (a row that fits them spilled 280 of them).
 __device__ inline void keep_packed(slot_t &s) { asm volatile("" : "+v"(s)); }
+
+// Makes the compiler work a value out by here.
+__device__ inline void keep_here(float &v) { asm volatile("" : "+v"(v)); }
 
 // The greatest of three numbers (NaNs lose).  (fmaxf of values from memory costs an instruction more for each of them, which
 // makes signalling NaNs quiet: two and a half instructions for two elements instead of one.)

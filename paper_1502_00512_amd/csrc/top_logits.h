@@ -2,7 +2,7 @@
 // A row is cut into chunks that fit a workgroup's registers, so it is read once.  A word is ranked by one 64-bit key, the
 // logit's bits in an order that integers have, above the complement of the id: keys differ, so the order is total and a result
 // does not depend on which wave arrives first.  (A NaN ranks with the masked words, -inf; -0 ranks with +0.)
-//   1. maxima of groups of elements (two groups a thread), maximum and sum of exponentials of the chunk
+//   1. maxima of groups of elements (two groups a thread), sum of exponentials of the chunk
 //   2. a threshold that at least K of the maxima reach, so at least K elements do: bisection over the maxima by one wave
 //   3. elements that reach it into LDS (K to about 1.5 K of them for rows without structure)
 //   4. their ranks among each other by counting
@@ -14,7 +14,7 @@
 namespace rnnlm_dev {
 
 constexpr int TOP_K_MAX = 256;
-constexpr int TOP_THREADS = 256, TOP_CAP = 1024, TOP_MERGE_LDS = 2048;
+constexpr int TOP_WIDE = 512, TOP_MERGE_THREADS = 256, TOP_CAP = 1024, TOP_MERGE_LDS = 2048;
 constexpr int TOP_V_MAX = 1 << 20;  // ids fit 20 bits
 constexpr unsigned TOP_MASKED = 0x007fffffu;  // order of -inf
 
@@ -39,7 +39,8 @@ struct TopArgs {
   int32_t *ids;
   float *vals, *lse;
   unsigned long long *part;  // [row][chunk][K], descending; 0 behind a chunk's last element
-  float2 *stat;              // [row][chunk]: maximum, sum of exponentials at tau relative to it
+  float2 *stat;              // [row][chunk]: a reference, sum of exponentials at tau relative to it
+  bool once;                 // read past the caches
 };
 
 __device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned long long key) {
@@ -51,11 +52,38 @@ __device__ inline float row_lse(float m, float s, float tau) {
   return s == 0.0f ? -INFINITY : (float)((double)m / (double)tau + log((double)s));
 }
 
-template <typename T, int NV>
-__global__ void __launch_bounds__(TOP_THREADS, 4) top_chunk_kernel(const TopArgs a) {
-  constexpr int N = SlotOf<T>::N, WAVES = TOP_THREADS / 64;
-  __shared__ float sh_m[WAVES], sh_s[WAVES];
-  __shared__ unsigned group[2 * TOP_THREADS];
+// A threshold that at least K of 64 G numbers reach, and few more; by one wave.  (Bisection: a count takes 2 G instructions.)
+template <int G>
+__device__ inline unsigned top_threshold(const unsigned *group, int K, unsigned greatest) {
+  unsigned g[G], low = 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    g[i] = group[i * 64 + (threadIdx.x & 63)];
+    low = min(low, g[i]);
+  }
+  low = wave_reduce(low, [](unsigned p, unsigned q) { return min(p, q); });
+  // at least K reach lo (all of them, to begin with), fewer reach hi
+  unsigned lo = __builtin_amdgcn_readfirstlane(low), hi = greatest + 1;
+  while (hi - lo > 1) {
+    const unsigned mid = lo + (hi - lo) / 2;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < G; ++i) n += __popcll(__ballot(g[i] >= mid));
+    if (n >= K) {
+      lo = mid;
+      if (n <= K + K / 8) break;
+    } else {
+      hi = mid;
+    }
+  }
+  return lo;
+}
+
+template <typename T, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) {
+  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
+  __shared__ float sh_m[WAVES], sh_s[WAVES], sh_ref[WAVES];
+  __shared__ unsigned group[2 * THREADS];
   __shared__ unsigned long long cand[TOP_CAP];
   __shared__ unsigned sh_t, sh_n, sh_count[2][WAVES];
   const long row = blockIdx.x / a.chunks;
@@ -63,85 +91,98 @@ __global__ void __launch_bounds__(TOP_THREADS, 4) top_chunk_kernel(const TopArgs
   const T *z = static_cast<const T *>(a.z) + row * a.ld;
   const int full = a.V / N, first = chunk * a.per, slots = min(a.per, full - first), K = a.K;
   slot_t raw[NV];
+  if (a.once) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int j = i * TOP_THREADS + tid;
-    raw[i] = j < slots ? load_slot(z, first + j) : empty_slot<T>();
+    for (int i = 0; i < NV; ++i) raw[i] = i * THREADS + tid < slots ? load_slot<T, true>(z + (first + i * THREADS) * N, tid) : empty_slot<T>();
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) raw[i] = i * THREADS + tid < slots ? load_slot(z + (first + i * THREADS) * N, tid) : empty_slot<T>();
   }
   const int tail = chunk == a.chunks - 1 ? full * N + tid : a.V;  // the last chunk has the row's last elements, one a thread
   const float zt = tail < a.V ? to_f32(z[tail]) : -INFINITY;
   if (tid == 0) sh_n = 0;
-  // 1.
-  float top[NV], half[2] = {zt, -INFINITY};
+  // 1.  The sum is relative to the greatest element of the wave's first slots, so it runs while the rest arrives.
+  const float c = LOG2E / a.tau, ref = wave_max(slot_max<T>(zt, raw[0])), b = ref == -INFINITY ? 0.0f : -ref * c;
+  float top[NV], half[2] = {max3(zt, -INFINITY, -INFINITY), -INFINITY}, s = exp2_32(fmaf(zt, c, b));
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     top[i] = slot_max<T>(-INFINITY, raw[i]);
-    half[i & 1] = fmaxf(half[i & 1], top[i]);
-    keep_packed(raw[i]);
-  }
-  group[tid] = logit_order(half[0]);
-  group[TOP_THREADS + tid] = logit_order(half[1]);
-  float mx = wave_max(fmaxf(half[0], half[1]));
-  if (lane == 0) sh_m[wave] = mx;
-  __syncthreads();
-  mx = sh_m[0];
-#pragma unroll
-  for (int i = 1; i < WAVES; ++i) mx = fmaxf(mx, sh_m[i]);
-  // 2.
-  if (wave == 0) {
-    unsigned g[2 * WAVES], low = 0xffffffffu;
-#pragma unroll
-    for (int i = 0; i < 2 * WAVES; ++i) {
-      g[i] = group[i * 64 + lane];
-      low = min(low, g[i]);
-    }
-    low = wave_reduce(low, [](unsigned p, unsigned q) { return min(p, q); });
-    // at least K of the maxima reach lo (0: all of them do), fewer reach hi; a little more than K will do
-    unsigned lo = K <= 2 * TOP_THREADS ? low : 0, hi = logit_order(mx) + 1;
-    while (hi - lo > 1) {
-      const unsigned mid = lo + (hi - lo) / 2;
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < 2 * WAVES; ++i) n += __popcll(__ballot(g[i] >= mid));
-      if (n >= K) {
-        lo = mid;
-        if (n <= K + K / 8) break;
-      } else {
-        hi = mid;
-      }
-    }
-    if (lane == 0) sh_t = lo;
-  }
-  const float base = mx == -INFINITY ? 0.0f : mx, c = LOG2E / a.tau, b = -base * c;
-  float s = exp2_32(fmaf(zt, c, b));
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (i * TOP_THREADS + wave * 64 >= slots) break;
+    half[i & 1] = max3(half[i & 1], top[i], -INFINITY);
 #pragma unroll
     for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(raw[i], e), c, b));
     keep_packed(raw[i]);
+    keep_here(s);  // (with the exponentials of many slots put off the kernel spilled 100 registers)
   }
+  const float both = max3(half[0], half[1], -INFINITY), mine = wave_max(both);
+  const bool pairs = K > THREADS / 4;  // two groups a thread for long lists
+  group[tid] = logit_order(pairs ? half[0] : both);
+  if (pairs) group[THREADS + tid] = logit_order(half[1]);
   s = wave_sum(s);
-  if (lane == 0) sh_s[wave] = s;
+  if (!(s - s == 0.0f) || (ref == -INFINITY && mine > -INFINITY)) {
+    // no number, or the first slots are masked throughout: once more, relative to the wave's maximum
+    const float again = mine == -INFINITY ? 0.0f : -mine * c;
+    s = exp2_32(fmaf(zt, c, again));
+    for (int j = tid; j < slots; j += THREADS) {
+      const slot_t q = load_slot(z, first + j);
+#pragma unroll
+      for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(q, e), c, again));
+    }
+    s = wave_sum(s);
+    if (lane == 0) sh_ref[wave] = mine;
+  } else if (lane == 0) {
+    sh_ref[wave] = ref;
+  }
+  if (lane == 0) {
+    sh_m[wave] = mine;
+    sh_s[wave] = s;
+  }
+  __syncthreads();
+  // 2.
+  if (wave == 0) {
+    const float mx = waves_max<WAVES>(sh_m);
+    const unsigned top_order = __builtin_amdgcn_readfirstlane(logit_order(mx));
+    const unsigned lo = pairs ? top_threshold<2 * WAVES>(group, K, top_order) : top_threshold<WAVES>(group, K, top_order);
+    if (lane == 0) sh_t = lo;
+  }
   __syncthreads();
   // 3.
   const unsigned thr = sh_t;
   const bool few = thr <= TOP_MASKED;  // some of the K are masked, or no element at all
   if (!few) {
+    // Of its slots that reach the threshold a lane takes one at a time, each lane its own (selected from the registers): the
+    // 64 lanes' few finds share the instructions.
     const float t = order_logit(thr);
-    auto take = [&](float v, int id) {
-      if (v >= t) {
-        const unsigned at = atomicAdd(&sh_n, 1u);
-        if (at < TOP_CAP) cand[at] = top_key(logit_order(v), id);
-      }
-    };
-    take(zt, tail);
+    unsigned left = 0;  // slots with finds
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (top[i] >= t) {
+    for (int i = 0; i < NV; ++i) left |= (top[i] >= t ? 1u : 0u) << i;
+    if (zt >= t) {
+      const unsigned at = atomicAdd(&sh_n, 1u);
+      if (at < TOP_CAP) cand[at] = top_key(logit_order(zt), tail);
+    }
+    while (__any(left != 0)) {
+      const int mine_at = left ? __builtin_ctz(left) : NV;
+      left &= left - 1;
+      slot_t q = empty_slot<T>();
 #pragma unroll
-        for (int e = 0; e < N; ++e) take(slot_elem<T>(raw[i], e), (first + i * TOP_THREADS + tid) * N + e);
+      for (int i = 0; i < NV; ++i)
+        if (i == mine_at) q = raw[i];
+      unsigned finds = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) finds |= (slot_elem<T>(q, e) >= t ? 1u : 0u) << e;
+      unsigned at = finds ? atomicAdd(&sh_n, (unsigned)__popc(finds)) : 0u;
+      const int id0 = (first + mine_at * THREADS + tid) * N;
+      while (__any(finds != 0)) {
+        if (finds) {
+          const int f = __builtin_ctz(finds);
+          float v = slot_elem<T>(q, 0);
+#pragma unroll
+          for (int e = 1; e < N; ++e) v = e == f ? slot_elem<T>(q, e) : v;
+          if (at < TOP_CAP) cand[at] = top_key(logit_order(v), id0 + f);
+          ++at;
+          finds &= finds - 1;
+        }
       }
+    }
     __syncthreads();
   }
   int n = (int)sh_n;
@@ -152,11 +193,12 @@ __global__ void __launch_bounds__(TOP_THREADS, 4) top_chunk_kernel(const TopArgs
       if (tail < a.V) element(logit_order(zt), tail);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int j = i * TOP_THREADS + tid;
-        if (j >= slots) break;
-#pragma unroll
-        for (int e = 0; e < N; ++e) element(logit_order(slot_elem<T>(raw[i], e)), (first + j) * N + e);
+        const int j = i * THREADS + tid;
         keep_packed(raw[i]);
+        if (j < slots) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) element(logit_order(slot_elem<T>(raw[i], e)), (first + j) * N + e);
+        }
       }
     };
     auto count = [&](auto &&reaches) {
@@ -186,41 +228,47 @@ __global__ void __launch_bounds__(TOP_THREADS, 4) top_chunk_kernel(const TopArgs
     __syncthreads();
     n = (int)sh_n;
   }
-  // 4.
-  for (int i = tid; i < n; i += TOP_THREADS) {
-    const unsigned long long key = cand[i];
+  // 4.  Eight lanes to a candidate: each counts an eighth of the others.
+  for (int i0 = 0; i0 < n; i0 += THREADS / 8) {
+    const int i = i0 + tid / 8;
+    const unsigned long long key = i < n ? cand[i] : ~0ull;
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += cand[j] > key;
-    if (rank < K) {
-      if (a.chunks == 1)
-        top_store(a, row, rank, key);
-      else
-        a.part[(long)blockIdx.x * K + rank] = key;
+#pragma unroll 4
+    for (int j = tid & 7; j < n; j += 8) rank += cand[j] > key;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
+    if (i < n && rank < K && (tid & 7) == 0) {
+      if (a.chunks == 1) top_store(a, row, rank, key);
+      else a.part[(long)blockIdx.x * K + rank] = key;
     }
   }
   if (a.chunks > 1)
-    for (int i = n + tid; i < K; i += TOP_THREADS) a.part[(long)blockIdx.x * K + i] = 0;
-  if (tid == 0) {
-    s = sh_s[0];
-    for (int i = 1; i < WAVES; ++i) s += sh_s[i];
-    if (a.chunks > 1) a.stat[blockIdx.x] = make_float2(mx, s);
-    else if (a.lse) a.lse[row] = row_lse(mx, s, a.tau);
+    for (int i = n + tid; i < K; i += THREADS) a.part[(long)blockIdx.x * K + i] = 0;
+  if (wave == 0) {
+    const float q = sh_ref[lane & (WAVES - 1)], m = waves_max<WAVES>(sh_ref), base = m == -INFINITY ? 0.0f : m;
+    float v = sh_s[lane & (WAVES - 1)] * exp2_32((q - base) * c);
+#pragma unroll
+    for (int o = WAVES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    if (lane == 0) {
+      if (a.chunks > 1) a.stat[blockIdx.x] = make_float2(m, v);
+      else if (a.lse) a.lse[row] = row_lse(m, v, a.tau);
+    }
   }
 }
 
 // Joins the chunks of a row.  A key's rank: its place in its own chunk's list, and how many keys of the other lists are above
 // it (each by bisection).
-__global__ void __launch_bounds__(TOP_THREADS) top_merge_kernel(const TopArgs a) {
+__global__ void __launch_bounds__(TOP_MERGE_THREADS) top_merge_kernel(const TopArgs a) {
   __shared__ unsigned long long lds[TOP_MERGE_LDS];
   const long row = blockIdx.x;
   const int n = a.chunks * a.K, K = a.K;
   const unsigned long long *key = a.part + row * n;
   if (n <= TOP_MERGE_LDS) {  // (more: the widest vocabularies with the longest lists)
-    for (int i = threadIdx.x; i < n; i += TOP_THREADS) lds[i] = key[i];
+    for (int i = threadIdx.x; i < n; i += TOP_MERGE_THREADS) lds[i] = key[i];
     __syncthreads();
     key = lds;
   }
-  for (int i = threadIdx.x; i < n; i += TOP_THREADS) {
+  for (int i = threadIdx.x; i < n; i += TOP_MERGE_THREADS) {
     const unsigned long long k = key[i];
     if (k == 0) continue;
     const int mine = i / K;

@@ -86,7 +86,7 @@ def test_top_logits_sizes(rows, V, K, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("kind", ["equal", "masked", "few", "rising", "falling", "ties", "zeros", "nan", "infinite", "clustered", "lowest"])
+@pytest.mark.parametrize("kind", ["equal", "masked", "few", "rising", "falling", "ties", "zeros", "nan", "infinite", "clustered", "lowest", "steep"])
 @pytest.mark.parametrize("V,K", [(300, 256), (5000, 40), (20011, 256)])
 def test_top_logits_patterns(V, K, kind, dtype):
     check_top(patterns(kind, 3, V, 7), K, 1.0, dtype, 0)
