@@ -316,7 +316,8 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
  * where all of a text's drafts are accepted, from the row behind them.  draft NULL: drafts without probabilities (q_i has
  * all its mass on d_i).  The drawn word is the first v whose sum of weights over words <= v exceeds u[K] times the whole
  * sum (in 64 bits); weights that are all zero: p_n itself.  -inf marks masked words.  A row with no probability (all masked,
- * a NaN or +inf) accepts no draft and draws the word -1.  Drafts outside [0, V) are rejected and raise *range_flag.
+ * a NaN or +inf) accepts no draft and draws the word -1;
+ * a draft row of nothing but masked words counts as q_i = 0, one with a NaN or +inf as a row with no probability.  Drafts outside [0, V) are rejected and raise *range_flag.
  * K = 0 (draft and drafts NULL) draws one word of each row.
  * target: dev [K+1][B] rows, draft: dev [K][B] rows, both of dtype; drafts: dev int32[K][B]; lengths: dev int32[B], a text's
  * own number of drafts (clamped to [0, K]; rows behind it are not read), or NULL: K; u: dev float[K+1][B], in [0, 1);

@@ -14,8 +14,12 @@ def lse(z, tau=1.0):
 
 
 def softmax(z, tau=1.0):
-    n = lse(z, tau)
-    return np.zeros(len(z)) if np.isneginf(n) else np.exp(np.asarray(z, np.float64) / tau - n)
+    z = np.asarray(z, np.float64)
+    if np.isneginf(z).all():
+        return np.zeros(len(z))
+    with np.errstate(invalid="ignore"):
+        e = np.exp((z - z.max()) / tau)  # (not by way of lse, which swallows ln V where z is huge)
+        return e / e.sum()
 
 
 def top(z, K, tau=1.0):

@@ -4,7 +4,7 @@
 //   dz[v] = w g (alpha tau (pi q_tau(v) - sum_{k: id_k = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
 // The sum over the list is pi (A / S + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (t_k - z_k / tau):
 // a pass over the row needs a sum of exponentials only, and the listed words are read one by one.
-// A sum is taken relative to a reference m: sum_v e^{(z_v - m) / tau}.  Any m will do that leaves it finite and far from 0.
+// A sum is taken relative to a reference; any will do that leaves it finite and far from 0.
 #pragma once
 #include "rows.h"
 
@@ -35,40 +35,34 @@ struct DistillEntry {  // a word of the list, or (last) the label
   float t, z, p;       // teacher's logit / tau, student's logit, e^{t - t_max}
 };
 
-// What a row's softmax is made of: a reference, and the sums of exponentials relative to it at tau and at 1.
+// What a row's softmax is made of: sums of exponentials of z - shift at tau and at 1, relative to 2^power and 2^power1.
 struct RowSums {
-  float m, s, s1;
+  float shift, power, power1, s, s1;
 };
 
+// Exponentials of a row that are relative to whole powers of 2 (shift = 0).
 template <int MODE>
 struct DistillExp {
   float c, b, b1;
-  __device__ DistillExp(float m, float tau) : c(LOG2E / tau), b(-m * c), b1(-m * LOG2E) {}
+  __device__ DistillExp(float m, float tau) : c(LOG2E / tau), b(-whole_power(m, c)), b1(-whole_power(m, LOG2E)) {}
   __device__ void add(float z, float &s, float &s1) const {
     const float e = exp2_32(fmaf(z, c, b));
     s += e;
     if (MODE == DISTILL_SQUARE) s1 = fmaf(e, e, s1);
     if (MODE == DISTILL_TWO) s1 += exp2_32(fmaf(z, LOG2E, b1));
   }
-  // The sums, from reference m to this one.
-  __device__ void move(float m, float &s, float &s1) const {
-    const float e = exp2_32(fmaf(m, c, b));
-    s *= e;
-    if (MODE == DISTILL_SQUARE) s1 *= e * e;
-    if (MODE == DISTILL_TWO) s1 *= exp2_32(fmaf(m, LOG2E, b1));
-  }
+  __device__ float power1() const { return MODE == DISTILL_SQUARE ? -2.0f * b : -b1; }
 };
 
 // The dense part of a row's gradient: pi g alpha tau q_tau(v) + g (1 - alpha) q_1(v).  The factors (of one sign) go into the
 // exponents, or (SQUARE) d = e (a + a1 e).
 template <int MODE>
 struct DistillDense {
-  float c, b, a, a1;
+  float c, b, a, a1, shift;
   unsigned sign;
-  __device__ DistillDense(const RowSums &r, float tau, float soft, float hard) {
-    c = LOG2E / tau;
+  __device__ DistillDense(const RowSums &r, float tau, float soft, float hard) : c(LOG2E / tau), shift(r.shift) {
     const float s1 = MODE == DISTILL_ONE ? r.s : r.s1;
-    b = -r.m * c;
+    b = -r.power;
     sign = 0u;
     if (MODE == DISTILL_SQUARE) {
       a = r.s == 0.0f ? 0.0f : soft / r.s;
@@ -77,15 +71,21 @@ struct DistillDense {
       a = MODE == DISTILL_ONE ? soft + hard : soft;
       if (a < 0.0f || hard < 0.0f) sign = 0x80000000u;
       b += r.s == 0.0f ? -INFINITY : __log2f(fabsf(a)) - __log2f(r.s);
-      a1 = -r.m * LOG2E + (s1 == 0.0f ? -INFINITY : __log2f(fabsf(hard)) - __log2f(s1));
+      a1 = -r.power1 + (s1 == 0.0f ? -INFINITY : __log2f(fabsf(hard)) - __log2f(s1));
     }
   }
+  // SHIFT: rows whose sums have one
+  template <bool SHIFT = false>
   __device__ float bare(float z) const {
+    if (SHIFT) z -= shift;
     const float e = exp2_32(fmaf(z, c, b));
     if (MODE == DISTILL_SQUARE) return e * fmaf(a1, e, a);
     return MODE == DISTILL_TWO ? e + exp2_32(fmaf(z, LOG2E, a1)) : e;
   }
-  __device__ float operator()(float z) const { return sign ? -bare(z) : bare(z); }
+  __device__ float operator()(float z) const {
+    const float d = bare<true>(z);
+    return sign ? -d : d;
+  }
   template <typename T>
   __device__ unsigned flip() const { return sizeof(T) == 4 ? sign : sign | sign >> 16; }
 };
@@ -137,7 +137,7 @@ __device__ inline void distill_list_sums(DistillEntry *ent, int K, float inv_tau
 // Sums over the workgroup's waves, by way of LDS.
 template <int WAVES>
 struct DistillShared {
-  float m[WAVES], t[WAVES], s[WAVES], s1[WAVES], S[WAVES], again[WAVES];
+  float m[WAVES], m1[WAVES], t[WAVES], s[WAVES], s1[WAVES], S[WAVES], again[WAVES];
   double A[WAVES];
 };
 
@@ -185,9 +185,13 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
       double A = 0.0;
       for (int i = 0; i < waves; ++i) A += A_of_wave[i];
       const double n = a.lse ? (double)a.lse[m] : (double)l.tmax + log((double)l.S);
-      loss = (double)a.alpha * tau * tau * (double)l.pi * (A / (double)l.S + (double)r.m / tau + log((double)r.s) - n);
+      const double lse = (double)r.shift / tau + ((double)r.power + log2((double)r.s)) * LN2_64;
+      loss = (double)a.alpha * tau * tau * (double)l.pi * (A / (double)l.S + lse - n);
     }
-    if (hard) loss += (double)(1.0f - a.alpha) * ((double)r.m - (double)label.z + log((double)(MODE == DISTILL_ONE ? r.s : r.s1)));
+    if (hard) {
+      const double sum = MODE == DISTILL_ONE ? (double)r.power + log2((double)r.s) : (double)r.power1 + log2((double)r.s1);
+      loss += (double)(1.0f - a.alpha) * ((double)r.shift - (double)label.z + sum * LN2_64);
+    }
   }
   a.loss[m] = (float)((double)w * loss);
 }
@@ -224,43 +228,21 @@ __device__ inline void distill_without_weight(const DistillArgs<T> &a, long m) {
   if (at < a.V) drow[at] = from_f32<T>(0.0f);
 }
 
-// The waves' sums joined: references may differ.
-template <int THREADS, int MODE>
-__device__ inline RowSums distill_join(const DistillShared<THREADS / 64> &sh, float tau) {
-  constexpr int WAVES = THREADS / 64;
-  RowSums r = {waves_max<WAVES>(sh.m), 0.0f, 0.0f};
-  if (r.m == -INFINITY) r.m = 0.0f;
-  const int wave = threadIdx.x & (WAVES - 1);
-  r.s = sh.s[wave];
-  r.s1 = MODE == DISTILL_ONE ? 0.0f : sh.s1[wave];
-  DistillExp<MODE>(r.m, tau).move(sh.m[wave], r.s, r.s1);
-#pragma unroll
-  for (int o = WAVES / 2; o > 0; o >>= 1) {
-    r.s += __shfl_xor(r.s, o, 64);
-    if (MODE != DISTILL_ONE) r.s1 += __shfl_xor(r.s1, o, 64);
-  }
-  return r;
-}
-
-// A wave's sums and their reference, for the workgroup.
-template <int MODE, int WAVES>
-__device__ inline void distill_publish(DistillShared<WAVES> &sh, float ref, float s, float s1) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  s = wave_sum(s);
-  if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
-  if ((threadIdx.x & 63) == 0) {
-    sh.m[wave] = ref;
-    sh.s[wave] = s;
-    sh.s1[wave] = s1;
-  }
-}
-
-// The row's sums in one pass with a running maximum and sum of each thread (zt: its element behind the whole slots).
-template <typename T, int THREADS, int MODE, int FLIGHT, bool ONCE = false>
-__device__ inline void distill_stream(const DistillArgs<T> &a, const T *row, float zt, DistillShared<THREADS / 64> &sh) {
-  constexpr int N = SlotOf<T>::N;
-  const int tid = threadIdx.x, full = a.V / N;
+// A row by two passes over memory: sums with a running maximum and sum of each thread (all at z - maximum: for logits of any
+// size), then the gradient.  zt: this thread's element behind the whole slots; te: the greatest t of its list entries.
+template <typename T, int THREADS, int MODE, int FLIGHT, bool ONCE>
+__device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float w, const T *row, float zt, float te, DistillEntry *ent,
+                                         DistillShared<THREADS / 64> &sh) {
+  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
+  const float c = LOG2E / a.tau;
   float mx = zt, s = zt == -INFINITY ? 0.0f : 1.0f, s1 = s;
+  auto move = [&](float to) {  // (from -inf: the sums are 0, and so is the factor)
+    const float e = exp2_32((mx - to) * c);
+    s *= e;
+    if (MODE == DISTILL_SQUARE) s1 *= e * e;
+    if (MODE == DISTILL_TWO) s1 *= exp2_32((mx - to) * LOG2E);
+  };
   for (int j0 = tid; j0 < full; j0 += FLIGHT * THREADS) {
     slot_t raw[FLIGHT];
 #pragma unroll
@@ -271,26 +253,61 @@ __device__ inline void distill_stream(const DistillArgs<T> &a, const T *row, flo
     float top = mx;
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i) top = slot_max<T>(top, raw[i]);
-    const DistillExp<MODE> ex(top == -INFINITY ? 0.0f : top, a.tau);
-    if (top > mx) {  // (mx = -inf: the sums are 0, and so is the factor)
-      ex.move(mx, s, s1);
+    const float base = top == -INFINITY ? 0.0f : top;
+    if (top > mx) {
+      move(base);
       mx = top;
     }
 #pragma unroll
     for (int i = 0; i < FLIGHT; ++i)
 #pragma unroll
-      for (int e = 0; e < N; ++e) ex.add(slot_elem<T>(raw[i], e), s, s1);
+      for (int e = 0; e < N; ++e) {
+        const float z = slot_elem<T>(raw[i], e) - base, x = exp2_32(z * c);
+        s += x;
+        if (MODE == DISTILL_SQUARE) s1 = fmaf(x, x, s1);
+        if (MODE == DISTILL_TWO) s1 += exp2_32(z * LOG2E);
+      }
   }
   const float top = wave_max(mx);
-  DistillExp<MODE>(top == -INFINITY ? 0.0f : top, a.tau).move(mx, s, s1);
-  distill_publish<MODE>(sh, top, s, s1);
+  if (lane == 0) {
+    sh.m[wave] = top;
+    sh.t[wave] = te;
+  }
+  __syncthreads();
+  RowSums r = {waves_max<WAVES>(sh.m), 0.0f, 0.0f, 0.0f, 0.0f};
+  if (r.shift == -INFINITY) r.shift = 0.0f;
+  move(r.shift);
+  s = wave_sum(s);
+  if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
+  if (lane == 0) {
+    sh.s[wave] = s;
+    sh.s1[wave] = s1;
+  }
+  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);  // (a barrier)
+  r.s = waves_sum<WAVES>(sh.s);
+  if (MODE != DISTILL_ONE) r.s1 = waves_sum<WAVES>(sh.s1);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
+  if (!a.dz) return;
+  const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
+  const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
+  T *drow = a.dz + m * a.ldd;
+  for (int j = tid; j < full; j += THREADS) {
+    const slot_t raw = load_slot(row, j);
+    float d[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] = dense.template bare<true>(slot_elem<T>(raw, e));
+    store_slot(drow, j, d, dense.template flip<T>());
+  }
+  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense(zt));
+  __syncthreads();
+  distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
 }
 
 // A workgroup's row stays in registers between the sums and the gradient: the row is read once and its gradient written once,
 // which is all that bounds the call (HBM, with the exponentials' instructions not far behind).  NV: slots of a thread.
-// The sums run while the row arrives: a wave's reference is the greatest element of its first slots, so a later element of
+// The sums run while the row arrives: a wave's reference is near the greatest element of its first slots, so a later element of
 // it can only overflow by being e^88 times greater, and the sum cannot vanish.  Where a sum is no number after all, or a wave's
-// first slots are masked throughout, the row's maximum is formed and the sums are repeated.
+// first slots are masked throughout (or beyond the references' range), the row goes by way of memory.
 template <typename T, int THREADS, int NV, int MODE>
 __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillArgs<T> a) {
   constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
@@ -311,30 +328,42 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
     for (int i = 0; i < NV; ++i) raw[i] = i * THREADS + tid < full ? load_slot(row + i * THREADS * N, tid) : empty_slot<T>();
   }
   const float zt = tail_elem(row, tid, a.V);
-  const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
+  const float te = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
   const float ref = wave_max(slot_max<T>(zt, raw[0]));
-  const DistillExp<MODE> ex(ref == -INFINITY ? 0.0f : ref, a.tau);
+  const DistillExp<MODE> ex(ref, a.tau);
   float s = 0.0f, s1 = 0.0f;
   ex.add(zt, s, s1);
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e) ex.add(slot_elem<T>(raw[i], e), s, s1);
-  distill_publish<MODE>(sh, ref, s, s1);
+  s = wave_sum(s);
+  if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
   const float sum = s + s1;
-  const bool again = __any(!(sum - sum == 0.0f)) || (ref == -INFINITY && wave * 64 < full);
+  const bool again = !(sum - sum == 0.0f) || (wave * 64 < full && !(near_power(ref, ex.c) && near_power(ref, LOG2E)));
   if (lane == 0) {
-    sh.t[wave] = tw;
+    sh.m[wave] = s == 0.0f ? -INFINITY : -ex.b;
+    sh.m1[wave] = s1 == 0.0f ? -INFINITY : ex.power1();
+    sh.s[wave] = s;
+    sh.s1[wave] = s1;
+    sh.t[wave] = te;
     sh.again[wave] = again ? 1.0f : 0.0f;
   }
   __syncthreads();
   if (waves_max<WAVES>(sh.again) != 0.0f) {
     __syncthreads();
-    distill_stream<T, THREADS, MODE, 1>(a, row, zt, sh);
-    __syncthreads();
+    return distill_by_memory<T, THREADS, MODE, 1, false>(a, m, w, row, zt, te, ent, sh);
   }
   const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);
-  const RowSums r = distill_join<THREADS, MODE>(sh, a.tau);
+  auto join = [&](const float *power, const float *of_wave, float &top) {
+    top = waves_max<WAVES>(power);
+    if (top == -INFINITY) top = 0.0f;
+    const int i = tid & (WAVES - 1);
+    return group_reduce<WAVES>(of_wave[i] * exp2_32(power[i] - top), [](float x, float y) { return x + y; });
+  };
+  RowSums r = {};
+  r.s = join(sh.m, sh.s, r.power);
+  if (MODE != DISTILL_ONE) r.s1 = join(sh.m1, sh.s1, r.power1);
   const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
   const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
   T *drow = a.dz + m * a.ldd;
@@ -354,42 +383,19 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
   distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
 }
 
-// Rows that do not fit the registers, and calls without a gradient: one pass with a running maximum and sum of each thread,
-// then (with a gradient) a second one.
+// Rows that do not fit the registers, and calls without a gradient.
 template <typename T, int THREADS, int MODE>
 __global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillArgs<T> a) {
-  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
   extern __shared__ __align__(16) unsigned char lds[];
   DistillEntry *ent = reinterpret_cast<DistillEntry *>(lds);
-  __shared__ DistillShared<WAVES> sh;
+  __shared__ DistillShared<THREADS / 64> sh;
   const long m = blockIdx.x;
   const float w = a.weight ? a.weight[m] : 1.0f;
   if (w == 0.0f) return distill_without_weight<T, THREADS>(a, m);
   const T *row = a.z + m * a.ldz;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, full = a.V / N;
-  const float tw = wave_max(distill_entries<T, THREADS>(a, m, row, ent));
-  const float zt = tail_elem(row, tid, a.V);
-  if (a.once && !a.dz) distill_stream<T, THREADS, MODE, 4, true>(a, row, zt, sh);
-  else distill_stream<T, THREADS, MODE, 4>(a, row, zt, sh);
-  if (lane == 0) sh.t[wave] = tw;
-  __syncthreads();
-  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);
-  const RowSums r = distill_join<THREADS, MODE>(sh, a.tau);
-  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
-  if (!a.dz) return;
-  const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
-  const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
-  T *drow = a.dz + m * a.ldd;
-  for (int j = tid; j < full; j += THREADS) {
-    const slot_t raw = load_slot(row, j);
-    float d[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) d[e] = dense.bare(slot_elem<T>(raw, e));
-    store_slot(drow, j, d, dense.template flip<T>());
-  }
-  if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense(zt));
-  __syncthreads();
-  distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
+  const float te = wave_max(distill_entries<T, THREADS>(a, m, row, ent)), zt = tail_elem(row, threadIdx.x, a.V);
+  if (a.once && !a.dz) distill_by_memory<T, THREADS, MODE, 4, true>(a, m, w, row, zt, te, ent, sh);
+  else distill_by_memory<T, THREADS, MODE, 4, false>(a, m, w, row, zt, te, ent, sh);
 }
 
 // Sum of n losses in 64 bits, in a fixed order, by one workgroup.

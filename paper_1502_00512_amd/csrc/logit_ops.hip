@@ -70,7 +70,7 @@ TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
 }
 size_t top_bytes(const TopPlan &p, int64_t rows, int32_t K) {
   if (p.chunks == 1) return 0;
-  return align256((size_t)rows * p.chunks * K * 8) + align256((size_t)rows * p.chunks * 8);
+  return align256((size_t)rows * p.chunks * K * 8) + align256((size_t)rows * p.chunks * 16);
 }
 bool top_sizes_ok(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   return rows >= 0 && rows <= GRID_MAX / 1024 && V >= 1 && V <= TOP_V_MAX && K >= 1 && K <= std::min(V, TOP_K_MAX) &&
@@ -140,16 +140,16 @@ int distill_call(DistillArgs<T> a, int64_t rows, hipStream_t st) {
 
 // ---- verification ----
 struct VerifyPlan {
-  int parts, per;
+  int parts, chunks;
   size_t stat, sums, rest, seq, total;
 };
+int verify_blocks(int32_t V, int32_t dtype) { return (slots_of(V, dtype) + 63) / 64; }
 VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
   VerifyPlan p;
   const int slots = slots_of(V, RNNLM_DTYPE_BF16);  // (fp32 rows have twice as many: parts of twice the slots)
-  const int64_t rows = (int64_t)(2 * K + 1) * B;
-  int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, std::min<int64_t>(rows, 2048)));
-  want = std::max<int64_t>(want, std::max<int64_t>(1, 1024 / B));
-  p.parts = (int)std::min<int64_t>({want, VERIFY_PARTS, (slots + VERIFY_THREADS - 1) / VERIFY_THREADS});
+  const int64_t rows = (int64_t)(2 * K + 1) * B, fill = 8192;
+  p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({fill / std::min(rows, fill), VERIFY_PARTS, slots / VERIFY_THREADS}));
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / std::min<int64_t>(B, 1024), VERIFY_PARTS, slots / VERIFY_THREADS}));
   size_t o = 0;
   auto take = [&](size_t n) {
     const size_t at = o;
@@ -157,8 +157,8 @@ VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
     return at;
   };
   p.stat = take((size_t)rows * p.parts * 8);
-  p.sums = take((size_t)B * p.parts * 16);
-  p.rest = take((size_t)B * p.parts * 8);
+  p.sums = take((size_t)B * p.chunks * 16);
+  p.rest = take((size_t)B * verify_blocks(V, RNNLM_DTYPE_FP32) * 8);
   p.seq = take((size_t)B * sizeof(VerifySeq));
   p.total = o;
   return p;
@@ -172,9 +172,12 @@ int verify_call(const VerifyArgs &a, hipStream_t st) {
   const dim3 threads(VERIFY_THREADS);
   const int64_t rows = (int64_t)(a.draft ? 2 * a.K + 1 : a.K + 1) * a.B;
   hipLaunchKernelGGL(verify_stats_kernel<T>, dim3((unsigned)(rows * a.parts)), threads, 0, st, a);
-  hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.parts)), threads, 0, st, a);
-  hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.parts)), threads, 0, st, a);
-  hipLaunchKernelGGL(verify_draw_kernel<T>, dim3((unsigned)a.B), threads, 0, st, a);
+  if (a.blocks <= VERIFY_ONE_BLOCKS) {
+    hipLaunchKernelGGL(verify_one_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_ONE_THREADS), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
+    hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
+  }
   LAUNCHED();
   return RNNLM_OK;
 }
@@ -210,7 +213,7 @@ int rnnlm_top_logits(const void *logits, int32_t dtype, int64_t rows, int32_t V,
   a.once = read_once(rows, V, dtype);
   if (need) {
     a.part = static_cast<unsigned long long *>(workspace);
-    a.stat = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + align256((size_t)rows * p.chunks * K * 8));
+    a.stat = reinterpret_cast<double2 *>(static_cast<char *>(workspace) + align256((size_t)rows * p.chunks * K * 8));
   }
   hipStream_t st = (hipStream_t)stream;
   if (dtype == RNNLM_DTYPE_FP32) launch_top<float>(a, rows, p, st);
@@ -296,6 +299,9 @@ int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft
   a.K = K;
   a.parts = p.parts;
   a.per = (slots_of(V, dtype) + p.parts - 1) / p.parts;
+  a.blocks = verify_blocks(V, dtype);
+  a.chunks = std::min(p.chunks, a.blocks);
+  a.span = (a.blocks + a.chunks - 1) / a.chunks;
   a.tau = tau;
   a.tau_d = tau_draft;
   a.accepted = accepted;

@@ -120,20 +120,58 @@ __device__ inline float slot_max(float m, const slot_t &s) {
 
 __device__ inline float exp2_32(float x) { return __builtin_amdgcn_exp2f(x); }
 
-template <typename X, class Op>
-__device__ inline X wave_reduce(X v, Op &&op) {
+// References of a sum of exponentials 2^{z c}: whole powers of 2 near 2^{m c}, so that z c - power is rounded once and sums move
+// from one to another by exact factors.  Logits whose power is beyond 2^22 (and masked ones) have none.
+__device__ inline bool near_power(float m, float c) { return fabsf(m * c) < 4194304.0f; }
+__device__ inline float whole_power(float m, float c) { return near_power(m, c) ? rintf(m * c) : 0.0f; }
+// 2^(from - to); 0 from -inf.
+__device__ inline float power_between(double from, double to) { return from == -INFINITY ? 0.0f : exp2_32((float)(from - to)); }
+
+// Exchanges within 16 lanes: a mirrored or swapped lane's value in two instructions' time, where an exchange by way of LDS takes
+// about a hundred cycles.
+template <int CTRL, typename X>
+__device__ inline X lane_swap(X v) {
+  constexpr int WORDS = sizeof(X) / 4;
+  union {
+    X x;
+    int w[WORDS];
+  } u;
+  u.x = v;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
+  for (int i = 0; i < WORDS; ++i) u.w[i] = __builtin_amdgcn_update_dpp(0, u.w[i], CTRL, 0xf, 0xf, true);
+  return u.x;
+}
+template <typename X>
+__device__ inline X lane_value(X v, int lane) {
+  constexpr int WORDS = sizeof(X) / 4;
+  union {
+    X x;
+    int w[WORDS];
+  } u;
+  u.x = v;
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i) u.w[i] = __builtin_amdgcn_readlane(u.w[i], lane);
+  return u.x;
+}
+// Over groups of G lanes (2 to 16, aligned): every lane gets its group's.
+template <int G, typename X, class Op>
+__device__ inline X group_reduce(X v, Op &&op) {
+  if (G >= 2) v = op(v, lane_swap<0xB1>(v));   // the neighbour
+  if (G >= 4) v = op(v, lane_swap<0x4E>(v));   // the other pair of four
+  if (G >= 8) v = op(v, lane_swap<0x141>(v));  // mirrored among eight
+  if (G >= 16) v = op(v, lane_swap<0x140>(v)); // mirrored among sixteen
   return v;
 }
-// The same over WAVES numbers of LDS (a power of two, one a wave of the workgroup), for every lane: each group of WAVES lanes
-// reads them all.  (Unrolled over registers instead, 16 waves' numbers took 16 registers for each sum.)
+// Over the 64 lanes; all of them have to be active.
+template <typename X, class Op>
+__device__ inline X wave_reduce(X v, Op &&op) {
+  v = group_reduce<16>(v, op);
+  return op(op(lane_value(v, 0), lane_value(v, 16)), op(lane_value(v, 32), lane_value(v, 48)));
+}
+// The same over WAVES numbers of LDS (a power of two, one a wave of the workgroup), for every lane.
 template <int WAVES, class Op>
 __device__ inline float waves_reduce(const float *of_wave, Op &&op) {
-  float v = of_wave[threadIdx.x & (WAVES - 1)];
-#pragma unroll
-  for (int o = WAVES / 2; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-  return v;
+  return group_reduce<WAVES>(of_wave[threadIdx.x & (WAVES - 1)], op);
 }
 template <int WAVES>
 __device__ inline float waves_max(const float *of_wave) {
@@ -142,6 +180,16 @@ __device__ inline float waves_max(const float *of_wave) {
 template <int WAVES>
 __device__ inline float waves_sum(const float *of_wave) {
   return waves_reduce<WAVES>(of_wave, [](float a, float b) { return a + b; });
+}
+// Sums of the lanes up to each one.
+template <typename X>
+__device__ inline X wave_scan(X v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const X add = __shfl_up(v, o, 64);
+    if ((int)(threadIdx.x & 63) >= o) v += add;
+  }
+  return v;
 }
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });

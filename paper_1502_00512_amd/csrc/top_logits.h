@@ -39,7 +39,7 @@ struct TopArgs {
   int32_t *ids;
   float *vals, *lse;
   unsigned long long *part;  // [row][chunk][K], descending; 0 behind a chunk's last element
-  float2 *stat;              // [row][chunk]: a reference, sum of exponentials at tau relative to it
+  double2 *stat;             // [row][chunk]: base-2 logarithm of a reference, sum of exponentials at tau relative to it
   bool once;                 // read past the caches
 };
 
@@ -48,9 +48,8 @@ __device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned 
   a.vals[row * a.K + rank] = order_logit((unsigned)(key >> 32));
 }
 
-__device__ inline float row_lse(float m, float s, float tau) {
-  return s == 0.0f ? -INFINITY : (float)((double)m / (double)tau + log((double)s));
-}
+// ln of the sum s relative to 2^ref.
+__device__ inline float row_lse(double ref, float s) { return s == 0.0f ? -INFINITY : (float)((ref + log2((double)s)) * LN2_64); }
 
 // A threshold that at least K of 64 G numbers reach, and few more; by one wave.  (Bisection: a count takes 2 G instructions.)
 template <int G>
@@ -82,7 +81,8 @@ __device__ inline unsigned top_threshold(const unsigned *group, int K, unsigned 
 template <typename T, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) {
   constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
-  __shared__ float sh_m[WAVES], sh_s[WAVES], sh_ref[WAVES];
+  __shared__ float sh_m[WAVES], sh_s[WAVES];
+  __shared__ double sh_ref[WAVES];
   __shared__ unsigned group[2 * THREADS];
   __shared__ unsigned long long cand[TOP_CAP];
   __shared__ unsigned sh_t, sh_n, sh_count[2][WAVES];
@@ -101,8 +101,9 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   const int tail = chunk == a.chunks - 1 ? full * N + tid : a.V;  // the last chunk has the row's last elements, one a thread
   const float zt = tail < a.V ? to_f32(z[tail]) : -INFINITY;
   if (tid == 0) sh_n = 0;
-  // 1.  The sum is relative to the greatest element of the wave's first slots, so it runs while the rest arrives.
-  const float c = LOG2E / a.tau, ref = wave_max(slot_max<T>(zt, raw[0])), b = ref == -INFINITY ? 0.0f : -ref * c;
+  // 1.  The sum is relative to about the greatest element of the wave's first slots (a whole power of 2), so it runs while the
+  // rest arrives.
+  const float c = LOG2E / a.tau, ref = wave_max(slot_max<T>(zt, raw[0])), b = -whole_power(ref, c);
   float top[NV], half[2] = {max3(zt, -INFINITY, -INFINITY), -INFINITY}, s = exp2_32(fmaf(zt, c, b));
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -118,20 +119,20 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   group[tid] = logit_order(pairs ? half[0] : both);
   if (pairs) group[THREADS + tid] = logit_order(half[1]);
   s = wave_sum(s);
-  if (!(s - s == 0.0f) || (ref == -INFINITY && mine > -INFINITY)) {
+  double power = -(double)b;
+  if (!(s - s == 0.0f) || (!near_power(ref, c) && mine > -INFINITY)) {
     // no number, or the first slots are masked throughout: once more, relative to the wave's maximum
-    const float again = mine == -INFINITY ? 0.0f : -mine * c;
-    s = exp2_32(fmaf(zt, c, again));
+    const float base = mine == -INFINITY ? 0.0f : mine;
+    s = exp2_32((zt - base) * c);
     for (int j = tid; j < slots; j += THREADS) {
       const slot_t q = load_slot(z, first + j);
 #pragma unroll
-      for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(q, e), c, again));
+      for (int e = 0; e < N; ++e) s += exp2_32((slot_elem<T>(q, e) - base) * c);
     }
     s = wave_sum(s);
-    if (lane == 0) sh_ref[wave] = mine;
-  } else if (lane == 0) {
-    sh_ref[wave] = ref;
+    power = (double)base * (LOG2E_64 / (double)a.tau);
   }
+  if (lane == 0) sh_ref[wave] = s == 0.0f ? -INFINITY : power;
   if (lane == 0) {
     sh_m[wave] = mine;
     sh_s[wave] = s;
@@ -235,8 +236,7 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
     int rank = 0;
 #pragma unroll 4
     for (int j = tid & 7; j < n; j += 8) rank += cand[j] > key;
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
+    rank = group_reduce<8>(rank, [](int x, int y) { return x + y; });
     if (i < n && rank < K && (tid & 7) == 0) {
       if (a.chunks == 1) top_store(a, row, rank, key);
       else a.part[(long)blockIdx.x * K + rank] = key;
@@ -245,13 +245,11 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   if (a.chunks > 1)
     for (int i = n + tid; i < K; i += THREADS) a.part[(long)blockIdx.x * K + i] = 0;
   if (wave == 0) {
-    const float q = sh_ref[lane & (WAVES - 1)], m = waves_max<WAVES>(sh_ref), base = m == -INFINITY ? 0.0f : m;
-    float v = sh_s[lane & (WAVES - 1)] * exp2_32((q - base) * c);
-#pragma unroll
-    for (int o = WAVES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    const double q = sh_ref[lane & (WAVES - 1)], top_ref = group_reduce<WAVES>(q, [](double x, double y) { return fmax(x, y); });
+    const float v = group_reduce<WAVES>(sh_s[lane & (WAVES - 1)] * power_between(q, top_ref), [](float x, float y) { return x + y; });
     if (lane == 0) {
-      if (a.chunks > 1) a.stat[blockIdx.x] = make_float2(m, v);
-      else if (a.lse) a.lse[row] = row_lse(m, v, a.tau);
+      if (a.chunks > 1) a.stat[blockIdx.x] = make_double2(top_ref, (double)v);
+      else if (a.lse) a.lse[row] = row_lse(top_ref, v);
     }
   }
 }
@@ -286,17 +284,17 @@ __global__ void __launch_bounds__(TOP_MERGE_THREADS) top_merge_kernel(const TopA
     if (rank < K) top_store(a, row, rank, k);
   }
   if (threadIdx.x < 64 && a.lse) {
-    const float c = LOG2E / a.tau;
-    float m = -INFINITY, s = 0.0f;
+    double ref = -INFINITY;
+    float s = 0.0f;
     for (int l = threadIdx.x; l < a.chunks; l += 64) {
-      const float2 q = a.stat[row * a.chunks + l];
-      const float top = fmaxf(m, q.x), base = top == -INFINITY ? 0.0f : top;
-      s = s * exp2_32((m - base) * c) + q.y * exp2_32((q.x - base) * c);
-      m = top;
+      const double2 q = a.stat[row * a.chunks + l];
+      const double top_ref = fmax(ref, q.x);
+      s = s * power_between(ref, top_ref) + (float)q.y * power_between(q.x, top_ref);
+      ref = top_ref;
     }
-    const float top = wave_max(m), base = top == -INFINITY ? 0.0f : top;
-    s = wave_sum(s * exp2_32((m - base) * c));
-    if (threadIdx.x == 0) a.lse[row] = row_lse(top, s, a.tau);
+    const double top_ref = wave_reduce(ref, [](double x, double y) { return fmax(x, y); });
+    s = wave_sum(s * power_between(ref, top_ref));
+    if (threadIdx.x == 0) a.lse[row] = row_lse(top_ref, s);
   }
 }
 

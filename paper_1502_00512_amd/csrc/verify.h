@@ -8,18 +8,23 @@
 // acceptance of a draft compares two probabilities and gets by with 32-bit sums.
 //   1. maximum and sum of exponentials of every row that can matter, by parts of a row (HBM-bound; all the bytes are here)
 //   2. how many drafts are accepted; sums of exponentials of the one row pair that is drawn from, in 64 bits
-//   3. sums of r by parts      4. the part, the thread's stretch of it and the word on which u_K falls
+//   3. sums of r by blocks of one slot a lane, and by the last workgroup of a text to finish: the block on which u_K falls, and
+//      the word in it
+// Short rows do 2 and 3 in one workgroup a text.
 #pragma once
 #include "rows.h"
 
 namespace rnnlm_dev {
 
 constexpr int VERIFY_THREADS = 256, VERIFY_PARTS = 64;
+constexpr int VERIFY_ONE_THREADS = 1024, VERIFY_ONE_BLOCKS = 64;  // a text in one workgroup: rows of at most so many blocks
 
 struct VerifySeq {  // what the steps behind the second one know of a text
   int n;            // accepted
   int mixed;        // the drawn row is p - q (else p alone)
   float mp, mq;     // maxima of the drawn rows
+  int ok;           // they are numbers, and p has any
+  unsigned done;    // workgroups of the third step that have finished
 };
 
 struct VerifyArgs {
@@ -27,12 +32,13 @@ struct VerifyArgs {
   long ldt, ldd;
   const int32_t *drafts, *lengths;  // lengths may be nullptr
   const float *u;
-  int V, B, K, parts, per;  // per: slots of a part
+  int V, B, K, parts, per;    // parts of a row in the first step; slots of each
+  int chunks, blocks, span;   // workgroups of a text in the others; blocks of a row; blocks of each workgroup
   float tau, tau_d;
   int32_t *accepted, *tokens, *range_flag;
   float2 *stat;    // [row][part], rows of the target then of the draft
-  double *sums;    // [text][part][2]: sums of exponentials of p, q
-  double *rest;    // [text][part]: sums of r
+  double *sums;    // [text][chunk][2]: sums of exponentials of p, q
+  double *rest;    // [text][block]: sums of r
   VerifySeq *seq;  // [text]
 };
 
@@ -40,32 +46,37 @@ __device__ inline int draft_length(const VerifyArgs &a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.K) : a.K;
 }
 
-// 2^x to 64 bits: x = n + f with |f| <= 1/2 and the series of 2^f, whose 12th term is below 2e-14.
-__device__ inline double exp2_64(double x) {
-  x = x < -1100.0 ? -1100.0 : x;  // (a NaN stays one)
-  const double n = rint(x), f = (x - n) * LN2_64;
-  double p = 1.0 / 39916800.0;
-  p = fma(p, f, 1.0 / 3628800.0);
-  p = fma(p, f, 1.0 / 362880.0);
-  p = fma(p, f, 1.0 / 40320.0);
-  p = fma(p, f, 1.0 / 5040.0);
-  p = fma(p, f, 1.0 / 720.0);
-  p = fma(p, f, 1.0 / 120.0);
-  p = fma(p, f, 1.0 / 24.0);
-  p = fma(p, f, 1.0 / 6.0);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.0);
-  p = fma(p, f, 1.0);
-  return ldexp(p, (int)n);
-}
-// e^{(z - m) / tau} of a row: z c + b.
+// e^{(z - m) / tau} of a row in 64 bits: 2^x, x = (z - m) c = n + f with |f| <= 1/2, and the polynomial of degree 9 that meets 2^f
+// at the ten Chebyshev nodes of [-1/2, 1/2]: 1.8e-14 relative off at most, so a hundred thousand such terms place a step of
+// their sum to about 1e-14.  n is what adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer
+// addition (rounding, conversion and scaling instructions run at a quarter of the additions' rate).  Logits more than 690 tau
+// below the maximum, and masked ones, give 0.  No NaNs: the caller knows the row.
 struct Exp64 {
-  double c, b;
-  __device__ Exp64(float m, float tau) {
+  double c, m;
+  float least;
+  __device__ Exp64(float top, float tau) {
+    if (top == -INFINITY) top = 0.0f;
     c = LOG2E_64 / (double)tau;
-    b = m == -INFINITY ? 0.0 : -(double)m * c;
+    m = (double)top;
+    least = top - 690.0f * tau;
   }
-  __device__ double operator()(float z) const { return exp2_64(fma((double)z, c, b)); }
+  __device__ double operator()(float z) const {
+    constexpr double SHIFT = 6755399441055744.0;
+    const double x = ((double)fmaxf(z, least) - m) * c, t = x + SHIFT, f = x - (t - SHIFT);
+    double p = 1.0205905413765595e-07;
+    p = fma(p, f, 1.325964524488711e-06);
+    p = fma(p, f, 1.5252672924850737e-05);
+    p = fma(p, f, 0.0001540343375125101);
+    p = fma(p, f, 0.0013333558200794592);
+    p = fma(p, f, 0.009618129193934313);
+    p = fma(p, f, 0.05550410866465167);
+    p = fma(p, f, 0.2402265069564034);
+    p = fma(p, f, 0.6931471805599462);
+    p = fma(p, f, 1.0000000000000135);
+    const unsigned hi = (unsigned)__double2hiint(p) + ((unsigned)__double2loint(t) << 20);
+    const double e = __hiloint2double((int)hi, __double2loint(p));
+    return z >= least ? e : 0.0;
+  }
 };
 
 template <typename T>
@@ -91,20 +102,20 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_stats_kernel(const Veri
     float top = mx;
 #pragma unroll
     for (int k = 0; k < FLIGHT; ++k) top = slot_max<T>(top, raw[k]);
-    const float base = top == -INFINITY ? 0.0f : top, bias = -base * c;
+    const float base = top == -INFINITY ? 0.0f : top;
     if (top > mx) {
-      s *= exp2_32(fmaf(mx, c, bias));
+      s *= exp2_32((mx - base) * c);
       mx = top;
     }
 #pragma unroll
     for (int k = 0; k < FLIGHT; ++k)
 #pragma unroll
-      for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(raw[k], e), c, bias));
+      for (int e = 0; e < N; ++e) s += exp2_32((slot_elem<T>(raw[k], e) - base) * c);
   }
   const float own = mx;
   mx = wave_max(mx);
   float base = mx == -INFINITY ? 0.0f : mx;
-  s = wave_sum(s * exp2_32(fmaf(own, c, -base * c)));
+  s = wave_sum(s * exp2_32((own - base) * c));
   if ((threadIdx.x & 63) == 0) {
     sh_m[threadIdx.x >> 6] = mx;
     sh_s[threadIdx.x >> 6] = s;
@@ -114,7 +125,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_stats_kernel(const Veri
     for (int k = 1; k < WAVES; ++k) mx = fmaxf(mx, sh_m[k]);
     base = mx == -INFINITY ? 0.0f : mx;
     s = 0.0f;
-    for (int k = 0; k < WAVES; ++k) s += sh_s[k] * exp2_32(fmaf(sh_m[k], c, -base * c));
+    for (int k = 0; k < WAVES; ++k) s += sh_s[k] * exp2_32((sh_m[k] - base) * c);
     a.stat[(long)r * a.parts + part] = make_float2(mx, s);
   }
 }
@@ -125,7 +136,7 @@ __device__ inline float2 verify_row(const VerifyArgs &a, long r, float tau) {
   const float c = LOG2E / tau;
   const float2 q = lane < a.parts ? a.stat[r * a.parts + lane] : make_float2(-INFINITY, 0.0f);
   const float m = wave_max(q.x), base = m == -INFINITY ? 0.0f : m;
-  return make_float2(m, wave_sum(q.y * exp2_32(fmaf(q.x, c, -base * c))));
+  return make_float2(m, wave_sum(q.y * exp2_32((q.x - base) * c)));
 }
 
 template <typename T>
@@ -141,7 +152,7 @@ __device__ inline const T *verify_draft(const VerifyArgs &a, int i, int b) {
 template <typename T, int THREADS>
 __device__ inline VerifySeq verify_decide(const VerifyArgs &a, int b) {
   __shared__ int sh_n;
-  __shared__ float2 sh_max;
+  __shared__ VerifySeq sh_seq;
   const int len = draft_length(a, b), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (threadIdx.x == 0) sh_n = len;
   __syncthreads();
@@ -152,33 +163,34 @@ __device__ inline VerifySeq verify_decide(const VerifyArgs &a, int b) {
     if (d < 0 || d >= a.V) {
       if (a.range_flag) *a.range_flag = 1;
     } else {
+      const float zp = to_f32(verify_target<T>(a, i, b)[d]), zq = a.draft ? to_f32(verify_draft<T>(a, i, b)[d]) : 0.0f;
       const float2 p = verify_row(a, at, a.tau);
-      const double zp = (double)to_f32(verify_target<T>(a, i, b)[d]);
-      const double pd = exp2_64((zp - (double)p.x) * (LOG2E_64 / (double)a.tau)) / (double)p.y;
+      const double pd = exp(((double)zp - (double)p.x) / (double)a.tau) / (double)p.y;
       double qd = 1.0;
       if (a.draft) {
         const float2 q = verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d);
-        const double zq = (double)to_f32(verify_draft<T>(a, i, b)[d]);
-        qd = exp2_64((zq - (double)q.x) * (LOG2E_64 / (double)a.tau_d)) / (double)q.y;
+        qd = q.y == 0.0f ? 0.0 : exp(((double)zq - (double)q.x) / (double)a.tau_d) / (double)q.y;
       }
-      accept = (double)a.u[at] * qd < pd;
+      accept = (double)a.u[at] * qd < pd;  // (false where one is a NaN)
     }
     if (!accept && (threadIdx.x & 63) == 0) atomicMin(&sh_n, i);
   }
   __syncthreads();
-  VerifySeq s;
-  s.n = sh_n;
-  s.mixed = s.n < len;
   if (wave == 0) {
+    VerifySeq s = {};
+    s.n = sh_n;
+    s.mixed = s.n < len;
     const long at = (long)s.n * a.B + b;
-    const float mp = verify_row(a, at, a.tau).x;
-    const float mq = s.mixed && a.draft ? verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d).x : -INFINITY;
-    if (threadIdx.x == 0) sh_max = make_float2(mp, mq);
+    const float2 p = verify_row(a, at, a.tau);
+    float2 q = make_float2(-INFINITY, 0.0f);
+    if (s.mixed && a.draft) q = verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d);
+    s.mp = p.x;
+    s.mq = q.x;
+    s.ok = p.y > 0.0f && p.y - p.y == 0.0f && q.y - q.y == 0.0f;
+    if (threadIdx.x == 0) sh_seq = s;
   }
   __syncthreads();
-  s.mp = sh_max.x;
-  s.mq = sh_max.y;
-  return s;
+  return sh_seq;
 }
 
 template <int THREADS>
@@ -194,187 +206,232 @@ __device__ inline double block_sum(double v) {
   return v;
 }
 
-// One part of the drawn row pair: sums of exponentials.
-template <typename T>
-__global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const VerifyArgs a) {
-  constexpr int N = SlotOf<T>::N;
-  const int b = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const VerifySeq s = verify_decide<T, VERIFY_THREADS>(a, b);
-  if (part == 0 && threadIdx.x == 0) a.seq[b] = s;
-  const bool with_q = s.mixed && a.draft;
-  const T *p = verify_target<T>(a, s.n, b), *q = with_q ? verify_draft<T>(a, s.n, b) : nullptr;
-  const Exp64 ep(s.mp, a.tau), eq(s.mq, a.tau_d);
-  const int first = part * a.per, last = min(first + a.per, (a.V + N - 1) / N);
-  double sp = 0.0, sq = 0.0;
-  for (int j = first + threadIdx.x; j < last; j += VERIFY_THREADS) {
-    const slot_t rp = load_any_slot(p, j, a.V), rq = with_q ? load_any_slot(q, j, a.V) : empty_slot<T>();
-#pragma unroll
-    for (int e = 0; e < N; ++e) sp += ep(slot_elem<T>(rp, e));
-    if (with_q)
-#pragma unroll
-      for (int e = 0; e < N; ++e) sq += eq(slot_elem<T>(rq, e));
-  }
-  sp = block_sum<VERIFY_THREADS>(sp);
-  sq = block_sum<VERIFY_THREADS>(sq);
-  if (threadIdx.x == 0) {
-    a.sums[((long)b * a.parts + part) * 2] = sp;
-    a.sums[((long)b * a.parts + part) * 2 + 1] = sq;
-  }
-}
-
-// r of the drawn row pair, up to a common factor.
+// r of the drawn row pair of a text, and sums over it.  A block is one slot of each lane of a wave.
 template <typename T>
 struct Rest {
-  const T *p, *q;
+  static constexpr int N = SlotOf<T>::N;
+  const T *p, *q;  // q: nullptr where p is drawn from alone
   Exp64 ep, eq;
-  double sp, sq;
-  int V, drop;  // drop: a word without mass (the rejected draft of a text without draft logits), or -1
-  __device__ Rest(const VerifyArgs &a, int b, const VerifySeq &s, const double *sums, bool plain)
+  double sp = 1.0, sq = 1.0;  // 1 / the sums of exponentials
+  int V, drop;                // drop: a word without mass (the rejected draft of a text without draft logits), or -1
+  __device__ Rest(const VerifyArgs &a, int b, const VerifySeq &s)
       : p(verify_target<T>(a, s.n, b)), q(nullptr), ep(s.mp, a.tau), eq(s.mq, a.tau_d), V(a.V), drop(-1) {
-    sp = sq = 0.0;
-    for (int i = 0; i < a.parts; ++i) {
-      sp += sums[2 * i];
-      sq += sums[2 * i + 1];
-    }
-    sp = 1.0 / sp;
-    sq = 1.0 / sq;
-    if (!s.mixed || plain) return;
+    if (!s.mixed) return;
     if (a.draft) q = verify_draft<T>(a, s.n, b);
     else drop = a.drafts[(long)s.n * a.B + b];
   }
-  __device__ double one(float zp, float zq, int v) const {
-    const double r = ep(zp) * sp;
-    if (q) {
-      const double d = r - eq(zq) * sq;
-      return d < 0.0 ? 0.0 : d;  // (a NaN stays one)
-    }
-    return v == drop ? 0.0 : r;
+  __device__ void normalise(double Sp, double Sq) {
+    sp = 1.0 / Sp;
+    sq = Sq == 0.0 ? 0.0 : 1.0 / Sq;  // (a draft row of nothing but masked words has no mass anywhere)
   }
-  __device__ void slot(int j, double (&r)[SlotOf<T>::N]) const {
-    constexpr int N = SlotOf<T>::N;
-    const slot_t rp = load_any_slot(p, j, V), rq = q ? load_any_slot(q, j, V) : empty_slot<T>();
+  __device__ void alone() {
+    q = nullptr;
+    drop = -1;
+  }
+  // Sums of exponentials over blocks [first, last), every so many of them: this lane's.
+  __device__ void exponentials(int first, int last, int step, double &Sp, double &Sq) const {
+    Sp = Sq = 0.0;
+    for (int k = first; k < last; k += step) {
+      const int j = k * 64 + (threadIdx.x & 63);
+      const slot_t rp = load_any_slot(p, j, V), rq = q ? load_any_slot(q, j, V) : empty_slot<T>();
 #pragma unroll
-    for (int e = 0; e < N; ++e) r[e] = one(slot_elem<T>(rp, e), slot_elem<T>(rq, e), j * N + e);
+      for (int e = 0; e < N; ++e) Sp += ep(slot_elem<T>(rp, e));
+      if (q)
+#pragma unroll
+        for (int e = 0; e < N; ++e) Sq += eq(slot_elem<T>(rq, e));
+    }
+  }
+  // This lane's r in block k; returns their sum.
+  __device__ double block(int k, double (&r)[N]) const {
+#pragma clang fp contract(off)  // equal probabilities leave 0: both products are rounded
+    const int j = k * 64 + (threadIdx.x & 63);
+    const slot_t rp = load_any_slot(p, j, V), rq = q ? load_any_slot(q, j, V) : empty_slot<T>();
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      r[e] = ep(slot_elem<T>(rp, e)) * sp;
+      if (q) r[e] = fmax(r[e] - eq(slot_elem<T>(rq, e)) * sq, 0.0);
+      else if (j * N + e == drop) r[e] = 0.0;
+      sum += r[e];
+    }
+    return sum;
+  }
+  __device__ double block_sum_of(int k) const {
+    double r[N];
+    return wave_sum(block(k, r));
   }
 };
 
+// The word on which goal falls in block k, `before` it the sum of the blocks in front of it; by one wave.  Where rounding
+// lets no word's sum pass the goal: the block's last word with any mass (-1: it has none).
 template <typename T>
-__global__ void __launch_bounds__(VERIFY_THREADS) verify_rest_kernel(const VerifyArgs a) {
+__device__ inline int word_of_block(const Rest<T> &rest, int k, double before, double goal) {
   constexpr int N = SlotOf<T>::N;
-  const int b = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
-  const VerifySeq s = a.seq[b];
-  const Rest<T> rest(a, b, s, a.sums + (long)b * a.parts * 2, false);
-  const int first = part * a.per, last = min(first + a.per, (a.V + N - 1) / N);
-  double sum = 0.0;
-  for (int j = first + threadIdx.x; j < last; j += VERIFY_THREADS) {
-    double r[N];
-    rest.slot(j, r);
+  const int lane = threadIdx.x & 63;
+  double r[N];
+  const double mine = rest.block(k, r);
+  const double upto = wave_scan(mine);
+  double c = before + (upto - mine);
+  int found = INT32_MAX, last = -1;
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum += r[e];
+  for (int e = 0; e < N; ++e) {
+    c += r[e];
+    const int v = (k * 64 + lane) * N + e;
+    if (r[e] > 0.0) {
+      last = v;
+      if (c > goal && found == INT32_MAX) found = v;
+    }
   }
-  sum = block_sum<VERIFY_THREADS>(sum);
-  if (threadIdx.x == 0) a.rest[(long)b * a.parts + part] = sum;
+  found = wave_reduce(found, [](int x, int y) { return min(x, y); });
+  last = wave_reduce(last, [](int x, int y) { return max(x, y); });
+  return found == INT32_MAX ? last : found;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(VERIFY_THREADS) verify_draw_kernel(const VerifyArgs a) {
-  constexpr int N = SlotOf<T>::N;
-  __shared__ double sh_sum[VERIFY_THREADS];
-  __shared__ int sh_word;
-  const int b = blockIdx.x, tid = threadIdx.x;
-  const VerifySeq s = a.seq[b];
-  const double *sums = a.sums + (long)b * a.parts * 2, *rests = a.rest + (long)b * a.parts;
-  double total = 0.0;
-  for (int i = 0; i < a.parts; ++i) total += rests[i];
-  const bool plain = total == 0.0;  // p <= q everywhere: p itself
-  const Rest<T> rest(a, b, s, sums, plain);
-  auto of_part = [&](int i) { return plain ? sums[2 * i] * rest.sp : rests[i]; };
-  if (plain) {
-    total = 0.0;
-    for (int i = 0; i < a.parts; ++i) total += of_part(i);
-  }
-  // the first part whose end lies above the number; rounding of the product can leave none: the last one with any mass
-  const double goal = (double)a.u[(long)a.K * a.B + b] * total;
-  double before = 0.0, sum = 0.0, mass_before = 0.0;
-  int part = -1, mass = -1;
-  for (int i = 0; i < a.parts; ++i) {
-    const double next = of_part(i);
-    if (next > 0.0) {
-      mass = i;
-      mass_before = sum;
-    }
-    if (sum + next > goal) {
-      part = i;
-      before = sum;
-      break;
-    }
-    sum += next;
-  }
-  if (part < 0) {
-    part = mass;
-    before = mass_before;
-  }
-  if (tid == 0) sh_word = -1;
-  __syncthreads();
-  if (part >= 0 && total - total == 0.0) {
-    // stretches of neighbouring slots, one for each thread
-    const int first = part * a.per, last = min(first + a.per, (a.V + N - 1) / N);
-    const int stretch = (last - first + VERIFY_THREADS - 1) / VERIFY_THREADS;
-    const int j0 = min(first + tid * stretch, last), j1 = min(j0 + stretch, last);
-    double mine = 0.0;
-    int final = -1;  // last word with any mass
-    for (int j = j0; j < j1; ++j) {
-      double r[N];
-      rest.slot(j, r);
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        mine += r[e];
-        if (r[e] > 0.0) final = j * N + e;
+// The first block whose sums up to it pass u times the whole, by one wave.  Returns the block, or the last with any mass
+// where rounding lets none pass, or -1; before: the sum in front of it; total = 0: there is no mass.
+template <class Load>
+__device__ inline int block_of_number(int blocks, double u, Load &&load, double &before, double &goal, double &total) {
+  const int lane = threadIdx.x & 63, stretch = (blocks + 63) / 64, k0 = min(lane * stretch, blocks), k1 = min(k0 + stretch, blocks);
+  double mine = 0.0;
+  for (int k = k0; k < k1; ++k) mine += load(k);
+  const double upto = wave_scan(mine), from = upto - mine;
+  total = lane_value(upto, 63);
+  goal = u * total;
+  double c = from, in_front = 0.0, last_front = 0.0;
+  int found = INT32_MAX, last = -1;
+  for (int k = k0; k < k1; ++k) {
+    const double s = load(k);
+    if (s > 0.0) {
+      last = k;
+      last_front = c;
+      if (c + s > goal && found == INT32_MAX) {
+        found = k;
+        in_front = c;
       }
     }
-    sh_sum[tid] = mine;
-    __syncthreads();
-    for (int o = 1; o < VERIFY_THREADS; o <<= 1) {
-      const double add = tid >= o ? sh_sum[tid - o] : 0.0;
-      __syncthreads();
-      sh_sum[tid] += add;
-      __syncthreads();
-    }
-    const double upto = before + sh_sum[tid], from = before + (tid ? sh_sum[tid - 1] : 0.0);
-    // sums of stretches rise from thread to thread, so one thread at most sees the number pass; where rounding lets none,
-    // the part's last word with any mass
-    if (from <= goal && upto > goal) {
-      double c = from;
-      int word = final;
-      for (int j = j0; j < j1; ++j) {
-        double r[N];
-        rest.slot(j, r);
-        bool found = false;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          c += r[e];
-          if (!found && c > goal) {
-            found = true;
-            word = j * N + e;
-          }
-        }
-        if (found) break;
-      }
-      sh_word = word | 1 << 30;
-    }
-    __syncthreads();
-    if (sh_word < 0) {
-      __syncthreads();
-      if (final >= 0) atomicMax(&sh_word, final);
-    }
-    __syncthreads();
+    c += s;
   }
-  const int word = sh_word < 0 ? -1 : sh_word & ~(1 << 30);
-  if (tid == 0) a.accepted[b] = s.n;
-  for (int i = tid; i <= a.K; i += VERIFY_THREADS) {
+  const int first = wave_reduce(found, [](int x, int y) { return min(x, y); });
+  const int end = wave_reduce(last, [](int x, int y) { return max(x, y); });
+  const int k = first != INT32_MAX ? first : end;
+  before = 0.0;
+  if (k >= 0) before = lane_value(first != INT32_MAX ? in_front : last_front, __builtin_amdgcn_readfirstlane(k / stretch));
+  return k;
+}
+
+__device__ inline void verify_store(const VerifyArgs &a, int b, int n, int word) {
+  if (threadIdx.x == 0) a.accepted[b] = n;
+  for (int i = threadIdx.x; i <= a.K; i += blockDim.x) {
     const long at = (long)i * a.B + b;
-    a.tokens[at] = i < s.n ? a.drafts[at] : i == s.n ? word : -1;
+    a.tokens[at] = i < n ? a.drafts[at] : i == n ? word : -1;
   }
+}
+
+// The drawn word, by all threads of a workgroup: load(k) is the sum of r over block k; again(): forms the sums of p alone in
+// their place.
+template <typename T, class Load, class Again>
+__device__ inline int verify_draw(const VerifyArgs &a, int b, Rest<T> &rest, Load &&load, Again &&again) {
+  __shared__ int sh_word;
+  constexpr int NONE = -2;  // no mass anywhere
+  auto draw = [&]() {
+    if (threadIdx.x < 64) {
+      double before, goal, total;
+      const int k = block_of_number(a.blocks, (double)a.u[(long)a.K * a.B + b], load, before, goal, total);
+      const int word = total == 0.0 ? NONE : k < 0 ? -1 : word_of_block(rest, k, before, goal);
+      if (threadIdx.x == 0) sh_word = word;
+    }
+    __syncthreads();
+  };
+  draw();
+  if (sh_word == NONE) {  // p <= q everywhere: p itself
+    rest.alone();
+    again();
+    draw();
+  }
+  return max(sh_word, -1);
+}
+
+// One share of the drawn row pair: sums of exponentials.
+template <typename T>
+__global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const VerifyArgs a) {
+  const int b = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const VerifySeq s = verify_decide<T, VERIFY_THREADS>(a, b);
+  if (chunk == 0 && threadIdx.x == 0) a.seq[b] = s;
+  if (!s.ok) return;
+  const Rest<T> rest(a, b, s);
+  const int first = chunk * a.span, last = min(first + a.span, a.blocks);
+  double sp, sq;
+  rest.exponentials(first + (threadIdx.x >> 6), last, VERIFY_THREADS / 64, sp, sq);
+  sp = block_sum<VERIFY_THREADS>(sp);
+  sq = block_sum<VERIFY_THREADS>(sq);
+  if (threadIdx.x == 0) {
+    a.sums[((long)b * a.chunks + chunk) * 2] = sp;
+    a.sums[((long)b * a.chunks + chunk) * 2 + 1] = sq;
+  }
+}
+
+// Sums of r by blocks; the last workgroup of a text draws its word.  (What it reads of the others' moves with agent-scope
+// accesses, each workgroup's before its arrival at the text's counter.)
+template <typename T>
+__global__ void __launch_bounds__(VERIFY_THREADS) verify_rest_kernel(const VerifyArgs a) {
+  __shared__ int sh_last;
+  const int b = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const VerifySeq s = a.seq[b];
+  if (!s.ok) {
+    if (chunk == 0) verify_store(a, b, s.n, -1);
+    return;
+  }
+  Rest<T> rest(a, b, s);
+  double sp = 0.0, sq = 0.0;
+  for (int i = threadIdx.x & 63; i < a.chunks; i += 64) {
+    sp += a.sums[((long)b * a.chunks + i) * 2];
+    sq += a.sums[((long)b * a.chunks + i) * 2 + 1];
+  }
+  rest.normalise(wave_sum(sp), wave_sum(sq));
+  double *const of_block = a.rest + (long)b * a.blocks;
+  auto load = [&](int k) { return __hip_atomic_load(of_block + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  auto form = [&](int first, int last) {
+    for (int k = first + wave; k < last; k += VERIFY_THREADS / 64) {
+      const double r = rest.block_sum_of(k);
+      if ((threadIdx.x & 63) == 0) __hip_atomic_store(of_block + k, r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  form(chunk * a.span, min((chunk + 1) * a.span, a.blocks));
+  if (threadIdx.x == 0)
+    sh_last = __hip_atomic_fetch_add(&a.seq[b].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (unsigned)a.chunks;
+  __syncthreads();
+  if (!sh_last) return;
+  const int word = verify_draw<T>(a, b, rest, load, [&] { form(0, a.blocks); });
+  verify_store(a, b, s.n, word);
+}
+
+// Steps 2 and 3 of a text whose rows are short.
+template <typename T>
+__global__ void __launch_bounds__(VERIFY_ONE_THREADS) verify_one_kernel(const VerifyArgs a) {
+  __shared__ double of_block[VERIFY_ONE_BLOCKS];
+  const int b = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const VerifySeq s = verify_decide<T, VERIFY_ONE_THREADS>(a, b);
+  int word = -1;
+  if (s.ok) {
+    Rest<T> rest(a, b, s);
+    double sp, sq;
+    rest.exponentials(wave, a.blocks, VERIFY_ONE_THREADS / 64, sp, sq);
+    sp = block_sum<VERIFY_ONE_THREADS>(sp);
+    sq = block_sum<VERIFY_ONE_THREADS>(sq);
+    rest.normalise(sp, sq);
+    auto form = [&] {
+      for (int k = wave; k < a.blocks; k += VERIFY_ONE_THREADS / 64) {
+        const double r = rest.block_sum_of(k);
+        if ((threadIdx.x & 63) == 0) of_block[k] = r;
+      }
+      __syncthreads();
+    };
+    form();
+    word = verify_draw<T>(a, b, rest, [&](int k) { return of_block[k]; }, form);
+  }
+  verify_store(a, b, s.n, word);
 }
 
 }  // namespace rnnlm_dev

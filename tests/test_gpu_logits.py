@@ -58,6 +58,12 @@ def patterns(kind, rows, V, seed):
         z[:, : min(V, 300)] += 40.0
     elif kind == "steep":  # far apart: later words dwarf the earlier ones
         z = np.linspace(-200.0, 250.0, V)[None] + z
+    elif kind == "offset":  # far from zero altogether
+        z += 3e4
+    elif kind == "all lowest":  # a mask that leaves nothing, of the type's lowest value
+        z[:] = -3e38
+    elif kind == "huge":
+        z *= 1e30
     elif kind == "lowest":  # masks of the type's lowest value
         z[rng.random((rows, V)) < 0.9] = -3e38
     return z
@@ -86,7 +92,7 @@ def test_top_logits_sizes(rows, V, K, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("kind", ["equal", "masked", "few", "rising", "falling", "ties", "zeros", "nan", "infinite", "clustered", "lowest", "steep"])
+@pytest.mark.parametrize("kind", ["equal", "masked", "few", "rising", "falling", "ties", "zeros", "nan", "infinite", "clustered", "lowest", "steep", "offset", "all lowest", "huge"])
 @pytest.mark.parametrize("V,K", [(300, 256), (5000, 40), (20011, 256)])
 def test_top_logits_patterns(V, K, kind, dtype):
     check_top(patterns(kind, 3, V, 7), K, 1.0, dtype, 0)
@@ -183,7 +189,7 @@ def test_distill_sizes(rows, V, K, pad, dtype):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
-@pytest.mark.parametrize("kind", ["equal", "steep", "falling", "clustered", "lowest", "late"])
+@pytest.mark.parametrize("kind", ["equal", "steep", "falling", "clustered", "lowest", "late", "offset", "all lowest", "huge"])
 @pytest.mark.parametrize("V", [1203, 9001, 70001])
 def test_distill_patterns(V, kind, tau, dtype):
     z = patterns("normal" if kind == "late" else kind, 2, V, 5)
@@ -331,8 +337,21 @@ def test_verify_without_drafts_draws_from_the_row(B, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_verify_masked_rows_and_rows_that_are_no_numbers(dtype):
-    K, B, V = 2, 8, 515
+@pytest.mark.parametrize("kind", ["equal", "steep", "offset", "all lowest", "lowest", "huge", "ties"])
+@pytest.mark.parametrize("V", [900, 50001])
+def test_verify_patterns(V, kind, dtype):
+    K, B = 2, 3
+    target, draft = (patterns(kind, n * B, V, s).reshape(n, B, V) for n, s in ((K + 1, 1), (K, 2)))
+    rng = np.random.default_rng(3)
+    drafts = np.array([[rng.choice(np.argsort(draft[i, b])[-20:]) for b in range(B)] for i in range(K)], np.int32)
+    for d in (draft, None):
+        check_verify(target, drafts, rng.random((K + 1, B)) * 0.5, d, None, 1.0, 2.0, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [515, 40007])
+def test_verify_masked_rows_and_rows_that_are_no_numbers(V, dtype):
+    K, B = 2, 10
     target, draft, drafts, u, _ = texts(K, B, V, 11)
     target[:, 0] = -np.inf                    # nothing left: no draft accepted, no word
     target[0, 1, 17] = np.nan
@@ -346,14 +365,17 @@ def test_verify_masked_rows_and_rows_that_are_no_numbers(dtype):
     draft[:, 7], target[:, 7] = -np.inf, -np.inf
     draft[:, 7, 9] = target[:, 7, 9] = 0.0    # one word left in both, and it is the draft
     drafts[:, 7] = 9
+    draft[:, 8] = -np.inf                     # a drafter without a word
+    draft[0, 9, 7], u[0, 9] = np.nan, 0.9
     n, tokens, _ = check_verify(target, drafts, u, draft, dtype=dtype)
     assert tokens[:, 0].tolist() == tokens[:, 1].tolist() == tokens[:, 5].tolist() == [-1, -1, -1]
     assert n[4] == K and tokens[:, 7].tolist() == [9, 9, 9]
     check_verify(target, drafts, u, None, dtype=dtype)
 
 
-def test_verify_numbers_at_the_ends():
-    K, B, V = 1, 6, 1000
+@pytest.mark.parametrize("V", [1000, 20000, 100003])
+def test_verify_numbers_at_the_ends(V):
+    K, B = 1, 6
     target, draft, drafts, u, _ = texts(K, B, V, 4)
     u[:, :2], u[:, 2:4] = 0.0, np.float32(1.0) - np.float32(2.0 ** -24)
     check_verify(target, drafts, u, draft)
@@ -363,6 +385,16 @@ def test_verify_numbers_at_the_ends():
     z[:, :, :2] = 0.0
     assert check_verify(z, np.zeros((1, 1), np.int32), np.array([[0.5], [0.2]]))[0].tolist() == [0]
     assert check_verify(z, np.zeros((1, 1), np.int32), np.array([[0.49999997], [0.2]]))[0].tolist() == [1]
+
+
+@pytest.mark.parametrize("V", [3000, 33000, 100000])
+def test_verify_a_draft_model_that_is_the_target(V):
+    """Every draft of positive probability is accepted; one that is not drawn from the model's words leaves r = 0: p itself."""
+    K, B = 2, 4
+    target, draft, drafts, u, _ = texts(K, B, V, 3, 0.0)
+    assert check_verify(target, drafts, u, draft)[0].tolist() == [K] * B
+    target[0, :, drafts[0]] = draft[0, :, drafts[0]] = -np.inf
+    assert check_verify(target, drafts, u, draft)[0].tolist() == [0] * B
 
 
 def test_verify_drafts_out_of_range_and_lengths_beyond_the_batch():

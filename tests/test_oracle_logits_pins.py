@@ -15,6 +15,12 @@ def test_lse_and_top_by_hand():
     assert L.lse([-np.inf, -np.inf]) == -np.inf and np.isnan(L.lse([0.0, np.nan])) and np.isnan(L.lse([0.0, np.inf]))
 
 
+def test_softmax_sums_to_one_wherever_the_logits_are():
+    for z in ([1.0, 2.0, 3.0], [-3e38] * 7, [1e30, 1e30, -1e30], [5e4, 5e4 + 1.0, -np.inf]):
+        assert L.softmax(z, 0.7).sum() == pytest.approx(1.0, abs=1e-15)
+    assert L.softmax([-np.inf] * 3).tolist() == [0.0] * 3 and np.isnan(L.softmax([0.0, np.inf])).any() and np.isnan(L.softmax([np.nan, 0.0])).all()
+
+
 def test_distillation_from_the_student_itself_costs_nothing():
     z = np.random.default_rng(0).normal(size=50)
     loss, grad = L.distill(z, np.arange(50), z, L.lse(z, 2.0), tau=2.0)
