@@ -17,6 +17,7 @@
 namespace rnnlm_dev {
 
 constexpr int VERIFY_THREADS = 256, VERIFY_PARTS = 64;
+constexpr int VERIFY_STAGED = 1024;  // sums of blocks that the drawing workgroup holds in LDS
 constexpr int VERIFY_ONE_THREADS = 1024, VERIFY_ONE_BLOCKS = 64;  // a text in one workgroup: rows of at most so many blocks
 
 struct VerifySeq {  // what the steps behind the second one know of a text
@@ -148,49 +149,56 @@ __device__ inline const T *verify_draft(const VerifyArgs &a, int i, int b) {
   return static_cast<const T *>(a.draft) + ((long)i * a.B + b) * a.ldd;
 }
 
-// How many drafts of text b are accepted: a wave to each draft.  All threads of the workgroup take part.
+// How many drafts of text b are accepted: a wave to each row, all loads but the drafts' own logits at once (what is read of
+// rows behind the text's drafts was never written, and counts for nothing).  All threads of the workgroup take part.
 template <typename T, int THREADS>
 __device__ inline VerifySeq verify_decide(const VerifyArgs &a, int b) {
-  __shared__ int sh_n;
-  __shared__ VerifySeq sh_seq;
+  constexpr int WAVES = THREADS / 64, KEPT = 2 * WAVES;
+  __shared__ float4 sh_row[KEPT];  // maximum and sum of p, of q
+  __shared__ int sh_reject[WAVES];
   const int len = draft_length(a, b), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (threadIdx.x == 0) sh_n = len;
-  __syncthreads();
-  for (int i = wave; i < len; i += THREADS / 64) {
+  int reject = INT32_MAX;
+  for (int i = wave; i <= a.K; i += WAVES) {
     const long at = (long)i * a.B + b;
-    const int d = a.drafts[at];
-    bool accept = false;
-    if (d < 0 || d >= a.V) {
-      if (a.range_flag) *a.range_flag = 1;
-    } else {
-      const float zp = to_f32(verify_target<T>(a, i, b)[d]), zq = a.draft ? to_f32(verify_draft<T>(a, i, b)[d]) : 0.0f;
-      const float2 p = verify_row(a, at, a.tau);
-      const double pd = exp(((double)zp - (double)p.x) / (double)a.tau) / (double)p.y;
-      double qd = 1.0;
-      if (a.draft) {
-        const float2 q = verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d);
-        qd = q.y == 0.0f ? 0.0 : exp(((double)zq - (double)q.x) / (double)a.tau_d) / (double)q.y;
-      }
-      accept = (double)a.u[at] * qd < pd;  // (false where one is a NaN)
+    const bool drafted = i < a.K;
+    const int d = drafted ? a.drafts[at] : 0;
+    const bool in_range = d >= 0 && d < a.V;
+    float zp = 0.0f, zq = 0.0f;
+    if (drafted && in_range) {
+      zp = to_f32(verify_target<T>(a, i, b)[d]);
+      if (a.draft) zq = to_f32(verify_draft<T>(a, i, b)[d]);
     }
-    if (!accept && (threadIdx.x & 63) == 0) atomicMin(&sh_n, i);
-  }
-  __syncthreads();
-  if (wave == 0) {
-    VerifySeq s = {};
-    s.n = sh_n;
-    s.mixed = s.n < len;
-    const long at = (long)s.n * a.B + b;
     const float2 p = verify_row(a, at, a.tau);
-    float2 q = make_float2(-INFINITY, 0.0f);
-    if (s.mixed && a.draft) q = verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d);
-    s.mp = p.x;
-    s.mq = q.x;
-    s.ok = p.y > 0.0f && p.y - p.y == 0.0f && q.y - q.y == 0.0f;
-    if (threadIdx.x == 0) sh_seq = s;
+    const float2 q = drafted && a.draft ? verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d) : make_float2(-INFINITY, 0.0f);
+    if (i < KEPT && (threadIdx.x & 63) == 0) sh_row[i] = make_float4(p.x, p.y, q.x, q.y);
+    if (i >= len) continue;
+    bool accept = false;
+    if (in_range) {
+      const double pd = exp(((double)zp - (double)p.x) / (double)a.tau) / (double)p.y;
+      const double qd = !a.draft ? 1.0 : q.y == 0.0f ? 0.0 : exp(((double)zq - (double)q.x) / (double)a.tau_d) / (double)q.y;
+      accept = (double)a.u[at] * qd < pd;  // (false where one is a NaN)
+    } else if (a.range_flag) {
+      *a.range_flag = 1;
+    }
+    if (!accept) reject = min(reject, i);
   }
+  if ((threadIdx.x & 63) == 0) sh_reject[wave] = reject;
   __syncthreads();
-  return sh_seq;
+  VerifySeq s = {};
+  s.n = min(len, group_reduce<WAVES>(sh_reject[threadIdx.x & (WAVES - 1)], [](int x, int y) { return min(x, y); }));
+  s.n = __builtin_amdgcn_readfirstlane(s.n);
+  s.mixed = s.n < len;
+  if (s.n >= KEPT) {
+    const long at = (long)s.n * a.B + b;
+    const float2 p = verify_row(a, at, a.tau), q = s.mixed && a.draft ? verify_row(a, (long)(a.K + 1) * a.B + at, a.tau_d) : make_float2(-INFINITY, 0.0f);
+    if (threadIdx.x == 0) sh_row[0] = make_float4(p.x, p.y, q.x, q.y);
+    __syncthreads();
+  }
+  const float4 row = sh_row[s.n < KEPT ? s.n : 0];
+  s.mp = row.x;
+  s.mq = row.z;
+  s.ok = row.y > 0.0f && row.y - row.y == 0.0f && (!s.mixed || row.w - row.w == 0.0f);
+  return s;
 }
 
 template <int THREADS>
@@ -228,37 +236,49 @@ struct Rest {
     q = nullptr;
     drop = -1;
   }
-  // Sums of exponentials over blocks [first, last), every so many of them: this lane's.
-  __device__ void exponentials(int first, int last, int step, double &Sp, double &Sq) const {
-    Sp = Sq = 0.0;
+  struct Block {
+    slot_t p, q;
+  };
+  // This lane's slots of block k, both loads at once.
+  __device__ __forceinline__ Block load(int k) const {
+    const int j = k * 64 + (threadIdx.x & 63);
+    Block o;
+    o.q = empty_slot<T>();
+    if ((k + 1) * 64 * N <= V) {
+      o.p = load_slot(p, j);
+      if (q) o.q = load_slot(q, j);
+    } else {
+      o.p = load_any_slot(p, j, V);
+      if (q) o.q = load_any_slot(q, j, V);
+    }
+    return o;
+  }
+  // Calls f(k, block) for blocks first, first + step, ... < last, the next one's loads ahead of it.
+  template <class F>
+  __device__ __forceinline__ void each(int first, int last, int step, F &&f) const {
+    if (first >= last) return;
+    Block next = load(first);
     for (int k = first; k < last; k += step) {
-      const int j = k * 64 + (threadIdx.x & 63);
-      const slot_t rp = load_any_slot(p, j, V), rq = q ? load_any_slot(q, j, V) : empty_slot<T>();
-#pragma unroll
-      for (int e = 0; e < N; ++e) Sp += ep(slot_elem<T>(rp, e));
-      if (q)
-#pragma unroll
-        for (int e = 0; e < N; ++e) Sq += eq(slot_elem<T>(rq, e));
+      const Block now = next;
+      if (k + step < last) next = load(k + step);
+      f(k, now);
     }
   }
   // This lane's r in block k; returns their sum.
-  __device__ double block(int k, double (&r)[N]) const {
+  __device__ __forceinline__ double rest(int k, const Block &o, double (&r)[N]) const {
 #pragma clang fp contract(off)  // equal probabilities leave 0: both products are rounded
-    const int j = k * 64 + (threadIdx.x & 63);
-    const slot_t rp = load_any_slot(p, j, V), rq = q ? load_any_slot(q, j, V) : empty_slot<T>();
+    const int v0 = (k * 64 + (threadIdx.x & 63)) * N;
     double sum = 0.0;
+    if (q) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      r[e] = ep(slot_elem<T>(rp, e)) * sp;
-      if (q) r[e] = fmax(r[e] - eq(slot_elem<T>(rq, e)) * sq, 0.0);
-      else if (j * N + e == drop) r[e] = 0.0;
-      sum += r[e];
+      for (int e = 0; e < N; ++e) r[e] = fmax(ep(slot_elem<T>(o.p, e)) * sp - eq(slot_elem<T>(o.q, e)) * sq, 0.0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) r[e] = v0 + e == drop ? 0.0 : ep(slot_elem<T>(o.p, e)) * sp;
     }
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum += r[e];
     return sum;
-  }
-  __device__ double block_sum_of(int k) const {
-    double r[N];
-    return wave_sum(block(k, r));
   }
 };
 
@@ -269,7 +289,7 @@ __device__ inline int word_of_block(const Rest<T> &rest, int k, double before, d
   constexpr int N = SlotOf<T>::N;
   const int lane = threadIdx.x & 63;
   double r[N];
-  const double mine = rest.block(k, r);
+  const double mine = rest.rest(k, rest.load(k), r);
   const double upto = wave_scan(mine);
   double c = before + (upto - mine);
   int found = INT32_MAX, last = -1;
@@ -351,6 +371,19 @@ __device__ inline int verify_draw(const VerifyArgs &a, int b, Rest<T> &rest, Loa
   return max(sh_word, -1);
 }
 
+// This lane's sums of exponentials over blocks [first, last) of the drawn row pair.
+template <typename T, int THREADS>
+__device__ __forceinline__ void verify_exponentials(const Rest<T> &rest, int first, int last, double &sp, double &sq) {
+  sp = sq = 0.0;
+  rest.each(first + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), last, THREADS / 64, [&](int, const typename Rest<T>::Block &o) {
+#pragma unroll
+    for (int e = 0; e < SlotOf<T>::N; ++e) sp += rest.ep(slot_elem<T>(o.p, e));
+    if (rest.q)
+#pragma unroll
+      for (int e = 0; e < SlotOf<T>::N; ++e) sq += rest.eq(slot_elem<T>(o.q, e));
+  });
+}
+
 // One share of the drawn row pair: sums of exponentials.
 template <typename T>
 __global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const VerifyArgs a) {
@@ -361,7 +394,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const Verif
   const Rest<T> rest(a, b, s);
   const int first = chunk * a.span, last = min(first + a.span, a.blocks);
   double sp, sq;
-  rest.exponentials(first + (threadIdx.x >> 6), last, VERIFY_THREADS / 64, sp, sq);
+  verify_exponentials<T, VERIFY_THREADS>(rest, first, last, sp, sq);
   sp = block_sum<VERIFY_THREADS>(sp);
   sq = block_sum<VERIFY_THREADS>(sq);
   if (threadIdx.x == 0) {
@@ -390,11 +423,19 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_rest_kernel(const Verif
   rest.normalise(wave_sum(sp), wave_sum(sq));
   double *const of_block = a.rest + (long)b * a.blocks;
   auto load = [&](int k) { return __hip_atomic_load(of_block + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  __shared__ double staged[VERIFY_STAGED];
+  const bool stage = a.blocks <= VERIFY_STAGED;
+  auto fetch = [&] {  // all loads at once: one after the other each takes a trip to memory
+    if (!stage) return;
+    for (int k = threadIdx.x; k < a.blocks; k += VERIFY_THREADS) staged[k] = load(k);
+    __syncthreads();
+  };
   auto form = [&](int first, int last) {
-    for (int k = first + wave; k < last; k += VERIFY_THREADS / 64) {
-      const double r = rest.block_sum_of(k);
-      if ((threadIdx.x & 63) == 0) __hip_atomic_store(of_block + k, r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    rest.each(first + wave, last, VERIFY_THREADS / 64, [&](int k, const typename Rest<T>::Block &o) {
+      double r[Rest<T>::N];
+      const double sum = wave_sum(rest.rest(k, o, r));
+      if ((threadIdx.x & 63) == 0) __hip_atomic_store(of_block + k, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
   };
@@ -403,7 +444,11 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_rest_kernel(const Verif
     sh_last = __hip_atomic_fetch_add(&a.seq[b].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == (unsigned)a.chunks;
   __syncthreads();
   if (!sh_last) return;
-  const int word = verify_draw<T>(a, b, rest, load, [&] { form(0, a.blocks); });
+  fetch();
+  const int word = verify_draw<T>(a, b, rest, [&](int k) { return stage ? staged[k] : load(k); }, [&] {
+    form(0, a.blocks);
+    fetch();
+  });
   verify_store(a, b, s.n, word);
 }
 
@@ -417,15 +462,16 @@ __global__ void __launch_bounds__(VERIFY_ONE_THREADS) verify_one_kernel(const Ve
   if (s.ok) {
     Rest<T> rest(a, b, s);
     double sp, sq;
-    rest.exponentials(wave, a.blocks, VERIFY_ONE_THREADS / 64, sp, sq);
+    verify_exponentials<T, VERIFY_ONE_THREADS>(rest, 0, a.blocks, sp, sq);
     sp = block_sum<VERIFY_ONE_THREADS>(sp);
     sq = block_sum<VERIFY_ONE_THREADS>(sq);
     rest.normalise(sp, sq);
     auto form = [&] {
-      for (int k = wave; k < a.blocks; k += VERIFY_ONE_THREADS / 64) {
-        const double r = rest.block_sum_of(k);
-        if ((threadIdx.x & 63) == 0) of_block[k] = r;
-      }
+      rest.each(wave, a.blocks, VERIFY_ONE_THREADS / 64, [&](int k, const typename Rest<T>::Block &o) {
+        double r[Rest<T>::N];
+        const double sum = wave_sum(rest.rest(k, o, r));
+        if ((threadIdx.x & 63) == 0) of_block[k] = sum;
+      });
       __syncthreads();
     };
     form();
