@@ -58,10 +58,11 @@ TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   auto chunks = [&]() { return (slots + p.nv * p.threads - 1) / (p.nv * p.threads); };
   if (chunks() == 1) {
     while (p.nv > 2 && p.nv / 2 * p.threads >= slots) p.nv /= 2;
-  } else if (slots <= TOP_WIDE * 16 && rows >= 512) {
+  } else if (slots <= TOP_WIDE * 20 && rows >= 512) {
     p.threads = TOP_WIDE;
+    if (slots > TOP_WIDE * 16) p.nv = 20;
   } else {
-    while (p.nv > 2 && rows * chunks() < 512 && 2 * chunks() * K <= TOP_MERGE_LDS) p.nv /= 2;
+    while (p.nv > 4 && rows * chunks() < 512 && 2 * chunks() * K <= TOP_CAP) p.nv /= 2;
   }
   p.chunks = chunks();
   p.per = (slots + p.chunks - 1) / p.chunks;
@@ -82,7 +83,8 @@ void launch_top_chunks(const TopArgs &a, int64_t rows, hipStream_t st) {
 }
 template <typename T>
 void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st) {
-  if (p.threads == TOP_WIDE) launch_top_chunks<T, TOP_WIDE, 16>(a, rows, st);
+  if (p.threads == TOP_WIDE && p.nv == 20) launch_top_chunks<T, TOP_WIDE, 20>(a, rows, st);
+  else if (p.threads == TOP_WIDE) launch_top_chunks<T, TOP_WIDE, 16>(a, rows, st);
   else if (p.nv == 2) launch_top_chunks<T, 256, 2>(a, rows, st);
   else if (p.nv == 4) launch_top_chunks<T, 256, 4>(a, rows, st);
   else if (p.nv == 8) launch_top_chunks<T, 256, 8>(a, rows, st);

@@ -51,6 +51,20 @@ __device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned 
 // ln of the sum s relative to 2^ref.
 __device__ inline float row_lse(double ref, float s) { return s == 0.0f ? -INFINITY : (float)((ref + log2((double)s)) * LN2_64); }
 
+// store(rank, key) for the K greatest of n keys in LDS: eight lanes to a key, each counts an eighth of the others.
+template <int THREADS, class Store>
+__device__ inline void top_ranks(const unsigned long long *cand, int n, int K, Store &&store) {
+  for (int i0 = 0; i0 < n; i0 += THREADS / 8) {
+    const int i = i0 + threadIdx.x / 8;
+    const unsigned long long key = i < n ? cand[i] : ~0ull;
+    int rank = 0;
+#pragma unroll 4
+    for (int j = threadIdx.x & 7; j < n; j += 8) rank += cand[j] > key;
+    rank = group_reduce<8>(rank, [](int x, int y) { return x + y; });
+    if (i < n && rank < K && (threadIdx.x & 7) == 0) store(rank, key);
+  }
+}
+
 // A threshold that at least K of 64 G numbers reach, and few more; by one wave.  (Bisection: a count takes 2 G instructions.)
 template <int G>
 __device__ inline unsigned top_threshold(const unsigned *group, int K, unsigned greatest) {
@@ -229,19 +243,11 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
     __syncthreads();
     n = (int)sh_n;
   }
-  // 4.  Eight lanes to a candidate: each counts an eighth of the others.
-  for (int i0 = 0; i0 < n; i0 += THREADS / 8) {
-    const int i = i0 + tid / 8;
-    const unsigned long long key = i < n ? cand[i] : ~0ull;
-    int rank = 0;
-#pragma unroll 4
-    for (int j = tid & 7; j < n; j += 8) rank += cand[j] > key;
-    rank = group_reduce<8>(rank, [](int x, int y) { return x + y; });
-    if (i < n && rank < K && (tid & 7) == 0) {
-      if (a.chunks == 1) top_store(a, row, rank, key);
-      else a.part[(long)blockIdx.x * K + rank] = key;
-    }
-  }
+  // 4.
+  top_ranks<THREADS>(cand, n, K, [&](int rank, unsigned long long key) {
+    if (a.chunks == 1) top_store(a, row, rank, key);
+    else a.part[(long)blockIdx.x * K + rank] = key;
+  });
   if (a.chunks > 1)
     for (int i = n + tid; i < K; i += THREADS) a.part[(long)blockIdx.x * K + i] = 0;
   if (wave == 0) {
@@ -254,34 +260,57 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   }
 }
 
-// Joins the chunks of a row.  A key's rank: its place in its own chunk's list, and how many keys of the other lists are above
-// it (each by bisection).
+// Joins the chunks of a row.  Each list's K / chunks greatest are at least K keys together, so no key below the least of them
+// is wanted: the others (K to 3 K of them) are ranked among each other.  Where that leaves too many, a key's rank is its place in
+// its own list and how many keys of the other lists are above it, each by bisection.
 __global__ void __launch_bounds__(TOP_MERGE_THREADS) top_merge_kernel(const TopArgs a) {
-  __shared__ unsigned long long lds[TOP_MERGE_LDS];
+  __shared__ unsigned long long lds[TOP_MERGE_LDS], cand[TOP_CAP];
+  __shared__ unsigned long long sh_least;
+  __shared__ unsigned sh_n;
   const long row = blockIdx.x;
-  const int n = a.chunks * a.K, K = a.K;
+  const int n = a.chunks * a.K, K = a.K, tid = threadIdx.x;
   const unsigned long long *key = a.part + row * n;
-  if (n <= TOP_MERGE_LDS) {  // (more: the widest vocabularies with the longest lists)
-    for (int i = threadIdx.x; i < n; i += TOP_MERGE_THREADS) lds[i] = key[i];
-    __syncthreads();
-    key = lds;
+  if (tid == 0) sh_n = 0;
+  if (tid < 64) {
+    unsigned long long least = ~0ull;
+    for (int l = tid; l < a.chunks; l += 64) least = min(least, key[l * K + (K + a.chunks - 1) / a.chunks - 1]);
+    least = wave_reduce(least, [](unsigned long long x, unsigned long long y) { return x < y ? x : y; });
+    if (tid == 0) sh_least = least;
   }
-  for (int i = threadIdx.x; i < n; i += TOP_MERGE_THREADS) {
+  const bool in_lds = n <= TOP_MERGE_LDS;  // (more: the widest vocabularies with the longest lists)
+  if (in_lds)
+    for (int i = tid; i < n; i += TOP_MERGE_THREADS) lds[i] = key[i];
+  __syncthreads();
+  if (in_lds) key = lds;
+  const unsigned long long least = sh_least;
+  for (int i = tid; i < n; i += TOP_MERGE_THREADS) {
     const unsigned long long k = key[i];
-    if (k == 0) continue;
-    const int mine = i / K;
-    int rank = i - mine * K;
-    for (int l = 0; l < a.chunks && rank < K; ++l) {
-      if (l == mine) continue;
-      int lo = 0, hi = K;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (key[l * K + mid] > k) lo = mid + 1;
-        else hi = mid;
-      }
-      rank += lo;
+    if (k >= least && k != 0) {
+      const unsigned at = atomicAdd(&sh_n, 1u);
+      if (at < TOP_CAP) cand[at] = k;
     }
-    if (rank < K) top_store(a, row, rank, k);
+  }
+  __syncthreads();
+  if (sh_n <= TOP_CAP) {
+    top_ranks<TOP_MERGE_THREADS>(cand, (int)sh_n, K, [&](int rank, unsigned long long k) { top_store(a, row, rank, k); });
+  } else {
+    for (int i = tid; i < n; i += TOP_MERGE_THREADS) {
+      const unsigned long long k = key[i];
+      if (k == 0) continue;
+      const int mine = i / K;
+      int rank = i - mine * K;
+      for (int l = 0; l < a.chunks && rank < K; ++l) {
+        if (l == mine) continue;
+        int lo = 0, hi = K;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (key[l * K + mid] > k) lo = mid + 1;
+          else hi = mid;
+        }
+        rank += lo;
+      }
+      if (rank < K) top_store(a, row, rank, k);
+    }
   }
   if (threadIdx.x < 64 && a.lse) {
     double ref = -INFINITY;
