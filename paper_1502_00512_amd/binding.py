@@ -168,53 +168,68 @@ def rnnlm_sort_segments_static(x, V: int, perm, seg_start, nseg, range_flag=None
 
 
 # -- operators on arrays of logits: device tensors, no handle ------------------------------------------------
-def _need(ok, call: str, what: str):
-    if not ok:
-        raise RnnlmError(-1, f"{call}: {what}")
+# (A call's checks are a good part of its time where its kernels take some 5 us: no message is formed unless it is raised.)
+def _refuse(call: str, what: str):
+    raise RnnlmError(-1, f"{call}: {what}")
 
 
-def _rows(call, name, t, device=None, dtype=None):
-    """(rows, V, elements from row to row, dtype) of a tensor [..., V] whose rows are evenly spaced and dense in V."""
+def _rows(call, name, t, like=None):
+    """(rows, V, elements from row to row, dtype) of a tensor [..., V] whose rows are evenly spaced and dense in V; like: a
+    tensor whose device and type it has to share."""
     import torch
-    _need(t.dim() >= 2 and t.shape[-1] >= 1 and t.is_cuda, call, f"{name}: rows of logits on a GPU are wanted")
-    _need(t.dtype in (torch.float32, torch.bfloat16), call, f"{name}: float32 or bfloat16 is wanted")
-    _need(device is None or t.device == device, call, f"{name}: on another device")
-    _need(dtype is None or t.dtype == dtype, call, f"{name}: of another type")
-    V, rows, ld = t.shape[-1], 1, None
-    _need(V == 1 or t.stride(-1) == 1, call, f"{name}: a row's elements have to be neighbours")
-    for n, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    dtype = t.dtype
+    if not t.is_cuda or (dtype is not torch.float32 and dtype is not torch.bfloat16):
+        _refuse(call, f"{name}: float32 or bfloat16 rows on a GPU are wanted")
+    if like is not None and (dtype is not like.dtype or t.get_device() != like.get_device()):
+        _refuse(call, f"{name}: another type or device than the other logits'")
+    shape, stride = t.shape, t.stride()
+    if len(shape) < 2 or (V := shape[-1]) < 1 or (stride[-1] != 1 and V > 1):
+        _refuse(call, f"{name}: rows of neighbouring logits are wanted")
+    rows, ld = 1, None
+    for i in range(len(shape) - 2, -1, -1):
+        n = shape[i]
         if n != 1:
-            ld = step if ld is None else ld
-            _need(step == ld * rows, call, f"{name}: rows have to be evenly spaced")
-        rows *= n
-    ld = V if ld is None else ld
-    _need(ld >= V or rows == 0, call, f"{name}: rows overlap")
-    return rows, V, max(ld, V), RNNLM_DTYPE_FP32 if t.dtype == torch.float32 else RNNLM_DTYPE_BF16
+            if ld is None:
+                ld = stride[i]
+            if stride[i] != ld * rows:
+                _refuse(call, f"{name}: rows have to be evenly spaced")
+            rows *= n
+    if ld is None or rows == 0:
+        ld = V
+    elif ld < V:
+        _refuse(call, f"{name}: rows overlap")
+    return rows, V, ld, RNNLM_DTYPE_FP32 if dtype is torch.float32 else RNNLM_DTYPE_BF16
 
 
-def _dense(call, name, t, dtype, shape, device):
-    """A contiguous tensor of that many elements (its last dimension as given), or None."""
+def _at(call, name, t, dtype, n, device, last=None):
+    """Address of a contiguous tensor of n elements (its last dimension, if given) on that device; None of None."""
     if t is None:
-        return
-    n = 1
-    for s in shape:
-        n *= s
-    _need(t.dtype == dtype and t.device == device and t.is_contiguous() and t.numel() == n and
-          (len(shape) < 2 or t.shape[-1] == shape[-1]), call, f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is wanted")
+        return None
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous() or (last is not None and t.shape[-1] != last):
+        _refuse(call, f"{name}: a contiguous {dtype} tensor of {n} elements on device {device} is wanted"
+                + ("" if last is None else f", {last} in its last dimension"))
+    return t.data_ptr()
 
 
-def _scratch(call, t, nbytes, device):
+def _scratch(call, t, device, nbytes):
+    """(address, bytes, the tensor) of the workspace given, or of a new one of nbytes() bytes."""
     import torch
     if t is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _need(t.device == device and t.is_contiguous(), call, "workspace: a contiguous tensor on the logits' device is wanted")
-    return t
+        t = torch.empty(max(nbytes(), 1), dtype=torch.uint8, device=torch.device("cuda", device))
+    elif t.get_device() != device or not t.is_contiguous():
+        _refuse(call, "workspace: a contiguous tensor on the logits' device is wanted")
+    return t.data_ptr(), t.nbytes, t
 
 
-def _on(device, stream):
-    """(guard that makes the device current, the stream)"""
+def _launch(device, stream, f, *args):
+    """f(*args, the stream) with that device current."""
     import torch
-    return torch.cuda.device(device), C.c_void_p((torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if torch.cuda.current_device() == device:
+        return f(*args, stream.cuda_stream)
+    with torch.cuda.device(device):
+        return f(*args, stream.cuda_stream)
 
 
 def rnnlm_top_logits_workspace_bytes(rows: int, V: int, K: int, dtype: int) -> int:
@@ -227,20 +242,16 @@ def rnnlm_top_logits(logits, K: int, tau: float = 1.0, ids=None, vals=None, lse=
     import torch
     call = "rnnlm_top_logits"
     rows, V, ld, dt = _rows(call, "logits", logits)
-    dev, lead = logits.device, logits.shape[:-1]
-    nbytes = rnnlm_top_logits_workspace_bytes(rows, V, K, dt)
-    _need(nbytes > 0, call, f"K = {K} of V = {V}, {rows} rows")
-    ids = torch.empty(*lead, K, dtype=torch.int32, device=dev) if ids is None else ids
-    vals = torch.empty(*lead, K, dtype=torch.float32, device=dev) if vals is None else vals
-    lse = torch.empty(lead, dtype=torch.float32, device=dev) if lse is None else lse
-    _dense(call, "ids", ids, torch.int32, (rows, K), dev)
-    _dense(call, "vals", vals, torch.float32, (rows, K), dev)
-    _dense(call, "lse", lse, torch.float32, (rows,), dev)
-    workspace = _scratch(call, workspace, nbytes, dev)
-    guard, st = _on(dev, stream)
-    with guard:
-        _ok(load().rnnlm_top_logits(_ptr(logits), dt, rows, V, ld, K, tau, _ptr(ids), _ptr(vals), _ptr(lse), _ptr(workspace),
-                                    workspace.nbytes, st), call)
+    dev, lead = logits.get_device(), logits.shape[:-1]
+    if not 1 <= K <= V:
+        _refuse(call, f"K = {K} of V = {V}")
+    ids = torch.empty(*lead, K, dtype=torch.int32, device=logits.device) if ids is None else ids
+    vals = torch.empty(*lead, K, dtype=torch.float32, device=logits.device) if vals is None else vals
+    lse = torch.empty(lead, dtype=torch.float32, device=logits.device) if lse is None else lse
+    at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_top_logits_workspace_bytes(rows, V, K, dt))
+    _ok(_launch(dev, stream, load().rnnlm_top_logits, logits.data_ptr(), dt, rows, V, ld, K, tau,
+                _at(call, "ids", ids, torch.int32, rows * K, dev, K), _at(call, "vals", vals, torch.float32, rows * K, dev, K),
+                _at(call, "lse", lse, torch.float32, rows, dev), at, nbytes), call)
     return ids, vals, lse
 
 
@@ -249,26 +260,22 @@ def rnnlm_distill_loss(logits, ids, vals, lse=None, y=None, weight=None, tau: fl
     """logits: float32 or bfloat16 [..., V]; ids, vals [..., K]: the teacher's lists; lse [...]: the teacher's, or None.
     Returns loss float32 [...].  dlogits (a tensor like logits, or logits itself) receives the gradient; sum_loss float64 [1]."""
     import torch
-    call = "rnnlm_distill_loss"
+    call, f32, i32 = "rnnlm_distill_loss", torch.float32, torch.int32
     rows, V, ld, dt = _rows(call, "logits", logits)
-    dev, K = logits.device, ids.shape[-1]
-    loss = torch.empty(logits.shape[:-1], dtype=torch.float32, device=dev) if loss is None else loss
-    for name, t, dtype, shape in (("ids", ids, torch.int32, (rows, K)), ("vals", vals, torch.float32, (rows, K)),
-                                  ("lse", lse, torch.float32, (rows,)), ("y", y, torch.int32, (rows,)),
-                                  ("weight", weight, torch.float32, (rows,)), ("loss", loss, torch.float32, (rows,)),
-                                  ("sum_loss", sum_loss, torch.float64, (1,)), ("range_flag", range_flag, torch.int32, (1,))):
-        _dense(call, name, t, dtype, shape, dev)
-    ldd = 0
+    dev, K = logits.get_device(), ids.shape[-1]
+    loss = torch.empty(logits.shape[:-1], dtype=f32, device=logits.device) if loss is None else loss
+    z, dz, ldd = logits.data_ptr(), None, 0
     if dlogits is not None:
-        _need(dlogits.shape == logits.shape, call, "dlogits: the logits' shape is wanted")
-        ldd = _rows(call, "dlogits", dlogits, dev, logits.dtype)[2]
-        if dlogits.data_ptr() == logits.data_ptr():  # in place (one row has no distance to the next)
-            ldd = ld if rows <= 1 else ldd
-    guard, st = _on(dev, stream)
-    with guard:
-        _ok(load().rnnlm_distill_loss(_ptr(logits), dt, rows, V, ld, _ptr(ids), _ptr(vals), K, _ptr(lse), _ptr(y), _ptr(weight),
-                                      tau, alpha, scale, _ptr(loss), _ptr(sum_loss), _ptr(dlogits), ldd, _ptr(range_flag), st),
-            call)
+        if dlogits.shape != logits.shape:
+            _refuse(call, "dlogits: the logits' shape is wanted")
+        dz, ldd = dlogits.data_ptr(), _rows(call, "dlogits", dlogits, logits)[2]
+        if dz == z and rows <= 1:  # in place (one row has no distance to the next)
+            ldd = ld
+    _ok(_launch(dev, stream, load().rnnlm_distill_loss, z, dt, rows, V, ld, _at(call, "ids", ids, i32, rows * K, dev, K),
+                _at(call, "vals", vals, f32, rows * K, dev, K), K, _at(call, "lse", lse, f32, rows, dev),
+                _at(call, "y", y, i32, rows, dev), _at(call, "weight", weight, f32, rows, dev), tau, alpha, scale,
+                _at(call, "loss", loss, f32, rows, dev), _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd,
+                _at(call, "range_flag", range_flag, i32, 1, dev)), call)
     return loss
 
 
@@ -281,29 +288,25 @@ def rnnlm_verify_drafts(target, drafts, u, draft=None, lengths=None, tau: float 
     """target: float32 or bfloat16 [K+1][B][V]; drafts int32 [K][B] (K = 0: None); u float32 [K+1][B]; draft [K][B][V] or None:
     drafts without probabilities; lengths int32 [B] or None.  Returns (accepted int32 [B], tokens int32 [K+1][B])."""
     import torch
-    call = "rnnlm_verify_drafts"
-    _need(target.dim() == 3, call, "target: [K+1][B][V] is wanted")
+    call, i32 = "rnnlm_verify_drafts", torch.int32
     rows, V, ld, dt = _rows(call, "target", target)
-    K, B, dev = target.shape[0] - 1, target.shape[1], target.device
-    nbytes = rnnlm_verify_workspace_bytes(K, B, V)
-    _need(nbytes > 0, call, f"K = {K}, B = {B}, V = {V}")
-    ldd = 0
+    if target.dim() != 3 or rows == 0:
+        _refuse(call, "target: [K+1][B][V] is wanted")
+    K, B, dev = target.shape[0] - 1, target.shape[1], target.get_device()
+    q, ldd = None, 0
     if draft is not None and K > 0:
-        _need(tuple(draft.shape) == (K, B, V), call, f"draft: [{K}][{B}][{V}] is wanted")
-        ldd = _rows(call, "draft", draft, dev, target.dtype)[2]
-    _need(drafts is not None or K == 0, call, "drafts are wanted")
-    accepted = torch.empty(B, dtype=torch.int32, device=dev) if accepted is None else accepted
-    tokens = torch.empty(K + 1, B, dtype=torch.int32, device=dev) if tokens is None else tokens
-    for name, t, dtype, shape in (("drafts", drafts, torch.int32, (K, B)), ("u", u, torch.float32, (K + 1, B)),
-                                  ("lengths", lengths, torch.int32, (B,)), ("accepted", accepted, torch.int32, (B,)),
-                                  ("tokens", tokens, torch.int32, (K + 1, B)), ("range_flag", range_flag, torch.int32, (1,))):
-        _dense(call, name, t, dtype, shape, dev)
-    workspace = _scratch(call, workspace, nbytes, dev)
-    guard, st = _on(dev, stream)
-    with guard:
-        _ok(load().rnnlm_verify_drafts(_ptr(target), ld, _ptr(draft) if K > 0 else None, ldd, dt, K, B, V, _ptr(drafts),
-                                       _ptr(lengths), _ptr(u), tau, tau_draft, _ptr(accepted), _ptr(tokens), _ptr(range_flag),
-                                       _ptr(workspace), workspace.nbytes, st), call)
+        if tuple(draft.shape) != (K, B, V):
+            _refuse(call, f"draft: [{K}][{B}][{V}] is wanted")
+        q, ldd = draft.data_ptr(), _rows(call, "draft", draft, target)[2]
+    if drafts is None and K > 0:
+        _refuse(call, "drafts are wanted")
+    accepted = torch.empty(B, dtype=i32, device=target.device) if accepted is None else accepted
+    tokens = torch.empty(K + 1, B, dtype=i32, device=target.device) if tokens is None else tokens
+    at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_verify_workspace_bytes(K, B, V))
+    _ok(_launch(dev, stream, load().rnnlm_verify_drafts, target.data_ptr(), ld, q, ldd, dt, K, B, V,
+                _at(call, "drafts", drafts, i32, K * B, dev, B) if K > 0 else None, _at(call, "lengths", lengths, i32, B, dev),
+                _at(call, "u", u, torch.float32, rows, dev, B), tau, tau_draft, _at(call, "accepted", accepted, i32, B, dev),
+                _at(call, "tokens", tokens, i32, rows, dev, B), _at(call, "range_flag", range_flag, i32, 1, dev), at, nbytes), call)
     return accepted, tokens
 
 
@@ -480,45 +483,45 @@ class Rnnlm:
 
     # -- windows whose logits are the caller's -----------------------------------------------------
     def _logit_rows(self, call, T, logits):
-        """A tensor [T][B][V] of the compute type (allocated if None) and the distance of its rows."""
+        """A tensor [T][B][V] of the compute type (a new one if None) and the distance of its rows."""
         import torch
         dtype = torch.float32 if self.precision == RNNLM_FP32 else torch.bfloat16
         if logits is None:
             return torch.empty(T, self.B, self.V, dtype=dtype, device=self.device), self.V
-        _need(tuple(logits.shape) == (T, self.B, self.V), call, f"logits: [{T}][{self.B}][{self.V}] is wanted")
-        return logits, _rows(call, "logits", logits, self.device, dtype)[2]
+        if tuple(logits.shape) != (T, self.B, self.V) or logits.dtype is not dtype or logits.get_device() != self.device.index:
+            _refuse(call, f"logits: {dtype} [{T}][{self.B}][{self.V}] on {self.device} is wanted")
+        return logits, _rows(call, "logits", logits)[2]
 
     def _window(self, call, x):
         import torch
-        _need(x.dim() == 2 and x.shape[1] == self.B, call, f"x: [T][{self.B}] is wanted")
-        _dense(call, "x", x, torch.int32, tuple(x.shape), self.device)
-        return x.shape[0]
+        if x.dim() != 2:
+            _refuse(call, f"x: [T][{self.B}] is wanted")
+        return x.shape[0], _at(call, "x", x, torch.int32, x.shape[0] * self.B, self.device.index, self.B)
 
     def rnnlm_forward_logits(self, x, logits=None, stream=None):
-        T = self._window("rnnlm_forward_logits", x)
-        logits, ld = self._logit_rows("rnnlm_forward_logits", T, logits)
-        _ok(self.lib.rnnlm_forward_logits(self.handle, _ptr(x), T, _ptr(logits), ld, _stream(stream)), "rnnlm_forward_logits")
+        call = "rnnlm_forward_logits"
+        T, at = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        _ok(self.lib.rnnlm_forward_logits(self.handle, at, T, logits.data_ptr(), ld, _stream(stream)), call)
         return logits
 
     def _distill(self, call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss):
         import torch
-        T = self._window(call, x)
+        T, at = self._window(call, x)
         logits, ld = self._logit_rows(call, T, logits)
-        n, K = T * self.B, ids.shape[-1]
-        for name, t, dtype, shape in (("y", y, torch.int32, (n,)), ("ids", ids, torch.int32, (n, K)), ("vals", vals, torch.float32, (n, K)),
-                                      ("lse", lse, torch.float32, (n,)), ("weight", weight, torch.float32, (n,)),
-                                      ("loss", loss, torch.float32, (n,)), ("sum_loss", sum_loss, torch.float64, (1,))):
-            _dense(call, name, t, dtype, shape, self.device)
-        at = lambda t: None if t is None else t.data_ptr()
-        return rnnlm_distill(at(ids), at(vals), at(lse), at(weight), K, tau, alpha, logits.data_ptr(), ld), logits, T
+        n, K, dev, f32, i32 = T * self.B, ids.shape[-1], self.device.index, torch.float32, torch.int32
+        d = rnnlm_distill(_at(call, "ids", ids, i32, n * K, dev, K), _at(call, "vals", vals, f32, n * K, dev, K),
+                          _at(call, "lse", lse, f32, n, dev), _at(call, "weight", weight, f32, n, dev), K, tau, alpha,
+                          logits.data_ptr(), ld)
+        return (d, logits, T, at, _at(call, "y", y, i32, n, dev), _at(call, "loss", loss, f32, n, dev),
+                _at(call, "sum_loss", sum_loss, torch.float64, 1, dev))
 
     def rnnlm_distill_train_chunk(self, x, y, ids, vals, lr: float, lse=None, weight=None, tau: float = 1.0, alpha: float = 1.0,
                                   logits=None, loss=None, sum_loss=None, stream=None):
         """ids, vals [T][B][K], lse [T][B] or None: the teacher's (rnnlm_top_logits of its rnnlm_forward_logits at the same tau)."""
         call = "rnnlm_distill_train_chunk"
-        d, _keep, T = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss)
-        _ok(self.lib.rnnlm_distill_train_chunk(self.handle, _ptr(x), _ptr(y), T, C.byref(d), lr, _ptr(loss), _ptr(sum_loss),
-                                               _stream(stream)), call)
+        d, _keep, T, at, y_at, loss_at, sum_at = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss)
+        _ok(self.lib.rnnlm_distill_train_chunk(self.handle, at, y_at, T, C.byref(d), lr, loss_at, sum_at, _stream(stream)), call)
 
     def rnnlm_distill_grad_chunk(self, x, y, ids, vals, lse=None, weight=None, tau: float = 1.0, alpha: float = 1.0, logits=None,
                                  stream=None):
@@ -526,35 +529,29 @@ class Rnnlm:
         call = "rnnlm_distill_grad_chunk" + ("_compressed" if self.P else "")
         z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
         loss = z(x.shape[0], self.B)
-        d, _keep, T = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, None)
+        d, _keep, T, at, y_at, loss_at, _ = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, None)
         if self.P:
             g = dict(gE=z(self.V, self.P), gA=z(self.H, self.P), gU=z(self.H, self.H), gC=z(self.P, self.H), gb=z(self.V))
         else:
             g = dict(gE=z(self.V, self.H), gU=z(self.H, self.H), gWo=z(self.V, self.H), gb=z(self.V))
-        _ok(getattr(self.lib, call)(self.handle, _ptr(x), _ptr(y), T, C.byref(d), *map(_ptr, g.values()), _ptr(loss), _stream(stream)),
-            call)
+        _ok(getattr(self.lib, call)(self.handle, at, y_at, T, C.byref(d), *map(_ptr, g.values()), loss_at, _stream(stream)), call)
         return dict(loss=loss, **g)
 
     def rnnlm_verify_chunk(self, x, u, draft=None, lengths=None, tau: float = 1.0, tau_draft: float = 1.0, logits=None, accepted=None,
                            tokens=None, workspace=None, stream=None):
         """x int32 [K+1][B]: the word not read yet, then the drafts.  Returns (accepted [B], tokens [K+1][B])."""
         import torch
-        call = "rnnlm_verify_chunk"
-        K = self._window(call, x) - 1
-        logits, ld = self._logit_rows(call, K + 1, logits)
-        ldd = 0
-        if draft is not None and K > 0:
-            ldd = self._logit_rows(call, K, draft)[1]
-        nbytes = rnnlm_verify_workspace_bytes(K, self.B, self.V)
-        accepted = torch.empty(self.B, dtype=torch.int32, device=self.device) if accepted is None else accepted
-        tokens = torch.empty(K + 1, self.B, dtype=torch.int32, device=self.device) if tokens is None else tokens
-        for name, t, dtype, shape in (("u", u, torch.float32, (K + 1, self.B)), ("lengths", lengths, torch.int32, (self.B,)),
-                                      ("accepted", accepted, torch.int32, (self.B,)), ("tokens", tokens, torch.int32, (K + 1, self.B))):
-            _dense(call, name, t, dtype, shape, self.device)
-        workspace = _scratch(call, workspace, nbytes, self.device)
-        v = rnnlm_verify(draft.data_ptr() if ldd else None, ldd, None if lengths is None else lengths.data_ptr(), u.data_ptr(), tau,
-                         tau_draft, logits.data_ptr(), ld, workspace.data_ptr(), workspace.nbytes)
-        _ok(self.lib.rnnlm_verify_chunk(self.handle, _ptr(x), K, C.byref(v), _ptr(accepted), _ptr(tokens), _stream(stream)), call)
+        call, i32, B, dev = "rnnlm_verify_chunk", torch.int32, self.B, self.device.index
+        T, x_at = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        ldd = self._logit_rows(call, T - 1, draft)[1] if draft is not None and T > 1 else 0
+        accepted = torch.empty(B, dtype=i32, device=self.device) if accepted is None else accepted
+        tokens = torch.empty(T, B, dtype=i32, device=self.device) if tokens is None else tokens
+        at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_verify_workspace_bytes(T - 1, B, self.V))
+        v = rnnlm_verify(draft.data_ptr() if ldd else None, ldd, _at(call, "lengths", lengths, i32, B, dev),
+                         _at(call, "u", u, torch.float32, T * B, dev, B), tau, tau_draft, logits.data_ptr(), ld, at, nbytes)
+        _ok(self.lib.rnnlm_verify_chunk(self.handle, x_at, T - 1, C.byref(v), _at(call, "accepted", accepted, i32, B, dev),
+                                        _at(call, "tokens", tokens, i32, T * B, dev, B), _stream(stream)), call)
         return accepted, tokens
 
     def rnnlm_reset_state(self, stream=None):
