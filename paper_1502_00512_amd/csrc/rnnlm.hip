@@ -1141,8 +1141,16 @@ int distill_gradient(rnnlm_t *h, int Tn, int Mp, const DistillCall &c, const Win
                           1.0f / (float)n, loss, nullptr, d.logits, d.ld, p_flags(h), st);
   if (rc) return rc;
   hipLaunchKernelGGL(losses_sum_kernel, dim3(1), dim3(1024), 0, st, loss, n, ws);
-  hipLaunchKernelGGL(rows_to_logits_kernel<T>, dim3(h->Vp / LW_TILE), dim3(256), 0, st, static_cast<const T *>(d.logits),
-                     at<T>(h, h->L.ZT), Mp, b, b_out, alpha, lr, logit_window(h, Tn, d.ld));
+  // shares of the positions: some four workgroups to a compute unit, as far as the scratch (of the contraction that follows) goes
+  const int tiles = h->Vp / LW_TILE;
+  const long most = std::min<long>({16, Mp / LW_TILE, std::max<long>(1, 1024 / tiles), h->L.partElems / h->Vp});
+  const int per = most > 1 ? (int)round_up((Mp + most - 1) / most, LW_TILE) : Mp, shares = (Mp + per - 1) / per;
+  float *sums = shares > 1 ? at<float>(h, h->L.part32) : nullptr;
+  hipLaunchKernelGGL(rows_to_logits_kernel<T>, dim3(tiles, shares), dim3(256), 0, st, static_cast<const T *>(d.logits),
+                     at<T>(h, h->L.ZT), Mp, per, sums, (long)h->Vp, b, b_out, alpha, lr, logit_window(h, Tn, d.ld));
+  if (sums)
+    hipLaunchKernelGGL(bias_update_kernel, dim3(blocks_for(h->cfg.V, 256)), dim3(256), 0, st, sums, (long)h->Vp, shares, h->cfg.V, b,
+                       b_out, alpha, lr);
   HIP_TRY(hipGetLastError());
   return RNNLM_OK;
 }
