@@ -151,7 +151,7 @@ VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
   const int slots = slots_of(V, RNNLM_DTYPE_BF16);  // (fp32 rows have twice as many: parts of twice the slots)
   const int64_t rows = (int64_t)(2 * K + 1) * B, fill = 8192;
   p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({fill / std::min(rows, fill), VERIFY_PARTS, slots / VERIFY_THREADS}));
-  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>({1024 / std::min<int64_t>(B, 1024), VERIFY_PARTS, slots / VERIFY_THREADS}));
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / std::min<int64_t>(B, 4096), VERIFY_PARTS, slots / VERIFY_THREADS}));
   size_t o = 0;
   auto take = [&](size_t n) {
     const size_t at = o;
@@ -177,7 +177,8 @@ int verify_call(const VerifyArgs &a, hipStream_t st) {
   if (a.blocks <= VERIFY_ONE_BLOCKS) {
     hipLaunchKernelGGL(verify_one_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_ONE_THREADS), 0, st, a);
   } else {
-    hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
+    hipLaunchKernelGGL(verify_decide_kernel<T>, dim3((unsigned)a.B), threads, 0, st, a);
+    if (a.draft) hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
     hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
   }
   LAUNCHED();
@@ -302,8 +303,10 @@ int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft
   a.parts = p.parts;
   a.per = (slots_of(V, dtype) + p.parts - 1) / p.parts;
   a.blocks = verify_blocks(V, dtype);
-  a.chunks = std::min(p.chunks, a.blocks);
-  a.span = (a.blocks + a.chunks - 1) / a.chunks;
+  // whole rounds of a workgroup's waves
+  const int waves = VERIFY_THREADS / 64;
+  a.span = (a.blocks + p.chunks * waves - 1) / (p.chunks * waves) * waves;
+  a.chunks = (a.blocks + a.span - 1) / a.span;
   a.tau = tau;
   a.tau_d = tau_draft;
   a.accepted = accepted;
