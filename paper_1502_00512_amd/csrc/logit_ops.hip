@@ -177,7 +177,7 @@ int verify_call(const VerifyArgs &a, hipStream_t st) {
   if (a.blocks <= VERIFY_ONE_BLOCKS) {
     hipLaunchKernelGGL(verify_one_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_ONE_THREADS), 0, st, a);
   } else {
-    hipLaunchKernelGGL(verify_decide_kernel<T>, dim3((unsigned)a.B), threads, 0, st, a);
+    hipLaunchKernelGGL(verify_decide_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_DECIDE_THREADS), 0, st, a);
     if (a.draft) hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
     hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
   }

@@ -181,15 +181,16 @@ template <int WAVES>
 __device__ inline float waves_sum(const float *of_wave) {
   return waves_reduce<WAVES>(of_wave, [](float a, float b) { return a + b; });
 }
-// Sums of the lanes up to each one.
+// Sums of the lanes up to each one: within sixteen lanes, then the rows of sixteen in front.
 template <typename X>
 __device__ inline X wave_scan(X v) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const X add = __shfl_up(v, o, 64);
-    if ((int)(threadIdx.x & 63) >= o) v += add;
-  }
-  return v;
+  v += lane_swap<0x111>(v);  // the value 1, 2, 4, 8 lanes below (0 from outside the sixteen)
+  v += lane_swap<0x112>(v);
+  v += lane_swap<0x114>(v);
+  v += lane_swap<0x118>(v);
+  const X r0 = lane_value(v, 15), r1 = r0 + lane_value(v, 31), r2 = r1 + lane_value(v, 47);
+  const int row = (threadIdx.x & 63) >> 4;
+  return row == 0 ? v : v + (row == 1 ? r0 : row == 2 ? r1 : r2);
 }
 __device__ inline float wave_max(float v) {
   return wave_reduce(v, [](float a, float b) { return fmaxf(a, b); });

@@ -21,6 +21,7 @@
 namespace rnnlm_dev {
 
 constexpr int VERIFY_THREADS = 256, VERIFY_PARTS = 64;
+constexpr int VERIFY_DECIDE_THREADS = 512;  // a wave to each of up to eight rows
 constexpr int VERIFY_STAGED = 1024;  // sums of blocks that the drawing workgroup holds in LDS
 constexpr int VERIFY_ONE_THREADS = 1024, VERIFY_ONE_BLOCKS = 64;  // a text in one workgroup: rows of at most so many blocks
 
@@ -390,9 +391,9 @@ __device__ __forceinline__ void verify_exponentials(const Rest<T> &rest, int fir
 }
 
 template <typename T>
-__global__ void __launch_bounds__(VERIFY_THREADS) verify_decide_kernel(const VerifyArgs a) {
+__global__ void __launch_bounds__(VERIFY_DECIDE_THREADS) verify_decide_kernel(const VerifyArgs a) {
   const int b = blockIdx.x;
-  const VerifySeq s = verify_decide<T, VERIFY_THREADS>(a, b);
+  const VerifySeq s = verify_decide<T, VERIFY_DECIDE_THREADS>(a, b);
   if (threadIdx.x == 0) a.seq[b] = s;
 }
 
