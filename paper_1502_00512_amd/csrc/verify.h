@@ -52,23 +52,25 @@ __device__ inline int draft_length(const VerifyArgs &a, int b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.K) : a.K;
 }
 
-// e^{(z - m) / tau} of a row in 64 bits: 2^x, x = (z - m) c = n + f with |f| <= 1/2, and the polynomial of degree 9 that meets 2^f
-// at the ten Chebyshev nodes of [-1/2, 1/2]: 1.8e-14 relative off at most, so a hundred thousand such terms place a step of
-// their sum to about 1e-14.  n is what adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer
-// addition (rounding, conversion and scaling instructions run at a quarter of the additions' rate).  Logits more than 690 tau
-// below the maximum, and masked ones, give 0.  No NaNs: the caller knows the row.
+// e^{(z - m) / tau} of a row in 64 bits, up to a factor that the row has in common: 2^x, x = z c + b = n + f with |f| <= 1/2,
+// and the polynomial of degree 9 that meets 2^f at the ten Chebyshev nodes of [-1/2, 1/2]: 1.8e-14 relative off at most, so a
+// hundred thousand such terms place a step of their sum to about 1e-14.  (b = -m c is rounded: the common factor.)  n is what
+// adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer addition.  Logits more than 690 tau below
+// the maximum, and masked ones, give 0.  Where m c passes 2^50 only logits equal to the maximum are as near: e = 1.  No NaNs:
+// the caller knows the row.
 struct Exp64 {
-  double c, m;
+  double c, b;
   float least;
-  __device__ Exp64(float top, float tau) {
-    if (top == -INFINITY) top = 0.0f;
+  __device__ Exp64(float m, float tau) {
+    if (m == -INFINITY) m = 0.0f;
     c = LOG2E_64 / (double)tau;
-    m = (double)top;
-    least = top - 690.0f * tau;
+    b = -(double)m * c;
+    if (fabs(b) > 1125899906842624.0) c = b = 0.0;
+    least = m - 690.0f * tau;
   }
   __device__ double operator()(float z) const {
     constexpr double SHIFT = 6755399441055744.0;
-    const double x = ((double)fmaxf(z, least) - m) * c, t = x + SHIFT, f = x - (t - SHIFT);
+    const double x = fma((double)z, c, b), t = x + SHIFT, f = x - (t - SHIFT);
     double p = 1.0205905413765595e-07;
     p = fma(p, f, 1.325964524488711e-06);
     p = fma(p, f, 1.5252672924850737e-05);
