@@ -204,13 +204,14 @@ __device__ inline void distill_listed(const DistillArgs<T> &a, const DistillDens
     const int id = ent[e].id;
     if (id < 0) continue;
     float p = 0.0f;
-    bool first = true;
-    for (int j = 0; j < a.K; ++j)
-      if (ent[j].id == id) {
-        p += ent[j].p;
-        first = first && j >= e;
-      }
-    if (!first) continue;
+    int first = a.K;
+#pragma unroll 8
+    for (int j = a.K - 1; j >= 0; --j) {
+      const DistillEntry x = ent[j];
+      p += x.id == id ? x.p : 0.0f;
+      first = x.id == id ? j : first;
+    }
+    if (first < e) continue;
     float off = coef * p;
     if (ent[a.K].id == id) off += hard;
     drow[id] = from_f32<T>(dense(ent[e].z) - off);

@@ -92,6 +92,7 @@ void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st
 }
 
 // ---- distillation ----
+constexpr int64_t DISTILL_MANY_ROWS = 1024;
 template <typename T, int THREADS, int NV, int MODE>
 void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, MODE>), dim3((unsigned)rows), dim3(THREADS),
@@ -100,9 +101,17 @@ void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
 template <typename T, int MODE>
 void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   const int slots = a.V / SlotOf<T>::N;  // whole ones: what a thread's registers hold
+  // Many short rows: a wave each, four times as many in flight (a row's time is the latency of its steps, not its bytes).
+  const bool wave_each = rows >= DISTILL_MANY_ROWS && slots <= 64 * 8;
   if (!a.dz || slots > 1024 * 25) {
     hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
                        st, a);
+  } else if (wave_each && slots <= 64 * 2) {
+    launch_distill_row<T, 64, 2, MODE>(a, rows, st);
+  } else if (wave_each && slots <= 64 * 4) {
+    launch_distill_row<T, 64, 4, MODE>(a, rows, st);
+  } else if (wave_each) {
+    launch_distill_row<T, 64, 8, MODE>(a, rows, st);
   } else if (slots <= 256) {
     launch_distill_row<T, 256, 1, MODE>(a, rows, st);
   } else if (slots <= 256 * 2) {
@@ -174,12 +183,18 @@ int verify_call(const VerifyArgs &a, hipStream_t st) {
   const dim3 threads(VERIFY_THREADS);
   const int64_t rows = (int64_t)(a.draft ? 2 * a.K + 1 : a.K + 1) * a.B;
   hipLaunchKernelGGL(verify_stats_kernel<T>, dim3((unsigned)(rows * a.parts)), threads, 0, st, a);
-  if (a.blocks <= VERIFY_ONE_BLOCKS) {
+  const dim3 shares((unsigned)(a.B * a.chunks));
+  if (a.blocks <= (a.draft ? VERIFY_ONE_BLOCKS / 2 : VERIFY_ONE_BLOCKS)) {
     hipLaunchKernelGGL(verify_one_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_ONE_THREADS), 0, st, a);
+  } else if (shares.x <= VERIFY_DECIDE_INSIDE && a.draft) {
+    hipLaunchKernelGGL((verify_sums_kernel<T, true>), shares, threads, 0, st, a);
+    hipLaunchKernelGGL((verify_rest_kernel<T, false>), shares, threads, 0, st, a);
+  } else if (shares.x <= VERIFY_DECIDE_INSIDE) {
+    hipLaunchKernelGGL((verify_rest_kernel<T, true>), shares, threads, 0, st, a);
   } else {
     hipLaunchKernelGGL(verify_decide_kernel<T>, dim3((unsigned)a.B), dim3(VERIFY_DECIDE_THREADS), 0, st, a);
-    if (a.draft) hipLaunchKernelGGL(verify_sums_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
-    hipLaunchKernelGGL(verify_rest_kernel<T>, dim3((unsigned)(a.B * a.chunks)), threads, 0, st, a);
+    if (a.draft) hipLaunchKernelGGL((verify_sums_kernel<T, false>), shares, threads, 0, st, a);
+    hipLaunchKernelGGL((verify_rest_kernel<T, false>), shares, threads, 0, st, a);
   }
   LAUNCHED();
   return RNNLM_OK;

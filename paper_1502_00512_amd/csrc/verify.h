@@ -23,7 +23,11 @@ namespace rnnlm_dev {
 constexpr int VERIFY_THREADS = 256, VERIFY_PARTS = 64;
 constexpr int VERIFY_DECIDE_THREADS = 512;  // a wave to each of up to eight rows
 constexpr int VERIFY_STAGED = 1024;  // sums of blocks that the drawing workgroup holds in LDS
-constexpr int VERIFY_ONE_THREADS = 1024, VERIFY_ONE_BLOCKS = 64;  // a text in one workgroup: rows of at most so many blocks
+// A text in one workgroup: rows of at most so many blocks, half as many where there is a draft row (two passes over two rows).
+// In one workgroup and in shares: 15 texts x 4 drafts over 22650 words 31 and 22 us, over 13250 words 23 and 23.
+constexpr int VERIFY_ONE_THREADS = 1024, VERIFY_ONE_BLOCKS = 64;
+// Up to so many workgroups, all at work at once, step 2 is part of the next: it takes them less than its launch does.
+constexpr int VERIFY_DECIDE_INSIDE = 1024;
 
 struct VerifySeq {  // what the steps behind the second one know of a text
   int n;            // accepted
@@ -94,6 +98,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_stats_kernel(const Veri
   const int r = blockIdx.x / a.parts, part = blockIdx.x % a.parts, targets = (a.K + 1) * a.B;
   const bool is_draft = r >= targets;
   const int row = is_draft ? r - targets : r, i = row / a.B, b = row % a.B, len = draft_length(a, b);
+  if (r < a.B && part == 0 && threadIdx.x == 0) a.seq[r].done = 0;
   if (is_draft ? i >= len : i > len) return;  // a row behind the text's drafts
   const T *z = is_draft ? static_cast<const T *>(a.draft) + row * a.ldd : static_cast<const T *>(a.target) + row * a.ldt;
   const int first = part * a.per, last = min(first + a.per, a.V / N);
@@ -399,11 +404,17 @@ __global__ void __launch_bounds__(VERIFY_DECIDE_THREADS) verify_decide_kernel(co
   if (threadIdx.x == 0) a.seq[b] = s;
 }
 
-// One share of a row pair that p - q is drawn from: sums of exponentials.
-template <typename T>
+// One share of a row pair that p - q is drawn from: sums of exponentials.  DECIDE: the workgroup works step 2 out for itself.
+template <typename T, bool DECIDE>
 __global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const VerifyArgs a) {
   const int b = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  const VerifySeq s = a.seq[b];
+  VerifySeq s;
+  if constexpr (DECIDE) {
+    s = verify_decide<T, VERIFY_THREADS>(a, b);
+    if (chunk == 0 && threadIdx.x == 0) a.seq[b] = s;
+  } else {
+    s = a.seq[b];
+  }
   if (!s.ok || !s.mixed) return;
   const Rest<T> rest(a, b, s);
   double sp, sq;
@@ -418,11 +429,13 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_sums_kernel(const Verif
 
 // Sums of r by blocks; the last workgroup of a text draws its word.  (What it reads of the others' moves with agent-scope
 // accesses, each workgroup's before its arrival at the text's counter.)
-template <typename T>
+template <typename T, bool DECIDE>
 __global__ void __launch_bounds__(VERIFY_THREADS) verify_rest_kernel(const VerifyArgs a) {
   __shared__ int sh_last;
   const int b = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const VerifySeq s = a.seq[b];
+  VerifySeq s;
+  if constexpr (DECIDE) s = verify_decide<T, VERIFY_THREADS>(a, b);
+  else s = a.seq[b];
   if (!s.ok) {
     if (chunk == 0) verify_store(a, b, s.n, -1);
     return;
