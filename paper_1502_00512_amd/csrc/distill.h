@@ -35,6 +35,11 @@ struct DistillEntry {  // a word of the list, or (last) the label
   float t, z, p;       // teacher's logit / tau, student's logit, e^{t - t_max}
 };
 
+// The list in LDS: K entries and the label, behind them the entries' ids by themselves (four to a read, four reads
+// at once), padded with -2.
+__host__ __device__ inline int distill_ids(int K) { return (K + 15) / 16 * 16; }
+__host__ __device__ inline size_t distill_lds(int K) { return (size_t)(K + 1) * sizeof(DistillEntry) + (size_t)distill_ids(K) * 4; }
+
 // What a row's softmax is made of: sums of exponentials of z - shift at tau and at 1, relative to 2^power and 2^power1.
 struct RowSums {
   float shift, power, power1, s, s1;
@@ -96,6 +101,8 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
   float tmax = -INFINITY;
   const float inv_tau = 1.0f / a.tau;
   const bool label = a.y && a.alpha < 1.0f;
+  int *ids = reinterpret_cast<int *>(ent + a.K + 1);
+  for (int e = a.K + threadIdx.x; e < distill_ids(a.K); e += THREADS) ids[e] = -2;
   for (int e = threadIdx.x; e <= a.K; e += THREADS) {
     DistillEntry d;
     d.t = -INFINITY;
@@ -115,6 +122,7 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
       if (e < a.K) tmax = fmaxf(tmax, d.t);
     }
     ent[e] = d;
+    if (e < a.K) ids[e] = d.id;
   }
   return tmax;
 }
@@ -196,25 +204,40 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
   a.loss[m] = (float)((double)w * loss);
 }
 
-// The listed words' gradients, behind the dense pass: each word is written once, with everything that the list takes off it.
+// The listed words' gradients, behind the dense pass: each word is written once, with everything that the list and the label
+// take off it.  Every entry looks for its like among all ids; only a word that is listed twice has its probabilities added up.
 template <typename T, int THREADS, int MODE>
 __device__ inline void distill_listed(const DistillArgs<T> &a, const DistillDense<MODE> &dense, float coef, float hard,
                                       const DistillEntry *ent, T *drow) {
+  const int4 *ids = reinterpret_cast<const int4 *>(ent + a.K + 1);
+  const int label = ent[a.K].id;
   for (int e = threadIdx.x; e <= a.K; e += THREADS) {
-    const int id = ent[e].id;
-    if (id < 0) continue;
-    float p = 0.0f;
-    int first = a.K;
-#pragma unroll 8
-    for (int j = a.K - 1; j >= 0; --j) {
-      const DistillEntry x = ent[j];
-      p += x.id == id ? x.p : 0.0f;
-      first = x.id == id ? j : first;
+    const DistillEntry d = ent[e];
+    if (d.id < 0) continue;
+    int alike = 0;
+    for (int j = 0; j < distill_ids(a.K) / 4; j += 4) {
+      int4 q[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = ids[j + i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) alike += (q[i].x == d.id) + (q[i].y == d.id) + (q[i].z == d.id) + (q[i].w == d.id);
     }
-    if (first < e) continue;
-    float off = coef * p;
-    if (ent[a.K].id == id) off += hard;
-    drow[id] = from_f32<T>(dense(ent[e].z) - off);
+    float p = d.p;
+    if (e == a.K) {
+      if (alike) continue;  // the entry takes it off
+      p = 0.0f;
+    } else if (alike > 1) {
+      p = 0.0f;
+      int first = a.K;
+#pragma unroll 8
+      for (int j = a.K - 1; j >= 0; --j) {
+        const DistillEntry x = ent[j];
+        p += x.id == d.id ? x.p : 0.0f;
+        first = x.id == d.id ? j : first;
+      }
+      if (first < e) continue;
+    }
+    drow[d.id] = from_f32<T>(dense(d.z) - (coef * p + (d.id == label ? hard : 0.0f)));
   }
 }
 

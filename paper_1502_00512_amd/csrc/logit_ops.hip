@@ -96,7 +96,7 @@ constexpr int64_t DISTILL_MANY_ROWS = 1024;
 template <typename T, int THREADS, int NV, int MODE>
 void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, MODE>), dim3((unsigned)rows), dim3(THREADS),
-                     (a.K + 1) * sizeof(DistillEntry), st, a);
+                     distill_lds(a.K), st, a);
 }
 template <typename T, int MODE>
 void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
@@ -104,8 +104,7 @@ void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   // Many short rows: a wave each, four times as many in flight (a row's time is the latency of its steps, not its bytes).
   const bool wave_each = rows >= DISTILL_MANY_ROWS && slots <= 64 * 8;
   if (!a.dz || slots > 1024 * 25) {
-    hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), (a.K + 1) * sizeof(DistillEntry),
-                       st, a);
+    hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), distill_lds(a.K), st, a);
   } else if (wave_each && slots <= 64 * 2) {
     launch_distill_row<T, 64, 2, MODE>(a, rows, st);
   } else if (wave_each && slots <= 64 * 4) {
