@@ -278,7 +278,8 @@ int rnnlm_sort_segments_static(const int32_t *x, int32_t T, int32_t B, int32_t V
  * A row holds the V logits of one position; rows lie ld elements apart (ld >= V, any alignment of their element type) and
  * are ordered like a window's positions (row t*B + s).  All rows, lists and outputs are device arrays.  The calls allocate
  * nothing, run on the CURRENT device, which must be the stream's, keep nothing between calls, and may be captured into a
- * graph; calls that overlap in time need workspaces of their own.  V <= 2^20; tau in [0.001, 1000]. */
+ * graph; calls that overlap in time need workspaces of their own.  V <= 2^20; at most 2^22 - 64
+ * rows; tau in [0.001, 1000]. */
 typedef enum { RNNLM_DTYPE_FP32 = 0, RNNLM_DTYPE_BF16 = 1 } rnnlm_dtype;
 
 /* The K greatest logits of every row in descending order (equal ones: the lower id first) and lse = ln sum_v exp(z[v]/tau)
@@ -317,12 +318,13 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
  * all its mass on d_i).  The drawn word is the first v whose sum of weights over words <= v exceeds u[K] times the whole
  * sum (in 64 bits); weights that are all zero: p_n itself.  -inf marks masked words.  A row with no probability (all masked,
  * a NaN or +inf) accepts no draft and draws the word -1;
- * a draft row of nothing but masked words counts as q_i = 0, one with a NaN or +inf as a row with no probability.  Drafts outside [0, V) are rejected and raise *range_flag.
+ * a draft row of nothing but masked words counts as q_i = 0, one with a NaN or +inf as a row with no probability.  Drafts
+ * outside [0, V) are rejected and raise *range_flag.
  * K = 0 (draft and drafts NULL) draws one word of each row.
  * target: dev [K+1][B] rows, draft: dev [K][B] rows, both of dtype; drafts: dev int32[K][B]; lengths: dev int32[B], a text's
- * own number of drafts (clamped to [0, K]; rows behind it are not read), or NULL: K; u: dev float[K+1][B], in [0, 1);
+ * own number of drafts (clamped to [0, K]; rows behind them may hold anything), or NULL: K; u: dev float[K+1][B], in [0, 1);
  * accepted: dev int32[B] = n; tokens: dev int32[K+1][B]: the n accepted drafts, the drawn word, then -1.
- * 0 <= K <= 1024, B <= 2^20; workspace as above, rnnlm_verify_workspace_bytes; range_flag as above. */
+ * 0 <= K <= 1024, (2 K + 1) B <= 2^22 - 64, B <= 2^20; workspace as above, rnnlm_verify_workspace_bytes; range_flag as above. */
 size_t rnnlm_verify_workspace_bytes(int32_t K, int32_t B, int32_t V);
 int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft, int64_t ld_draft, int32_t dtype, int32_t K,
                         int32_t B, int32_t V, const int32_t *drafts, const int32_t *lengths, const float *u, float tau,
@@ -376,7 +378,7 @@ typedef struct {
 } rnnlm_verify;
 
 /* One step of drafting and verifying: x: dev int32[K+1][B]: row 0 the last word of every text that the model has not read
- * yet, rows 1..K the drafts, 0 <= K < T_max.  Runs the model over them from h_state, verifies, and leaves in h_state the state
+ * yet, rows 1..K the drafts (behind a text's own drafts any valid words), 0 <= K < T_max.  Runs the model over them from h_state, verifies, and leaves in h_state the state
  * after row 0 and the accepted drafts of each text (bf16: as the recurrence carries it, rounded to bf16), so that the drawn
  * words are row 0 of the next call.  accepted, tokens: as rnnlm_verify_drafts. */
 int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,

@@ -19,7 +19,8 @@ namespace {
     if (hipGetLastError() != hipSuccess) return RNNLM_ERR_HIP; \
   } while (0)
 
-constexpr int64_t GRID_MAX = (int64_t(1) << 31) - 1;
+// What a launch can hold is less than 2^32 threads, with up to 1024 of them to a row.
+constexpr int64_t ROWS_MAX = (int64_t(1) << 22) - 64, THREADS_MAX = (int64_t(1) << 32) - 1;
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -32,7 +33,7 @@ bool tau_ok(float tau) { return std::isfinite(tau) && tau >= 1e-3f && tau <= 1e3
 // rows of V elements, ld apart: addresses stay within what 64 bits and the kernels' 32-bit element counts reach
 bool rows_ok(const void *p, int32_t dtype, int64_t rows, int32_t V, int64_t ld) {
   if ((!p && rows != 0) || (dtype != RNNLM_DTYPE_FP32 && dtype != RNNLM_DTYPE_BF16) || !aligned(p, elem_bytes(dtype))) return false;
-  return rows >= 0 && V >= 1 && V <= TOP_V_MAX && ld >= V && ld <= (int64_t(1) << 40) && rows <= GRID_MAX &&
+  return rows >= 0 && V >= 1 && V <= TOP_V_MAX && ld >= V && ld <= (int64_t(1) << 40) && rows <= ROWS_MAX &&
          (rows == 0 || ld <= (int64_t(1) << 60) / rows);
 }
 
@@ -57,12 +58,12 @@ TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   p.nv = 16;
   auto chunks = [&]() { return (slots + p.nv * p.threads - 1) / (p.nv * p.threads); };
   if (chunks() == 1) {
-    while (p.nv > 2 && p.nv / 2 * p.threads >= slots) p.nv /= 2;
-  } else if (slots <= TOP_WIDE * 20 && rows >= 512) {
+    while (p.nv > 1 && p.nv / 2 * p.threads >= slots) p.nv /= 2;
+  } else if (slots <= TOP_WIDE * 20) {
     p.threads = TOP_WIDE;
     if (slots > TOP_WIDE * 16) p.nv = 20;
   } else {
-    while (p.nv > 4 && rows * chunks() < 512 && 2 * chunks() * K <= TOP_CAP) p.nv /= 2;
+    while (p.nv > 4 && rows * chunks() < 256 && 2 * chunks() * K <= TOP_CAP) p.nv /= 2;
   }
   p.chunks = chunks();
   p.per = (slots + p.chunks - 1) / p.chunks;
@@ -74,8 +75,10 @@ size_t top_bytes(const TopPlan &p, int64_t rows, int32_t K) {
   return align256((size_t)rows * p.chunks * K * 8) + align256((size_t)rows * p.chunks * 16);
 }
 bool top_sizes_ok(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
-  return rows >= 0 && rows <= GRID_MAX / 1024 && V >= 1 && V <= TOP_V_MAX && K >= 1 && K <= std::min(V, TOP_K_MAX) &&
-         (dtype == RNNLM_DTYPE_FP32 || dtype == RNNLM_DTYPE_BF16);
+  if (rows < 0 || rows > ROWS_MAX || V < 1 || V > TOP_V_MAX || K < 1 || K > std::min(V, TOP_K_MAX)) return false;
+  if (dtype != RNNLM_DTYPE_FP32 && dtype != RNNLM_DTYPE_BF16) return false;
+  const TopPlan p = top_plan(rows, V, K, dtype);
+  return rows * p.chunks * p.threads <= THREADS_MAX;
 }
 template <typename T, int THREADS, int NV>
 void launch_top_chunks(const TopArgs &a, int64_t rows, hipStream_t st) {
@@ -85,6 +88,7 @@ template <typename T>
 void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st) {
   if (p.threads == TOP_WIDE && p.nv == 20) launch_top_chunks<T, TOP_WIDE, 20>(a, rows, st);
   else if (p.threads == TOP_WIDE) launch_top_chunks<T, TOP_WIDE, 16>(a, rows, st);
+  else if (p.nv == 1) launch_top_chunks<T, 256, 1>(a, rows, st);
   else if (p.nv == 2) launch_top_chunks<T, 256, 2>(a, rows, st);
   else if (p.nv == 4) launch_top_chunks<T, 256, 4>(a, rows, st);
   else if (p.nv == 8) launch_top_chunks<T, 256, 8>(a, rows, st);
@@ -175,7 +179,7 @@ VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
 }
 bool verify_sizes_ok(int32_t K, int32_t B, int32_t V) {
   return K >= 0 && K <= 1024 && B >= 1 && B <= (1 << 20) && V >= 1 && V <= TOP_V_MAX &&
-         (int64_t)(2 * K + 1) * B <= GRID_MAX / VERIFY_PARTS;
+         (int64_t)(2 * K + 1) * B <= ROWS_MAX;
 }
 template <typename T>
 int verify_call(const VerifyArgs &a, hipStream_t st) {

@@ -1105,7 +1105,6 @@ int sort_segments(rnnlm_t *h, int Tn, int32_t *perm, int32_t *seg, int32_t *nseg
   return RNNLM_OK;
 }
 
-// One call of the noise-contrastive criterion (Sec. 4.2): K noise words shared by the window.
 // ---- windows whose logits are the caller's (criteria and decisions on arrays of logits) ----
 template <typename T>
 constexpr int32_t logit_dtype() {
@@ -1155,6 +1154,7 @@ int distill_gradient(rnnlm_t *h, int Tn, int Mp, const DistillCall &c, const Win
   return RNNLM_OK;
 }
 
+// One call of the noise-contrastive criterion (Sec. 4.2): K noise words shared by the window.
 struct NceCall {
   const int32_t *noise;
   int K;
@@ -2172,15 +2172,18 @@ int rnnlm_forward_score_shortlist(rnnlm_t *h, const int32_t *x, const int32_t *c
 
 namespace {
 // Arguments of the calls on rows of logits that their own checks would refuse after the window has started.
-bool logit_rows_ok(const rnnlm_t *h, const void *p, int64_t ld) {
+// (Positions: what a launch holds of 64 x 64 tiles.)
+bool logit_rows_ok(const rnnlm_t *h, int32_t T, const void *p, int64_t ld) {
   const uintptr_t es = h->cfg.precision == RNNLM_FP32 ? 4 : 2;
-  return p && reinterpret_cast<uintptr_t>(p) % es == 0 && ld >= h->cfg.V && ld <= (int64_t(1) << 31) && h->cfg.V <= (1 << 20);
+  return p && reinterpret_cast<uintptr_t>(p) % es == 0 && ld >= h->cfg.V && ld <= (int64_t(1) << 31) && h->cfg.V <= (1 << 20) &&
+         (int64_t)T * h->Bp <= (int64_t)65535 * LW_TILE;
 }
 bool tau_in_range(float tau) { return tau >= 1e-3f && tau <= 1e3f; }
-bool distill_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d) {
-  if (!h || !x || !d || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, d->logits, d->ld)) return false;
+bool distill_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, const float *loss,
+                     const double *sum_loss = nullptr) {
+  if (!h || !x || !d || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, T, d->logits, d->ld)) return false;
   if (!d->ids || !d->vals || d->K < 1 || d->K > 1024 || !tau_in_range(d->tau) || !(d->alpha >= 0.0f && d->alpha <= 1.0f)) return false;
-  if (d->alpha < 1.0f && !y) return false;
+  if ((d->alpha < 1.0f && !y) || (reinterpret_cast<uintptr_t>(loss) & 3) || (reinterpret_cast<uintptr_t>(sum_loss) & 7)) return false;
   return ((reinterpret_cast<uintptr_t>(d->ids) | reinterpret_cast<uintptr_t>(d->vals) | reinterpret_cast<uintptr_t>(d->lse) |
            reinterpret_cast<uintptr_t>(d->weight) | reinterpret_cast<uintptr_t>(y)) & 3) == 0;
 }
@@ -2193,7 +2196,7 @@ int distill_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, con
 }  // namespace
 
 int rnnlm_forward_logits(rnnlm_t *h, const int32_t *x, int32_t T, void *logits, int64_t ld, void *stream) {
-  if (!h || !x || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, logits, ld)) return RNNLM_ERR_ARG;
+  if (!h || !x || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, T, logits, ld)) return RNNLM_ERR_ARG;
   hipStream_t st = (hipStream_t)stream;
   return (h->cfg.precision == RNNLM_FP32) ? logits_call<float>(h, x, T, logits, ld, true, st)
                                           : logits_call<bf16_t>(h, x, T, logits, ld, true, st);
@@ -2201,7 +2204,7 @@ int rnnlm_forward_logits(rnnlm_t *h, const int32_t *x, int32_t T, void *logits, 
 
 int rnnlm_distill_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float lr,
                               float *loss, double *sum_loss, void *stream) {
-  if (!distill_args_ok(h, x, y, T, d) || !(lr == lr)) return RNNLM_ERR_ARG;
+  if (!distill_args_ok(h, x, y, T, d, loss, sum_loss) || !(lr == lr)) return RNNLM_ERR_ARG;
   UpdateTargets u{h->buf.E, h->buf.U, h->buf.Wo, h->buf.b, 1.0f, lr, true, true};
   u.A = h->buf.A;
   u.C = h->buf.C;
@@ -2210,7 +2213,7 @@ int rnnlm_distill_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, in
 
 int rnnlm_distill_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE, float *dU,
                              float *dWo, float *db, float *loss, void *stream) {
-  if (!distill_args_ok(h, x, y, T, d) || !dE || !dU || !dWo || !db || h->cfg.P > 0) return RNNLM_ERR_ARG;
+  if (!distill_args_ok(h, x, y, T, d, loss) || !dE || !dU || !dWo || !db || h->cfg.P > 0) return RNNLM_ERR_ARG;
   if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dU) | reinterpret_cast<uintptr_t>(dWo) |
        reinterpret_cast<uintptr_t>(db)) & 15)
     return RNNLM_ERR_ARG;
@@ -2223,7 +2226,7 @@ int rnnlm_distill_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int
 
 int rnnlm_distill_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE,
                                         float *dA, float *dU, float *dC, float *db, float *loss, void *stream) {
-  if (!distill_args_ok(h, x, y, T, d) || !dE || !dA || !dU || !dC || !db || h->cfg.P <= 0) return RNNLM_ERR_ARG;
+  if (!distill_args_ok(h, x, y, T, d, loss) || !dE || !dA || !dU || !dC || !db || h->cfg.P <= 0) return RNNLM_ERR_ARG;
   if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dA) | reinterpret_cast<uintptr_t>(dU) |
        reinterpret_cast<uintptr_t>(dC) | reinterpret_cast<uintptr_t>(db)) & 15)
     return RNNLM_ERR_ARG;
@@ -2235,13 +2238,13 @@ int rnnlm_distill_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int3
 
 int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,
                        void *stream) {
-  if (!h || !x || !v || K < 0 || K >= h->cfg.T_max || !logit_rows_ok(h, v->logits, v->ld) || !v->u || !accepted || !tokens ||
-      !tau_in_range(v->tau) || !tau_in_range(v->tau_draft) || (v->draft && K > 0 && !logit_rows_ok(h, v->draft, v->ld_draft)))
+  if (!h || !x || !v || K < 0 || K >= h->cfg.T_max || !logit_rows_ok(h, K + 1, v->logits, v->ld) || !v->u || !accepted || !tokens ||
+      !tau_in_range(v->tau) || !tau_in_range(v->tau_draft) || (v->draft && K > 0 && !logit_rows_ok(h, K, v->draft, v->ld_draft)))
     return RNNLM_ERR_ARG;
   const size_t need = rnnlm_verify_workspace_bytes(K, h->cfg.B, h->cfg.V);
   if (need == 0 || !v->workspace || (reinterpret_cast<uintptr_t>(v->workspace) & 255) || v->workspace_bytes < need ||
       ((reinterpret_cast<uintptr_t>(v->lengths) | reinterpret_cast<uintptr_t>(v->u) | reinterpret_cast<uintptr_t>(accepted) |
-        reinterpret_cast<uintptr_t>(tokens)) & 3))
+        reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(x)) & 3))
     return RNNLM_ERR_ARG;
   hipStream_t st = (hipStream_t)stream;
   return (h->cfg.precision == RNNLM_FP32) ? verify_call<float>(h, x, K, *v, accepted, tokens, st)

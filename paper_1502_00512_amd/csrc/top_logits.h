@@ -2,12 +2,15 @@
 // A row is cut into chunks that fit a workgroup's registers, so it is read once.  A word is ranked by one 64-bit key, the
 // logit's bits in an order that integers have, above the complement of the id: keys differ, so the order is total and a result
 // does not depend on which wave arrives first.  (A NaN ranks with the masked words, -inf; -0 ranks with +0.)
-//   1. maxima of groups of elements (two groups a thread), sum of exponentials of the chunk
+//   1. maxima of groups of elements (one group a thread or several), sum of exponentials of the chunk
 //   2. a threshold that at least K of the maxima reach, so at least K elements do: bisection over the maxima by one wave
-//   3. elements that reach it into LDS (K to about 1.5 K of them for rows without structure)
-//   4. their ranks among each other by counting
-// Where step 3 finds more than LDS holds, or fewer than K elements are numbers, the exact K-th key is found by bisection over
-// the bits of logit and id with a count of the whole chunk for each: 32 + 20 counts, right for every input.
+//   3. elements that reach it into LDS: of G groups without structure some G ln(G / (G - K)), so several a thread where one
+//      a thread would leave more than 1.15 K (5968 bf16 rows of 1582 words, K = 155: 102 us with two a
+//      thread, 53 with four)
+//   4. their ranks among each other
+// Where step 3 finds more than LDS holds, or the groups that hold a number are fewer than K, the exact K-th key is found by
+// bisection over the bits of logit and id with a count of the whole chunk for each: 32 + 20 counts, right for every input.
+// (Rows of few words are ranked whole then.)
 #pragma once
 #include "rows.h"
 
@@ -15,6 +18,8 @@ namespace rnnlm_dev {
 
 constexpr int TOP_K_MAX = 256;
 constexpr int TOP_WIDE = 512, TOP_MERGE_THREADS = 256, TOP_CAP = 1024, TOP_MERGE_LDS = 2048;
+constexpr int TOP_COUNTED = 128;  // keys that are ranked by counting
+constexpr int TOP_WHOLE = 512;  // rows of so many words may be ranked as they are
 constexpr int TOP_V_MAX = 1 << 20;  // ids fit 20 bits
 constexpr unsigned TOP_MASKED = 0x007fffffu;  // order of -inf
 
@@ -51,9 +56,74 @@ __device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned 
 // ln of the sum s relative to 2^ref.
 __device__ inline float row_lse(double ref, float s) { return s == 0.0f ? -INFINITY : (float)((ref + log2((double)s)) * LN2_64); }
 
-// store(rank, key) for the K greatest of n keys in LDS: eight lanes to a key, each counts an eighth of the others.
+// The value of the lane whose number differs in the bits of X.
+template <int X>
+__device__ inline unsigned long long lane_xor(unsigned long long v) {
+  if constexpr (X == 1) return lane_swap<0xB1>(v);
+  else if constexpr (X == 2) return lane_swap<0x4E>(v);
+  else if constexpr (X == 3) return lane_swap<0x1B>(v);
+  else if constexpr (X == 4) return lane_swap<0x1B>(lane_swap<0x141>(v));
+  else if constexpr (X == 7) return lane_swap<0x141>(v);
+  else if constexpr (X == 8) return lane_swap<0x128>(v);
+  else if constexpr (X == 15) return lane_swap<0x140>(v);
+  else return __shfl_xor(v, X);
+}
+// Sorts a wave's keys, descending: sorted runs of BITS lanes are joined to runs of twice as many, the first exchange of each
+// join a mirrored one.
+template <int X, int BIT>
+__device__ inline void top_exchange(unsigned long long &key) {
+  const unsigned long long other = lane_xor<X>(key);
+  const bool lower = (threadIdx.x & BIT) == 0;
+  key = (other > key) == lower ? other : key;
+}
+template <int BITS>
+__device__ inline void top_settle(unsigned long long &key) {
+  if constexpr (BITS >= 1) {
+    top_exchange<BITS, BITS>(key);
+    top_settle<BITS / 2>(key);
+  }
+}
+template <int BITS = 1>
+__device__ inline void top_sort(unsigned long long &key) {
+  if constexpr (BITS <= 32) {
+    top_exchange<2 * BITS - 1, BITS>(key);
+    top_settle<BITS / 2>(key);
+    top_sort<2 * BITS>(key);
+  }
+}
+
+// store(rank, key) for the K greatest of n keys in LDS (room for whole 64s).  Few keys: eight lanes to a key, each counts an eighth
+// of the others.  Many: lists of 64, sorted by a wave each; a key's rank is what bisection finds above it in every list.  (Counted
+// and sorted: K = 64 of 64000 words, 2560 rows 66.7 and 69.8 us; K = 120 of 10000, one row 12.0 and 11.1; K = 155 of 1582,
+// 5968 rows 54 and 40; K = 256 of 109430, 3 rows 45.8 and 30.3.)
 template <int THREADS, class Store>
-__device__ inline void top_ranks(const unsigned long long *cand, int n, int K, Store &&store) {
+__device__ inline void top_ranks(unsigned long long *cand, int n, int K, Store &&store) {
+  if (n > TOP_COUNTED) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lists = (n + 63) / 64;
+    for (int l = wave; l < lists; l += THREADS / 64) {
+      unsigned long long key = l * 64 + lane < n ? cand[l * 64 + lane] : 0;
+      top_sort(key);
+      cand[l * 64 + lane] = key;
+    }
+    __syncthreads();
+    for (int l = wave; l < lists; l += THREADS / 64) {
+      const unsigned long long key = cand[l * 64 + lane];
+      int rank = 0;
+      for (int other = 0; other < lists; other += 4) {  // (its own list among them)
+        int above[4] = {};
+#pragma unroll
+        for (int step = 32; step; step >>= 1)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (other + i < lists && cand[(other + i) * 64 + above[i] + step - 1] > key) above[i] += step;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (other + i < lists) rank += above[i] + (cand[(other + i) * 64 + above[i]] > key);
+      }
+      if (key != 0 && rank < K) store(rank, key);
+    }
+    return;
+  }
   for (int i0 = 0; i0 < n; i0 += THREADS / 8) {
     const int i = i0 + threadIdx.x / 8;
     const unsigned long long key = i < n ? cand[i] : ~0ull;
@@ -94,10 +164,10 @@ __device__ inline unsigned top_threshold(const unsigned *group, int K, unsigned 
 
 template <typename T, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) {
-  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
+  constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64, PARTS = NV <= 8 ? 4 : 2;  // groups of a thread where they are fine
   __shared__ float sh_m[WAVES], sh_s[WAVES];
   __shared__ double sh_ref[WAVES];
-  __shared__ unsigned group[2 * THREADS];
+  __shared__ unsigned group[PARTS * THREADS];
   __shared__ unsigned long long cand[TOP_CAP];
   __shared__ unsigned sh_t, sh_n, sh_count[2][WAVES];
   const long row = blockIdx.x / a.chunks;
@@ -118,20 +188,36 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   // 1.  The sum is relative to about the greatest element of the wave's first slots (a whole power of 2), so it runs while the
   // rest arrives.
   const float c = LOG2E / a.tau, ref = wave_max(slot_max<T>(zt, raw[0])), b = -whole_power(ref, c);
-  float top[NV], half[2] = {max3(zt, -INFINITY, -INFINITY), -INFINITY}, s = exp2_32(fmaf(zt, c, b));
+  float top[NV], part[PARTS], s = exp2_32(fmaf(zt, c, b));
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) part[i] = i == 0 ? max3(zt, -INFINITY, -INFINITY) : -INFINITY;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    top[i] = slot_max<T>(-INFINITY, raw[i]);
-    half[i & 1] = max3(half[i & 1], top[i], -INFINITY);
+    if constexpr (NV < 4) {  // groups of a slot's quarters
+      float of_slot[4];
+#pragma unroll
+      for (int e = 0; e < N; e += N / 4) of_slot[e / (N / 4)] = max3(slot_elem<T>(raw[i], e), slot_elem<T>(raw[i], e + N / 4 - 1), -INFINITY);
+      top[i] = max3(max3(of_slot[0], of_slot[1], of_slot[2]), of_slot[3], -INFINITY);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[e] = max3(part[e], of_slot[e], -INFINITY);
+    } else {
+      top[i] = slot_max<T>(-INFINITY, raw[i]);
+      part[i % PARTS] = max3(part[i % PARTS], top[i], -INFINITY);
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(raw[i], e), c, b));
     keep_packed(raw[i]);
     keep_here(s);  // (with the exponentials of many slots put off the kernel spilled 100 registers)
   }
-  const float both = max3(half[0], half[1], -INFINITY), mine = wave_max(both);
-  const bool pairs = K > THREADS / 4;  // two groups a thread for long lists
-  group[tid] = logit_order(pairs ? half[0] : both);
-  if (pairs) group[THREADS + tid] = logit_order(half[1]);
+  float all = part[0];
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) all = max3(all, part[i], -INFINITY);
+  const float mine = wave_max(all);
+  const bool fine = 4 * K > min(slots, THREADS);
+  group[tid] = logit_order(fine ? part[0] : all);
+  if (fine)
+#pragma unroll
+    for (int i = 1; i < PARTS; ++i) group[i * THREADS + tid] = logit_order(part[i]);
   s = wave_sum(s);
   double power = -(double)b;
   if (!(s - s == 0.0f) || (!near_power(ref, c) && mine > -INFINITY)) {
@@ -156,13 +242,13 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   if (wave == 0) {
     const float mx = waves_max<WAVES>(sh_m);
     const unsigned top_order = __builtin_amdgcn_readfirstlane(logit_order(mx));
-    const unsigned lo = pairs ? top_threshold<2 * WAVES>(group, K, top_order) : top_threshold<WAVES>(group, K, top_order);
+    const unsigned lo = fine ? top_threshold<PARTS * WAVES>(group, K, top_order) : top_threshold<WAVES>(group, K, top_order);
     if (lane == 0) sh_t = lo;
   }
   __syncthreads();
   // 3.
   const unsigned thr = sh_t;
-  const bool few = thr <= TOP_MASKED;  // some of the K are masked, or no element at all
+  const bool few = thr <= TOP_MASKED;  // fewer than K groups with a number
   if (!few) {
     // Of its slots that reach the threshold a lane takes one at a time, each lane its own (selected from the registers): the
     // 64 lanes' few finds share the instructions.
@@ -201,21 +287,25 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
     __syncthreads();
   }
   int n = (int)sh_n;
-  if (few || n > TOP_CAP) {
+  auto each = [&](auto &&element) {
+    if (tail < a.V) element(logit_order(zt), tail);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = i * THREADS + tid;
+      keep_packed(raw[i]);
+      if (j < slots) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) element(logit_order(slot_elem<T>(raw[i], e)), (first + j) * N + e);
+      }
+    }
+  };
+  if (NV == 1 && few && a.V <= TOP_WHOLE) {
+    each([&](unsigned k, int id) { cand[id] = top_key(k, id); });
+    __syncthreads();
+    n = a.V;
+  } else if (few || n > TOP_CAP) {
     // exact: the order of the K-th element, then the id up to which elements of that order belong
     int turn = 0;
-    auto each = [&](auto &&element) {
-      if (tail < a.V) element(logit_order(zt), tail);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int j = i * THREADS + tid;
-        keep_packed(raw[i]);
-        if (j < slots) {
-#pragma unroll
-          for (int e = 0; e < N; ++e) element(logit_order(slot_elem<T>(raw[i], e)), (first + j) * N + e);
-        }
-      }
-    };
     auto count = [&](auto &&reaches) {
       int mine = 0;
       each([&](unsigned k, int id) { mine += reaches(k, id); });

@@ -286,6 +286,41 @@ def test_a_verification_step_can_be_captured():
         assert torch.equal(n, n2) and torch.equal(tokens, tokens2) and torch.equal(logits, logits2) and torch.equal(g.h_state, e.h_state)
 
 
+@pytest.mark.parametrize("precision", [FP32, BF16])
+def test_a_distilled_training_window_can_be_captured(precision):
+    V, H, B, T, K = 3001, 128, 8, 4, 10
+    g, _ = handle(V, H, 0, B, T, precision, 1)
+    e, _ = handle(V, H, 0, B, T, precision, 1)
+    x = torch.zeros(T, B, dtype=torch.int32, device="cuda")
+    mk = lambda: [cuda(a) for a in teacher(T, B, V, K, 1.0, 0)]  # noqa: E731
+    ids, vals, lse, weight, y = mk()
+    out = lambda: (torch.empty(T, B, device="cuda"), torch.zeros(1, dtype=torch.float64, device="cuda"),  # noqa: E731
+                   torch.empty(T, B, V, device="cuda", dtype=torch.float32 if precision == FP32 else torch.bfloat16))
+    (loss, total, z), (loss2, total2, z2) = out(), out()
+    call = lambda h, l, s, r, lr: h.rnnlm_distill_train_chunk(x, y, ids, vals, lr, lse, weight, 1.0, 0.5, logits=r, loss=l, sum_loss=s)  # noqa: E731
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for h in (g, e):
+            call(h, loss, total, z, 0.5)  # (the first call outside of a capture)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(g, loss, total, z, 0.5)
+    for k in range(4):
+        x.copy_(cuda(synth.zipf_tokens(T * B, V, 1.0, k).reshape(T, B).astype(np.int32)))
+        for kept, new in zip((ids, vals, lse, weight, y), teacher(T, B, V, K, 1.0, k)):
+            kept.copy_(torch.as_tensor(new))
+        graph.replay()
+        call(e, loss2, total2, z2, 0.5)
+        torch.cuda.synchronize()
+        assert torch.equal(loss, loss2) and torch.equal(total, total2) and torch.equal(z, z2) and torch.equal(g.h_state, e.h_state), k
+        for name in ("E", "U", "Wo", "b"):
+            assert torch.equal(getattr(g, name), getattr(e, name)), (k, name)
+    g.rnnlm_check()
+
+
 def test_teacher_to_student_by_way_of_lists():
     """The three calls as they are used together: a teacher's window, its lists, the student's window; the student's gradients
     against autograd on the teacher's own lists."""

@@ -99,6 +99,14 @@ def test_top_logits_patterns(V, K, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["normal", "ties", "few"])
+@pytest.mark.parametrize("V", [257, 500, 512, 513, 1000, 1031, 2047, 2050, 4099, 8200])
+def test_top_logits_long_lists_of_short_rows(V, kind, dtype):
+    for K in (64, 129, 256):
+        check_top(patterns(kind, 3, V, V + K), K, 1.0, dtype, 1)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_top_logits_of_many_rows_in_one_chunk_and_of_the_widest_vocabulary(dtype):
     check_top(patterns("normal", 700, 9000, 1), 31, 0.7, dtype, 0)  # a chunk a row
     check_top(patterns("ties", 2, 1 << 20, 2), 256, 1.0, dtype, 0)
@@ -291,6 +299,7 @@ def test_distill_gradient_is_the_loss_difference():
 # ---- verification -----------------------------------------------------------------------------------------------------
 def check_verify(target, drafts, u, draft=None, lengths=None, tau=1.0, tau_d=1.0, dtype="fp32", pad=0):
     K1, B, V = target.shape
+    tau, tau_d = float(np.float32(tau)), float(np.float32(tau_d))  # as the call gets them: a drawn word may hang on 1e-9
     t, ref = place(target.reshape(-1, V), dtype, pad)
     q = qref = None
     if draft is not None:
@@ -320,7 +329,7 @@ def texts(K, B, V, seed, close=0.5):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("with_draft", [True, False])
 @pytest.mark.parametrize("K,B,V,pad", [(1, 1, 1, 0), (2, 3, 2, 1), (3, 5, 7, 0), (4, 2, 100, 0), (8, 37, 1001, 3), (2, 300, 260, 0), (5, 2, 33278, 1),
-                                       (3, 1, 100000, 0), (40, 2, 60, 0)])
+                                       (3, 1, 100000, 0), (40, 2, 60, 0), (1, 1100, 20011, 0)])
 def test_verify_sizes(K, B, V, pad, with_draft, dtype):
     target, draft, drafts, u, lengths = texts(K, B, V, K + B + V)
     n = check_verify(target, drafts, u, draft if with_draft else None, None, 1.0, 1.0, dtype, pad)[0]
@@ -452,6 +461,37 @@ def test_calls_follow_their_stream_and_can_be_captured():
         for k in kept:
             if k not in ("w1", "w2"):
                 assert torch.equal(kept[k], eager[k]), (i, k)
+
+
+def test_calls_on_two_streams_at_once():
+    M, V, K, B, D = 300, 20011, 150, 20, 4
+    i32 = torch.int32
+
+    def make(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        z = torch.randn(M, V, device="cuda", generator=g).bfloat16()
+        return dict(z=z, u=torch.rand(D + 1, B, device="cuda", generator=g), d=torch.empty_like(z),
+                    drafts=torch.randint(0, V, (D, B), device="cuda", generator=g, dtype=i32))
+
+    def calls(s):
+        ids, vals, lse = binding.rnnlm_top_logits(s["z"], K)
+        loss = binding.rnnlm_distill_loss(s["z"], ids, vals, lse, dlogits=s["d"])
+        n, tokens = binding.rnnlm_verify_drafts(s["z"][: (D + 1) * B].view(D + 1, B, V), s["drafts"], s["u"], s["z"][M - D * B:].view(D, B, V))
+        return [ids, vals, lse, loss, s["d"].clone(), n, tokens]
+
+    states = [make(1), make(2)]
+    alone = [calls(s) for s in states]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for k in (0, 1):
+            with torch.cuda.stream(streams[k]):
+                got[k].append(calls(states[k]))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        for turn in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(alone[k], turn))
 
 
 def test_rows_behind_and_between_are_left_as_they_were():
