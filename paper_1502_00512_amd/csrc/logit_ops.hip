@@ -50,7 +50,13 @@ bool meet(Span a, Span b) { return a.at < b.end && b.at < a.end; }
 struct TopPlan {
   int chunks, per, threads, nv;
 };
-// Whole rows in a workgroup's registers where they fit (no second launch), else chunks, shorter ones where the rows are few.
+// A workgroup holds THREADS x NV slots of a row.  The measured calls: bf16, K = 64 unless said.
+// Up to 4096 slots 256 threads, with as few slots each as hold the row.  Up to 10240 one workgroup of 512, no second launch: 64000
+// words, 1 row 9.4 us against 12.5 in chunks, 256 rows 14.0 and 20.3, 2560 rows 66 and 76.  Up to 20480 one of 1024, where the rows
+// are no more than the compute units or the lists long: 100000 words, K = 200, 1 row 16.2 against 23.6, 256 rows 21.7 and 38.5,
+// 2560 rows 178 and 212; K = 16, 256 rows 17.9 and 19.7, but 1 to 64 rows 12.5 to 13.8 and 12.5, 512 rows 32.8 and 28.6, 2560 rows
+// 142 and 95 (one such workgroup on a compute unit: nothing runs while it waits).  Else chunks, halved while the workgroups are
+// fewer than the compute units: 64 rows of 100000 words 16.9 us so, 18.7 halved up to 512 workgroups.
 TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   const int slots = slots_of(V, dtype);
   TopPlan p;
@@ -62,6 +68,9 @@ TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   } else if (slots <= TOP_WIDE * 20) {
     p.threads = TOP_WIDE;
     if (slots > TOP_WIDE * 16) p.nv = 20;
+  } else if (slots <= TOP_WIDEST * 20 && (rows <= 256 || K > TOP_COUNTED)) {
+    p.threads = TOP_WIDEST;
+    if (slots > TOP_WIDEST * 16) p.nv = 20;
   } else {
     while (p.nv > 4 && rows * chunks() < 256 && 2 * chunks() * K <= TOP_CAP) p.nv /= 2;
   }
@@ -86,7 +95,9 @@ void launch_top_chunks(const TopArgs &a, int64_t rows, hipStream_t st) {
 }
 template <typename T>
 void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st) {
-  if (p.threads == TOP_WIDE && p.nv == 20) launch_top_chunks<T, TOP_WIDE, 20>(a, rows, st);
+  if (p.threads == TOP_WIDEST && p.nv == 20) launch_top_chunks<T, TOP_WIDEST, 20>(a, rows, st);
+  else if (p.threads == TOP_WIDEST) launch_top_chunks<T, TOP_WIDEST, 16>(a, rows, st);
+  else if (p.threads == TOP_WIDE && p.nv == 20) launch_top_chunks<T, TOP_WIDE, 20>(a, rows, st);
   else if (p.threads == TOP_WIDE) launch_top_chunks<T, TOP_WIDE, 16>(a, rows, st);
   else if (p.nv == 1) launch_top_chunks<T, 256, 1>(a, rows, st);
   else if (p.nv == 2) launch_top_chunks<T, 256, 2>(a, rows, st);
@@ -96,7 +107,6 @@ void launch_top(const TopArgs &a, int64_t rows, const TopPlan &p, hipStream_t st
 }
 
 // ---- distillation ----
-constexpr int64_t DISTILL_MANY_ROWS = 1024;
 template <typename T, int THREADS, int NV, int MODE>
 void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   hipLaunchKernelGGL((distill_row_kernel<T, THREADS, NV, MODE>), dim3((unsigned)rows), dim3(THREADS),
@@ -105,8 +115,10 @@ void launch_distill_row(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
 template <typename T, int MODE>
 void launch_distill(const DistillArgs<T> &a, int64_t rows, hipStream_t st) {
   const int slots = a.V / SlotOf<T>::N;  // whole ones: what a thread's registers hold
-  // Many short rows: a wave each, four times as many in flight (a row's time is the latency of its steps, not its bytes).
-  const bool wave_each = rows >= DISTILL_MANY_ROWS && slots <= 64 * 8;
+  // Many short rows: a wave each, four times as many in flight (a row's time is the latency of its steps, not its bytes): bf16,
+  // K = 40, 6000 rows of 1000 words 14.0 us and 19.6 with four waves each, of 3000 words 21.9 and 24.1; 512 to 2048 rows 11 either
+  // way.
+  const bool wave_each = rows >= 1024 && slots <= 64 * 8;
   if (!a.dz || slots > 1024 * 25) {
     hipLaunchKernelGGL((distill_stream_kernel<T, 512, MODE>), dim3((unsigned)rows), dim3(512), distill_lds(a.K), st, a);
   } else if (wave_each && slots <= 64 * 2) {
@@ -161,6 +173,8 @@ int verify_blocks(int32_t V, int32_t dtype) { return (slots_of(V, dtype) + 63) /
 VerifyPlan verify_plan(int32_t K, int32_t B, int32_t V) {
   VerifyPlan p;
   const int slots = slots_of(V, RNNLM_DTYPE_BF16);  // (fp32 rows have twice as many: parts of twice the slots)
+  // Parts of a row until there are 8192 workgroups (4096 and 16384: the same within 2 us for 128 texts x 4 drafts over 100000
+  // words); shares of a text until there are 4096 (2048 and 8192 in place of it: as fast or slower).
   const int64_t rows = (int64_t)(2 * K + 1) * B, fill = 8192;
   p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({fill / std::min(rows, fill), VERIFY_PARTS, slots / VERIFY_THREADS}));
   p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>({4096 / std::min<int64_t>(B, 4096), VERIFY_PARTS, slots / VERIFY_THREADS}));
