@@ -12,6 +12,8 @@
 //      common factor)
 //   4. sums of r by blocks of one slot a lane, and by the last workgroup of a text to finish: the block on which u_K falls, and
 //      the word in it
+// 128 texts of up to 5 drafts over 100000 bf16 words take 34, 5, 15 and 30 us (rows behind a text's drafts are left out: 154 of 282 MB
+// read), 37 without draft logits over 33278 fp32 words 6 and 10 (2 inside of 4).
 // Short rows do 2 to 4 in one workgroup a text.  Steps 3 and 4 are bound by 64-bit instructions (some 23 an exponential); texts
 // differ in what they need, so they are cut fine (a chunk is a few blocks) and every workgroup knows at once whether it has
 // anything to do: with step 2 inside step 3 and eight chunks a text, 128 texts over 100000 words took 26 and 31 us in the two.

@@ -99,6 +99,13 @@ def test_top_logits_patterns(V, K, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["equal", "masked", "few", "ties", "nan", "clustered", "rising", "lowest"])
+@pytest.mark.parametrize("slots,K", [(5001, 60), (9001, 256), (11001, 9), (18001, 256)])
+def test_top_logits_of_wide_rows(slots, K, kind, dtype):
+    check_top(patterns(kind, 2, slots * (4 if dtype == "fp32" else 8) - 3, 11), K, 1.0, dtype, 0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("kind", ["normal", "ties", "few"])
 @pytest.mark.parametrize("V", [257, 500, 512, 513, 1000, 1031, 2047, 2050, 4099, 8200])
 def test_top_logits_long_lists_of_short_rows(V, kind, dtype):
@@ -109,6 +116,7 @@ def test_top_logits_long_lists_of_short_rows(V, kind, dtype):
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_top_logits_of_many_rows_in_one_chunk_and_of_the_widest_vocabulary(dtype):
     check_top(patterns("normal", 700, 9000, 1), 31, 0.7, dtype, 0)  # a chunk a row
+    check_top(patterns("normal", 300, 45007 if dtype == "fp32" else 90007, 3), 20, 1.0, dtype, 0)  # chunks
     check_top(patterns("ties", 2, 1 << 20, 2), 256, 1.0, dtype, 0)
     check_top(patterns("clustered", 1, (1 << 20) - 3, 2), 256, 1.0, dtype, 1)
 
