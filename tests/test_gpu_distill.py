@@ -182,6 +182,41 @@ def test_distill_training_windows_fp32(V, H, P, B, T):
     assert (np.abs(lp - ref) <= 2e-4 * np.abs(ref) + 1e-5).all()
 
 
+@pytest.mark.parametrize("precision", [FP32, BF16])
+@pytest.mark.parametrize("V,H,P", [(777, 50, 0), (700, 64, 32)])
+def test_windows_of_all_kinds_and_lengths_on_one_handle(V, H, P, precision):
+    """What longer windows and other criteria leave in the workspace does not reach a shorter distilled one."""
+    B, T_max, K = 5, 20, 7
+    g, w = handle(V, H, P, B, T_max, precision, 5)
+    fresh, _ = handle(V, H, P, B, T_max, precision, 5)
+
+    def window(T, seed):
+        x = synth.zipf_tokens(T * B, V, 1.0, seed).reshape(T, B).astype(np.int32)
+        return x, teacher(T, B, V, K, 2.0, seed)
+
+    for T, T2 in ((20, 2), (3, 7), (1, 20)):
+        x, (ids, vals, lse, weight, y) = window(T, T)
+        g.rnnlm_distill_train_chunk(cuda(x), cuda(y), cuda(ids), cuda(vals), 0.0, cuda(lse), cuda(weight), 2.0, 0.6)
+        g.rnnlm_train_chunk(cuda(x), cuda(np.maximum(y, 0)), 0.0)
+        g.rnnlm_verify_chunk(cuda(x), torch.full((T, B), 0.5, device="cuda"))
+        g.rnnlm_check()
+        g.rnnlm_reset_state()
+        x, (ids, vals, lse, weight, y) = window(T2, 50 + T2)
+        call = lambda h: h.rnnlm_distill_grad_chunk(cuda(x), cuda(y), cuda(ids), cuda(vals), cuda(lse), cuda(weight), 2.0, 0.6)  # noqa: E731
+        got, ref = call(g), call(fresh)
+        g.rnnlm_check()
+        for v in w.values():
+            v.grad = None
+        loss64(logits64(w, x, torch.zeros(B, H, dtype=torch.float64))[0], ids, vals, lse, weight, y, 2.0, 0.6).mean().backward()
+        for name, v in w.items():
+            assert torch.equal(got["g" + name], ref["g" + name]), name
+            close(name, got["g" + name], v.grad, 1e-3 if precision == FP32 else 3e-2 if P else 2e-2)
+        z, z2 = g.rnnlm_forward_logits(cuda(x)), fresh.rnnlm_forward_logits(cuda(x))
+        assert torch.equal(z, z2)
+        g.rnnlm_reset_state()
+        fresh.rnnlm_reset_state()
+
+
 def test_what_a_distilled_window_reports():
     V, H, B, T = 300, 32, 3, 4
     g, _ = handle(V, H, 0, B, T, FP32, 1)

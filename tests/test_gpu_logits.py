@@ -423,6 +423,21 @@ def test_verify_drafts_out_of_range_and_lengths_beyond_the_batch():
     check_verify(target, drafts, u, None, [9, 9, 3, 2])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tau", [1e-3, 1e3])
+@pytest.mark.parametrize("V", [1203, 20011, 90001])
+def test_temperatures_at_the_ends(V, tau, dtype):
+    tau = float(np.float32(tau))
+    z = patterns("normal", 4, V, V)
+    check_top(z, 20, tau, dtype, 1)
+    ids, vals, y, w = lists(4, V, 20, 3, False)
+    for alpha in (0.5, 1.0):
+        check_distill(z, ids, vals, y, w, dtype, tau=tau, alpha=alpha)
+    target, draft, drafts, u, lengths = texts(2, 3, V, V)
+    check_verify(target, drafts, u, draft, lengths, tau, tau, dtype)
+    check_verify(target, drafts, u, draft, None, 1.0, tau, dtype)
+
+
 # ---- streams, graphs, workspaces --------------------------------------------------------------------------------------
 def test_calls_follow_their_stream_and_can_be_captured():
     """The three calls one after the other in a graph, replayed on new inputs with eager work between, against eager calls."""
