@@ -161,7 +161,7 @@ def check_distill(z, ids, vals, y, w, dtype, pad=0, tau=1.0, alpha=0.5, scale=0.
         nr = None if n is None else float(n[r])
         l, gr = L.distill(ref[r], ids[r], vals[r], nr, yr, float(w_[r]), tau, alpha, scale)
         if abs(l) > float(torch.finfo(torch.float32).max):  # a label's or a listed word's logit at the type's lowest value
-            l = np.inf
+            l = np.copysign(np.inf, l)
         there = (ids[r] >= 0) & (ids[r] < V) & np.isfinite(vals[r])
         t = vals[r][there].astype(np.float64) / tau
         norm = nr if nr is not None else (L.lse(t) if len(t) else 0.0)
@@ -201,6 +201,22 @@ def check_distill(z, ids, vals, y, w, dtype, pad=0, tau=1.0, alpha=0.5, scale=0.
                                           (1, 300001, 16, 0)])
 def test_distill_sizes(rows, V, K, pad, dtype):
     check_distill(patterns("normal", rows, V, V), *lists(rows, V, K, V + 1, False), dtype, pad, tau=2.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("slots", [200, 500, 1000, 1500, 2048, 3000, 4000, 6000, 8100, 10000, 12700, 18000, 25500, 25700])
+def test_distill_widths(slots, dtype):
+    V = slots * (4 if dtype == "fp32" else 8) + 1
+    check_distill(patterns("normal", 3, V, slots), *lists(3, V, 30, slots, True), dtype, tau=1.0 if slots % 3 else 2.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["normal", "steep", "lowest", "huge"])
+@pytest.mark.parametrize("slots,K", [(30, 20), (127, 1024), (255, 64), (511, 100)])
+def test_distill_many_short_rows(slots, K, kind, dtype):
+    V = slots * (4 if dtype == "fp32" else 8) + 3
+    for tau, grad in ((2.0, "inplace"), (1.5, "apart"), (1.0, "apart")):
+        check_distill(patterns(kind, 1025, V, slots), *lists(1025, V, K, slots, tau != 1.0), dtype, 1, tau, grad=grad)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
