@@ -544,6 +544,23 @@ def test_rows_behind_and_between_are_left_as_they_were():
         assert not bool((buf[1: M + 1, :V] == 3).any())
 
 
+@pytest.mark.parametrize("V", [700, 5001])
+def test_rows_further_apart_than_32_bits_reach(V):
+    ld, M = (1 << 30) + 1, 5
+    buf = torch.empty((M - 1) * ld + V, device="cuda", dtype=torch.bfloat16)  # 8.6 GB: the last row starts behind 2^32 elements
+    far = buf.as_strided((M, V), (ld, 1))
+    near = torch.randn(M, V, device="cuda").bfloat16()
+    far.copy_(near)
+    got, want = binding.rnnlm_top_logits(far, 30), binding.rnnlm_top_logits(near, 30)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    drafts, u = torch.randint(0, V, (2, 1), device="cuda", dtype=torch.int32), torch.rand(3, 1, device="cuda")
+    got = binding.rnnlm_verify_drafts(far[:3, None], drafts, u, far[3:, None])
+    assert all(torch.equal(a, b) for a, b in zip(got, binding.rnnlm_verify_drafts(near[:3, None], drafts, u, near[3:, None])))
+    ids, vals, lse = want
+    loss, loss2 = binding.rnnlm_distill_loss(far, ids, vals, lse, dlogits=far), binding.rnnlm_distill_loss(near, ids, vals, lse, dlogits=near)
+    assert torch.equal(loss, loss2) and torch.equal(far, near)
+
+
 def test_same_inputs_same_bits():
     z = torch.randn(50, 3001, device="cuda").to(torch.bfloat16)
     ids, vals, lse = binding.rnnlm_top_logits(z, 200)
