@@ -55,8 +55,7 @@ __global__ void __launch_bounds__(256) logits_to_rows_kernel(const T *__restrict
 
 // The way back for gradients: padding (words and positions) becomes zero.  A workgroup owns 64 words and walks a share of `per`
 // positions in order.  sums[share][v] receives its sum over them (bias gradients), which bias_update_kernel joins; sums = nullptr:
-// there is one share, and b_out[v] = alpha b[v] - lr sum.  With all
-// positions of 64 words to a workgroup 10000 words ran on 157 compute units: 77 us for 2560 positions, 27 in shares.
+// there is one share, and b_out[v] = alpha b[v] - lr sum.  With all positions of 64 words to a workgroup 10000 words ran on 157 compute units: 77 us for 2560 positions, 27 in shares.
 template <typename T>
 __global__ void __launch_bounds__(256) rows_to_logits_kernel(const T *__restrict__ in, T *__restrict__ ZT, int Mp, int per,
                                                              float *__restrict__ sums, long ld_sums, const float *__restrict__ b,

@@ -906,8 +906,9 @@ bool short_output_update(rnnlm_t *h, int Tn) {
   return 2.0 * n * window_plan(h, (long)Tn * h->Bp).Mp / rate + 8.0 * n / 4e6 < 15.0;
 }
 
-// train: a backward pass follows.  logits_only: the window ends with its logits, no statistics are formed.  sort_inputs: its embedding update wants the input ids sorted: started on the side
-// stream as soon as the padded ids exist (the update runs on that stream too).
+// train: a backward pass follows.  sort_inputs: its embedding update wants the input ids sorted: started on the side
+// stream as soon as the padded ids exist (the update runs on that stream too).  logits_only: the window ends with its
+// logits, no statistics are merged.
 template <typename T>
 int forward_window(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float *logp_out, bool advance_state,
                    bool with_output, hipStream_t st, bool train = false, bool sort_inputs = false, bool need_feat = false,

@@ -50,8 +50,8 @@ __device__ inline slot_t empty_slot() {  // -inf in every element
   return slot_t{w, w, w, w};
 }
 
-// Whole slot j of a row (store_slot: flip is laid over each 32 bits, the sign bits of a gradient with a negative factor).  The elements behind a row's last whole slot are taken one by one (tail_elem).
-// once: nobody reads it again soon, it need not displace anything in the caches.
+// Whole slot j of a row (store_slot: flip is laid over each 32 bits, the sign bits of a gradient with a negative factor).  The
+// elements behind a row's last whole slot are taken one by one (tail_elem).  ONCE: nobody reads it again soon, it need not displace anything in the caches.
 template <typename T, bool ONCE = false>
 __device__ inline slot_t load_slot(const T *row, int j) {
   // (an unsigned 32-bit offset from a row that all lanes share: no 64-bit address in registers)
