@@ -221,15 +221,24 @@ def _scratch(call, t, device, nbytes):
     return t.data_ptr(), t.nbytes, t
 
 
-def _launch(device, stream, f, *args):
-    """f(*args, the stream) with that device current."""
+def _on(call, stream, device, f, *args):
+    """f(*args) with `stream` the current one, so that what is allocated in there (scratch that is dropped when the call
+    returns, above all) comes from this stream's pool: memory of another one's may still be at work there, or be again."""
     import torch
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
+    if stream.device.index != device:
+        _refuse(call, f"stream: one of device {device} is wanted")
+    with torch.cuda.stream(stream):
+        return f(*args)
+
+
+def _launch(device, f, *args):
+    """f(*args, the current stream of that device) with that device current."""
+    import torch
+    stream = torch.cuda.current_stream(device).cuda_stream
     if torch.cuda.current_device() == device:
-        return f(*args, stream.cuda_stream)
+        return f(*args, stream)
     with torch.cuda.device(device):
-        return f(*args, stream.cuda_stream)
+        return f(*args, stream)
 
 
 def rnnlm_top_logits_workspace_bytes(rows: int, V: int, K: int, dtype: int) -> int:
@@ -242,6 +251,8 @@ def rnnlm_top_logits(logits, K: int, tau: float = 1.0, ids=None, vals=None, lse=
     import torch
     call = "rnnlm_top_logits"
     rows, V, ld, dt = _rows(call, "logits", logits)
+    if stream is not None:
+        return _on(call, stream, logits.get_device(), rnnlm_top_logits, logits, K, tau, ids, vals, lse, workspace)
     dev, lead = logits.get_device(), logits.shape[:-1]
     if not 1 <= K <= V:
         _refuse(call, f"K = {K} of V = {V}")
@@ -249,7 +260,7 @@ def rnnlm_top_logits(logits, K: int, tau: float = 1.0, ids=None, vals=None, lse=
     vals = torch.empty(*lead, K, dtype=torch.float32, device=logits.device) if vals is None else vals
     lse = torch.empty(lead, dtype=torch.float32, device=logits.device) if lse is None else lse
     at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_top_logits_workspace_bytes(rows, V, K, dt))
-    _ok(_launch(dev, stream, load().rnnlm_top_logits, logits.data_ptr(), dt, rows, V, ld, K, tau,
+    _ok(_launch(dev, load().rnnlm_top_logits, logits.data_ptr(), dt, rows, V, ld, K, tau,
                 _at(call, "ids", ids, torch.int32, rows * K, dev, K), _at(call, "vals", vals, torch.float32, rows * K, dev, K),
                 _at(call, "lse", lse, torch.float32, rows, dev), at, nbytes), call)
     return ids, vals, lse
@@ -262,6 +273,9 @@ def rnnlm_distill_loss(logits, ids, vals, lse=None, y=None, weight=None, tau: fl
     import torch
     call, f32, i32 = "rnnlm_distill_loss", torch.float32, torch.int32
     rows, V, ld, dt = _rows(call, "logits", logits)
+    if stream is not None:
+        return _on(call, stream, logits.get_device(), rnnlm_distill_loss, logits, ids, vals, lse, y, weight, tau, alpha, scale, loss,
+                   dlogits, sum_loss, range_flag)
     dev, K = logits.get_device(), ids.shape[-1]
     loss = torch.empty(logits.shape[:-1], dtype=f32, device=logits.device) if loss is None else loss
     z, dz, ldd = logits.data_ptr(), None, 0
@@ -271,7 +285,7 @@ def rnnlm_distill_loss(logits, ids, vals, lse=None, y=None, weight=None, tau: fl
         dz, ldd = dlogits.data_ptr(), _rows(call, "dlogits", dlogits, logits)[2]
         if dz == z and rows <= 1:  # in place (one row has no distance to the next)
             ldd = ld
-    _ok(_launch(dev, stream, load().rnnlm_distill_loss, z, dt, rows, V, ld, _at(call, "ids", ids, i32, rows * K, dev, K),
+    _ok(_launch(dev, load().rnnlm_distill_loss, z, dt, rows, V, ld, _at(call, "ids", ids, i32, rows * K, dev, K),
                 _at(call, "vals", vals, f32, rows * K, dev, K), K, _at(call, "lse", lse, f32, rows, dev),
                 _at(call, "y", y, i32, rows, dev), _at(call, "weight", weight, f32, rows, dev), tau, alpha, scale,
                 _at(call, "loss", loss, f32, rows, dev), _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd,
@@ -290,6 +304,9 @@ def rnnlm_verify_drafts(target, drafts, u, draft=None, lengths=None, tau: float 
     import torch
     call, i32 = "rnnlm_verify_drafts", torch.int32
     rows, V, ld, dt = _rows(call, "target", target)
+    if stream is not None:
+        return _on(call, stream, target.get_device(), rnnlm_verify_drafts, target, drafts, u, draft, lengths, tau, tau_draft, accepted,
+                   tokens, workspace, range_flag)
     if target.dim() != 3 or rows == 0:
         _refuse(call, "target: [K+1][B][V] is wanted")
     K, B, dev = target.shape[0] - 1, target.shape[1], target.get_device()
@@ -303,7 +320,7 @@ def rnnlm_verify_drafts(target, drafts, u, draft=None, lengths=None, tau: float 
     accepted = torch.empty(B, dtype=i32, device=target.device) if accepted is None else accepted
     tokens = torch.empty(K + 1, B, dtype=i32, device=target.device) if tokens is None else tokens
     at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_verify_workspace_bytes(K, B, V))
-    _ok(_launch(dev, stream, load().rnnlm_verify_drafts, target.data_ptr(), ld, q, ldd, dt, K, B, V,
+    _ok(_launch(dev, load().rnnlm_verify_drafts, target.data_ptr(), ld, q, ldd, dt, K, B, V,
                 _at(call, "drafts", drafts, i32, K * B, dev, B) if K > 0 else None, _at(call, "lengths", lengths, i32, B, dev),
                 _at(call, "u", u, torch.float32, rows, dev, B), tau, tau_draft, _at(call, "accepted", accepted, i32, B, dev),
                 _at(call, "tokens", tokens, i32, rows, dev, B), _at(call, "range_flag", range_flag, i32, 1, dev), at, nbytes), call)
@@ -500,9 +517,11 @@ class Rnnlm:
 
     def rnnlm_forward_logits(self, x, logits=None, stream=None):
         call = "rnnlm_forward_logits"
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_forward_logits, x, logits)
         T, at = self._window(call, x)
         logits, ld = self._logit_rows(call, T, logits)
-        _ok(self.lib.rnnlm_forward_logits(self.handle, at, T, logits.data_ptr(), ld, _stream(stream)), call)
+        _ok(_launch(self.device.index, self.lib.rnnlm_forward_logits, self.handle, at, T, logits.data_ptr(), ld), call)
         return logits
 
     def _distill(self, call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss):
@@ -520,13 +539,18 @@ class Rnnlm:
                                   logits=None, loss=None, sum_loss=None, stream=None):
         """ids, vals [T][B][K], lse [T][B] or None: the teacher's (rnnlm_top_logits of its rnnlm_forward_logits at the same tau)."""
         call = "rnnlm_distill_train_chunk"
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_distill_train_chunk, x, y, ids, vals, lr, lse, weight, tau, alpha,
+                       logits, loss, sum_loss)
         d, _keep, T, at, y_at, loss_at, sum_at = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, sum_loss)
-        _ok(self.lib.rnnlm_distill_train_chunk(self.handle, at, y_at, T, C.byref(d), lr, loss_at, sum_at, _stream(stream)), call)
+        _ok(_launch(self.device.index, self.lib.rnnlm_distill_train_chunk, self.handle, at, y_at, T, C.byref(d), lr, loss_at, sum_at), call)
 
     def rnnlm_distill_grad_chunk(self, x, y, ids, vals, lse=None, weight=None, tau: float = 1.0, alpha: float = 1.0, logits=None,
                                  stream=None):
         import torch
         call = "rnnlm_distill_grad_chunk" + ("_compressed" if self.P else "")
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_distill_grad_chunk, x, y, ids, vals, lse, weight, tau, alpha, logits)
         z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
         loss = z(x.shape[0], self.B)
         d, _keep, T, at, y_at, loss_at, _ = self._distill(call, x, y, ids, vals, lse, weight, tau, alpha, logits, loss, None)
@@ -534,7 +558,7 @@ class Rnnlm:
             g = dict(gE=z(self.V, self.P), gA=z(self.H, self.P), gU=z(self.H, self.H), gC=z(self.P, self.H), gb=z(self.V))
         else:
             g = dict(gE=z(self.V, self.H), gU=z(self.H, self.H), gWo=z(self.V, self.H), gb=z(self.V))
-        _ok(getattr(self.lib, call)(self.handle, at, y_at, T, C.byref(d), *map(_ptr, g.values()), loss_at, _stream(stream)), call)
+        _ok(_launch(self.device.index, getattr(self.lib, call), self.handle, at, y_at, T, C.byref(d), *map(_ptr, g.values()), loss_at), call)
         return dict(loss=loss, **g)
 
     def rnnlm_verify_chunk(self, x, u, draft=None, lengths=None, tau: float = 1.0, tau_draft: float = 1.0, logits=None, accepted=None,
@@ -542,6 +566,9 @@ class Rnnlm:
         """x int32 [K+1][B]: the word not read yet, then the drafts.  Returns (accepted [B], tokens [K+1][B])."""
         import torch
         call, i32, B, dev = "rnnlm_verify_chunk", torch.int32, self.B, self.device.index
+        if stream is not None:
+            return _on(call, stream, dev, self.rnnlm_verify_chunk, x, u, draft, lengths, tau, tau_draft, logits, accepted, tokens,
+                       workspace)
         T, x_at = self._window(call, x)
         logits, ld = self._logit_rows(call, T, logits)
         ldd = self._logit_rows(call, T - 1, draft)[1] if draft is not None and T > 1 else 0
@@ -550,8 +577,8 @@ class Rnnlm:
         at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_verify_workspace_bytes(T - 1, B, self.V))
         v = rnnlm_verify(draft.data_ptr() if ldd else None, ldd, _at(call, "lengths", lengths, i32, B, dev),
                          _at(call, "u", u, torch.float32, T * B, dev, B), tau, tau_draft, logits.data_ptr(), ld, at, nbytes)
-        _ok(self.lib.rnnlm_verify_chunk(self.handle, x_at, T - 1, C.byref(v), _at(call, "accepted", accepted, i32, B, dev),
-                                        _at(call, "tokens", tokens, i32, T * B, dev, B), _stream(stream)), call)
+        _ok(_launch(dev, self.lib.rnnlm_verify_chunk, self.handle, x_at, T - 1, C.byref(v), _at(call, "accepted", accepted, i32, B, dev),
+                    _at(call, "tokens", tokens, i32, T * B, dev, B)), call)
         return accepted, tokens
 
     def rnnlm_reset_state(self, stream=None):
