@@ -50,8 +50,8 @@ __device__ inline slot_t empty_slot() {  // -inf in every element
   return slot_t{w, w, w, w};
 }
 
-// Whole slot j of a row (store_slot: flip is laid over each 32 bits, the sign bits of a gradient with a negative factor).  The
-// elements behind a row's last whole slot are taken one by one (tail_elem).  ONCE: nobody reads it again soon, it need not displace anything in the caches.
+// Whole slot j of a row; the elements behind a row's last whole slot are taken one by one (tail_elem).  ONCE: nobody reads it
+// again soon, it need not displace anything in the caches.
 template <typename T, bool ONCE = false>
 __device__ inline slot_t load_slot(const T *row, int j) {
   // (an unsigned 32-bit offset from a row that all lanes share: no 64-bit address in registers)
@@ -63,7 +63,7 @@ __device__ inline slot_t load_slot(const T *row, int j) {
 // workgroups are about to read were displaced (2560 rows of 10000 bf16 words 30.2 -> 24.5 us, of 64000 149 -> 138; 8192 of
 // 100000 733 -> 691).
 template <typename T>
-__device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N], unsigned flip = 0) {
+__device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N]) {
   constexpr int N = SlotOf<T>::N;
   union {
     slot_t s;
@@ -71,8 +71,6 @@ __device__ inline void store_slot(T *row, int j, const float (&v)[SlotOf<T>::N],
   } o;
 #pragma unroll
   for (int e = 0; e < N; ++e) o.t[e] = from_f32<T>(v[e]);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o.s[e] ^= flip;
   __builtin_nontemporal_store(o.s, reinterpret_cast<typename SlotOf<T>::type *>(reinterpret_cast<char *>(row) + (unsigned)j * 16u));
 }
 // Element of the row behind its whole slots that thread tid takes; -inf for the others.
