@@ -2,7 +2,7 @@
 //   t_k = val_k / tau,  p_k = exp(t_k - n),  n = the teacher's ln sum_v exp(t_v) as given, or ln sum_k exp(t_k);  pi = sum_k p_k
 //   loss  = w (alpha tau^2 sum_k p_k (ln p_k - ln q_tau(id_k)) - (1 - alpha) ln q_1(y)),   q_tau = softmax(z / tau)
 //   dz[v] = w g (alpha tau (pi q_tau(v) - sum_{k: id_k = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
-// The sum over the list is pi (A / S + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (t_k - z_k / tau):
+// The sum over the list is pi (A / (tau S) + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (val_k - z_k):
 // a pass over the row needs a sum of exponentials only, and the listed words are read one by one.
 // A sum is taken relative to a reference; any will do that leaves it finite and far from 0.
 #pragma once
@@ -23,6 +23,7 @@ struct DistillArgs {
   float tau, alpha, scale;
   int V, K;
   bool once;  // read past the caches
+  double inv_tau;
 };
 
 // Exponentials of an element.  ONE: a single temperature (tau = 1, or no labels).  SQUARE: tau = 2 and labels, whose
@@ -32,7 +33,7 @@ enum DistillMode { DISTILL_ONE, DISTILL_SQUARE, DISTILL_TWO };
 
 struct DistillEntry {  // a word of the list, or (last) the label
   int id;              // -1: absent
-  float t, z, p;       // teacher's logit / tau, student's logit, e^{t - t_max}
+  float val, z, p;     // teacher's logit, student's logit, e^{t - t_max}
 };
 
 // The list in LDS: K entries and the label, behind them the entries' ids by themselves (four to a read, four reads
@@ -92,62 +93,62 @@ struct DistillDense {
   }
 };
 
-// Reads the list of row m: this thread's entries e = tid, tid + THREADS, ...  Returns the greatest t among them.
+// Reads the list of row m: this thread's entries e = tid, tid + THREADS, ...  Returns the greatest logit among them.
 template <typename T, int THREADS>
 __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T *row, DistillEntry *ent) {
-  float tmax = -INFINITY;
-  const float inv_tau = 1.0f / a.tau;
+  float most = -INFINITY;
   const bool label = a.y && a.alpha < 1.0f;
   int *ids = reinterpret_cast<int *>(ent + a.K + 1);
   for (int e = a.K + threadIdx.x; e < distill_ids(a.K); e += THREADS) ids[e] = -2;
   for (int e = threadIdx.x; e <= a.K; e += THREADS) {
     DistillEntry d;
-    d.t = -INFINITY;
+    d.val = -INFINITY;
     d.z = d.p = 0.0f;
     if (e < a.K) {
       d.id = a.ids[m * a.K + e];
-      d.t = a.vals[m * a.K + e] * inv_tau;
+      d.val = a.vals[m * a.K + e];
     } else {
       d.id = label ? a.y[m] : -1;
     }
     if (d.id >= a.V && a.range_flag) *a.range_flag = 1;
     if (d.id < 0 || d.id >= a.V) {
       d.id = -1;
-      d.t = -INFINITY;
+      d.val = -INFINITY;
     } else {
       d.z = to_f32(row[d.id]);
-      if (e < a.K) tmax = fmaxf(tmax, d.t);
+      if (e < a.K) most = fmaxf(most, d.val);
     }
     ent[e] = d;
     if (e < a.K) ids[e] = d.id;
   }
-  return tmax;
+  return most;
 }
 
-// The list's sums S and A over this thread's entries.  (A in 64 bits: masked words may be on the list, at the type's lowest
-// value.)
+// The list's sums S and A over this thread's entries.  (Differences of logits first: a list's probabilities do not hang on how
+// far from zero it lies.  A and S in 64 bits: the loss has A / S, a mean of differences of any size, and masked words may be on
+// the list, at the type's lowest value.)
 template <int THREADS>
-__device__ inline void distill_list_sums(DistillEntry *ent, int K, float inv_tau, float tmax, float &S, double &A) {
+__device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, double &S, double &A) {
   for (int e = threadIdx.x; e < K; e += THREADS) {
     const DistillEntry d = ent[e];
-    if (d.t == -INFINITY) continue;  // absent, or a probability of zero: no term
-    const float p = exp2_32((d.t - tmax) * LOG2E);
+    if (d.val == -INFINITY) continue;  // absent, or a probability of zero: no term
+    const float p = exp2_32((d.val - most) * c);
     ent[e].p = p;
     if (p == 0.0f) continue;
-    S += p;
-    A += (double)p * ((double)d.t - (double)d.z * (double)inv_tau);
+    S += (double)p;
+    A += (double)p * ((double)d.val - (double)d.z);
   }
 }
 
 // Sums over the workgroup's waves, by way of LDS.
 template <int WAVES>
 struct DistillShared {
-  float m[WAVES], m1[WAVES], t[WAVES], s[WAVES], s1[WAVES], S[WAVES], again[WAVES];
-  double A[WAVES];
+  float m[WAVES], m1[WAVES], t[WAVES], s[WAVES], s1[WAVES], again[WAVES];
+  double S[WAVES], A[WAVES];
 };
 
 struct DistillList {
-  float tmax, S, factor, pi;  // p_k = factor e^{t_k - t_max}
+  float most, S, factor, pi;  // greatest logit; p_k = factor e^{t_k - t_max}
 };
 
 // The list's sums (the barrier in between also publishes the waves' sums of the row): all threads take part.
@@ -155,12 +156,11 @@ template <typename T, int THREADS>
 __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, DistillEntry *ent, DistillShared<THREADS / 64> &sh) {
   constexpr int WAVES = THREADS / 64;
   DistillList l;
-  l.tmax = waves_max<WAVES>(sh.t);
+  l.most = waves_max<WAVES>(sh.t);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float S = 0.0f;
-  double A = 0.0;
+  double S = 0.0, A = 0.0;
   if (wave * 64 < a.K) {
-    distill_list_sums<THREADS>(ent, a.K, 1.0f / a.tau, l.tmax, S, A);
+    distill_list_sums<THREADS>(ent, a.K, LOG2E / a.tau, l.most, S, A);
     S = wave_sum(S);
     A = wave_sum(A);
   }
@@ -169,17 +169,18 @@ __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, Dist
     sh.A[wave] = A;
   }
   __syncthreads();
-  l.S = waves_sum<WAVES>(sh.S);
+  l.S = (float)waves_sum<WAVES>(sh.S);
   // (a NaN in the list stays one)
-  l.factor = l.S == 0.0f ? 0.0f : a.lse ? exp2_32((l.tmax - a.lse[m]) * LOG2E) : 1.0f / l.S;
+  l.factor = l.S == 0.0f ? 0.0f : a.lse ? exp2_32((float)(((double)l.most * a.inv_tau - (double)a.lse[m]) * LOG2E_64)) : 1.0f / l.S;
   l.pi = l.S == 0.0f ? 0.0f : a.lse ? l.factor * l.S : l.S / l.S;
   return l;
 }
 
-// The row's loss, by one thread.  (In 64 bits: it is a difference of numbers ten times its size.)
+// The row's loss, by one thread.  In 64 bits: it is a difference of numbers that may be any times its size, so each goes back to
+// units of a logit by the factor that was used for it (c in 32 bits is not log2 e / tau).
 template <typename T, int MODE>
 __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, const RowSums &r, const DistillList &l,
-                                    const DistillEntry &label, const double *A_of_wave, int waves) {
+                                    const DistillEntry &label, const double *S_of_wave, const double *A_of_wave, int waves) {
   const bool hard = label.id >= 0;
   double loss = 0.0;
   if (r.s == 0.0f) {  // no word left
@@ -187,15 +188,18 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
   } else {
     const double tau = a.tau;
     if (a.alpha > 0.0f && l.pi != 0.0f) {
-      double A = 0.0;
-      for (int i = 0; i < waves; ++i) A += A_of_wave[i];
-      const double n = a.lse ? (double)a.lse[m] : (double)l.tmax + log((double)l.S);
-      const double lse = (double)r.shift / tau + ((double)r.power + log2((double)r.s)) * LN2_64;
-      loss = (double)a.alpha * tau * tau * (double)l.pi * (A / (double)l.S + lse - n);
+      double S = 0.0, A = 0.0;
+      for (int i = 0; i < waves; ++i) {
+        S += S_of_wave[i];
+        A += A_of_wave[i];
+      }
+      const double n = a.lse ? (double)a.lse[m] : (double)l.most / tau + log(S);
+      const double ln_sum = (double)r.shift + ((double)r.power + log2((double)r.s)) / (double)(LOG2E / a.tau);  // times tau
+      loss = (double)a.alpha * tau * tau * (double)l.pi * ((A / S + ln_sum) / tau - n);
     }
     if (hard) {
       const double sum = MODE == DISTILL_ONE ? (double)r.power + log2((double)r.s) : (double)r.power1 + log2((double)r.s1);
-      loss += (double)(1.0f - a.alpha) * ((double)r.shift - (double)label.z + sum * LN2_64);
+      loss += (double)(1.0f - a.alpha) * ((double)r.shift - (double)label.z + sum / (double)LOG2E);
     }
   }
   a.loss[m] = (float)((double)w * loss);
@@ -250,7 +254,7 @@ __device__ inline void distill_without_weight(const DistillArgs<T> &a, long m) {
 }
 
 // A row by two passes over memory: sums with a running maximum and sum of each thread (all at z - maximum: for logits of any
-// size), then the gradient.  zt: this thread's element behind the whole slots; te: the greatest t of its list entries.
+// size), then the gradient.  zt: this thread's element behind the whole slots; te: the greatest logit of its list entries.
 template <typename T, int THREADS, int MODE, int FLIGHT, bool ONCE>
 __device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float w, const T *row, float zt, float te, DistillEntry *ent,
                                          DistillShared<THREADS / 64> &sh) {
@@ -307,7 +311,7 @@ __device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float 
   const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);  // (a barrier)
   r.s = waves_sum<WAVES>(sh.s);
   if (MODE != DISTILL_ONE) r.s1 = waves_sum<WAVES>(sh.s1);
-  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.S, sh.A, WAVES);
   if (!a.dz) return;
   const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
   const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
@@ -402,7 +406,7 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
     }
   }
   if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense.template at<true>(zt));
-  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.S, sh.A, WAVES);
   __syncthreads();  // the dense pass first, then the listed words on top of it
   distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
 }

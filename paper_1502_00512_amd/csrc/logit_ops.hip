@@ -286,11 +286,11 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
     int rc;
     if (dtype == RNNLM_DTYPE_FP32) {
       rc = distill_call(DistillArgs<float>{static_cast<const float *>(logits), ld, static_cast<float *>(dlogits), ld_dlogits, ids, y,
-                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once},
+                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, 1.0 / (double)tau},
                         rows, st);
     } else {
       rc = distill_call(DistillArgs<bf16_t>{static_cast<const bf16_t *>(logits), ld, static_cast<bf16_t *>(dlogits), ld_dlogits,
-                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once},
+                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, 1.0 / (double)tau},
                         rows, st);
     }
     if (rc) return rc;

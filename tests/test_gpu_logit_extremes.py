@@ -38,6 +38,49 @@ def reach(z, tau):
     return D, SUM + U * (L.softmax(z, tau) * (4 * D + 16)).sum()
 
 
+def check_distill(z, ids, vals, y, dtype, tau, alpha, n=None, scale=2.0 ** -13, grad=True):
+    """One call over the rows z against the oracle.  n: the teacher's lse [rows] (fp32 values) or None."""
+    rows, V = z.shape
+    tau = float(np.float32(tau))
+    d = rows_of(z, dtype)
+    out = torch.full((rows, V), 7.0, dtype=d.dtype, device="cuda") if grad else None
+    loss = binding.rnnlm_distill_loss(d, cuda(ids, np.int32), cuda(vals, np.float32), cuda(n, np.float32), cuda(y, np.int32), None, tau, alpha,
+                                      scale, dlogits=out).double().cpu().numpy()
+    g = out.double().cpu().numpy() if grad else None
+    half = torch.finfo(DTYPES[dtype]).eps / 2
+    a32 = float(np.float32(alpha))
+    for r in range(rows):
+        yr = -1 if y is None else int(y[r])
+        nr = None if n is None else float(np.float32(n[r]))
+        want, gr = L.distill(z[r], ids[r], vals[r], nr, yr, 1.0, tau, a32, scale)
+        there = ids[r] >= 0
+        t = vals[r][there].astype(np.float64) / tau
+        norm = L.lse(t) if nr is None else nr
+        p, spread = np.exp(t - norm), (t.max() - t) if len(t) else t
+        # e^(t - t_max), its sum and the factor in front of it
+        p_err = U * (4 * spread.max(initial=0.0) + 16 + 2 * (abs(t.max(initial=norm) - norm) if nr is not None else len(t)))
+        D, ln_err = reach(z[r], tau)
+        D1, ln_err1 = reach(z[r], 1.0)
+        gap = np.abs(t - norm) + np.abs(z[r][ids[r][there]] / tau - L.lse(z[r], tau))
+        tol = a32 * tau * tau * (p * (gap * p_err + ln_err)).sum()
+        tol += (1 - a32) * ln_err1 if yr >= 0 else 0.0
+        tol += 2 * U * abs(want) + 2.0 ** -40
+        assert abs(loss[r] - want) <= tol, (r, loss[r], want, tol)
+        if g is None:
+            continue
+        mass = np.zeros(V)
+        np.add.at(mass, ids[r][there], p)
+        size = a32 * tau * (p.sum() * L.softmax(z[r], tau) * (ln_err + p_err + U * (4 * D + 32)) + mass * (p_err + 8 * U))
+        if yr >= 0 and a32 < 1:
+            size += (1 - a32) * L.softmax(z[r]) * (ln_err1 + U * (8 * D1 + 32))
+            size[yr] += 8 * U
+        bound = scale * size + half * np.abs(gr) * (1 + 2.0 ** -9) + 1e-37
+        bad = ~(np.abs(g[r] - gr) <= bound)
+        assert not bad.any(), (r, np.nonzero(bad)[0][:5], g[r][bad][:5], gr[bad][:5], bound[bad][:5])
+        if nr is None and alpha == 1.0 and dtype == "fp32":  # what the list takes off is what the row adds
+            assert abs(g[r].sum()) <= scale * 2 * tau * (ln_err + p_err + 64 * U), g[r].sum()
+
+
 # ---- rows far from zero -----------------------------------------------------------------------------------------------
 def far_rows(rows, V, at, step, seed):
     """Logits around `at` in whole steps, which the type holds there."""
@@ -81,3 +124,26 @@ def test_distill_gradients_of_rows_far_from_zero(rows, V, dtype, at, step):
             assert not bad.any(), (tau, alpha, r, np.nonzero(bad)[0][:5], got[r][bad][:5], g[bad][:5], bound[bad][:5])
             if alpha == 1.0 and dtype == "fp32":
                 assert abs(got[r].sum()) <= 2 * tau * (err + p_err + 64 * U)
+
+
+@pytest.mark.parametrize("dtype,at,step", FAR)
+@pytest.mark.parametrize("rows,V", [(3, 1203), (2, 20011)])
+@pytest.mark.parametrize("grad", [True, False])
+def test_distill_losses_of_rows_far_from_zero(rows, V, grad, dtype, at, step):
+    """Students' and teachers' rows, each as far from zero as it likes: the losses do not change."""
+    z = far_rows(rows, V, at, step, V)
+    for teacher_at in (0.0, 2.0 ** 12, -2.0 ** 17):
+        ids, vals, y = far_lists(rows, V, 9, teacher_at, 0.125, 1)
+        for tau, alpha in ((1.0, 0.5), (1.5, 1.0), (2.0, 0.5), (0.7, 0.0)):
+            check_distill(z, ids, vals, y, dtype, tau, alpha, grad=grad)
+            n = np.float32(np.float64(vals.max(1)) / np.float32(tau) + 0.75)
+            check_distill(z, ids, vals, y, dtype, tau, alpha, n, grad=grad)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_distill_a_list_of_far_logits_at_the_lowest_temperature(dtype):
+    """Logits of 4096 over 0.001: a list's probabilities hang on differences, not on what they are taken from."""
+    z = far_rows(2, 1203, 0.0, 0.5, 3)
+    ids, vals, y = far_lists(2, 1203, 6, 4096.0, 2.0 ** -10, 4)
+    vals = (4096.0 + np.arange(6)[None] * 2.0 ** -10).repeat(2, 0).astype(np.float32)
+    check_distill(z, ids, vals, y, dtype, 1e-3, 1.0)
