@@ -2,7 +2,8 @@
 //   t_k = val_k / tau,  p_k = exp(t_k - n),  n = the teacher's ln sum_v exp(t_v) as given, or ln sum_k exp(t_k);  pi = sum_k p_k
 //   loss  = w (alpha tau^2 sum_k p_k (ln p_k - ln q_tau(id_k)) - (1 - alpha) ln q_1(y)),   q_tau = softmax(z / tau)
 //   dz[v] = w g (alpha tau (pi q_tau(v) - sum_{k: id_k = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
-// The sum over the list is pi (A / (tau S) + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (val_k - z_k):
+// The sum over the list is pi (A / (tau S) + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (val_k - z_k)
+// (of both their distances from a number near: neither lse_tau nor A / S is larger than what it says about the row):
 // a pass over the row needs a sum of exponentials only, and the listed words are read one by one.
 // A sum is taken relative to a reference; any will do that leaves it finite and far from 0.
 #pragma once
@@ -44,6 +45,8 @@ __host__ __device__ inline size_t distill_lds(int K) { return (size_t)(K + 1) * 
 // What a row's softmax is made of: sums of exponentials of z - shift at tau and at 1, relative to 2^power and 2^power1.
 struct RowSums {
   float shift, power, power1, s, s1;
+  // The logit that the sum at tau is relative to, as far as 32 bits go.
+  __device__ float pivot(float tau) const { return shift + power / (LOG2E / tau); }
 };
 
 // Exponentials of a row that are relative to whole powers of 2 (shift = 0).
@@ -124,11 +127,11 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
   return most;
 }
 
-// The list's sums S and A over this thread's entries.  (Differences of logits first: a list's probabilities do not hang on how
+// The list's sums S and A over this thread's entries (A: distances from the greatest logit and from the row's pivot).  (Differences of logits first: a list's probabilities do not hang on how
 // far from zero it lies.  A and S in 64 bits: the loss has A / S, a mean of differences of any size, and masked words may be on
 // the list, at the type's lowest value.)
 template <int THREADS>
-__device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, double &S, double &A) {
+__device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, float pivot, double &S, double &A) {
   for (int e = threadIdx.x; e < K; e += THREADS) {
     const DistillEntry d = ent[e];
     if (d.val == -INFINITY) continue;  // absent, or a probability of zero: no term
@@ -136,7 +139,7 @@ __device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, floa
     ent[e].p = p;
     if (p == 0.0f) continue;
     S += (double)p;
-    A += (double)p * ((double)d.val - (double)d.z);
+    A += (double)p * (((double)d.val - (double)most) - ((double)d.z - (double)pivot));
   }
 }
 
@@ -153,14 +156,15 @@ struct DistillList {
 
 // The list's sums (the barrier in between also publishes the waves' sums of the row): all threads take part.
 template <typename T, int THREADS>
-__device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, DistillEntry *ent, DistillShared<THREADS / 64> &sh) {
+__device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, float pivot, DistillEntry *ent,
+                                           DistillShared<THREADS / 64> &sh) {
   constexpr int WAVES = THREADS / 64;
   DistillList l;
   l.most = waves_max<WAVES>(sh.t);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double S = 0.0, A = 0.0;
   if (wave * 64 < a.K) {
-    distill_list_sums<THREADS>(ent, a.K, LOG2E / a.tau, l.most, S, A);
+    distill_list_sums<THREADS>(ent, a.K, LOG2E / a.tau, l.most, pivot, S, A);
     S = wave_sum(S);
     A = wave_sum(A);
   }
@@ -193,8 +197,9 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
         S += S_of_wave[i];
         A += A_of_wave[i];
       }
-      const double n = a.lse ? (double)a.lse[m] : (double)l.most / tau + log(S);
-      const double ln_sum = (double)r.shift + ((double)r.power + log2((double)r.s)) / (double)(LOG2E / a.tau);  // times tau
+      const double c = (double)(LOG2E / a.tau);
+      const double ln_sum = ((double)r.shift + (double)r.power / c - (double)r.pivot(a.tau)) + log2((double)r.s) / c;  // times tau
+      const double n = a.lse ? (double)a.lse[m] - (double)l.most / tau : log(S);  // both from the pivot and the greatest logit
       loss = (double)a.alpha * tau * tau * (double)l.pi * ((A / S + ln_sum) / tau - n);
     }
     if (hard) {
@@ -308,7 +313,7 @@ __device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float 
     sh.s[wave] = s;
     sh.s1[wave] = s1;
   }
-  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);  // (a barrier)
+  const DistillList l = distill_list<T, THREADS>(a, m, r.pivot(a.tau), ent, sh);  // (a barrier)
   r.s = waves_sum<WAVES>(sh.s);
   if (MODE != DISTILL_ONE) r.s1 = waves_sum<WAVES>(sh.s1);
   if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.S, sh.A, WAVES);
@@ -382,16 +387,20 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
     __syncthreads();
     return distill_by_memory<T, THREADS, MODE, 1, false>(a, m, w, row, zt, te, ent, sh);
   }
-  const DistillList l = distill_list<T, THREADS>(a, m, ent, sh);
-  auto join = [&](const float *power, const float *of_wave, float &top) {
-    top = waves_max<WAVES>(power);
-    if (top == -INFINITY) top = 0.0f;
-    const int i = tid & (WAVES - 1);
-    return group_reduce<WAVES>(of_wave[i] * exp2_32(power[i] - top), [](float x, float y) { return x + y; });
-  };
   RowSums r = {};
+  const float most = waves_max<WAVES>(sh.m);
+  r.power = most == -INFINITY ? 0.0f : most;
+  const DistillList l = distill_list<T, THREADS>(a, m, r.pivot(a.tau), ent, sh);
+  const int of = tid & (WAVES - 1);
+  auto join = [&](const float *power, const float *of_wave, float top) {
+    return group_reduce<WAVES>(of_wave[of] * exp2_32(power[of] - top), [](float x, float y) { return x + y; });
+  };
   r.s = join(sh.m, sh.s, r.power);
-  if (MODE != DISTILL_ONE) r.s1 = join(sh.m1, sh.s1, r.power1);
+  if (MODE != DISTILL_ONE) {
+    const float most1 = waves_max<WAVES>(sh.m1);
+    r.power1 = most1 == -INFINITY ? 0.0f : most1;
+    r.s1 = join(sh.m1, sh.s1, r.power1);
+  }
   const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
   const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
   T *drow = a.dz + m * a.ldd;

@@ -38,8 +38,9 @@ def reach(z, tau):
     return D, SUM + U * (L.softmax(z, tau) * (4 * D + 16)).sum()
 
 
-def check_distill(z, ids, vals, y, dtype, tau, alpha, n=None, scale=2.0 ** -13, grad=True):
-    """One call over the rows z against the oracle.  n: the teacher's lse [rows] (fp32 values) or None."""
+def check_distill(z, ids, vals, y, dtype, tau, alpha, n=None, scale=2.0 ** -13, grad=True, at=0.0, teacher_at=0.0):
+    """One call over the rows z against the oracle.  n: the teacher's lse [rows] (fp32 values) or None.  at, teacher_at: what the
+    rows and the lists (n = None) have in common, which changes nothing and which the oracle does without (far enough from zero its 64 bits hold no difference of logits either)."""
     rows, V = z.shape
     tau = float(np.float32(tau))
     d = rows_of(z, dtype)
@@ -49,12 +50,13 @@ def check_distill(z, ids, vals, y, dtype, tau, alpha, n=None, scale=2.0 ** -13, 
     g = out.double().cpu().numpy() if grad else None
     half = torch.finfo(DTYPES[dtype]).eps / 2
     a32 = float(np.float32(alpha))
+    z, vals = z - at, vals.astype(np.float64) - teacher_at
     for r in range(rows):
         yr = -1 if y is None else int(y[r])
         nr = None if n is None else float(np.float32(n[r]))
         want, gr = L.distill(z[r], ids[r], vals[r], nr, yr, 1.0, tau, a32, scale)
         there = ids[r] >= 0
-        t = vals[r][there].astype(np.float64) / tau
+        t = vals[r][there] / tau
         norm = L.lse(t) if nr is None else nr
         p, spread = np.exp(t - norm), (t.max() - t) if len(t) else t
         # e^(t - t_max), its sum and the factor in front of it
@@ -147,3 +149,20 @@ def test_distill_a_list_of_far_logits_at_the_lowest_temperature(dtype):
     ids, vals, y = far_lists(2, 1203, 6, 4096.0, 2.0 ** -10, 4)
     vals = (4096.0 + np.arange(6)[None] * 2.0 ** -10).repeat(2, 0).astype(np.float32)
     check_distill(z, ids, vals, y, dtype, 1e-3, 1.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [9, 1203, 20011])
+@pytest.mark.parametrize("at", [-2.0 ** 40, 2.0 ** 60, -2.0 ** 127])
+def test_distill_losses_of_rows_beyond_64_bits(at, V, dtype):
+    """Half a row is masked, the others are equal: the losses hang on how many there are, whatever they are."""
+    z = np.full((2, V), at)
+    z[:, V // 2 + 1:] = -np.inf
+    ids, y = np.array([[0, 1, V // 2], [1, 0, V // 2]]), np.array([1, V // 2])
+    for teacher_at in (0.0, at):
+        vals = np.full((2, 3), teacher_at, np.float32)
+        vals[1, 0] = -np.inf
+        ids[1, 0] = -1
+        for tau, alpha in ((1.0, 0.5), (1.5, 1.0), (2.0, 0.5), (0.7, 0.0)):
+            for grad in (True, False):
+                check_distill(z, ids, vals, y, dtype, tau, alpha, grad=grad, at=at, teacher_at=teacher_at)
