@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
   s = wave_sum(s);
   if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
   const float sum = s + s1;
-  const bool again = !(sum - sum == 0.0f) || (wave * 64 < full && !(near_power(ref, ex.c) && near_power(ref, LOG2E)));
+  const bool holds = wave == 0 || wave * 64 < full;  // (the first wave: also a row of less than a slot)
+  const bool again = !(sum - sum == 0.0f) || (holds && !(near_power(ref, ex.c) && near_power(ref, LOG2E)));
   if (lane == 0) {
     sh.m[wave] = s == 0.0f ? -INFINITY : -ex.b;
     sh.m1[wave] = s1 == 0.0f ? -INFINITY : ex.power1();

@@ -166,3 +166,32 @@ def test_distill_losses_of_rows_beyond_64_bits(at, V, dtype):
         for tau, alpha in ((1.0, 0.5), (1.5, 1.0), (2.0, 0.5), (0.7, 0.0)):
             for grad in (True, False):
                 check_distill(z, ids, vals, y, dtype, tau, alpha, grad=grad, at=at, teacher_at=teacher_at)
+
+
+# ---- rows of fewer words than a load holds ----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 9])
+@pytest.mark.parametrize("at", [-2.0 ** 23, -2.0 ** 40, -2.0 ** 127, 2.0 ** 23])
+def test_distill_of_a_few_words_far_from_zero(at, V, dtype):
+    z = np.full((3, V), at)
+    z[1] += np.arange(V) % 2 * (2.0 ** 16 if dtype == "bf16" else 1.0) if abs(at) == 2.0 ** 23 else 0.0  # (whole steps of the type)
+    z[2, V // 2:] = z[2].max()
+    ids, vals, y = np.arange(2)[None].repeat(3, 0) % V, np.array([[0.0, 1.0]] * 3, np.float32), np.array([0, V - 1, -1])
+    for tau, alpha in ((1.0, 0.5), (2.0, 0.5), (4.0, 0.25), (2.0, 1.0)):
+        for grad in (True, False):
+            check_distill(z, ids, vals, y, dtype, tau, alpha, grad=grad, at=at)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 3, 7])
+def test_distill_of_a_few_words_at_the_lowest_temperature(V, dtype):
+    """-2^13 / 0.001 is beyond the references' range: every word has 1 / V (the loss at tau is tested with the rows far from zero)."""
+    z = torch.full((2, V), -(2.0 ** 13), dtype=DTYPES[dtype], device="cuda")
+    out = torch.empty_like(z)
+    ids = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    loss = binding.rnnlm_distill_loss(z, ids, torch.zeros(2, 1, device="cuda"), tau=1e-3, dlogits=out)
+    tau = float(np.float32(1e-3))
+    want = np.full(V, tau / V)
+    want[0] -= tau
+    assert np.abs(out.double().cpu().numpy() - want).max() <= tau * (2.0 ** -9 if dtype == "bf16" else 64 * U)
+    assert bool(torch.isfinite(loss).all())
