@@ -101,12 +101,29 @@ __device__ inline void keep_packed(slot_t &s) { asm volatile("" : "+v"(s)); }
 // Makes the compiler work a value out by here.
 __device__ inline void keep_here(float &v) { asm volatile("" : "+v"(v)); }
 
-// The greatest of three numbers (NaNs lose).  (fmaxf of values from memory costs an instruction more for each of them, which
-// makes signalling NaNs quiet: two and a half instructions for two elements instead of one.)
+// The greatest of three numbers.  Quiet NaNs lose; a signalling one makes a quiet NaN of its maximum with the number in front of
+// it, which is lost then: wherever that matters the elements go through without_nans first.  (fmaxf of values from memory costs
+// an instruction more for each of them, which makes signalling NaNs quiet: two and a half instructions for two elements instead
+// of one.)
 __device__ inline float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
+}
+// -inf in place of a slot's NaNs.
+template <typename T>
+__device__ inline void without_nans(slot_t &s) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned w = s[i];
+    if constexpr (sizeof(T) == 4) {
+      w = (w & 0x7fffffffu) > 0x7f800000u ? 0xff800000u : w;
+    } else {
+      w = (w & 0x7fffu) > 0x7f80u ? (w & 0xffff0000u) | 0xff80u : w;
+      w = (w & 0x7fff0000u) > 0x7f800000u ? (w & 0xffffu) | 0xff800000u : w;
+    }
+    s[i] = w;
+  }
 }
 // The greatest of m and the elements of a slot.
 template <typename T>

@@ -2,7 +2,7 @@
 // A row, or a chunk of a long one, fits a workgroup's registers, so it is read once, which is what bounds calls of many rows (2560
 // of 64000 bf16 words, K = 64: 66 us, 4.9 TB/s); few rows are bound by the steps' latency.  A word is ranked by one 64-bit key, the
 // logit's bits in an order that integers have, above the complement of the id: keys differ, so the order is total and a result
-// does not depend on which wave arrives first.  (A NaN ranks with the masked words, -inf; -0 ranks with +0.)
+// does not depend on which wave arrives first.  (A NaN of either kind ranks with the masked words, -inf; -0 ranks with +0.)
 //   1. maxima of groups of elements (one group a thread or several), sum of exponentials of the chunk
 //   2. a threshold that at least K of the maxima reach, so at least K elements do: bisection over the maxima by one wave
 //   3. elements that reach it into LDS: of G groups without structure some G ln(G / (G - K)), so several a thread where one
@@ -190,10 +190,7 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
   // rest arrives.
   const float c = LOG2E / a.tau, ref = wave_max(slot_max<T>(zt, raw[0])), b = -whole_power(ref, c);
   float top[NV], part[PARTS], s = exp2_32(fmaf(zt, c, b));
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) part[i] = i == 0 ? max3(zt, -INFINITY, -INFINITY) : -INFINITY;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
+  auto maxima = [&](int i) {
     if constexpr (NV < 4) {  // groups of a slot's quarters
       float of_slot[4];
 #pragma unroll
@@ -205,22 +202,41 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
       top[i] = slot_max<T>(-INFINITY, raw[i]);
       part[i % PARTS] = max3(part[i % PARTS], top[i], -INFINITY);
     }
+  };
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) part[i] = i == 0 ? max3(zt, -INFINITY, -INFINITY) : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    maxima(i);
 #pragma unroll
     for (int e = 0; e < N; ++e) s += exp2_32(fmaf(slot_elem<T>(raw[i], e), c, b));
     keep_packed(raw[i]);
     keep_here(s);  // (with the exponentials of many slots put off the kernel spilled 100 registers)
   }
-  float all = part[0];
-#pragma unroll
-  for (int i = 1; i < PARTS; ++i) all = max3(all, part[i], -INFINITY);
-  const float mine = wave_max(all);
   const bool fine = 4 * K > min(slots, THREADS);
-  group[tid] = logit_order(fine ? part[0] : all);
-  if (fine)
+  auto groups = [&] {
+    float all = part[0];
 #pragma unroll
-    for (int i = 1; i < PARTS; ++i) group[i * THREADS + tid] = logit_order(part[i]);
+    for (int i = 1; i < PARTS; ++i) all = max3(all, part[i], -INFINITY);
+    group[tid] = logit_order(fine ? part[0] : all);
+    if (fine)
+#pragma unroll
+      for (int i = 1; i < PARTS; ++i) group[i * THREADS + tid] = logit_order(part[i]);
+    return wave_max(all);
+  };
+  float mine = groups();
   s = wave_sum(s);
   double power = -(double)b;
+  if (s != s) {  // NaNs: they rank as masked words, and the maxima once more without them
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) part[i] = i == 0 ? max3(zt, -INFINITY, -INFINITY) : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      without_nans<T>(raw[i]);
+      maxima(i);
+    }
+    mine = groups();
+  }
   if (!(s - s == 0.0f) || (!near_power(ref, c) && mine > -INFINITY)) {
     // no number, or the first slots are masked throughout: once more, relative to the wave's maximum
     const float base = mine == -INFINITY ? 0.0f : mine;

@@ -195,3 +195,37 @@ def test_distill_of_a_few_words_at_the_lowest_temperature(V, dtype):
     want[0] -= tau
     assert np.abs(out.double().cpu().numpy() - want).max() <= tau * (2.0 ** -9 if dtype == "bf16" else 64 * U)
     assert bool(torch.isfinite(loss).all())
+
+
+# ---- NaNs of either kind ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,K", [(7, 3), (300, 40), (2050, 256), (5000, 40), (20011, 256), (70001, 64), (150001, 200), (400003, 20)])
+def test_top_logits_of_rows_that_hold_signalling_nans(V, K, dtype):
+    """They rank as masked words do, wherever in a load they stand: behind the greatest words, in front of them, or anywhere."""
+    rng = np.random.default_rng(V)
+    z = rng.normal(0.0, 3.0, (4, V))
+    if dtype == "bf16":
+        z = torch.as_tensor(z).to(torch.bfloat16).double().numpy()
+    else:
+        z = z.astype(np.float32).astype(np.float64)
+    nan = rng.random((4, V)) < 0.02
+    great = np.argsort(-z, 1)[:, : K + 5]
+    for r, step in ((0, 1), (1, -1)):
+        nan[r, np.clip(great[r] + step, 0, V - 1)] = True
+        nan[r, great[r]] = False
+    nan[2] = rng.random(V) < 0.3
+    nan[3] = True
+    nan[3, great[3][:2]] = False  # fewer numbers than asked for
+    d = torch.as_tensor(z).to(DTYPES[dtype])
+    bits = d.view(torch.int32 if dtype == "fp32" else torch.int16).clone()
+    pos, neg = (0x7f800001, 0xff812345 - 2 ** 32) if dtype == "fp32" else (0x7f81, 0xff83 - 2 ** 16)
+    bits[torch.as_tensor(nan)] = pos
+    bits[torch.as_tensor(nan & (rng.random((4, V)) < 0.5))] = neg
+    d = bits.cuda().view(DTYPES[dtype])
+    ids, vals, lse = binding.rnnlm_top_logits(d, K)
+    assert torch.isnan(lse).tolist() == nan.any(1).tolist()
+    z[nan] = -np.inf
+    for r in range(4):
+        i, v, _ = L.top(z[r], K)
+        assert np.array_equal(ids[r].cpu().numpy(), i), (r, np.nonzero(ids[r].cpu().numpy() != i)[0][:5])
+        assert np.array_equal(vals[r].double().cpu().numpy(), v)
