@@ -11,7 +11,7 @@ namespace rnnlm_dev {
 constexpr long READ_ONCE_BYTES = 128L << 20;
 
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr double LOG2E_64 = 1.44269504088896340736, LN2_64 = 0.693147180559945309417;
+constexpr double LOG2E_64 = 1.44269504088896340736;
 
 // A row starts where the one before ends, at any element: its slots are read and written at the elements' alignment.
 typedef u32x4_t slot_t;

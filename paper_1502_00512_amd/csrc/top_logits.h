@@ -54,8 +54,11 @@ __device__ inline void top_store(const TopArgs &a, long row, int rank, unsigned 
   a.vals[row * a.K + rank] = order_logit((unsigned)(key >> 32));
 }
 
-// ln of the sum s relative to 2^ref.
-__device__ inline float row_lse(double ref, float s) { return s == 0.0f ? -INFINITY : (float)((ref + log2((double)s)) * LN2_64); }
+// ln of the sum s of 2^{z c} relative to 2^ref, at tau.  (c is log2 e / tau in 32 bits: by ln 2 the logarithm of a row far from zero
+// would be off by as much as c is, once more than its own rounding.)
+__device__ inline float row_lse(const TopArgs &a, double ref, float s) {
+  return s == 0.0f ? -INFINITY : (float)((ref + log2((double)s)) / ((double)(LOG2E / a.tau) * (double)a.tau));
+}
 
 // The value of the lane whose number differs in the bits of X.
 template <int X>
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
       for (int e = 0; e < N; ++e) s += exp2_32((slot_elem<T>(q, e) - base) * c);
     }
     s = wave_sum(s);
-    power = (double)base * (LOG2E_64 / (double)a.tau);
+    power = (double)base * (double)c;
   }
   if (lane == 0) sh_ref[wave] = s == 0.0f ? -INFINITY : power;
   if (lane == 0) {
@@ -362,7 +365,7 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
     const float v = group_reduce<WAVES>(sh_s[lane & (WAVES - 1)] * power_between(q, top_ref), [](float x, float y) { return x + y; });
     if (lane == 0) {
       if (a.chunks > 1) a.stat[blockIdx.x] = make_double2(top_ref, (double)v);
-      else if (a.lse) a.lse[row] = row_lse(top_ref, v);
+      else if (a.lse) a.lse[row] = row_lse(a, top_ref, v);
     }
   }
 }
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(TOP_MERGE_THREADS) top_merge_kernel(const TopA
     }
     const double top_ref = wave_reduce(ref, [](double x, double y) { return fmax(x, y); });
     s = wave_sum(s * power_between(ref, top_ref));
-    if (threadIdx.x == 0) a.lse[row] = row_lse(top_ref, s);
+    if (threadIdx.x == 0) a.lse[row] = row_lse(a, top_ref, s);
   }
 }
 

@@ -168,6 +168,21 @@ def test_distill_losses_of_rows_beyond_64_bits(at, V, dtype):
                 check_distill(z, ids, vals, y, dtype, tau, alpha, grad=grad, at=at, teacher_at=teacher_at)
 
 
+@pytest.mark.parametrize("dtype,at,step", FAR)
+@pytest.mark.parametrize("V", [5, 1203, 20011, 70001, 200003])
+def test_top_logits_sums_of_rows_far_from_zero(V, dtype, at, step):
+    """The logarithm of the sum is rounded once, at its own size."""
+    z = far_rows(2, V, at, step, V)
+    z[1, : V // 2] = -np.inf
+    d = cuda(z).to(DTYPES[dtype])
+    for tau in (1.0, 1.3, 1.5, 0.7, 3.5, 0.03, 150.0):
+        tau = float(np.float32(tau))
+        lse = binding.rnnlm_top_logits(d, 2, tau)[2].double().cpu().numpy()
+        for r in range(2):
+            want = L.lse(z[r], tau)
+            assert abs(lse[r] - want) <= U * abs(want) * (1 + 2.0 ** -8) + reach(z[r], tau)[1], (tau, r, lse[r], want)
+
+
 # ---- rows of fewer words than a load holds ----------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("V", [1, 2, 3, 7, 9])
