@@ -71,13 +71,11 @@ template <int MODE>
 struct DistillDense {
   float c, b, a, b1, a1, shift;
   __device__ DistillDense(const RowSums &r, float tau, float soft, float hard) : c(LOG2E / tau), shift(r.shift) {
-    if (MODE == DISTILL_SQUARE) {  // d = e (a + a1 e)
-      b = -r.power;
+    term(MODE == DISTILL_ONE ? soft + hard : soft, r.power, r.s, a, b);
+    if (MODE == DISTILL_SQUARE) {  // d = e (a + a1 e), the sum of squares in the same units
       b1 = 0.0f;
-      a = r.s == 0.0f ? 0.0f : soft / r.s;
-      a1 = r.s1 == 0.0f ? 0.0f : hard / r.s1;
+      a1 = r.s1 == 0.0f ? 0.0f : hard / ldexpf(r.s1, 2 * (int)(b + r.power));
     } else {
-      term(MODE == DISTILL_ONE ? soft + hard : soft, r.power, r.s, a, b);
       term(hard, r.power1, r.s1, a1, b1);
     }
   }

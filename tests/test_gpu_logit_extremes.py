@@ -244,3 +244,19 @@ def test_top_logits_of_rows_that_hold_signalling_nans(V, K, dtype):
         i, v, _ = L.top(z[r], K)
         assert np.array_equal(ids[r].cpu().numpy(), i), (r, np.nonzero(ids[r].cpu().numpy() != i)[0][:5])
         assert np.array_equal(vals[r].double().cpu().numpy(), v)
+
+
+# ---- sums near the end of the range -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(2, 5008), (1030, 1008), (2, 70008)])
+def test_distill_of_a_row_whose_great_words_come_late(rows, V, dtype):
+    """The first words are 60 below the last ones: at tau = 2 sums of exponentials and of their squares relative to the first are
+    some 2^45 and 2^88, and the gradient of the labels a quotient by them, at a small factor."""
+    z = np.zeros((rows, V))
+    z[:, V - 3:] = 60.0
+    ids, vals = np.stack([[V - 1, 5, V - 2]] * rows), np.array([[1.0, 0.5, 0.25]] * rows, np.float32)
+    y = np.full(rows, V - 3)
+    for tau, alpha in ((2.0, 0.5), (2.0, 0.0), (1.0, 0.5), (1.5, 0.5)):
+        check_distill(z[:3], ids[:3], vals[:3], y[:3], dtype, tau, alpha, scale=2.0 ** -60)
+        if rows > 3:
+            check_distill(z, ids, vals, y, dtype, tau, alpha, scale=2.0 ** -60)
