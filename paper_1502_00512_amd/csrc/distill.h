@@ -46,7 +46,7 @@ __host__ __device__ inline size_t distill_lds(int K) { return (size_t)(K + 1) * 
 struct RowSums {
   float shift, power, power1, s, s1;
   // The logit that the sum at tau is relative to, as far as 32 bits go.
-  __device__ float pivot(float tau) const { return shift + power / (LOG2E / tau); }
+  __device__ float pivot(float tau) const { return shift + power * (tau / LOG2E); }
 };
 
 // Exponentials of a row that are relative to whole powers of 2 (shift = 0).
@@ -126,17 +126,16 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
 }
 
 // The list's sums S and A over this thread's entries (A: distances from the greatest logit and from the row's pivot).  (Differences of logits first: a list's probabilities do not hang on how
-// far from zero it lies.  A and S in 64 bits: the loss has A / S, a mean of differences of any size, and masked words may be on
-// the list, at the type's lowest value.)
+// far from zero it lies.  A in 64 bits: masked words may be on the list, at the type's lowest value.)
 template <int THREADS>
-__device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, float pivot, double &S, double &A) {
+__device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, float pivot, float &S, double &A) {
   for (int e = threadIdx.x; e < K; e += THREADS) {
     const DistillEntry d = ent[e];
     if (d.val == -INFINITY) continue;  // absent, or a probability of zero: no term
     const float p = exp2_32((d.val - most) * c);
     ent[e].p = p;
     if (p == 0.0f) continue;
-    S += (double)p;
+    S += p;
     A += (double)p * (((double)d.val - (double)most) - ((double)d.z - (double)pivot));
   }
 }
@@ -144,8 +143,8 @@ __device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, floa
 // Sums over the workgroup's waves, by way of LDS.
 template <int WAVES>
 struct DistillShared {
-  float m[WAVES], m1[WAVES], t[WAVES], s[WAVES], s1[WAVES], again[WAVES];
-  double S[WAVES], A[WAVES];
+  float m[WAVES], m1[WAVES], t[WAVES], s[WAVES], s1[WAVES], S[WAVES], again[WAVES];
+  double A[WAVES];
 };
 
 struct DistillList {
@@ -160,7 +159,8 @@ __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, floa
   DistillList l;
   l.most = waves_max<WAVES>(sh.t);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  double S = 0.0, A = 0.0;
+  float S = 0.0f;
+  double A = 0.0;
   if (wave * 64 < a.K) {
     distill_list_sums<THREADS>(ent, a.K, LOG2E / a.tau, l.most, pivot, S, A);
     S = wave_sum(S);
@@ -171,7 +171,7 @@ __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, floa
     sh.A[wave] = A;
   }
   __syncthreads();
-  l.S = (float)waves_sum<WAVES>(sh.S);
+  l.S = waves_sum<WAVES>(sh.S);
   // (a NaN in the list stays one)
   l.factor = l.S == 0.0f ? 0.0f : a.lse ? exp2_32((float)(((double)l.most * a.inv_tau - (double)a.lse[m]) * LOG2E_64)) : 1.0f / l.S;
   l.pi = l.S == 0.0f ? 0.0f : a.lse ? l.factor * l.S : l.S / l.S;
@@ -182,7 +182,7 @@ __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, floa
 // units of a logit by the factor that was used for it (c in 32 bits is not log2 e / tau).
 template <typename T, int MODE>
 __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, const RowSums &r, const DistillList &l,
-                                    const DistillEntry &label, const double *S_of_wave, const double *A_of_wave, int waves) {
+                                    const DistillEntry &label, const double *A_of_wave, int waves) {
   const bool hard = label.id >= 0;
   double loss = 0.0;
   if (r.s == 0.0f) {  // no word left
@@ -190,15 +190,12 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
   } else {
     const double tau = a.tau;
     if (a.alpha > 0.0f && l.pi != 0.0f) {
-      double S = 0.0, A = 0.0;
-      for (int i = 0; i < waves; ++i) {
-        S += S_of_wave[i];
-        A += A_of_wave[i];
-      }
+      double A = 0.0;
+      for (int i = 0; i < waves; ++i) A += A_of_wave[i];
       const double c = (double)(LOG2E / a.tau);
       const double ln_sum = ((double)r.shift + (double)r.power / c - (double)r.pivot(a.tau)) + log2((double)r.s) / c;  // times tau
-      const double n = a.lse ? (double)a.lse[m] - (double)l.most / tau : log(S);  // both from the pivot and the greatest logit
-      loss = (double)a.alpha * tau * tau * (double)l.pi * ((A / S + ln_sum) / tau - n);
+      const double n = a.lse ? (double)a.lse[m] - (double)l.most / tau : log((double)l.S);  // both from the pivot and the greatest logit
+      loss = (double)a.alpha * tau * tau * (double)l.pi * ((A / (double)l.S + ln_sum) / tau - n);
     }
     if (hard) {
       const double sum = MODE == DISTILL_ONE ? (double)r.power + log2((double)r.s) : (double)r.power1 + log2((double)r.s1);
@@ -314,7 +311,7 @@ __device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float 
   const DistillList l = distill_list<T, THREADS>(a, m, r.pivot(a.tau), ent, sh);  // (a barrier)
   r.s = waves_sum<WAVES>(sh.s);
   if (MODE != DISTILL_ONE) r.s1 = waves_sum<WAVES>(sh.s1);
-  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.S, sh.A, WAVES);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
   if (!a.dz) return;
   const float coef = w * a.scale * a.alpha * a.tau, hard = ent[a.K].id >= 0 ? w * a.scale * (1.0f - a.alpha) : 0.0f;
   const DistillDense<MODE> dense(r, a.tau, coef * l.pi, hard);
@@ -414,7 +411,7 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
     }
   }
   if (full * N + tid < a.V) drow[full * N + tid] = from_f32<T>(dense.template at<true>(zt));
-  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.S, sh.A, WAVES);
+  if (tid == 0) distill_loss<T, MODE>(a, m, w, r, l, ent[a.K], sh.A, WAVES);
   __syncthreads();  // the dense pass first, then the listed words on top of it
   distill_listed<T, THREADS, MODE>(a, dense, coef * l.factor, hard, ent, drow);
 }

@@ -184,17 +184,17 @@ __device__ inline X wave_reduce(X v, Op &&op) {
   return op(op(lane_value(v, 0), lane_value(v, 16)), op(lane_value(v, 32), lane_value(v, 48)));
 }
 // The same over WAVES numbers of LDS (a power of two, one a wave of the workgroup), for every lane.
-template <int WAVES, typename X, class Op>
-__device__ inline X waves_reduce(const X *of_wave, Op &&op) {
+template <int WAVES, class Op>
+__device__ inline float waves_reduce(const float *of_wave, Op &&op) {
   return group_reduce<WAVES>(of_wave[threadIdx.x & (WAVES - 1)], op);
 }
 template <int WAVES>
 __device__ inline float waves_max(const float *of_wave) {
   return waves_reduce<WAVES>(of_wave, [](float a, float b) { return fmaxf(a, b); });
 }
-template <int WAVES, typename X>
-__device__ inline X waves_sum(const X *of_wave) {
-  return waves_reduce<WAVES>(of_wave, [](X a, X b) { return a + b; });
+template <int WAVES>
+__device__ inline float waves_sum(const float *of_wave) {
+  return waves_reduce<WAVES>(of_wave, [](float a, float b) { return a + b; });
 }
 // Sums of the lanes up to each one: within sixteen lanes, then the rows of sixteen in front.
 template <typename X>
