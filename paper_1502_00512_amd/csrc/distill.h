@@ -334,8 +334,8 @@ __device__ inline void distill_by_memory(const DistillArgs<T> &a, long m, float 
 // (K = 100, tau = 2) 700 us (4.7; a copy of 2 GiB 4.9).  2560 of 10000 (K = 32, alpha = 1) 20.4 us (5.0).  fp32, 900 of 33278
 // (K = 37, tau = 1.5) 46.7 us (5.1).
 // The sums run while the row arrives: a wave's reference is near the greatest element of its first slots, so a later element of
-// it can only overflow by being e^88 times greater, and the sum cannot vanish.  Where a sum is no number after all, or a wave's
-// first slots are masked throughout (or beyond the references' range), the row goes by way of memory.
+// it can only make it too large by being e^69 times greater, and the sum cannot vanish.  Where that happens, a sum is no number, or a
+// wave's first slots are masked throughout (or beyond the references' range), the row goes by way of memory.
 template <typename T, int THREADS, int NV, int MODE>
 __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillArgs<T> a) {
   constexpr int N = SlotOf<T>::N, WAVES = THREADS / 64;
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(THREADS, 4) distill_row_kernel(const DistillAr
   if (MODE != DISTILL_ONE) s1 = wave_sum(s1);
   const float sum = s + s1;
   const bool holds = wave == 0 || wave * 64 < full;  // (the first wave: also a row of less than a slot)
-  const bool again = !(sum - sum == 0.0f) || (holds && !(near_power(ref, ex.c) && near_power(ref, LOG2E)));
+  const bool again = !joinable(sum) || (holds && !(near_power(ref, ex.c) && near_power(ref, LOG2E)));
   if (lane == 0) {
     sh.m[wave] = s == 0.0f ? -INFINITY : -ex.b;
     sh.m1[wave] = s1 == 0.0f ? -INFINITY : ex.power1();

@@ -139,6 +139,9 @@ __device__ inline float exp2_32(float x) { return __builtin_amdgcn_exp2f(x); }
 // from one to another by exact factors.  Logits whose power is beyond 2^22 (and masked ones) have none.
 __device__ inline bool near_power(float m, float c) { return fabsf(m * c) < 4194304.0f; }
 __device__ inline float whole_power(float m, float c) { return near_power(m, c) ? rintf(m * c) : 0.0f; }
+// Sums that are formed relative to a wave's first elements may be this large: those of all waves and chunks of a row stay in range
+// together, and so does what they are joined by.  (No: also where they are no numbers.)
+__device__ inline bool joinable(float sum) { return sum < 0x1p100f; }
 // 2^(from - to); 0 from -inf.
 __device__ inline float power_between(double from, double to) { return from == -INFINITY ? 0.0f : exp2_32((float)(from - to)); }
 

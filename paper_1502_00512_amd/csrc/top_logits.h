@@ -240,8 +240,8 @@ __global__ void __launch_bounds__(THREADS, 4) top_chunk_kernel(const TopArgs a) 
     }
     mine = groups();
   }
-  if (!(s - s == 0.0f) || (!near_power(ref, c) && mine > -INFINITY)) {
-    // no number, or the first slots are masked throughout: once more, relative to the wave's maximum
+  if (!joinable(s) || (!near_power(ref, c) && mine > -INFINITY)) {
+    // no number or too great a one, or the first slots are masked throughout: once more, relative to the wave's maximum
     const float base = mine == -INFINITY ? 0.0f : mine;
     s = exp2_32((zt - base) * c);
     for (int j = tid; j < slots; j += THREADS) {

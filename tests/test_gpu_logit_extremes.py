@@ -260,3 +260,28 @@ def test_distill_of_a_row_whose_great_words_come_late(rows, V, dtype):
         check_distill(z[:3], ids[:3], vals[:3], y[:3], dtype, tau, alpha, scale=2.0 ** -60)
         if rows > 3:
             check_distill(z, ids, vals, y, dtype, tau, alpha, scale=2.0 ** -60)
+
+
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("slots", [512, 2560, 8192, 16384, 25600])
+def test_sums_of_waves_that_are_in_range_and_their_sum_is_not(slots, dtype):
+    """Two words of 87.5 for every wave of a workgroup, behind its first loads: 2^127.2 a wave, more than the type holds together."""
+    n = 4 if dtype == "fp32" else 8
+    for threads in (256, 512, 1024):
+        if slots < 2 * threads:
+            continue
+        z = np.zeros((2, slots * n))
+        for wave in range(threads // 64):
+            first = (threads + wave * 64) * n
+            z[:, first: first + 2] = 87.5
+        ids, vals, y = np.array([[3, threads * n]] * 2), np.array([[0.0, 1.0]] * 2, np.float32), np.array([threads * n + 1, 0])
+        for tau, alpha in ((1.0, 0.5), (1.0, 1.0)):
+            check_distill(z, ids, vals, y, dtype, tau, alpha)
+        z2 = 2.0 * z  # (tau = 2: the same exponentials, their squares out of range)
+        check_distill(z2, ids, vals, y, dtype, 2.0, 1.0)
+        for rows, tau in ((z, 1.0), (z2, 2.0)):
+            lse = binding.rnnlm_top_logits(rows_of(rows, dtype), 5, tau)[2].double().cpu().numpy()
+            want = 87.5 + np.log(threads // 32)
+            assert np.abs(lse - want).max() <= U * want + SUM, (threads, lse, want)
