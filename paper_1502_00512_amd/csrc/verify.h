@@ -62,8 +62,8 @@ __device__ inline int draft_length(const VerifyArgs &a, int b) {
 // e^{(z - m) / tau} of a row in 64 bits, up to a factor that the row has in common: 2^x, x = z c + b = n + f with |f| <= 1/2,
 // and the polynomial of degree 9 that meets 2^f at the ten Chebyshev nodes of [-1/2, 1/2]: 1.8e-14 relative off at most, so a
 // hundred thousand such terms place a step of their sum to about 1e-14.  (b = -m c is rounded: the common factor.)  n is what
-// adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer addition.  Logits more than 690 tau below
-// the maximum, and masked ones, give 0.  Where m c passes 2^50 only logits equal to the maximum are as near: e = 1.  No NaNs:
+// adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer addition, which holds down to -1022.  Logits
+// more than some 690 tau (never 700) below the maximum, and masked ones, give 0.  Where m c passes 2^50 only logits equal to the maximum are as near: e = 1.  No NaNs:
 // the caller knows the row.
 struct Exp64 {
   double c, b;
@@ -74,6 +74,7 @@ struct Exp64 {
     b = -(double)m * c;
     if (fabs(b) > 1125899906842624.0) c = b = 0.0;
     least = m - 690.0f * tau;
+    if ((double)m - (double)least > 700.0 * (double)tau) least = nextafterf(least, m);  // (a step of m's size may be many tau)
   }
   __device__ double operator()(float z) const {
     constexpr double SHIFT = 6755399441055744.0;

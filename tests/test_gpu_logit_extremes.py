@@ -285,3 +285,26 @@ def test_sums_of_waves_that_are_in_range_and_their_sum_is_not(slots, dtype):
             lse = binding.rnnlm_top_logits(rows_of(rows, dtype), 5, tau)[2].double().cpu().numpy()
             want = 87.5 + np.log(threads // 32)
             assert np.abs(lse - want).max() <= U * want + SUM, (threads, lse, want)
+
+
+# ---- verification at temperatures far below a step of the logits ------------------------------------------------------
+@pytest.mark.parametrize("V", [5, 1001, 20011, 100003])
+@pytest.mark.parametrize("at", [1.5 * 2.0 ** 23, -1.5 * 2.0 ** 23, 1.5 * 2.0 ** 22, 2.0 ** 20, 1000.0])
+def test_verify_where_a_step_of_the_type_is_many_temperatures(at, V):
+    """tau = 0.001 and fp32 logits whose neighbours lie 1, 0.5, 0.125, 2^-14 apart: a step is hundreds of tau, or none."""
+    rng = np.random.default_rng(V)
+    step = float(np.spacing(np.float32(abs(at))))
+    K, B = 2, 4
+    target = at - step * rng.integers(0, 4, (K + 1, B, V))
+    target[:, :, rng.integers(0, V, 3)] = at
+    draft = target[:K] - step * (rng.random((K, B, V)) < 0.5)
+    draft[:, :, 0] = at
+    drafts = np.array([[rng.choice(np.nonzero(draft[i, b] == at)[0]) for b in range(B)] for i in range(K)])
+    u = rng.random((K + 1, B)).astype(np.float32)
+    tau = float(np.float32(1e-3))
+    for q in (draft, None):
+        n, tokens = binding.rnnlm_verify_drafts(rows_of(target, "fp32"), cuda(drafts, np.int32), cuda(u), None if q is None else rows_of(q, "fp32"),
+                                                None, tau, tau)
+        for b in range(B):
+            want = L.verify(target[:, b], drafts[:, b], u[:, b], None if q is None else q[:, b], None, tau, tau)
+            assert int(n[b]) == want[0] and tokens[:, b].tolist() == want[1].tolist(), (b, int(n[b]), tokens[:, b], want)
