@@ -390,19 +390,23 @@ class Rnnlm:
     # -- the calls of the C ABI, same names ----------------------------------------------------
     def rnnlm_stream_chunk(self, tok, k: int, T: int, x=None, y=None, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_stream_chunk", stream, self.device.index, self.rnnlm_stream_chunk, tok, k, T, x, y)
         if x is None:
             x = torch.empty(T, self.B, dtype=torch.int32, device=self.device)
             y = torch.empty(T, self.B, dtype=torch.int32, device=self.device)
-        _ok(self.lib.rnnlm_stream_chunk(self.handle, _ptr(tok), tok.numel(), k, T, _ptr(x), _ptr(y), _stream(stream)),
+        _ok(self.lib.rnnlm_stream_chunk(self.handle, _ptr(tok), tok.numel(), k, T, _ptr(x), _ptr(y), _stream(None)),
             "rnnlm_stream_chunk")
         return x, y
 
     def rnnlm_forward_logprob(self, x, y, logp=None, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_forward_logprob", stream, self.device.index, self.rnnlm_forward_logprob, x, y, logp)
         T = x.shape[0]
         if logp is None:
             logp = torch.empty(T, self.B, dtype=torch.float32, device=self.device)
-        _ok(self.lib.rnnlm_forward_logprob(self.handle, _ptr(x), _ptr(y), T, _ptr(logp), _stream(stream)),
+        _ok(self.lib.rnnlm_forward_logprob(self.handle, _ptr(x), _ptr(y), T, _ptr(logp), _stream(None)),
             "rnnlm_forward_logprob")
         return logp
 
@@ -412,26 +416,32 @@ class Rnnlm:
 
     def rnnlm_grad_chunk(self, x, y, want_logp=True, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_grad_chunk", stream, self.device.index, self.rnnlm_grad_chunk, x, y, want_logp)
         z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
         dE, dU, dWo, db = z(self.V, self.H), z(self.H, self.H), z(self.V, self.H), z(self.V)
         logp = z(x.shape[0], self.B) if want_logp else None
         _ok(self.lib.rnnlm_grad_chunk(self.handle, _ptr(x), _ptr(y), x.shape[0], _ptr(dE), _ptr(dU), _ptr(dWo),
-                                      _ptr(db), _ptr(logp), _stream(stream)), "rnnlm_grad_chunk")
+                                      _ptr(db), _ptr(logp), _stream(None)), "rnnlm_grad_chunk")
         return dict(gE=dE, gU=dU, gWo=dWo, gb=db, logp=logp)
 
     def rnnlm_grad_chunk_compressed(self, x, y, want_logp=True, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_grad_chunk_compressed", stream, self.device.index, self.rnnlm_grad_chunk_compressed, x, y, want_logp)
         z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
         dE, dA, dU, dC, db = z(self.V, self.P), z(self.H, self.P), z(self.H, self.H), z(self.P, self.H), z(self.V)
         logp = z(x.shape[0], self.B) if want_logp else None
         _ok(self.lib.rnnlm_grad_chunk_compressed(self.handle, _ptr(x), _ptr(y), x.shape[0], _ptr(dE), _ptr(dA),
-                                                 _ptr(dU), _ptr(dC), _ptr(db), _ptr(logp), _stream(stream)),
+                                                 _ptr(dU), _ptr(dC), _ptr(db), _ptr(logp), _stream(None)),
             "rnnlm_grad_chunk_compressed")
         return dict(gE=dE, gA=dA, gU=dU, gC=dC, gb=db, logp=logp)
 
     def rnnlm_quantize_weights(self, stream=None):
         """Returns dict name -> (codes int8 tensor, scale float tensor); the model then runs on the quantised values."""
         import torch
+        if stream is not None:
+            return _on("rnnlm_quantize_weights", stream, self.device.index, self.rnnlm_quantize_weights)
         out = {}
         ptrs = []
         for name, W in (("E", self.E), ("A", self.A), ("U", self.U), ("C", self.C)):
@@ -440,7 +450,7 @@ class Rnnlm:
             out[name] = (q, s)
             ptrs += [q.data_ptr(), s.data_ptr()]
         qs = rnnlm_quantized(*ptrs)
-        _ok(self.lib.rnnlm_quantize_weights(self.handle, C.byref(qs), _stream(stream)), "rnnlm_quantize_weights")
+        _ok(self.lib.rnnlm_quantize_weights(self.handle, C.byref(qs), _stream(None)), "rnnlm_quantize_weights")
         return out
 
     def rnnlm_perplexity(self, tok, T: int, stream=None):
@@ -467,20 +477,24 @@ class Rnnlm:
 
     def rnnlm_forward_score(self, x, y, lnZ: float = 0.0, score=None, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_forward_score", stream, self.device.index, self.rnnlm_forward_score, x, y, lnZ, score)
         T = x.shape[0]
         if score is None:
             score = torch.empty(T, self.B, dtype=torch.float32, device=self.device)
-        _ok(self.lib.rnnlm_forward_score(self.handle, _ptr(x), _ptr(y), T, lnZ, _ptr(score), _stream(stream)),
+        _ok(self.lib.rnnlm_forward_score(self.handle, _ptr(x), _ptr(y), T, lnZ, _ptr(score), _stream(None)),
             "rnnlm_forward_score")
         return score
 
     def rnnlm_forward_score_shortlist(self, x, cand, lnZ: float = 0.0, score=None, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_forward_score_shortlist", stream, self.device.index, self.rnnlm_forward_score_shortlist, x, cand, lnZ, score)
         T, C_ = x.shape[0], cand.shape[2]
         if score is None:
             score = torch.empty(T, self.B, C_, dtype=torch.float32, device=self.device)
         _ok(self.lib.rnnlm_forward_score_shortlist(self.handle, _ptr(x), _ptr(cand), C_, T, lnZ, _ptr(score),
-                                                   _stream(stream)), "rnnlm_forward_score_shortlist")
+                                                   _stream(None)), "rnnlm_forward_score_shortlist")
         return score
 
     def rnnlm_nce_train_chunk(self, x, y, noise, lnq, lnZ: float, lr: float, J=None, sum_J=None, stream=None):
@@ -490,12 +504,14 @@ class Rnnlm:
 
     def rnnlm_nce_grad_chunk(self, x, y, noise, lnq, lnZ: float, want_J=True, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_nce_grad_chunk", stream, self.device.index, self.rnnlm_nce_grad_chunk, x, y, noise, lnq, lnZ, want_J)
         z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)
         dE, dU, dWo, db = z(self.V, self.H), z(self.H, self.H), z(self.V, self.H), z(self.V)
         J = z(x.shape[0], self.B) if want_J else None
         _ok(self.lib.rnnlm_nce_grad_chunk(self.handle, _ptr(x), _ptr(y), x.shape[0], _ptr(noise), noise.numel(),
                                           _ptr(lnq), lnZ, _ptr(dE), _ptr(dU), _ptr(dWo), _ptr(db), _ptr(J),
-                                          _stream(stream)), "rnnlm_nce_grad_chunk")
+                                          _stream(None)), "rnnlm_nce_grad_chunk")
         return dict(gE=dE, gU=dU, gWo=dWo, gb=db, J=J)
 
     # -- windows whose logits are the caller's -----------------------------------------------------
@@ -613,11 +629,13 @@ class Rnnlm:
 
     def rnnlm_sort_segments(self, x, stream=None):
         import torch
+        if stream is not None:
+            return _on("rnnlm_sort_segments", stream, self.device.index, self.rnnlm_sort_segments, x)
         M = x.numel()
         perm = torch.empty(M, dtype=torch.int32, device=self.device)
         seg = torch.empty(M + 1, dtype=torch.int32, device=self.device)
         nseg = torch.zeros(1, dtype=torch.int32, device=self.device)
         _ok(self.lib.rnnlm_sort_segments(self.handle, _ptr(x), x.shape[0], _ptr(perm), _ptr(seg), _ptr(nseg),
-                                         _stream(stream)), "rnnlm_sort_segments")
+                                         _stream(None)), "rnnlm_sort_segments")
         n = int(nseg.item())
         return perm, seg[:n + 1]

@@ -1,4 +1,4 @@
-"""Calls on logits that are given a stream which is not the current one: everything they allocate themselves is this stream's.
+"""Calls that are given a stream which is not the current one: everything they allocate themselves is this stream's.
 (Memory of the current stream's pool could still be in use there when the call's kernels start, and scratch that is dropped with
 the call would be given away there while they run.)"""
 import numpy as np
@@ -57,7 +57,7 @@ def test_operators_on_rows(allocations):
 
 @pytest.mark.parametrize("precision", [FP32, BF16])
 @pytest.mark.parametrize("P", [0, 32])
-def test_windows(P, precision, allocations):
+def test_windows_with_rows_of_logits(P, precision, allocations):
     V, H, B, T, K = 5003, 64, 6, 4, 7
     if P:
         E, A, U, C_, b = synth.make_compressed_weights(V, H, P, "uniform", 0.3, 1)
@@ -93,3 +93,37 @@ def test_windows(P, precision, allocations):
     given_a_stream(fresh(lambda s: g.rnnlm_distill_grad_chunk(x, y, ids, vals, alpha=0.5, stream=s).values()), allocations)
     given_a_stream(fresh(train), allocations)
     g.rnnlm_check()
+
+
+@pytest.mark.parametrize("precision", [FP32, BF16])
+def test_windows_whose_outputs_the_binding_allocates(precision, allocations):
+    V, H, B, T, K, P = 5003, 64, 6, 4, 32, 32
+    E, U, Wo, b = synth.make_weights(V, H, "uniform", 0.3, 1)
+    g = binding.Rnnlm(E, U, Wo, b, B, T, precision, K_max=K)
+    E, A, U, C_, b = synth.make_compressed_weights(V, H, P, "uniform", 0.3, 1)
+    c = binding.Rnnlm(E, U, None, b, B, T, precision, A=A, C_=C_)
+    rng = np.random.default_rng(2)
+    cuda = lambda a, t: torch.as_tensor(a.astype(t)).cuda()  # noqa: E731
+    x, y = (cuda(rng.integers(0, V, (T, B)), np.int32) for _ in range(2))
+    noise, lnq = cuda(rng.integers(0, V, K), np.int32), torch.full((V,), -float(np.log(V)), device="cuda")
+    cand, tok = cuda(rng.integers(0, V, (T, B, 5)), np.int32), cuda(rng.integers(0, V, 2 * T * B + B), np.int32)
+
+    def from_the_start(call):
+        def run(s):
+            g.rnnlm_reset_state()
+            c.rnnlm_reset_state()
+            if s is not None:
+                s.wait_stream(torch.cuda.current_stream())
+            out = call(s)
+            out = out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else [out]
+            return [t for o in out for t in (o if isinstance(o, tuple) else [o])]
+        return run
+
+    for call in (lambda s: g.rnnlm_stream_chunk(tok, 0, T, stream=s), lambda s: g.rnnlm_forward_logprob(x, y, stream=s),
+                 lambda s: g.rnnlm_grad_chunk(x, y, stream=s), lambda s: c.rnnlm_grad_chunk_compressed(x, y, stream=s),
+                 lambda s: g.rnnlm_forward_score(x, y, stream=s), lambda s: g.rnnlm_forward_score_shortlist(x, cand, stream=s),
+                 lambda s: g.rnnlm_nce_grad_chunk(x, y, noise, lnq, 0.0, stream=s), lambda s: g.rnnlm_sort_segments(x, stream=s),
+                 lambda s: c.rnnlm_quantize_weights(stream=s)):
+        given_a_stream(from_the_start(call), allocations)
+    g.rnnlm_check()
+    c.rnnlm_check()

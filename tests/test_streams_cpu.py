@@ -1,4 +1,4 @@
-"""The stream that a call on logits is given: no GPU is needed for what is refused."""
+"""The stream that a call is given: no GPU is needed for what is refused."""
 from types import SimpleNamespace
 
 import pytest
