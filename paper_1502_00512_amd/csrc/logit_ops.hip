@@ -53,10 +53,14 @@ struct TopPlan {
 // A workgroup holds THREADS x NV slots of a row.  The measured calls: bf16, K = 64 unless said.
 // Up to 4096 slots 256 threads, with as few slots each as hold the row.  Up to 10240 one workgroup of 512, no second launch: 64000
 // words, 1 row 9.4 us against 12.5 in chunks, 256 rows 14.0 and 20.3, 2560 rows 66 and 76.  Up to 20480 one of 1024, where the rows
-// are no more than the compute units or the lists long: 100000 words, K = 200, 1 row 16.2 against 23.6, 256 rows 21.7 and 38.5,
-// 2560 rows 178 and 212; K = 16, 256 rows 17.9 and 19.7, but 1 to 64 rows 12.5 to 13.8 and 12.5, 512 rows 32.8 and 28.6, 2560 rows
-// 142 and 95 (one such workgroup on a compute unit: nothing runs while it waits).  Else chunks, halved while the workgroups are
-// fewer than the compute units: 64 rows of 100000 words 16.9 us so, 18.7 halved up to 512 workgroups.
+// are no more than the compute units or the lists long.  100000 words, that and chunks: K = 200, 1 row 16.2 and 23.6, 256 rows 21.7
+// and 38.5, 2560 rows 178 and 212; K = 64, 1 row 11.7 and 14.5, 256 rows 17.6 and 25.4; K = 16, 128 rows 14.9 and 15.9, 256 rows
+// 18.0 and 19.9, but 512 rows 32.8 and 28.6, 2560 rows 142 and 95 (one such workgroup on a compute unit: nothing runs while it
+// waits).  Short lists of few rows pay for it: K = 16, 1 to 64 rows 12.6 to 14.1 and 12.3 to 12.5, K = 3 15.2 to 15.8 and 12.3
+// to 12.7 (50000 fp32 words, K = 3 and 16, do not: 10.0 to 13.3 and 12.0 to 16.2).  (The widest of these kernels keeps 10 (fp32)
+// or 13 (bf16) registers of a thread in scratch.)
+// Else chunks of 4096 slots.  Half or a quarter as many, until the workgroups are as many as the compute units, gain nothing: 4 rows of
+// 200000 words 16.1 us and 16.3 whole, of 400000 words (K = 16) 15.6 and 12.9, one of 1000000 (K = 3) 16.3 and 13.2.
 TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   const int slots = slots_of(V, dtype);
   TopPlan p;
@@ -71,8 +75,6 @@ TopPlan top_plan(int64_t rows, int32_t V, int32_t K, int32_t dtype) {
   } else if (slots <= TOP_WIDEST * 20 && (rows <= 256 || K > TOP_COUNTED)) {
     p.threads = TOP_WIDEST;
     if (slots > TOP_WIDEST * 16) p.nv = 20;
-  } else {
-    while (p.nv > 4 && rows * chunks() < 256 && 2 * chunks() * K <= TOP_CAP) p.nv /= 2;
   }
   p.chunks = chunks();
   p.per = (slots + p.chunks - 1) / p.chunks;
