@@ -278,8 +278,8 @@ int rnnlm_sort_segments_static(const int32_t *x, int32_t T, int32_t B, int32_t V
  * A row holds the V logits of one position; rows lie ld elements apart (ld >= V, any alignment of their element type) and
  * are ordered like a window's positions (row t*B + s).  All rows, lists and outputs are device arrays.  The calls allocate
  * nothing, run on the CURRENT device, which must be the stream's, keep nothing between calls, and may be captured into a
- * graph; calls that overlap in time need workspaces of their own.  V <= 2^20; at most 2^22 - 64
- * rows; tau in [0.001, 1000]. */
+ * graph; calls that overlap in time need workspaces of their own.  Outputs and workspaces overlap neither inputs nor one
+ * another, except where a call says so.  V <= 2^20; at most 2^22 - 64 rows; tau in [0.001, 1000]. */
 typedef enum { RNNLM_DTYPE_FP32 = 0, RNNLM_DTYPE_BF16 = 1 } rnnlm_dtype;
 
 /* The K greatest logits of every row in descending order (equal ones: the lower id first) and lse = ln sum_v exp(z[v]/tau)

@@ -2,9 +2,9 @@
 //   t_k = val_k / tau,  p_k = exp(t_k - n),  n = the teacher's ln sum_v exp(t_v) as given, or ln sum_k exp(t_k);  pi = sum_k p_k
 //   loss  = w (alpha tau^2 sum_k p_k (ln p_k - ln q_tau(id_k)) - (1 - alpha) ln q_1(y)),   q_tau = softmax(z / tau)
 //   dz[v] = w g (alpha tau (pi q_tau(v) - sum_{k: id_k = v} p_k) + (1 - alpha) (q_1(v) - [v = y]))
-// The sum over the list is pi (A / (tau S) + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (val_k - z_k)
-// (of both their distances from a number near: neither lse_tau nor A / S is larger than what it says about the row):
-// a pass over the row needs a sum of exponentials only, and the listed words are read one by one.
+// The sum over the list is pi (A / (tau S) + lse_tau - n) with S = sum_k e^{t_k - t_max}, A = sum_k e^{t_k - t_max} (val_k - z_k): a
+// pass over the row needs a sum of exponentials only, and the listed words are read one by one.  (Logits are taken as distances, the
+// list's from its greatest one, the row's from its pivot, lse_tau and n as well: what is added up is no larger than the spread.)
 // A sum is taken relative to a reference; any will do that leaves it finite and far from 0.
 #pragma once
 #include "rows.h"
@@ -66,7 +66,8 @@ struct DistillExp {
 // The dense part of a row's gradient: pi g alpha tau q_tau(v) + g (1 - alpha) q_1(v).  Exponents stay whole powers away from z c
 // (the sum's own whole power is taken off, too: sums may be as large as fp32 goes), and what is left of the factors is multiplied:
 // with the factors' logarithms in the exponent, -power + log2(a / s) was rounded at the power's size and a row's gradient off
-// by 2e-4 at logits of 10^4.  (The multiplication costs nothing: 2560 rows of 64000 bf16 words 120.6 us and 120.3.)
+// by 2e-4 at logits of 10^4.  (Multiplied and in the exponent: 2560 rows of 64000 bf16 words 120.6 us and 120.3; of 10000, which
+// the memory-side cache holds, 21.9 and 21.2.)
 template <int MODE>
 struct DistillDense {
   float c, b, a, b1, a1, shift;
@@ -125,8 +126,8 @@ __device__ inline float distill_entries(const DistillArgs<T> &a, long m, const T
   return most;
 }
 
-// The list's sums S and A over this thread's entries (A: distances from the greatest logit and from the row's pivot).  (Differences of logits first: a list's probabilities do not hang on how
-// far from zero it lies.  A in 64 bits: masked words may be on the list, at the type's lowest value.)
+// The list's sums S and A over this thread's entries.  (Differences of logits first: neither a list's probabilities nor A hang on how
+// far from zero list and row lie.  A in 64 bits: masked words may be on the list, at the type's lowest value.)
 template <int THREADS>
 __device__ inline void distill_list_sums(DistillEntry *ent, int K, float c, float most, float pivot, float &S, double &A) {
   for (int e = threadIdx.x; e < K; e += THREADS) {
@@ -178,8 +179,8 @@ __device__ inline DistillList distill_list(const DistillArgs<T> &a, long m, floa
   return l;
 }
 
-// The row's loss, by one thread.  In 64 bits: it is a difference of numbers that may be any times its size, so each goes back to
-// units of a logit by the factor that was used for it (c in 32 bits is not log2 e / tau).
+// The row's loss, by one thread, in 64 bits.  Logarithms go back to units of a logit by the factor their sums were formed with
+// (c in 32 bits is not log2 e / tau), and are distances from the row's pivot and the list's greatest logit, as A is.
 template <typename T, int MODE>
 __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, const RowSums &r, const DistillList &l,
                                     const DistillEntry &label, const double *A_of_wave, int waves) {
@@ -194,7 +195,7 @@ __device__ inline void distill_loss(const DistillArgs<T> &a, long m, float w, co
       for (int i = 0; i < waves; ++i) A += A_of_wave[i];
       const double c = (double)(LOG2E / a.tau);
       const double ln_sum = ((double)r.shift + (double)r.power / c - (double)r.pivot(a.tau)) + log2((double)r.s) / c;  // times tau
-      const double n = a.lse ? (double)a.lse[m] - (double)l.most / tau : log((double)l.S);  // both from the pivot and the greatest logit
+      const double n = a.lse ? (double)a.lse[m] - (double)l.most / tau : log((double)l.S);
       loss = (double)a.alpha * tau * tau * (double)l.pi * ((A / (double)l.S + ln_sum) / tau - n);
     }
     if (hard) {

@@ -275,6 +275,7 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
     return RNNLM_ERR_ARG;
   const size_t es = elem_bytes(dtype);
   const bool once = read_once(rows, V, dtype);
+  const double inv_tau = 1.0 / (double)tau;
   if (dlogits) {
     if (!rows_ok(dlogits, dtype, rows, V, ld_dlogits)) return RNNLM_ERR_ARG;
     // in place row by row, or apart
@@ -288,11 +289,11 @@ int rnnlm_distill_loss(const void *logits, int32_t dtype, int64_t rows, int32_t 
     int rc;
     if (dtype == RNNLM_DTYPE_FP32) {
       rc = distill_call(DistillArgs<float>{static_cast<const float *>(logits), ld, static_cast<float *>(dlogits), ld_dlogits, ids, y,
-                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, 1.0 / (double)tau},
+                                           vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, inv_tau},
                         rows, st);
     } else {
       rc = distill_call(DistillArgs<bf16_t>{static_cast<const bf16_t *>(logits), ld, static_cast<bf16_t *>(dlogits), ld_dlogits,
-                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, 1.0 / (double)tau},
+                                            ids, y, vals, lse, weight, loss, range_flag, tau, alpha, scale, V, K, once, inv_tau},
                         rows, st);
     }
     if (rc) return rc;

@@ -62,9 +62,9 @@ __device__ inline int draft_length(const VerifyArgs &a, int b) {
 // e^{(z - m) / tau} of a row in 64 bits, up to a factor that the row has in common: 2^x, x = z c + b = n + f with |f| <= 1/2,
 // and the polynomial of degree 9 that meets 2^f at the ten Chebyshev nodes of [-1/2, 1/2]: 1.8e-14 relative off at most, so a
 // hundred thousand such terms place a step of their sum to about 1e-14.  (b = -m c is rounded: the common factor.)  n is what
-// adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer addition, which holds down to -1022.  Logits
-// more than some 690 tau (never 700) below the maximum, and masked ones, give 0.  Where m c passes 2^50 only logits equal to the maximum are as near: e = 1.  No NaNs:
-// the caller knows the row.
+// adding 1.5 * 2^52 leaves in the low word; 2^n goes into the exponent by an integer addition, which holds down to n = -1022.
+// Logits more than some 690 tau (never 700) below the maximum, and masked ones, give 0.  Where m c passes 2^50 only logits equal to
+// the maximum are as near: e = 1.  No NaNs: the caller knows the row.
 struct Exp64 {
   double c, b;
   float least;
