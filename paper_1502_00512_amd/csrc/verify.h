@@ -4,7 +4,8 @@
 //   the word after them is drawn from r = max(p_n - q_n, 0) (all of the text's drafts accepted, or r = 0: r = p_n): the first
 //   v with sum_{j <= v} r_j > u_K sum_j r_j
 // Which step of a sum over the vocabulary a random number falls on depends on every term: 100000 terms of 32 bits leave the
-// step open once in some hundred words, so the drawn word's row is summed in 64 bits with exponentials to 1e-14.  The
+// step open once in some hundred words, so the drawn word's row is summed in 64 bits with exponentials to 1e-14 (where p and q are
+// not equal and yet agree to that altogether, r is rounding: a draft from q is rejected there once in 1e13).  The
 // acceptance of a draft compares two probabilities and gets by with 32-bit sums.
 //   1. maximum and sum of exponentials of every row that can matter, by parts of a row (HBM-bound; all the bytes are here)
 //   2. how many drafts are accepted
