@@ -331,6 +331,49 @@ int rnnlm_verify_drafts(const void *target, int64_t ld_target, const void *draft
                         float tau_draft, int32_t *accepted, int32_t *tokens, int32_t *range_flag, void *workspace,
                         size_t workspace_bytes, void *stream);
 
+/* ---- Adapting ---------------------------------------------------------------------------------------------
+ * Operators that adapt a trained model: the policy and preference criteria with their gradients, on rows of logits, and
+ * low-rank adapters beside a shared projection.  What is said above of logits, streams, devices, graphs, workspaces and overlap
+ * holds here, too.
+ *
+ * Clipped policy loss: words y that the model drew from softmax(z/tau) (some steps ago) and how good they were.  Per row, with
+ * l = ln softmax(z/tau)(y), rho = exp(l - old_logp), d = ref_logp - l, A = advantage:
+ *     loss = weight * (-min(rho A, clamp(rho, 1 - clip_low, 1 + clip_high) A) + beta (exp(d) - d - 1))
+ *     dlogits[v] = scale * weight * g ([v = y] - softmax(z/tau)(v)) / tau,   g = beta (1 - exp(d)) - [not clipped] rho A
+ * (clipped: the second term of the minimum is the smaller one).  Nothing is clamped but rho.  old_logp NULL: the words come from
+ * this very model, rho = 1 with the gradient of the logarithm.  Positions with a negative y or of weight 0 do not count: loss and
+ * logp 0, a gradient of zeros whatever their row holds; y >= V counts as negative and raises *range_flag.  A word that its row
+ * masks (-inf) has logp = -inf, the loss of the formula (+inf where beta > 0), and a gradient of zeros for its row.
+ * y: dev int32[rows]; old_logp, ref_logp, advantage, weight: dev float[rows]; ref_logp may be NULL where beta = 0, weight NULL:
+ * all 1; 0 <= clip_low <= 1, clip_high >= 0, beta >= 0; loss: dev float[rows]; logp: dev float[rows] = l, or NULL; sum_loss,
+ * dlogits, ld_dlogits, scale, range_flag: as in rnnlm_distill_loss. */
+int rnnlm_policy_loss(const void *logits, int32_t dtype, int64_t rows, int32_t V, int64_t ld, const int32_t *y,
+                      const float *old_logp, const float *ref_logp, const float *advantage, const float *weight, float tau,
+                      float clip_low, float clip_high, float beta, float scale, float *loss, float *logp, double *sum_loss,
+                      void *dlogits, int64_t ld_dlogits, int32_t *range_flag, void *stream);
+
+/* Preference loss of `pairs` pairs of texts in [T][2 pairs] rows: the text of stream s < pairs is preferred to that of stream
+ * pairs + s.  S_s = sum_t ln softmax(z)(y) over the positions of stream s with y >= 0 (mean = 1: their mean; no such position:
+ * 0), r = (S_s - ref[s]) - (S_{pairs+s} - ref[pairs+s]):
+ *     RNNLM_PREFERENCE_LOGISTIC  loss = weight * (-(1 - smoothing) ln sigma(beta r) - smoothing ln sigma(-beta r))
+ *     RNNLM_PREFERENCE_SQUARED   loss = weight * (r - 1 / (2 beta))^2
+ *     RNNLM_PREFERENCE_HINGE     loss = weight * max(0, 1 - beta r)
+ *     dlogits[v] of a position = scale * weight * (d loss / d r) * (+1 preferred, -1 other) * (1 / their number, if mean)
+ *                                * ([v = y] - softmax(z)(v))
+ * Positions with a negative y (prompts, padding) and pairs of weight 0 have a gradient of zeros whatever their rows hold (the
+ * texts of such a pair count as empty); y >= V counts as negative and raises *range_flag.  A word that its row masks makes its
+ * text's sum -inf (and r infinite or no number); that row's gradient is zero.
+ * y: dev int32[T][2 pairs]; ref: dev float[2 pairs], a reference's sums (or means), or NULL: 0; weight: dev float[pairs] or NULL;
+ * beta > 0; 0 <= smoothing <= 0.5, 0 but for LOGISTIC; T >= 0; loss: dev float[pairs]; logp: dev float[2 pairs] = S, or NULL;
+ * sum_loss: of the pairs; dlogits, ld_dlogits, scale (1 / pairs for the mean), range_flag: as in rnnlm_distill_loss; workspace:
+ * 256-byte aligned, at least rnnlm_preference_workspace_bytes (0: sizes out of range). */
+typedef enum { RNNLM_PREFERENCE_LOGISTIC = 0, RNNLM_PREFERENCE_SQUARED = 1, RNNLM_PREFERENCE_HINGE = 2 } rnnlm_preference_kind;
+size_t rnnlm_preference_workspace_bytes(int32_t T, int32_t pairs);
+int rnnlm_preference_loss(const void *logits, int32_t dtype, int32_t T, int32_t pairs, int32_t V, int64_t ld, const int32_t *y,
+                          const float *ref, const float *weight, int32_t kind, float beta, float smoothing, int32_t mean, float scale,
+                          float *loss, float *logp, double *sum_loss, void *dlogits, int64_t ld_dlogits, int32_t *range_flag,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
 /* The operators above on a handle's own windows (both architectures).  Rows of logits are of the handle's compute type
  * (RNNLM_FP32: float, RNNLM_BF16_FP32MASTER: bf16), [T][B] rows ld elements apart, in the caller's memory.
  *

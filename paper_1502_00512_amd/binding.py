@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(HERE, "librnnlm_hip.so")
 RNNLM_FP32 = 0
 RNNLM_BF16_FP32MASTER = 1
 RNNLM_DTYPE_FP32, RNNLM_DTYPE_BF16 = 0, 1
+RNNLM_PREFERENCE_LOGISTIC, RNNLM_PREFERENCE_SQUARED, RNNLM_PREFERENCE_HINGE = 0, 1, 2
 RNNLM_EXCHANGE_AUTO, RNNLM_EXCHANGE_CHIP_WIDE, RNNLM_EXCHANGE_XCD_LOCAL = 0, 1, 2
 
 SYMBOLS = [
@@ -30,8 +31,10 @@ SYMBOLS = [
     "rnnlm_top_logits_workspace_bytes", "rnnlm_top_logits", "rnnlm_distill_loss", "rnnlm_verify_workspace_bytes",
     "rnnlm_verify_drafts", "rnnlm_forward_logits", "rnnlm_distill_train_chunk", "rnnlm_distill_grad_chunk",
     "rnnlm_distill_grad_chunk_compressed", "rnnlm_verify_chunk",
+    "rnnlm_policy_loss", "rnnlm_preference_workspace_bytes", "rnnlm_preference_loss",
 ]
-SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes"]  # return bytes
+SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes",
+         "rnnlm_preference_workspace_bytes"]  # return bytes
 
 STAGES = ["prep", "rnn_fwd", "out_fwd", "stats", "softmax_grad", "out_bwd_h", "rnn_bwd", "out_bwd_w", "rec_w", "emb", "reduce",
           "nce_score", "nce_grad", "nce_bwd_h", "nce_bwd_w", "nce_update", "rmsprop", "proj"]
@@ -124,6 +127,10 @@ def load():
     lib.rnnlm_distill_grad_chunk.argtypes = [vp, vp, vp, i32, C.POINTER(rnnlm_distill), vp, vp, vp, vp, vp, vp]
     lib.rnnlm_distill_grad_chunk_compressed.argtypes = [vp, vp, vp, i32, C.POINTER(rnnlm_distill), vp, vp, vp, vp, vp, vp, vp]
     lib.rnnlm_verify_chunk.argtypes = [vp, vp, i32, C.POINTER(rnnlm_verify), vp, vp, vp]
+    lib.rnnlm_policy_loss.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, f32, vp, vp, vp, vp, i64, vp, vp]
+    lib.rnnlm_preference_workspace_bytes.argtypes = [i32, i32]
+    lib.rnnlm_preference_loss.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, vp, i32, f32, f32, i32, f32, vp, vp, vp, vp, i64, vp,
+                                          vp, C.c_size_t, vp]
     for name in SIZES:
         getattr(lib, name).restype = C.c_size_t
     lib.rnnlm_profile_enable.argtypes = [vp, C.c_uint32]
@@ -325,6 +332,73 @@ def rnnlm_verify_drafts(target, drafts, u, draft=None, lengths=None, tau: float 
                 _at(call, "u", u, torch.float32, rows, dev, B), tau, tau_draft, _at(call, "accepted", accepted, i32, B, dev),
                 _at(call, "tokens", tokens, i32, rows, dev, B), _at(call, "range_flag", range_flag, i32, 1, dev), at, nbytes), call)
     return accepted, tokens
+
+
+# -- operators that adapt a trained model ---------------------------------------------------------------------
+def _gradient_rows(call, logits, rows, ld, dlogits):
+    """(address, elements from row to row) of the rows that receive the gradient; (None, 0) of None."""
+    if dlogits is None:
+        return None, 0
+    if dlogits.shape != logits.shape:
+        _refuse(call, "dlogits: the logits' shape is wanted")
+    at, ldd = dlogits.data_ptr(), _rows(call, "dlogits", dlogits, logits)[2]
+    if at == logits.data_ptr() and rows <= 1:  # in place (one row has no distance to the next)
+        ldd = ld
+    return at, ldd
+
+
+def rnnlm_policy_loss(logits, y, advantage, old_logp=None, ref_logp=None, weight=None, tau: float = 1.0, clip_low: float = 0.2,
+                      clip_high: float = 0.2, beta: float = 0.0, scale: float = 1.0, loss=None, logp=None, dlogits=None,
+                      sum_loss=None, range_flag=None, stream=None):
+    """logits: float32 or bfloat16 [..., V]; y int32 [...]; advantage, old_logp, ref_logp, weight float32 [...] (old_logp None: drawn
+    from this model; weight None: 1).  Returns (loss, logp) float32 [...].  dlogits (a tensor like logits, or logits itself)
+    receives the gradient; sum_loss float64 [1]."""
+    import torch
+    call, f32, i32 = "rnnlm_policy_loss", torch.float32, torch.int32
+    rows, V, ld, dt = _rows(call, "logits", logits)
+    if stream is not None:
+        return _on(call, stream, logits.get_device(), rnnlm_policy_loss, logits, y, advantage, old_logp, ref_logp, weight, tau, clip_low,
+                   clip_high, beta, scale, loss, logp, dlogits, sum_loss, range_flag)
+    dev = logits.get_device()
+    loss = torch.empty(logits.shape[:-1], dtype=f32, device=logits.device) if loss is None else loss
+    logp = torch.empty(logits.shape[:-1], dtype=f32, device=logits.device) if logp is None else logp
+    dz, ldd = _gradient_rows(call, logits, rows, ld, dlogits)
+    _ok(_launch(dev, load().rnnlm_policy_loss, logits.data_ptr(), dt, rows, V, ld, _at(call, "y", y, i32, rows, dev),
+                _at(call, "old_logp", old_logp, f32, rows, dev), _at(call, "ref_logp", ref_logp, f32, rows, dev),
+                _at(call, "advantage", advantage, f32, rows, dev), _at(call, "weight", weight, f32, rows, dev), tau, clip_low, clip_high,
+                beta, scale, _at(call, "loss", loss, f32, rows, dev), _at(call, "logp", logp, f32, rows, dev),
+                _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd, _at(call, "range_flag", range_flag, i32, 1, dev)), call)
+    return loss, logp
+
+
+def rnnlm_preference_workspace_bytes(T: int, pairs: int) -> int:
+    return int(load().rnnlm_preference_workspace_bytes(T, pairs))
+
+
+def rnnlm_preference_loss(logits, y, ref=None, weight=None, kind: int = RNNLM_PREFERENCE_LOGISTIC, beta: float = 0.1,
+                          smoothing: float = 0.0, mean: bool = False, scale: float = 1.0, loss=None, logp=None, dlogits=None,
+                          workspace=None, sum_loss=None, range_flag=None, stream=None):
+    """logits: float32 or bfloat16 [T][2 P][V], the text of stream s < P preferred to that of stream P + s; y int32 [T][2 P], negative
+    where a position does not count; ref float32 [2 P] or None; weight float32 [P] or None.  Returns (loss [P], logp [2 P])."""
+    import torch
+    call, f32, i32 = "rnnlm_preference_loss", torch.float32, torch.int32
+    rows, V, ld, dt = _rows(call, "logits", logits)
+    if stream is not None:
+        return _on(call, stream, logits.get_device(), rnnlm_preference_loss, logits, y, ref, weight, kind, beta, smoothing, mean, scale,
+                   loss, logp, dlogits, workspace, sum_loss, range_flag)
+    if logits.dim() != 3 or logits.shape[1] < 2 or logits.shape[1] % 2:
+        _refuse(call, "logits: [T][2 pairs][V] is wanted")
+    T, P, dev = logits.shape[0], logits.shape[1] // 2, logits.get_device()
+    loss = torch.empty(P, dtype=f32, device=logits.device) if loss is None else loss
+    logp = torch.empty(2 * P, dtype=f32, device=logits.device) if logp is None else logp
+    dz, ldd = _gradient_rows(call, logits, rows, ld, dlogits)
+    at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_preference_workspace_bytes(T, P))
+    _ok(_launch(dev, load().rnnlm_preference_loss, logits.data_ptr(), dt, T, P, V, ld, _at(call, "y", y, i32, rows, dev, 2 * P),
+                _at(call, "ref", ref, f32, 2 * P, dev), _at(call, "weight", weight, f32, P, dev), kind, beta, smoothing, int(mean), scale,
+                _at(call, "loss", loss, f32, P, dev), _at(call, "logp", logp, f32, 2 * P, dev),
+                _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd, _at(call, "range_flag", range_flag, i32, 1, dev), at,
+                nbytes), call)
+    return loss, logp
 
 
 class Rnnlm:

@@ -9,7 +9,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librnnlm_hip.so")
-SOURCES = [os.path.join(CSRC, "rnnlm.hip"), os.path.join(CSRC, "logit_ops.hip")]
+SOURCES = [os.path.join(CSRC, "rnnlm.hip"), os.path.join(CSRC, "logit_ops.hip"),
+           os.path.join(CSRC, "adapt_ops.hip")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
 

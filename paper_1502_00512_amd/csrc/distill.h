@@ -7,6 +7,7 @@
 // list's from its greatest one, the row's from its pivot, lse_tau and n as well: what is added up is no larger than the spread.)
 // A sum is taken relative to a reference; any will do that leaves it finite and far from 0.
 #pragma once
+#include "losses.h"
 #include "rows.h"
 
 namespace rnnlm_dev {
@@ -430,20 +431,6 @@ __global__ void __launch_bounds__(THREADS) distill_stream_kernel(const DistillAr
   const float te = wave_max(distill_entries<T, THREADS>(a, m, row, ent)), zt = tail_elem(row, threadIdx.x, a.V);
   if (a.once && !a.dz) distill_by_memory<T, THREADS, MODE, 4, true>(a, m, w, row, zt, te, ent, sh);
   else distill_by_memory<T, THREADS, MODE, 4, false>(a, m, w, row, zt, te, ent, sh);
-}
-
-// Sum of n losses in 64 bits, in a fixed order, by one workgroup.
-__global__ void __launch_bounds__(1024) sum_losses_kernel(const float *__restrict__ loss, long n, double *__restrict__ out) {
-  __shared__ double sh[16];
-  double a = 0.0;
-  for (long i = threadIdx.x; i < n; i += 1024) a += (double)loss[i];
-  a = wave_sum(a);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = a;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) a += sh[i];
-    *out = a;
-  }
 }
 
 }  // namespace rnnlm_dev
