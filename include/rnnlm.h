@@ -374,6 +374,34 @@ int rnnlm_preference_loss(const void *logits, int32_t dtype, int32_t T, int32_t 
                           float *loss, float *logp, double *sum_loss, void *dlogits, int64_t ld_dlogits, int32_t *range_flag,
                           void *workspace, size_t workspace_bytes, void *stream);
 
+/* Low-rank adapters of many texts at once beside a shared projection (the output layer, above all): row m of x belongs to
+ * adapter i = ids[m], or to none (ids[m] < 0; ids[m] >= n as well, which raises *range_flag).
+ *     inner = down[i] x (R numbers),    out = base + scale[i] up[i] inner
+ * Rows of one adapter may stand anywhere; an adapter is read once for every 32 of its rows or so.  A row without an adapter has
+ * out = base and inner = 0.  Weights that are not finite spoil the rows of their own adapter only.
+ * x: dev [rows][K], ld_x apart; base: dev [rows][N] or NULL (zeros); out: dev [rows][N]: may be base (same ld), else it overlaps
+ * nothing; inner: dev float[rows][R], what the backward pass wants, or NULL; x, down, up, base and out are of dtype (bf16: sums
+ * in fp32, inner not rounded, out rounded once).  down: dev [n][R][K], up: dev [n][N][R], scale: dev float[n] or NULL (1).
+ * rows <= 2^17, K <= 65536, N <= 2^20, n <= 65536, 1 <= R <= 64; workspace: 256-byte aligned, at least
+ * rnnlm_adapter_workspace_bytes (backward: 0 or 1; 0 bytes: sizes out of range). */
+typedef struct {
+  const void *down, *up;
+  const float *scale;
+  int32_t n, R;
+} rnnlm_adapters;
+size_t rnnlm_adapter_workspace_bytes(int64_t rows, int32_t K, int32_t N, int32_t n, int32_t R, int32_t dtype, int32_t backward);
+int rnnlm_adapter_forward(const void *x, int64_t ld_x, int32_t dtype, int64_t rows, int32_t K, int32_t N, const rnnlm_adapters *a,
+                          const int32_t *ids, const void *base, int64_t ld_base, void *out, int64_t ld_out, float *inner,
+                          int32_t *range_flag, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradients, from those of out (the gradient of base is dout itself) and the inner of the forward pass:
+ *     dinner = scale[i] up[i]^T dout,   dup[i] = scale[i] sum_m dout inner^T,   ddown[i] = sum_m dinner x^T,   dx = down[i]^T dinner
+ * dout: dev [rows][N]; ddown: dev float[n][R][K] and dup: dev float[n][N][R], zero for adapters without rows; dx: dev [rows][K]
+ * of dtype, zero for rows without an adapter, or NULL.  Sums in fp32 in an order that hangs on the sizes and ids only. */
+int rnnlm_adapter_backward(const void *dout, int64_t ld_dout, const void *x, int64_t ld_x, const float *inner, int32_t dtype, int64_t rows,
+                           int32_t K, int32_t N, const rnnlm_adapters *a, const int32_t *ids, float *ddown, float *dup, void *dx,
+                           int64_t ld_dx, int32_t *range_flag, void *workspace, size_t workspace_bytes, void *stream);
+
 /* The operators above on a handle's own windows (both architectures).  Rows of logits are of the handle's compute type
  * (RNNLM_FP32: float, RNNLM_BF16_FP32MASTER: bf16), [T][B] rows ld elements apart, in the caller's memory.
  *

@@ -32,9 +32,10 @@ SYMBOLS = [
     "rnnlm_verify_drafts", "rnnlm_forward_logits", "rnnlm_distill_train_chunk", "rnnlm_distill_grad_chunk",
     "rnnlm_distill_grad_chunk_compressed", "rnnlm_verify_chunk",
     "rnnlm_policy_loss", "rnnlm_preference_workspace_bytes", "rnnlm_preference_loss",
+    "rnnlm_adapter_workspace_bytes", "rnnlm_adapter_forward", "rnnlm_adapter_backward",
 ]
 SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes",
-         "rnnlm_preference_workspace_bytes"]  # return bytes
+         "rnnlm_preference_workspace_bytes", "rnnlm_adapter_workspace_bytes"]  # return bytes
 
 STAGES = ["prep", "rnn_fwd", "out_fwd", "stats", "softmax_grad", "out_bwd_h", "rnn_bwd", "out_bwd_w", "rec_w", "emb", "reduce",
           "nce_score", "nce_grad", "nce_bwd_h", "nce_bwd_w", "nce_update", "rmsprop", "proj"]
@@ -70,6 +71,10 @@ class rnnlm_verify(C.Structure):
     _fields_ = [("draft", C.c_void_p), ("ld_draft", C.c_int64), ("lengths", C.c_void_p), ("u", C.c_void_p), ("tau", C.c_float),
                 ("tau_draft", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t)]
+
+
+class rnnlm_adapters(C.Structure):
+    _fields_ = [("down", C.c_void_p), ("up", C.c_void_p), ("scale", C.c_void_p), ("n", C.c_int32), ("R", C.c_int32)]
 
 
 class RnnlmError(RuntimeError):
@@ -131,6 +136,11 @@ def load():
     lib.rnnlm_preference_workspace_bytes.argtypes = [i32, i32]
     lib.rnnlm_preference_loss.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, vp, i32, f32, f32, i32, f32, vp, vp, vp, vp, i64, vp,
                                           vp, C.c_size_t, vp]
+    lib.rnnlm_adapter_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32]
+    lib.rnnlm_adapter_forward.argtypes = [vp, i64, i32, i64, i32, i32, C.POINTER(rnnlm_adapters), vp, vp, i64, vp, i64, vp, vp, vp,
+                                          C.c_size_t, vp]
+    lib.rnnlm_adapter_backward.argtypes = [vp, i64, vp, i64, vp, i32, i64, i32, i32, C.POINTER(rnnlm_adapters), vp, vp, vp, vp, i64, vp,
+                                           vp, C.c_size_t, vp]
     for name in SIZES:
         getattr(lib, name).restype = C.c_size_t
     lib.rnnlm_profile_enable.argtypes = [vp, C.c_uint32]
@@ -399,6 +409,74 @@ def rnnlm_preference_loss(logits, y, ref=None, weight=None, kind: int = RNNLM_PR
                 _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd, _at(call, "range_flag", range_flag, i32, 1, dev), at,
                 nbytes), call)
     return loss, logp
+
+
+def rnnlm_adapter_workspace_bytes(rows: int, K: int, N: int, n: int, R: int, dtype: int, backward: bool = False) -> int:
+    return int(load().rnnlm_adapter_workspace_bytes(rows, K, N, n, R, dtype, int(backward)))
+
+
+def _adapters(call, like, down, up, scale, K):
+    """The adapters' description, N."""
+    import torch
+    dev = like.get_device()
+    if down.dim() != 3 or up.dim() != 3 or down.shape[0] != up.shape[0] or down.shape[1] != up.shape[2] or down.shape[2] != K:
+        _refuse(call, f"down: [n][R][{K}] and up: [n][N][R] are wanted")
+    (n, R, _), N = down.shape, up.shape[1]
+    return rnnlm_adapters(_at(call, "down", down, like.dtype, n * R * K, dev), _at(call, "up", up, like.dtype, n * N * R, dev),
+                          _at(call, "scale", scale, torch.float32, n, dev), n, R), N
+
+
+def _beside(call, name, t, x, width):
+    """(address, elements from row to row) of rows of `width` beside the rows of x."""
+    if tuple(t.shape) != (*x.shape[:-1], width):
+        _refuse(call, f"{name}: a tensor of shape {(*x.shape[:-1], width)} is wanted")
+    return t.data_ptr(), _rows(call, name, t, x)[2]
+
+
+def rnnlm_adapter_forward(x, down, up, ids, scale=None, base=None, out=None, inner=None, workspace=None, range_flag=None, stream=None):
+    """x: float32 or bfloat16 [..., K]; down [n][R][K], up [n][N][R] of the same type; ids int32 [...]: adapters of the rows (negative:
+    none); scale float32 [n] or None; base [..., N] or None (zeros).  Returns (out [..., N], inner float32 [..., R]); out may be base."""
+    import torch
+    call = "rnnlm_adapter_forward"
+    rows, K, ldx, dt = _rows(call, "x", x)
+    if stream is not None:
+        return _on(call, stream, x.get_device(), rnnlm_adapter_forward, x, down, up, ids, scale, base, out, inner, workspace, range_flag)
+    dev, i32 = x.get_device(), torch.int32
+    a, N = _adapters(call, x, down, up, scale, K)
+    out = torch.empty(*x.shape[:-1], N, dtype=x.dtype, device=x.device) if out is None else out
+    inner = torch.empty(*x.shape[:-1], a.R, dtype=torch.float32, device=x.device) if inner is None else inner
+    o, ldo = _beside(call, "out", out, x, N)
+    b, ldb = (None, 0) if base is None else _beside(call, "base", base, x, N)
+    if b == o and rows <= 1:  # in place (one row has no distance to the next)
+        ldb = ldo
+    at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_adapter_workspace_bytes(rows, K, N, a.n, a.R, dt))
+    _ok(_launch(dev, load().rnnlm_adapter_forward, x.data_ptr(), ldx, dt, rows, K, N, C.byref(a), _at(call, "ids", ids, i32, rows, dev), b, ldb,
+                o, ldo, _at(call, "inner", inner, torch.float32, rows * a.R, dev), _at(call, "range_flag", range_flag, i32, 1, dev), at, nbytes),
+        call)
+    return out, inner
+
+
+def rnnlm_adapter_backward(dout, x, inner, down, up, ids, scale=None, ddown=None, dup=None, dx=None, workspace=None, range_flag=None,
+                           stream=None):
+    """dout [..., N] and the forward call's x, inner, down, up, ids and scale.  Returns (ddown float32 [n][R][K], dup float32 [n][N][R]);
+    dx (a tensor like x) receives the gradient of x."""
+    import torch
+    call, f32, i32 = "rnnlm_adapter_backward", torch.float32, torch.int32
+    rows, K, ldx, dt = _rows(call, "x", x)
+    if stream is not None:
+        return _on(call, stream, x.get_device(), rnnlm_adapter_backward, dout, x, inner, down, up, ids, scale, ddown, dup, dx, workspace,
+                   range_flag)
+    dev = x.get_device()
+    a, N = _adapters(call, x, down, up, scale, K)
+    ddown = torch.empty(a.n, a.R, K, dtype=f32, device=x.device) if ddown is None else ddown
+    dup = torch.empty(a.n, N, a.R, dtype=f32, device=x.device) if dup is None else dup
+    d, ldd = _beside(call, "dout", dout, x, N)
+    g, ldg = (None, 0) if dx is None else _beside(call, "dx", dx, x, K)
+    at, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_adapter_workspace_bytes(rows, K, N, a.n, a.R, dt, True))
+    _ok(_launch(dev, load().rnnlm_adapter_backward, d, ldd, x.data_ptr(), ldx, _at(call, "inner", inner, f32, rows * a.R, dev, a.R), dt, rows, K,
+                N, C.byref(a), _at(call, "ids", ids, i32, rows, dev), _at(call, "ddown", ddown, f32, a.n * a.R * K, dev, K),
+                _at(call, "dup", dup, f32, a.n * N * a.R, dev, a.R), g, ldg, _at(call, "range_flag", range_flag, i32, 1, dev), at, nbytes), call)
+    return ddown, dup
 
 
 class Rnnlm:

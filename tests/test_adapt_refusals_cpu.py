@@ -63,3 +63,59 @@ def test_preference_workspaces(lib):
     ws = binding.rnnlm_preference_workspace_bytes
     assert ws(0, 1) > 0 and ws(20, 64) > ws(10, 64) > ws(0, 64) > 0 and ws(20, 64) % 256 == 0
     assert ws(-1, 1) == ws(1, 0) == ws(1, -1) == ws(1 << 22, 1) == ws(1, 1 << 21) == 0
+
+
+FORWARD = dict(x=LOGITS, ldx=40, dtype=1, rows=4, K=40, N=100, a=None, ids=Y, base=A, ldb=100, out=OUT, ldo=100, inner=MORE, flag=None, ws=WS,
+               bytes=1 << 20, stream=None)
+BACKWARD = dict(dout=A, ldd=100, x=LOGITS, ldx=40, inner=MORE, dtype=0, rows=4, K=40, N=100, a=None, ids=Y, ddown=B, dup=B + (1 << 30), dx=OUT,
+                ldx2=40, flag=None, ws=WS, bytes=1 << 20, stream=None)
+ADAPTERS = dict(down=BIG + (1 << 36), up=BIG + (1 << 37), scale=None, n=3, R=8)
+
+
+def with_adapters(good, change):
+    """The call's arguments; keys of the description are set in it."""
+    a = binding.rnnlm_adapters(*{**ADAPTERS, **{k: v for k, v in change.items() if k in ADAPTERS}}.values())
+    return {**good, "a": C.byref(a), **{k: v for k, v in change.items() if k not in ADAPTERS}}
+
+
+COMMON = [dict(a=None), dict(down=None), dict(up=None), dict(down=ADAPTERS["down"] + 1), dict(up=ADAPTERS["up"] + 1), dict(scale=2), dict(n=0), dict(n=65537), dict(R=0),
+          dict(R=65), dict(x=None), dict(x=LOGITS + 1), dict(ldx=39), dict(dtype=2), dict(rows=-1), dict(rows=(1 << 17) + 1), dict(K=0), dict(K=65537, ldx=1 << 17), dict(N=0),
+          dict(ids=None), dict(ids=Y + 2), dict(inner=MORE + 2), dict(flag=MORE + 1), dict(ws=None), dict(ws=WS + 64), dict(bytes=100)]
+
+
+@pytest.mark.parametrize("change", COMMON + [
+    dict(N=(1 << 20) + 1, ldb=1 << 21, ldo=1 << 21), dict(out=None), dict(out=OUT + 1), dict(ldo=99), dict(base=A + 1), dict(ldb=99), dict(base=OUT, ldb=101, ldo=100),
+    dict(base=OUT + 2), dict(out=LOGITS), dict(out=LOGITS + 8)], ids=str)
+def test_adapter_forward_refuses(lib, change):
+    assert lib.rnnlm_adapter_forward(*with_adapters(FORWARD, change).values()) == -1
+
+
+@pytest.mark.parametrize("change", COMMON + [
+    dict(N=(1 << 20) + 1, ldd=1 << 21), dict(dout=None), dict(dout=A + 2), dict(ldd=99), dict(inner=None), dict(ddown=None), dict(ddown=B + 2), dict(dup=None), dict(dup=B + 1),
+    dict(dx=OUT + 2), dict(ldx2=39), dict(dx=LOGITS), dict(dx=A + 400)], ids=str)
+def test_adapter_backward_refuses(lib, change):
+    assert lib.rnnlm_adapter_backward(*with_adapters(BACKWARD, change).values()) == -1
+
+
+def test_adapter_workspaces(lib):
+    ws = binding.rnnlm_adapter_workspace_bytes
+    assert ws(0, 1, 1, 1, 1, 0) > 0 and ws(1 << 17, 1, 1, 1, 64, 1) > 1 << 25
+    for good in ((2560, 1024, 64000, 16, 32, 1), (8192, 4096, 131072, 256, 64, 1), (1, 64, 131072, 1, 64, 0)):
+        assert 0 < ws(*good, False) < ws(*good, True) <= 1 << 30
+    assert [ws(-1, 1, 1, 1, 1, 0), ws((1 << 17) + 1, 1, 1, 1, 1, 0), ws(1, 0, 1, 1, 1, 0), ws(1, 65537, 1, 1, 1, 0), ws(1, 1, 0, 1, 1, 0), ws(1, 1, (1 << 20) + 1, 1, 1, 0),
+            ws(1, 1, 1, 0, 1, 0), ws(1, 1, 1, 65537, 1, 0), ws(1, 1, 1, 1, 0, 0), ws(1, 1, 1, 1, 65, 0), ws(1, 1, 1, 1, 1, 2)] == [0] * 11
+    assert lib.rnnlm_adapter_workspace_bytes(1, 1, 1, 1, 1, 0, 2) == 0
+
+
+def test_no_rows_of_a_forward_pass_are_fine(lib):
+    assert lib.rnnlm_adapter_forward(*with_adapters(FORWARD, dict(rows=0)).values()) == 0
+
+
+def test_binding_refuses_what_it_cannot_pass_on():
+    import torch
+    z = torch.zeros(2, 4, 10)
+    i = torch.zeros(2, 4, dtype=torch.int32)
+    for call in (lambda: binding.rnnlm_policy_loss(z, i, z[..., 0]), lambda: binding.rnnlm_preference_loss(z, i),
+                 lambda: binding.rnnlm_adapter_forward(z, z, z, i), lambda: binding.rnnlm_adapter_backward(z, z, z, z, z, i)):
+        with pytest.raises(binding.RnnlmError, match="on a GPU"):
+            call()
