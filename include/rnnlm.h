@@ -455,6 +455,50 @@ typedef struct {
 int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,
                        void *stream);
 
+/* rnnlm_train_chunk with the policy or the preference criterion ("Adapting") in place of the normalised cross-entropy: forward
+ * pass, gradients of the mean over the window's B*T positions (policy; weights and all) or over its B/2 pairs (preference: B is
+ * even, stream s < B/2 holds the preferred text of pair s), back-propagation and the same plain SGD step.  All arrays [T][B],
+ * [B] or [B/2] as there; logits: scratch of [T][B] rows (afterwards: the gradient with respect to the logits); loss, logp,
+ * sum_loss may be NULL.  A sum that is not finite and words out of range are reported by rnnlm_check. */
+typedef struct {
+  const float *old_logp, *ref_logp, *advantage, *weight;
+  float tau, clip_low, clip_high, beta;
+  void *logits;
+  int64_t ld;
+} rnnlm_policy;
+typedef struct {
+  const float *ref, *weight;
+  int32_t kind;
+  float beta, smoothing;
+  int32_t mean;
+  void *logits;
+  int64_t ld;
+  void *workspace; /* as rnnlm_preference_loss, of T and B/2 */
+  size_t workspace_bytes;
+} rnnlm_preference;
+int rnnlm_policy_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float lr, float *loss,
+                             float *logp, double *sum_loss, void *stream);
+int rnnlm_preference_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p, float lr,
+                                 float *loss, float *logp, double *sum_loss, void *stream);
+
+/* Their gradients into caller buffers, as rnnlm_grad_chunk and rnnlm_grad_chunk_compressed give theirs. */
+int rnnlm_policy_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float *dE, float *dU,
+                            float *dWo, float *db, float *loss, float *logp, void *stream);
+int rnnlm_policy_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float *dE,
+                                       float *dA, float *dU, float *dC, float *db, float *loss, float *logp, void *stream);
+int rnnlm_preference_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p, float *dE,
+                                float *dU, float *dWo, float *db, float *loss, float *logp, void *stream);
+int rnnlm_preference_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p,
+                                           float *dE, float *dA, float *dU, float *dC, float *db, float *loss, float *logp, void *stream);
+
+/* rnnlm_forward_logits with adapters beside the output layer: ids: dev int32[T][B], the adapter of every position (negative:
+ * none; >= n: none, reported by rnnlm_check).  states: dev [T][B] rows of the compute type, ld_states apart, receives what the
+ * output layer reads (H numbers, compressed architecture: P), inner: dev float[T][B][R] or NULL: what rnnlm_adapter_backward
+ * wants.  The adapters are of the compute type, down [n][R][H or P], up [n][V][R]; workspace: rnnlm_adapter_workspace_bytes of
+ * T*B rows, K = H or P, N = V, backward 0. */
+int rnnlm_forward_adapted(rnnlm_t *h, const int32_t *x, int32_t T, const rnnlm_adapters *a, const int32_t *ids, void *logits, int64_t ld,
+                          void *states, int64_t ld_states, float *inner, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Number of polls, of about 4 us each (or as many shorter ones as take that time), a wait of the persistent
  * recurrent kernels makes before it gives up, raises the flag that rnnlm_check reports as RNNLM_ERR_TIMEOUT and
  * lets the kernel run to its end (default 2^18, about a second).  A wait lasts longer than a step's few

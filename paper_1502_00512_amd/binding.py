@@ -33,6 +33,8 @@ SYMBOLS = [
     "rnnlm_distill_grad_chunk_compressed", "rnnlm_verify_chunk",
     "rnnlm_policy_loss", "rnnlm_preference_workspace_bytes", "rnnlm_preference_loss",
     "rnnlm_adapter_workspace_bytes", "rnnlm_adapter_forward", "rnnlm_adapter_backward",
+    "rnnlm_policy_train_chunk", "rnnlm_policy_grad_chunk", "rnnlm_policy_grad_chunk_compressed", "rnnlm_preference_train_chunk",
+    "rnnlm_preference_grad_chunk", "rnnlm_preference_grad_chunk_compressed", "rnnlm_forward_adapted",
 ]
 SIZES = ["rnnlm_workspace_bytes", "rnnlm_top_logits_workspace_bytes", "rnnlm_verify_workspace_bytes",
          "rnnlm_preference_workspace_bytes", "rnnlm_adapter_workspace_bytes"]  # return bytes
@@ -70,6 +72,17 @@ class rnnlm_distill(C.Structure):
 class rnnlm_verify(C.Structure):
     _fields_ = [("draft", C.c_void_p), ("ld_draft", C.c_int64), ("lengths", C.c_void_p), ("u", C.c_void_p), ("tau", C.c_float),
                 ("tau_draft", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
+class rnnlm_policy(C.Structure):
+    _fields_ = [("old_logp", C.c_void_p), ("ref_logp", C.c_void_p), ("advantage", C.c_void_p), ("weight", C.c_void_p), ("tau", C.c_float),
+                ("clip_low", C.c_float), ("clip_high", C.c_float), ("beta", C.c_float), ("logits", C.c_void_p), ("ld", C.c_int64)]
+
+
+class rnnlm_preference(C.Structure):
+    _fields_ = [("ref", C.c_void_p), ("weight", C.c_void_p), ("kind", C.c_int32), ("beta", C.c_float), ("smoothing", C.c_float),
+                ("mean", C.c_int32), ("logits", C.c_void_p), ("ld", C.c_int64), ("workspace", C.c_void_p),
                 ("workspace_bytes", C.c_size_t)]
 
 
@@ -141,6 +154,12 @@ def load():
                                           C.c_size_t, vp]
     lib.rnnlm_adapter_backward.argtypes = [vp, i64, vp, i64, vp, i32, i64, i32, i32, C.POINTER(rnnlm_adapters), vp, vp, vp, vp, i64, vp,
                                            vp, C.c_size_t, vp]
+    for of in ("policy", "preference"):
+        d = C.POINTER(globals()["rnnlm_" + of])
+        getattr(lib, f"rnnlm_{of}_train_chunk").argtypes = [vp, vp, vp, i32, d, f32, vp, vp, vp, vp]
+        getattr(lib, f"rnnlm_{of}_grad_chunk").argtypes = [vp, vp, vp, i32, d] + [vp] * 7
+        getattr(lib, f"rnnlm_{of}_grad_chunk_compressed").argtypes = [vp, vp, vp, i32, d] + [vp] * 8
+    lib.rnnlm_forward_adapted.argtypes = [vp, vp, i32, C.POINTER(rnnlm_adapters), vp, vp, i64, vp, i64, vp, vp, C.c_size_t, vp]
     for name in SIZES:
         getattr(lib, name).restype = C.c_size_t
     lib.rnnlm_profile_enable.argtypes = [vp, C.c_uint32]
@@ -728,6 +747,113 @@ class Rnnlm:
             g = dict(gE=z(self.V, self.H), gU=z(self.H, self.H), gWo=z(self.V, self.H), gb=z(self.V))
         _ok(_launch(self.device.index, getattr(self.lib, call), self.handle, at, y_at, T, C.byref(d), *map(_ptr, g.values()), loss_at), call)
         return dict(loss=loss, **g)
+
+    def _gradients(self):
+        import torch
+        z = lambda *s: torch.empty(*s, dtype=torch.float32, device=self.device)  # noqa: E731
+        if self.P:
+            return dict(gE=z(self.V, self.P), gA=z(self.H, self.P), gU=z(self.H, self.H), gC=z(self.P, self.H), gb=z(self.V))
+        return dict(gE=z(self.V, self.H), gU=z(self.H, self.H), gWo=z(self.V, self.H), gb=z(self.V))
+
+    def _policy(self, call, x, y, advantage, old_logp, ref_logp, weight, tau, clip_low, clip_high, beta, logits, loss, logp, sum_loss):
+        import torch
+        T, at = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        n, dev, f32 = T * self.B, self.device.index, torch.float32
+        p = rnnlm_policy(_at(call, "old_logp", old_logp, f32, n, dev), _at(call, "ref_logp", ref_logp, f32, n, dev),
+                         _at(call, "advantage", advantage, f32, n, dev), _at(call, "weight", weight, f32, n, dev), tau, clip_low, clip_high,
+                         beta, logits.data_ptr(), ld)
+        return (p, logits, T, at, _at(call, "y", y, torch.int32, n, dev), _at(call, "loss", loss, f32, n, dev),
+                _at(call, "logp", logp, f32, n, dev), _at(call, "sum_loss", sum_loss, torch.float64, 1, dev))
+
+    def rnnlm_policy_train_chunk(self, x, y, advantage, lr: float, old_logp=None, ref_logp=None, weight=None, tau: float = 1.0,
+                                 clip_low: float = 0.2, clip_high: float = 0.2, beta: float = 0.0, logits=None, loss=None, logp=None,
+                                 sum_loss=None, stream=None):
+        """y, advantage, old_logp, ref_logp, weight [T][B]: as rnnlm_policy_loss."""
+        call = "rnnlm_policy_train_chunk"
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_policy_train_chunk, x, y, advantage, lr, old_logp, ref_logp, weight, tau,
+                       clip_low, clip_high, beta, logits, loss, logp, sum_loss)
+        p, _keep, T, at, y_at, loss_at, logp_at, sum_at = self._policy(call, x, y, advantage, old_logp, ref_logp, weight, tau, clip_low,
+                                                                       clip_high, beta, logits, loss, logp, sum_loss)
+        _ok(_launch(self.device.index, self.lib.rnnlm_policy_train_chunk, self.handle, at, y_at, T, C.byref(p), lr, loss_at, logp_at, sum_at),
+            call)
+
+    def rnnlm_policy_grad_chunk(self, x, y, advantage, old_logp=None, ref_logp=None, weight=None, tau: float = 1.0, clip_low: float = 0.2,
+                                clip_high: float = 0.2, beta: float = 0.0, logits=None, stream=None):
+        import torch
+        call = "rnnlm_policy_grad_chunk" + ("_compressed" if self.P else "")
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_policy_grad_chunk, x, y, advantage, old_logp, ref_logp, weight, tau,
+                       clip_low, clip_high, beta, logits)
+        loss, logp = (torch.empty(x.shape[0], self.B, dtype=torch.float32, device=self.device) for _ in range(2))
+        p, _keep, T, at, y_at, loss_at, logp_at, _ = self._policy(call, x, y, advantage, old_logp, ref_logp, weight, tau, clip_low, clip_high,
+                                                                  beta, logits, loss, logp, None)
+        g = self._gradients()
+        _ok(_launch(self.device.index, getattr(self.lib, call), self.handle, at, y_at, T, C.byref(p), *map(_ptr, g.values()), loss_at, logp_at),
+            call)
+        return dict(loss=loss, logp=logp, **g)
+
+    def _preference(self, call, x, y, ref, weight, kind, beta, smoothing, mean, logits, workspace, loss, logp, sum_loss):
+        import torch
+        T, at = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        n, P, dev, f32 = T * self.B, self.B // 2, self.device.index, torch.float32
+        ws, nbytes, keep = _scratch(call, workspace, dev, lambda: rnnlm_preference_workspace_bytes(T, P))
+        p = rnnlm_preference(_at(call, "ref", ref, f32, 2 * P, dev), _at(call, "weight", weight, f32, P, dev), kind, beta, smoothing,
+                             int(mean), logits.data_ptr(), ld, ws, nbytes)
+        return (p, (logits, keep), T, at, _at(call, "y", y, torch.int32, n, dev), _at(call, "loss", loss, f32, P, dev),
+                _at(call, "logp", logp, f32, 2 * P, dev), _at(call, "sum_loss", sum_loss, torch.float64, 1, dev))
+
+    def rnnlm_preference_train_chunk(self, x, y, lr: float, ref=None, weight=None, kind: int = RNNLM_PREFERENCE_LOGISTIC, beta: float = 0.1,
+                                     smoothing: float = 0.0, mean: bool = False, logits=None, loss=None, logp=None, workspace=None,
+                                     sum_loss=None, stream=None):
+        """y [T][B], ref [B], weight [B/2]: as rnnlm_preference_loss."""
+        call = "rnnlm_preference_train_chunk"
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_preference_train_chunk, x, y, lr, ref, weight, kind, beta, smoothing, mean,
+                       logits, loss, logp, workspace, sum_loss)
+        p, _keep, T, at, y_at, loss_at, logp_at, sum_at = self._preference(call, x, y, ref, weight, kind, beta, smoothing, mean, logits,
+                                                                           workspace, loss, logp, sum_loss)
+        _ok(_launch(self.device.index, self.lib.rnnlm_preference_train_chunk, self.handle, at, y_at, T, C.byref(p), lr, loss_at, logp_at,
+                    sum_at), call)
+
+    def rnnlm_preference_grad_chunk(self, x, y, ref=None, weight=None, kind: int = RNNLM_PREFERENCE_LOGISTIC, beta: float = 0.1,
+                                    smoothing: float = 0.0, mean: bool = False, logits=None, workspace=None, stream=None):
+        import torch
+        call = "rnnlm_preference_grad_chunk" + ("_compressed" if self.P else "")
+        if stream is not None:
+            return _on(call, stream, self.device.index, self.rnnlm_preference_grad_chunk, x, y, ref, weight, kind, beta, smoothing, mean,
+                       logits, workspace)
+        loss, logp = (torch.empty(k, dtype=torch.float32, device=self.device) for k in (self.B // 2, self.B // 2 * 2))
+        p, _keep, T, at, y_at, loss_at, logp_at, _ = self._preference(call, x, y, ref, weight, kind, beta, smoothing, mean, logits, workspace,
+                                                                      loss, logp, None)
+        g = self._gradients()
+        _ok(_launch(self.device.index, getattr(self.lib, call), self.handle, at, y_at, T, C.byref(p), *map(_ptr, g.values()), loss_at, logp_at),
+            call)
+        return dict(loss=loss, logp=logp, **g)
+
+    def rnnlm_forward_adapted(self, x, down, up, ids, scale=None, logits=None, states=None, inner=None, workspace=None, stream=None):
+        """down [n][R][H or P], up [n][V][R] of the compute type, ids int32 [T][B].  Returns (logits [T][B][V], states [T][B][H or P],
+        inner float32 [T][B][R]): what rnnlm_adapter_backward wants of the forward pass."""
+        import torch
+        call, dev = "rnnlm_forward_adapted", self.device.index
+        if stream is not None:
+            return _on(call, stream, dev, self.rnnlm_forward_adapted, x, down, up, ids, scale, logits, states, inner, workspace)
+        T, at = self._window(call, x)
+        logits, ld = self._logit_rows(call, T, logits)
+        K, rows = self.P or self.H, T * self.B
+        states = torch.empty(T, self.B, K, dtype=logits.dtype, device=self.device) if states is None else states
+        a, N = _adapters(call, logits, down, up, scale, K)
+        if N != self.V:
+            _refuse(call, f"up: [n][{self.V}][R] is wanted")
+        inner = torch.empty(T, self.B, a.R, dtype=torch.float32, device=self.device) if inner is None else inner
+        s, lds = _beside(call, "states", states, logits, K)
+        dt = RNNLM_DTYPE_FP32 if self.precision == RNNLM_FP32 else RNNLM_DTYPE_BF16
+        ws, nbytes, _keep = _scratch(call, workspace, dev, lambda: rnnlm_adapter_workspace_bytes(rows, K, N, a.n, a.R, dt))
+        _ok(_launch(dev, self.lib.rnnlm_forward_adapted, self.handle, at, T, C.byref(a), _at(call, "ids", ids, torch.int32, rows, dev, self.B),
+                    logits.data_ptr(), ld, s, lds, _at(call, "inner", inner, torch.float32, rows * a.R, dev, a.R), ws, nbytes), call)
+        return logits, states, inner
 
     def rnnlm_verify_chunk(self, x, u, draft=None, lengths=None, tau: float = 1.0, tau_draft: float = 1.0, logits=None, accepted=None,
                            tokens=None, workspace=None, stream=None):

@@ -130,6 +130,16 @@ __global__ void __launch_bounds__(1024) losses_sum_kernel(const float *__restric
   window_sum(w, n, [&](int i) { return loss[i]; });
 }
 
+// What the output layer reads of every position (a row of `width`), as rows t*B + s.
+template <typename T>
+__global__ void __launch_bounds__(256) states_to_rows_kernel(const T *__restrict__ feat, int B, int Bp, int width, int pitch,
+                                                             T *__restrict__ out, long ld) {
+  const int t = blockIdx.x / B, s = blockIdx.x % B;
+  const T *src = feat + ((long)t * Bp + s) * pitch;
+  T *dst = out + (long)blockIdx.x * ld;
+  for (int j = threadIdx.x; j < width; j += 256) dst[j] = src[j];
+}
+
 // h_state of every text after the inputs it keeps: the first and its accepted drafts.
 template <typename T>
 __global__ void __launch_bounds__(256) keep_states_kernel(const T *__restrict__ Hs, const int32_t *__restrict__ accepted, int H,

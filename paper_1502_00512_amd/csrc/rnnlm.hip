@@ -1122,32 +1122,52 @@ int logits_to_rows(rnnlm_t *h, int Tn, void *logits, int64_t ld, hipStream_t st)
   HIP_TRY(hipGetLastError());
   return RNNLM_OK;
 }
-struct DistillCall {
-  const rnnlm_distill *d;
+// A criterion on rows of logits: one of the three descriptions.
+struct RowsCriterion {
+  const rnnlm_distill *distill;
+  const rnnlm_policy *policy;
+  const rnnlm_preference *preference;
   const int32_t *y;
-  float *loss;  // may be nullptr
+  float *loss, *logp;  // may be nullptr
+  void *logits() const { return distill ? distill->logits : policy ? policy->logits : preference->logits; }
+  int64_t ld() const { return distill ? distill->ld : policy ? policy->ld : preference->ld; }
+  // Losses of a window, and their gradients in place of the logits.  (The gradients of the mean over positions, or pairs.)
+  int losses(int Tn, int B) const { return preference ? B / 2 : Tn * B; }
+  int apply(int32_t dtype, int Tn, int B, int32_t V, float *out, int32_t *flag, hipStream_t st) const {
+    const float scale = 1.0f / (float)losses(Tn, B);
+    if (distill) {
+      const rnnlm_distill &d = *distill;
+      return rnnlm_distill_loss(d.logits, dtype, Tn * B, V, d.ld, d.ids, d.vals, d.K, d.lse, y, d.weight, d.tau, d.alpha, scale, out, nullptr,
+                                d.logits, d.ld, flag, st);
+    }
+    if (policy) {
+      const rnnlm_policy &d = *policy;
+      return rnnlm_policy_loss(d.logits, dtype, Tn * B, V, d.ld, y, d.old_logp, d.ref_logp, d.advantage, d.weight, d.tau, d.clip_low,
+                               d.clip_high, d.beta, scale, out, logp, nullptr, d.logits, d.ld, flag, st);
+    }
+    const rnnlm_preference &d = *preference;
+    return rnnlm_preference_loss(d.logits, dtype, Tn, B / 2, V, d.ld, y, d.ref, d.weight, d.kind, d.beta, d.smoothing, d.mean, scale, out, logp,
+                                 nullptr, d.logits, d.ld, flag, d.workspace, d.workspace_bytes, st);
+  }
 };
-// The place of the softmax gradient in a distilled window: the criterion on rows of logits, its sum, and the gradient of
+// The place of the softmax gradient in such a window: the criterion on rows of logits, its sum, and the gradient of
 // the logits back in the output layer's order with the bias update.
 template <typename T>
-int distill_gradient(rnnlm_t *h, int Tn, int Mp, const DistillCall &c, const WindowSum &ws, const float *b, float *b_out, float alpha,
-                     float lr, hipStream_t st) {
-  const rnnlm_distill &d = *c.d;
-  const int n = Tn * h->cfg.B;
+int rows_gradient(rnnlm_t *h, int Tn, int Mp, const RowsCriterion &c, const WindowSum &ws, const float *b, float *b_out, float alpha,
+                  float lr, hipStream_t st) {
   float *loss = c.loss ? c.loss : at<float>(h, h->L.logp_int);
-  int rc = logits_to_rows<T>(h, Tn, d.logits, d.ld, st);
+  int rc = logits_to_rows<T>(h, Tn, c.logits(), c.ld(), st);
   if (rc) return rc;
-  rc = rnnlm_distill_loss(d.logits, logit_dtype<T>(), n, h->cfg.V, d.ld, d.ids, d.vals, d.K, d.lse, c.y, d.weight, d.tau, d.alpha,
-                          1.0f / (float)n, loss, nullptr, d.logits, d.ld, p_flags(h), st);
+  rc = c.apply(logit_dtype<T>(), Tn, h->cfg.B, h->cfg.V, loss, p_flags(h), st);
   if (rc) return rc;
-  hipLaunchKernelGGL(losses_sum_kernel, dim3(1), dim3(1024), 0, st, loss, n, ws);
+  hipLaunchKernelGGL(losses_sum_kernel, dim3(1), dim3(1024), 0, st, loss, c.losses(Tn, h->cfg.B), ws);
   // shares of the positions: some four workgroups to a compute unit, as far as the scratch (of the contraction that follows) goes
   const int tiles = h->Vp / LW_TILE;
   const long most = std::min<long>({16, Mp / LW_TILE, std::max<long>(1, 1024 / tiles), h->L.partElems / h->Vp});
   const int per = most > 1 ? (int)round_up((Mp + most - 1) / most, LW_TILE) : Mp, shares = (Mp + per - 1) / per;
   float *sums = shares > 1 ? at<float>(h, h->L.part32) : nullptr;
-  hipLaunchKernelGGL(rows_to_logits_kernel<T>, dim3(tiles, shares), dim3(256), 0, st, static_cast<const T *>(d.logits),
-                     at<T>(h, h->L.ZT), Mp, per, sums, (long)h->Vp, b, b_out, alpha, lr, logit_window(h, Tn, d.ld));
+  hipLaunchKernelGGL(rows_to_logits_kernel<T>, dim3(tiles, shares), dim3(256), 0, st, static_cast<const T *>(c.logits()),
+                     at<T>(h, h->L.ZT), Mp, per, sums, (long)h->Vp, b, b_out, alpha, lr, logit_window(h, Tn, c.ld()));
   if (sums)
     hipLaunchKernelGGL(bias_update_kernel, dim3(blocks_for(h->cfg.V, 256)), dim3(256), 0, st, sums, (long)h->Vp, shares, h->cfg.V, b,
                        b_out, alpha, lr);
@@ -1356,7 +1376,7 @@ int launch_window_update(rnnlm_t *h, WindowUpdate<T> &w, int tile, int Mrows, hi
 // other stream is not.
 template <typename T>
 int backward_window(rnnlm_t *h, int Tn, const UpdateTargets &u, const NceCall *nce, hipStream_t st, hipStream_t *rec_stream,
-                    float *logp_out, const WindowSum &wsum, const DistillCall *distill = nullptr) {
+                    float *logp_out, const WindowSum &wsum, const RowsCriterion *rows = nullptr) {
   const rnnlm_config &c = h->cfg;
   const int Hp = h->Hp, Bp = h->Bp, Vp = h->Vp;
   const int Mrows = Tn * Bp;
@@ -1379,9 +1399,9 @@ int backward_window(rnnlm_t *h, int Tn, const UpdateTargets &u, const NceCall *n
     if (rc) return rc;
   } else {
   // fused softmax gradient + bias update, in place on the vocabulary-major logits
-  if (distill) {
+  if (rows) {
     StageTimer tm(h, RNNLM_STAGE_SOFTMAX_GRAD, st);
-    int rc = distill_gradient<T>(h, Tn, Mp, *distill, wsum, h->buf.b, u.b, u.alpha, u.lr, st);
+    int rc = rows_gradient<T>(h, Tn, Mp, *rows, wsum, h->buf.b, u.b, u.alpha, u.lr, st);
     if (rc) return rc;
   } else {
     StageTimer tm(h, RNNLM_STAGE_SOFTMAX_GRAD, st);
@@ -1750,8 +1770,8 @@ int window_call(rnnlm_t *h, const int32_t *x, const int32_t *y, int Tn, float *l
 }
 
 template <typename T>
-int distill_window_call(rnnlm_t *h, const int32_t *x, int Tn, const DistillCall &c, double *sum_loss, const UpdateTargets &u,
-                        bool advance_state, hipStream_t st) {
+int rows_window_call(rnnlm_t *h, const int32_t *x, int Tn, const RowsCriterion &c, double *sum_loss, const UpdateTargets &u,
+                     bool advance_state, hipStream_t st) {
   const WindowSum ws = {sum_loss ? sum_loss : p_sum(h), nullptr, p_flags(h), p_counter(h)};
   int rc = forward_window<T>(h, x, nullptr, Tn, nullptr, advance_state, true, st, true, !scan_ids(h, Tn, u), false, nullptr, true);
   if (rc) return rc;
@@ -1762,6 +1782,20 @@ template <typename T>
 int logits_call(rnnlm_t *h, const int32_t *x, int Tn, void *logits, int64_t ld, bool advance_state, hipStream_t st) {
   int rc = forward_window<T>(h, x, nullptr, Tn, nullptr, advance_state, true, st, false, false, false, nullptr, true);
   return rc ? rc : logits_to_rows<T>(h, Tn, logits, ld, st);
+}
+
+template <typename T>
+int adapted_call(rnnlm_t *h, const int32_t *x, int Tn, const rnnlm_adapters &a, const int32_t *ids, void *logits, int64_t ld, void *states,
+                 int64_t ld_states, float *inner, void *workspace, size_t workspace_bytes, hipStream_t st) {
+  int rc = logits_call<T>(h, x, Tn, logits, ld, true, st);
+  if (rc) return rc;
+  const int n = Tn * h->cfg.B;
+  const T *feat = h->cfg.P > 0 ? at<T>(h, h->L.P_c) : at<T>(h, h->L.Hs_c) + (long)h->Bp * h->Hp;
+  hipLaunchKernelGGL(states_to_rows_kernel<T>, dim3(n), dim3(256), 0, st, feat, h->cfg.B, h->Bp, h->D, h->Dp, static_cast<T *>(states),
+                     (long)ld_states);
+  HIP_TRY(hipGetLastError());
+  return rnnlm_adapter_forward(states, ld_states, logit_dtype<T>(), n, h->D, h->cfg.V, &a, ids, logits, ld, logits, ld, inner, p_flags(h), workspace,
+                               workspace_bytes, st);
 }
 
 template <typename T>
@@ -2188,11 +2222,62 @@ bool distill_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, 
   return ((reinterpret_cast<uintptr_t>(d->ids) | reinterpret_cast<uintptr_t>(d->vals) | reinterpret_cast<uintptr_t>(d->lse) |
            reinterpret_cast<uintptr_t>(d->weight) | reinterpret_cast<uintptr_t>(y)) & 3) == 0;
 }
-int distill_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, const UpdateTargets &u,
-                  float *loss, double *sum_loss, bool advance_state, hipStream_t st) {
-  const DistillCall c = {d, y, loss};
-  return (h->cfg.precision == RNNLM_FP32) ? distill_window_call<float>(h, x, T, c, sum_loss, u, advance_state, st)
-                                          : distill_window_call<bf16_t>(h, x, T, c, sum_loss, u, advance_state, st);
+int rows_chunk(rnnlm_t *h, const int32_t *x, int32_t T, const RowsCriterion &c, const UpdateTargets &u, double *sum_loss, bool advance_state,
+               hipStream_t st) {
+  return (h->cfg.precision == RNNLM_FP32) ? rows_window_call<float>(h, x, T, c, sum_loss, u, advance_state, st)
+                                          : rows_window_call<bf16_t>(h, x, T, c, sum_loss, u, advance_state, st);
+}
+int rows_train_chunk(rnnlm_t *h, const int32_t *x, int32_t T, const RowsCriterion &c, float lr, double *sum_loss, hipStream_t st) {
+  UpdateTargets u{h->buf.E, h->buf.U, h->buf.Wo, h->buf.b, 1.0f, lr, true, true};
+  u.A = h->buf.A;
+  u.C = h->buf.C;
+  return rows_chunk(h, x, T, c, u, sum_loss, true, st);
+}
+int rows_grad_chunk(rnnlm_t *h, const int32_t *x, int32_t T, const RowsCriterion &c, float *dE, float *dU, float *dWo, float *db,
+                    hipStream_t st) {
+  if (!dE || !dU || !dWo || !db || h->cfg.P > 0) return RNNLM_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dU) | reinterpret_cast<uintptr_t>(dWo) |
+       reinterpret_cast<uintptr_t>(db)) & 15)
+    return RNNLM_ERR_ARG;
+  const long nE = (long)h->cfg.V * h->cfg.H;
+  hipLaunchKernelGGL(fill_kernel<float>, dim3(std::min<long>(blocks_for(nE, 256), 65535)), dim3(256), 0, st, dE, nE, 0.0f);
+  HIP_TRY(hipGetLastError());
+  return rows_chunk(h, x, T, c, UpdateTargets{dE, dU, dWo, db, 0.0f, -1.0f, false, false}, nullptr, false, st);
+}
+int rows_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, int32_t T, const RowsCriterion &c, float *dE, float *dA, float *dU, float *dC,
+                               float *db, hipStream_t st) {
+  if (!dE || !dA || !dU || !dC || !db || h->cfg.P <= 0) return RNNLM_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dA) | reinterpret_cast<uintptr_t>(dU) |
+       reinterpret_cast<uintptr_t>(dC) | reinterpret_cast<uintptr_t>(db)) & 15)
+    return RNNLM_ERR_ARG;
+  UpdateTargets u{dE, dU, nullptr, db, 0.0f, -1.0f, false, false};
+  u.A = dA;
+  u.C = dC;
+  return rows_chunk(h, x, T, c, u, nullptr, false, st);
+}
+bool floats_ok(std::initializer_list<const void *> p) {
+  uintptr_t all = 0;
+  for (const void *q : p) all |= reinterpret_cast<uintptr_t>(q);
+  return (all & 3) == 0;
+}
+bool policy_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, const float *loss, const float *logp,
+                    const double *sum_loss = nullptr) {
+  if (!h || !x || !y || !p || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, T, p->logits, p->ld)) return false;
+  if (!p->advantage || (p->beta != 0.0f && !p->ref_logp) || !tau_in_range(p->tau) || !(p->clip_low >= 0.0f && p->clip_low <= 1.0f) ||
+      !(p->clip_high >= 0.0f && p->clip_high < INFINITY) || !(p->beta >= 0.0f && p->beta < INFINITY))
+    return false;
+  return floats_ok({x, y, p->old_logp, p->ref_logp, p->advantage, p->weight, loss, logp}) && (reinterpret_cast<uintptr_t>(sum_loss) & 7) == 0;
+}
+bool preference_args_ok(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p, const float *loss,
+                        const float *logp, const double *sum_loss = nullptr) {
+  if (!h || !x || !y || !p || T < 1 || T > h->cfg.T_max || h->cfg.B % 2 || !logit_rows_ok(h, T, p->logits, p->ld)) return false;
+  if (p->kind < RNNLM_PREFERENCE_LOGISTIC || p->kind > RNNLM_PREFERENCE_HINGE || !(p->beta > 0.0f && p->beta < INFINITY) ||
+      !(p->smoothing >= 0.0f && p->smoothing <= 0.5f) || (p->smoothing != 0.0f && p->kind != RNNLM_PREFERENCE_LOGISTIC) ||
+      (p->mean != 0 && p->mean != 1))
+    return false;
+  const size_t need = rnnlm_preference_workspace_bytes(T, h->cfg.B / 2);
+  if (need == 0 || !p->workspace || (reinterpret_cast<uintptr_t>(p->workspace) & 255) || p->workspace_bytes < need) return false;
+  return floats_ok({x, y, p->ref, p->weight, loss, logp}) && (reinterpret_cast<uintptr_t>(sum_loss) & 7) == 0;
 }
 }  // namespace
 
@@ -2206,35 +2291,76 @@ int rnnlm_forward_logits(rnnlm_t *h, const int32_t *x, int32_t T, void *logits, 
 int rnnlm_distill_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float lr,
                               float *loss, double *sum_loss, void *stream) {
   if (!distill_args_ok(h, x, y, T, d, loss, sum_loss) || !(lr == lr)) return RNNLM_ERR_ARG;
-  UpdateTargets u{h->buf.E, h->buf.U, h->buf.Wo, h->buf.b, 1.0f, lr, true, true};
-  u.A = h->buf.A;
-  u.C = h->buf.C;
-  return distill_chunk(h, x, y, T, d, u, loss, sum_loss, true, (hipStream_t)stream);
+  return rows_train_chunk(h, x, T, {d, nullptr, nullptr, y, loss, nullptr}, lr, sum_loss, (hipStream_t)stream);
 }
 
 int rnnlm_distill_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE, float *dU,
                              float *dWo, float *db, float *loss, void *stream) {
-  if (!distill_args_ok(h, x, y, T, d, loss) || !dE || !dU || !dWo || !db || h->cfg.P > 0) return RNNLM_ERR_ARG;
-  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dU) | reinterpret_cast<uintptr_t>(dWo) |
-       reinterpret_cast<uintptr_t>(db)) & 15)
-    return RNNLM_ERR_ARG;
-  hipStream_t st = (hipStream_t)stream;
-  const long nE = (long)h->cfg.V * h->cfg.H;
-  hipLaunchKernelGGL(fill_kernel<float>, dim3(std::min<long>(blocks_for(nE, 256), 65535)), dim3(256), 0, st, dE, nE, 0.0f);
-  HIP_TRY(hipGetLastError());
-  return distill_chunk(h, x, y, T, d, UpdateTargets{dE, dU, dWo, db, 0.0f, -1.0f, false, false}, loss, nullptr, false, st);
+  if (!distill_args_ok(h, x, y, T, d, loss)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk(h, x, T, {d, nullptr, nullptr, y, loss, nullptr}, dE, dU, dWo, db, (hipStream_t)stream);
 }
 
 int rnnlm_distill_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_distill *d, float *dE,
                                         float *dA, float *dU, float *dC, float *db, float *loss, void *stream) {
-  if (!distill_args_ok(h, x, y, T, d, loss) || !dE || !dA || !dU || !dC || !db || h->cfg.P <= 0) return RNNLM_ERR_ARG;
-  if ((reinterpret_cast<uintptr_t>(dE) | reinterpret_cast<uintptr_t>(dA) | reinterpret_cast<uintptr_t>(dU) |
-       reinterpret_cast<uintptr_t>(dC) | reinterpret_cast<uintptr_t>(db)) & 15)
+  if (!distill_args_ok(h, x, y, T, d, loss)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk_compressed(h, x, T, {d, nullptr, nullptr, y, loss, nullptr}, dE, dA, dU, dC, db, (hipStream_t)stream);
+}
+
+int rnnlm_policy_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float lr, float *loss,
+                             float *logp, double *sum_loss, void *stream) {
+  if (!policy_args_ok(h, x, y, T, p, loss, logp, sum_loss) || !(lr == lr)) return RNNLM_ERR_ARG;
+  return rows_train_chunk(h, x, T, {nullptr, p, nullptr, y, loss, logp}, lr, sum_loss, (hipStream_t)stream);
+}
+
+int rnnlm_policy_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float *dE, float *dU,
+                            float *dWo, float *db, float *loss, float *logp, void *stream) {
+  if (!policy_args_ok(h, x, y, T, p, loss, logp)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk(h, x, T, {nullptr, p, nullptr, y, loss, logp}, dE, dU, dWo, db, (hipStream_t)stream);
+}
+
+int rnnlm_policy_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_policy *p, float *dE,
+                                       float *dA, float *dU, float *dC, float *db, float *loss, float *logp, void *stream) {
+  if (!policy_args_ok(h, x, y, T, p, loss, logp)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk_compressed(h, x, T, {nullptr, p, nullptr, y, loss, logp}, dE, dA, dU, dC, db, (hipStream_t)stream);
+}
+
+int rnnlm_preference_train_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p, float lr,
+                                 float *loss, float *logp, double *sum_loss, void *stream) {
+  if (!preference_args_ok(h, x, y, T, p, loss, logp, sum_loss) || !(lr == lr)) return RNNLM_ERR_ARG;
+  return rows_train_chunk(h, x, T, {nullptr, nullptr, p, y, loss, logp}, lr, sum_loss, (hipStream_t)stream);
+}
+
+int rnnlm_preference_grad_chunk(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p, float *dE,
+                                float *dU, float *dWo, float *db, float *loss, float *logp, void *stream) {
+  if (!preference_args_ok(h, x, y, T, p, loss, logp)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk(h, x, T, {nullptr, nullptr, p, y, loss, logp}, dE, dU, dWo, db, (hipStream_t)stream);
+}
+
+int rnnlm_preference_grad_chunk_compressed(rnnlm_t *h, const int32_t *x, const int32_t *y, int32_t T, const rnnlm_preference *p,
+                                           float *dE, float *dA, float *dU, float *dC, float *db, float *loss, float *logp, void *stream) {
+  if (!preference_args_ok(h, x, y, T, p, loss, logp)) return RNNLM_ERR_ARG;
+  return rows_grad_chunk_compressed(h, x, T, {nullptr, nullptr, p, y, loss, logp}, dE, dA, dU, dC, db, (hipStream_t)stream);
+}
+
+int rnnlm_forward_adapted(rnnlm_t *h, const int32_t *x, int32_t T, const rnnlm_adapters *a, const int32_t *ids, void *logits, int64_t ld,
+                          void *states, int64_t ld_states, float *inner, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!h || !x || T < 1 || T > h->cfg.T_max || !logit_rows_ok(h, T, logits, ld) || !a || !a->down || !a->up || !ids || !states ||
+      ld_states < h->D || ld_states > (int64_t(1) << 31) || !floats_ok({x, ids, inner, a->scale}))
     return RNNLM_ERR_ARG;
-  UpdateTargets u{dE, dU, nullptr, db, 0.0f, -1.0f, false, false};
-  u.A = dA;
-  u.C = dC;
-  return distill_chunk(h, x, y, T, d, u, loss, nullptr, false, (hipStream_t)stream);
+  const int32_t dtype = h->cfg.precision == RNNLM_FP32 ? RNNLM_DTYPE_FP32 : RNNLM_DTYPE_BF16;
+  const uintptr_t es = dtype == RNNLM_DTYPE_FP32 ? 4 : 2, all = reinterpret_cast<uintptr_t>(states) | reinterpret_cast<uintptr_t>(a->down) |
+                                                                reinterpret_cast<uintptr_t>(a->up);
+  // (what the adapters' own checks would refuse after the window has started)
+  const int64_t rows = (int64_t)T * h->cfg.B;
+  const size_t need = rnnlm_adapter_workspace_bytes(rows, h->D, h->cfg.V, a->n, a->R, dtype, 0);
+  const uintptr_t s0 = reinterpret_cast<uintptr_t>(states), s1 = s0 + ((rows - 1) * ld_states + h->D) * es;
+  const uintptr_t l0 = reinterpret_cast<uintptr_t>(logits), l1 = l0 + ((rows - 1) * ld + h->cfg.V) * es;
+  if ((all & (es - 1)) || need == 0 || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need ||
+      (s0 < l1 && l0 < s1))
+    return RNNLM_ERR_ARG;
+  hipStream_t st = (hipStream_t)stream;
+  return dtype == RNNLM_DTYPE_FP32 ? adapted_call<float>(h, x, T, *a, ids, logits, ld, states, ld_states, inner, workspace, workspace_bytes, st)
+                                   : adapted_call<bf16_t>(h, x, T, *a, ids, logits, ld, states, ld_states, inner, workspace, workspace_bytes, st);
 }
 
 int rnnlm_verify_chunk(rnnlm_t *h, const int32_t *x, int32_t K, const rnnlm_verify *v, int32_t *accepted, int32_t *tokens,
