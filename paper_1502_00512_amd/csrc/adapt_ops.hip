@@ -91,33 +91,42 @@ int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
 
 // ---- adapters ----
 constexpr int64_t ADAPTER_ROWS_MAX = 1 << 17;  // (putting the rows in order compares each with each)
-constexpr int ADAPTER_GRAD_WAVES = 8;
 
 int adapter_r_tiles(int32_t R) { return (R + 15) / 16; }
 // Columns of a wave of adapter_grad_kernel, in 16s: as many as its accumulators and operands leave registers for.
-int adapter_grad_tiles(int32_t R, int32_t dtype) { return dtype == RNNLM_DTYPE_BF16 && adapter_r_tiles(R) <= 2 ? 8 : 4; }
+constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 ? (bf16 ? 8 : 4) : bf16 ? 4 : 2; }
+constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
-// A sum over rows for W columns: blocks of columns, positions of a chunk.  Chunks until there are some 512 workgroups.
+// A sum over rows for W columns, 16 tiles of them a wave: blocks of columns, positions of a chunk.  Chunks of at least `least`
+// tiles (what a chunk writes at its end is as much as several tiles of what it reads) until there are some 512 workgroups.
 struct GradPlan {
   int blocks, chunks, chunk;
 };
-GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int32_t dtype) {
+GradPlan adapter_grad_plan(int64_t rows, int32_t W, int tiles_of_wave, int least) {
   GradPlan p;
-  const int cols = ADAPTER_GRAD_WAVES * 16 * adapter_grad_tiles(R, dtype);
+  const int cols = ADAPTER_GRAD_WAVES * 16 * tiles_of_wave;
   p.blocks = (W + cols - 1) / cols;
   const int64_t tiles = std::max<int64_t>(1, (rows + ADAPTER_TILE - 1) / ADAPTER_TILE);
-  const int64_t want = std::min<int64_t>(tiles, std::max(1, 512 / p.blocks));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(tiles / least, 512 / p.blocks));
   p.chunk = (int)((tiles + want - 1) / want) * ADAPTER_TILE;
   p.chunks = (int)std::max<int64_t>(1, (rows + p.chunk - 1) / p.chunk);
   return p;
+}
+GradPlan adapter_up_plan(int64_t rows, int32_t N, int32_t R, int32_t dtype) {
+  return adapter_grad_plan(rows, N, adapter_grad_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16), 4);
+}
+GradPlan adapter_down_plan(int64_t rows, int32_t K, int32_t R, int32_t dtype) {
+  return adapter_grad_plan(rows, K, adapter_input_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16), 2);
 }
 
 // Rows in up to this many tiles are taken as they come: an adapter is read once for each tile that has it.
 constexpr int ADAPTER_UNORDERED = 4;
 
+// Sums of up to this many blocks of columns are formed where they are used, more in a launch of their own.
+constexpr int ADAPTER_BLOCKS_INSIDE = 8;
+
 struct AdapterPlan {
-  long Mp;
-  size_t perm, start, inner, tr_inner, tr_dinner, dinner, part, split, total;
+  size_t perm, sorted, start, inner, part, dinner, split_up, split_down, total;
 };
 AdapterPlan adapter_plan(int64_t rows, int32_t K, int32_t N, int32_t n, int32_t R, int32_t dtype, bool backward) {
   AdapterPlan p = {};
@@ -128,18 +137,16 @@ AdapterPlan adapter_plan(int64_t rows, int32_t K, int32_t N, int32_t n, int32_t 
     return at;
   };
   p.perm = take((size_t)rows * 4);
+  p.sorted = take((size_t)rows * 4);
   p.start = take(((size_t)n + 1) * 4);
   if (!backward) {
     p.inner = take((size_t)rows * R * 4);
   } else {
-    p.Mp = round_up(rows + ADAPTER_TILE, 64);
-    const size_t turned = (size_t)p.Mp * R * (dtype == RNNLM_DTYPE_FP32 ? 4 : 6);
-    const GradPlan up = adapter_grad_plan(rows, N, R, dtype), down = adapter_grad_plan(rows, K, R, dtype);
-    p.tr_inner = take(turned);
-    p.tr_dinner = take(turned);
-    p.dinner = take((size_t)rows * R * 4);
+    const GradPlan up = adapter_up_plan(rows, N, R, dtype), down = adapter_down_plan(rows, K, R, dtype);
     p.part = take((size_t)up.blocks * rows * R * 4);
-    p.split = take(std::max(up.chunks > 1 ? (size_t)2 * up.chunks * N : 0, down.chunks > 1 ? (size_t)2 * down.chunks * K : 0) * R * 4);
+    p.dinner = take((size_t)rows * R * 4);
+    p.split_up = take(up.chunks > 1 ? (size_t)2 * up.chunks * N * R * 4 : 0);
+    p.split_down = take(down.chunks > 1 ? (size_t)2 * down.chunks * K * R * 4 : 0);
   }
   p.total = std::max<size_t>(o, 256);
   return p;
@@ -152,77 +159,76 @@ bool adapters_ok(const rnnlm_adapters *a, int32_t dtype) {
   return a->down && a->up && aligned(a->down, elem_bytes(dtype)) && aligned(a->up, elem_bytes(dtype)) && aligned(a->scale, 4);
 }
 
-template <typename T>
-void launch_order(const AdapterRows &rows, void *perm, void *start, const float *inner, const Transposed<T> &tr, int32_t *flag, hipStream_t st) {
-  hipLaunchKernelGGL(adapter_order_kernel<T>, dim3((rows.M + rows.n + 64) / 64), dim3(1024), 0, st, rows, static_cast<int32_t *>(perm),
-                     static_cast<int32_t *>(start), inner, tr, flag);
+// The rows in order, and where each adapter's begin.
+AdapterRows order_rows(AdapterRows rows, char *ws, const AdapterPlan &p, int32_t *flag, hipStream_t st) {
+  int32_t *perm = reinterpret_cast<int32_t *>(ws + p.perm), *sorted = reinterpret_cast<int32_t *>(ws + p.sorted);
+  hipLaunchKernelGGL(adapter_order_kernel, dim3((rows.M + rows.n + 64) / 64), dim3(1024), 0, st, rows, perm, sorted,
+                     reinterpret_cast<int32_t *>(ws + p.start), flag);
+  rows.perm = perm;
+  rows.sorted = sorted;
+  return rows;
+}
+template <class F>
+void with_r_tiles(int32_t R, F &&f) {
+  switch (adapter_r_tiles(R)) {
+    case 1: f(std::integral_constant<int, 1>()); break;
+    case 2: f(std::integral_constant<int, 2>()); break;
+    case 3: f(std::integral_constant<int, 3>()); break;
+    default: f(std::integral_constant<int, 4>());
+  }
 }
 template <typename T>
 void launch_inner(const InnerArgs<T> &a, hipStream_t st) {
   const dim3 grid((a.rows.M + ADAPTER_TILE - 1) / ADAPTER_TILE, std::min(ADAPTER_TILE, a.rows.n));
-  switch (adapter_r_tiles(a.R)) {
-    case 1: hipLaunchKernelGGL((adapter_inner_kernel<T, 1>), grid, dim3(512), 0, st, a); break;
-    case 2: hipLaunchKernelGGL((adapter_inner_kernel<T, 2>), grid, dim3(512), 0, st, a); break;
-    case 3: hipLaunchKernelGGL((adapter_inner_kernel<T, 3>), grid, dim3(512), 0, st, a); break;
-    default: hipLaunchKernelGGL((adapter_inner_kernel<T, 4>), grid, dim3(512), 0, st, a);
-  }
+  with_r_tiles(a.R, [&](auto r) { hipLaunchKernelGGL((adapter_inner_kernel<T, decltype(r)::value>), grid, dim3(512), 0, st, a); });
 }
-template <typename T, int NF, bool PACKED, bool ACROSS>
+template <typename T, int NF, bool PACKED>
 void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
   const int64_t tiles = (a.rows.M + ADAPTER_TILE - 1) / ADAPTER_TILE, cols = (a.N + 255) / 256;
   // a wave's rows of inner are read once for `blocks` blocks, as long as some 2048 workgroups are left
   a.blocks = (int)std::max<int64_t>(std::min<int64_t>(4, std::max<int64_t>(1, tiles * cols / 2048)), (tiles * cols * 256 + THREADS_MAX - 1) / THREADS_MAX);
   const dim3 grid((unsigned)tiles, (unsigned)((cols + a.blocks - 1) / a.blocks));
-  hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED, ACROSS>), grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED>), grid, dim3(256), 0, st, a);
 }
-template <typename T, bool ACROSS>
+template <typename T>
 void launch_outer(const OuterArgs<T> &a, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
-    if (a.R <= 16) launch_outer_as<T, 1, true, ACROSS>(a, st);
-    else if (a.R <= 32) launch_outer_as<T, 1, false, ACROSS>(a, st);
-    else launch_outer_as<T, 2, false, ACROSS>(a, st);
+    if (a.R <= 16) launch_outer_as<T, 1, true>(a, st);
+    else if (a.R <= 32) launch_outer_as<T, 1, false>(a, st);
+    else launch_outer_as<T, 2, false>(a, st);
   } else {
-    switch (adapter_r_tiles(a.R)) {
-      case 1: launch_outer_as<T, 1, false, ACROSS>(a, st); break;
-      case 2: launch_outer_as<T, 2, false, ACROSS>(a, st); break;
-      case 3: launch_outer_as<T, 3, false, ACROSS>(a, st); break;
-      default: launch_outer_as<T, 4, false, ACROSS>(a, st);
-    }
+    with_r_tiles(a.R, [&](auto r) { launch_outer_as<T, decltype(r)::value, false>(a, st); });
   }
 }
-template <typename T, bool INNER>
-int grad_call(GradArgs<T> a, const GradPlan &p, hipStream_t st) {
-  const dim3 grid(p.blocks, p.chunks), threads(64 * ADAPTER_GRAD_WAVES);
-  a.chunk = p.chunk;
-  if (a.rows.M > 0) {
-    switch (adapter_r_tiles(a.R)) {
-      case 1: hipLaunchKernelGGL((adapter_grad_kernel<T, 1, sizeof(T) == 2 ? 8 : 4, INNER>), grid, threads, 0, st, a); break;
-      case 2: hipLaunchKernelGGL((adapter_grad_kernel<T, 2, sizeof(T) == 2 ? 8 : 4, INNER>), grid, threads, 0, st, a); break;
-      case 3: hipLaunchKernelGGL((adapter_grad_kernel<T, 3, 4, INNER>), grid, threads, 0, st, a); break;
-      default: hipLaunchKernelGGL((adapter_grad_kernel<T, 4, 4, INNER>), grid, threads, 0, st, a);
-    }
-    LAUNCHED();
-  }
-  const JoinArgs j = {a.start, a.split, a.scale, a.G, a.N, a.R, a.chunk, a.rows.n, a.across};
-  const int64_t size = (int64_t)a.N * a.R, parts = std::max<int64_t>(1, std::min<int64_t>((size + 2047) / 2048, 4096 / std::min(a.rows.n, 4096)));
-  hipLaunchKernelGGL(adapter_join_kernel, dim3((unsigned)parts, std::min(a.rows.n, 4096)), dim3(256), 0, st, j);
-  LAUNCHED();
-  return RNNLM_OK;
+template <typename T>
+void launch_grad(const GradArgs<T> &a, const GradPlan &p, hipStream_t st) {
+  with_r_tiles(a.R, [&](auto r) {
+    constexpr int JT = decltype(r)::value;
+    hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, sizeof(T) == 2)>), dim3(p.blocks, p.chunks),
+                       dim3(64 * ADAPTER_GRAD_WAVES), 0, st, a);
+  });
+}
+template <typename T>
+void launch_input_grad(const InputGradArgs<T> &a, const GradPlan &p, hipStream_t st) {
+  with_r_tiles(a.R, [&](auto r) {
+    constexpr int JT = decltype(r)::value;
+    hipLaunchKernelGGL((adapter_input_grad_kernel<T, JT, adapter_input_tiles(JT, sizeof(T) == 2)>), dim3(p.blocks, p.chunks),
+                       dim3(64 * ADAPTER_GRAD_WAVES), 0, st, a);
+  });
 }
 
 template <typename T>
 int adapter_forward(const T *x, int64_t ldx, int64_t M, int32_t K, int32_t N, const rnnlm_adapters &a, const int32_t *ids, const T *base,
                     int64_t ldb, T *out, int64_t ldo, float *inner, int32_t *flag, char *ws, const AdapterPlan &p, hipStream_t st) {
-  AdapterRows rows = {ids, nullptr, (int)M, a.n};
+  AdapterRows rows = {ids, nullptr, nullptr, (int)M, a.n};
   if (M > ADAPTER_UNORDERED * ADAPTER_TILE) {
-    launch_order<T>(rows, ws + p.perm, ws + p.start, nullptr, Transposed<T>{}, flag, st);
+    rows = order_rows(rows, ws, p, flag, st);
     LAUNCHED();
-    rows.perm = reinterpret_cast<int32_t *>(ws + p.perm);
   }
   if (!inner) inner = reinterpret_cast<float *>(ws + p.inner);
   launch_inner<T>({rows, x, static_cast<const T *>(a.down), ldx, K, a.R, inner, flag}, st);
   LAUNCHED();
-  launch_outer<T, false>({rows, inner, false, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1}, st);
+  launch_outer<T>({rows, inner, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1}, st);
   LAUNCHED();
   return RNNLM_OK;
 }
@@ -232,28 +238,32 @@ int adapter_backward(const T *dout, int64_t ldd, const T *x, int64_t ldx, const 
                      const rnnlm_adapters &a, const int32_t *ids, float *ddown, float *dup, T *dx, int64_t lddx, int32_t *flag, char *ws,
                      const AdapterPlan &p, hipStream_t st) {
   const int32_t dtype = sizeof(T) == 4 ? RNNLM_DTYPE_FP32 : RNNLM_DTYPE_BF16;
-  const AdapterRows rows = {ids, reinterpret_cast<int32_t *>(ws + p.perm), (int)M, a.n};
   const int32_t *start = reinterpret_cast<int32_t *>(ws + p.start);
-  const Transposed<T> tr_inner = {reinterpret_cast<T *>(ws + p.tr_inner), p.Mp, a.R};
-  const Transposed<T> tr_dinner = {reinterpret_cast<T *>(ws + p.tr_dinner), p.Mp, a.R};
-  float *dinner = reinterpret_cast<float *>(ws + p.dinner), *part = reinterpret_cast<float *>(ws + p.part);
-  float *split = reinterpret_cast<float *>(ws + p.split);
-  launch_order<T>(rows, ws + p.perm, ws + p.start, inner, tr_inner, flag, st);
+  const auto floats = [&](size_t at) { return reinterpret_cast<float *>(ws + at); };
+  const AdapterRows rows = order_rows({ids, nullptr, nullptr, (int)M, a.n}, ws, p, flag, st);
   LAUNCHED();
-  const GradPlan up = adapter_grad_plan(M, N, a.R, dtype), down = adapter_grad_plan(M, K, a.R, dtype);
-  int rc = grad_call<T, true>({rows, start, dout, ldd, tr_inner, static_cast<const T *>(a.up), a.scale, dup, split, part, N, a.R, 0, false}, up, st);
-  if (rc) return rc;
+  const GradPlan up = adapter_up_plan(M, N, a.R, dtype), down = adapter_down_plan(M, K, a.R, dtype);
   if (M > 0) {
-    hipLaunchKernelGGL(adapter_dinner_kernel<T>, dim3((unsigned)((M * a.R + 255) / 256)), dim3(256), 0, st,
-                       DinnerArgs<T>{rows, start, part, a.scale, dinner, tr_dinner, up.blocks, a.R});
+    launch_grad<T>({rows, start, dout, ldd, inner, static_cast<const T *>(a.up), a.scale, dup, floats(p.split_up), floats(p.part), N, a.R, up.chunk},
+                   up, st);
+    LAUNCHED();
+    const bool apart = up.blocks > ADAPTER_BLOCKS_INSIDE;
+    if (apart) {
+      hipLaunchKernelGGL(adapter_blocks_kernel, dim3((unsigned)((M * a.R + 63) / 64)), dim3(1024), 0, st, floats(p.part), up.blocks, (long)M * a.R,
+                         floats(p.dinner));
+      LAUNCHED();
+    }
+    launch_input_grad<T>({rows, start, x, static_cast<const T *>(a.down), a.scale, floats(apart ? p.dinner : p.part), ddown, floats(p.split_down), dx,
+                          ldx, lddx, K, a.R, down.chunk, apart ? 1 : up.blocks},
+                         down, st);
     LAUNCHED();
   }
-  rc = grad_call<T, false>({rows, start, x, ldx, tr_dinner, nullptr, nullptr, ddown, split, nullptr, K, a.R, 0, true}, down, st);
-  if (rc) return rc;
-  if (dx && M > 0) {
-    launch_outer<T, true>({rows, dinner, true, static_cast<const T *>(a.down), nullptr, nullptr, dx, 0, lddx, K, a.R, 1}, st);
-    LAUNCHED();
-  }
+  const int64_t size = (int64_t)std::max(N, K) * a.R;
+  const unsigned ids_y = std::min(a.n, 2048), parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>((size + 1023) / 1024, 4096 / ids_y));
+  hipLaunchKernelGGL(adapter_join_kernel, dim3(parts, ids_y, 2), dim3(256), 0, st, start, a.n,
+                     JoinArgs{floats(p.split_up), a.scale, dup, (int64_t)N * a.R, up.chunk},
+                     JoinArgs{floats(p.split_down), nullptr, ddown, (int64_t)K * a.R, down.chunk});
+  LAUNCHED();
   return RNNLM_OK;
 }
 

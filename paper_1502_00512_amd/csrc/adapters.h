@@ -16,7 +16,7 @@ constexpr int ADAPTER_TILE = 32;   // rows of a tile
 constexpr int ADAPTER_R_MAX = 64;
 
 struct AdapterRows {
-  const int32_t *ids, *perm;  // perm: rows in the order of their adapters; nullptr: as they are
+  const int32_t *ids, *perm, *sorted;  // rows in the order of their adapters, and those; perm = nullptr: rows as they are
   int M, n;
   // adapter of a row; n: none
   __device__ int key(int row) const {
@@ -24,6 +24,7 @@ struct AdapterRows {
     return a >= 0 && a < n ? a : n;
   }
   __device__ int row(int pos) const { return perm ? perm[pos] : pos; }
+  __device__ int key_at(int pos) const { return perm ? sorted[pos] : key(pos); }
 };
 
 // A lane's 16 bytes of an operand: VEC consecutive k of row (or column) l % 16, from k = (l / 16) VEC of a chunk of CHUNK on.
@@ -94,65 +95,51 @@ __device__ inline void bf16_parts(float x, bf16_t (&p)[PARTS]) {
   }
 }
 
-// Numbers of the rows in the order of their adapters, transposed: [part][r][position].
+// bf16 parts of a number whose products are summed in fp32.
 template <typename T>
-struct Transposed {
-  static constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
-  T *at;
-  long Mp;  // positions of a line, more than any tile reads
-  int R;
-  __device__ void put(int r, long pos, float v) const {
-    if constexpr (PARTS == 1) {
-      at[r * Mp + pos] = v;
-    } else {
-      bf16_t p[PARTS];
-      bf16_parts<PARTS>(v, p);
-#pragma unroll
-      for (int i = 0; i < PARTS; ++i) at[((long)i * R + r) * Mp + pos] = p[i];
-    }
-  }
-};
+constexpr int GRAD_PARTS = sizeof(T) == 2 ? 3 : 1;
 
-// perm: the rows ordered by (adapter, row), rows without one last; start[a]: first position of adapter a, start[n]: of those
-// rows.  64 questions a workgroup, each answered by counting all smaller keys: M (M + n) / 64 comparisons of a wave (2560 rows
-// 2 us).  inner (may be nullptr) is transposed on the way.
-template <typename T>
-__global__ void __launch_bounds__(1024) adapter_order_kernel(const AdapterRows rows, int32_t *__restrict__ perm, int32_t *__restrict__ start,
-                                                             const float *__restrict__ inner, const Transposed<T> tr, int32_t *range_flag) {
-  __shared__ int32_t keys[4096];
+// perm: the rows ordered by (adapter, row), rows without one last; sorted: their adapters; start[a]: first position of adapter
+// a, start[n]: of those rows.  64 questions a workgroup, each answered by counting smaller keys (equal ones of earlier rows,
+// too): M (M + n) / 64 comparisons of a wave.
+static __global__ void __launch_bounds__(1024) adapter_order_kernel(const AdapterRows rows, int32_t *__restrict__ perm,
+                                                                    int32_t *__restrict__ sorted, int32_t *__restrict__ start,
+                                                                    int32_t *range_flag) {
+  constexpr int KEYS = 4096;
+  __shared__ __align__(16) int32_t keys[KEYS];
   __shared__ int32_t cnt[16][64];
-  __shared__ int32_t rank_of[64];
-  const int lane = threadIdx.x & 63, slice = threadIdx.x >> 6, M = rows.M;
-  const int q = blockIdx.x * 64 + lane;
+  const int lane = threadIdx.x & 63, slice = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), M = rows.M, first = blockIdx.x * 64;
+  const int q = first + lane;
   const int mine = q < M ? rows.key(q) : q - M;
   if (slice == 0 && q < M && rows.ids[q] >= rows.n && range_flag) *range_flag = 1;
   int rank = 0;
-  for (int base = 0; base < M; base += 4096) {
-    const int n = min(4096, M - base);
-    for (int i = threadIdx.x; i < n; i += 1024) keys[i] = rows.key(base + i);
+  for (int base = 0; base < M; base += KEYS) {
+    const int n = min(KEYS, M - base);
+    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 1024) keys[i] = i < n ? rows.key(base + i) : 0x7fffffff;
     __syncthreads();
-    for (int i = slice; i < n; i += 16) {
-      const int k = keys[i];
-      rank += (k < mine) || (k == mine && base + i < q && q < M);
+    // 64 keys at a time: those in front of this workgroup's own rows count where they are equal, too
+    for (int i = slice * 64; i < n; i += 1024) {
+      const int4 *k = reinterpret_cast<const int4 *>(keys + i);
+      const bool own = base + i == first;
+      const int below = q < M && base + i < first ? mine + 1 : mine;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int4 v = k[j];
+        rank += (v.x < below) + (v.y < below) + (v.z < below) + (v.w < below);
+      }
+      if (own && q < M)
+        for (int j = 0; j < lane; ++j) rank += keys[i + j] == mine;
     }
     __syncthreads();
   }
   cnt[slice][lane] = rank;
   __syncthreads();
-  if (slice == 0) {
-    int r = 0;
-    for (int g = 0; g < 16; ++g) r += cnt[g][lane];
-    rank_of[lane] = r;
-    if (q < M) perm[r] = q;
-    else if (q - M <= rows.n) start[q - M] = r;
-  }
-  if (!inner) return;
-  __syncthreads();
-  const int here = min(64, M - (int)blockIdx.x * 64);
-  for (int i = threadIdx.x; i < here * tr.R; i += 1024) {
-    const int m = i / tr.R, r = i % tr.R;
-    tr.put(r, rank_of[m], inner[((long)blockIdx.x * 64 + m) * tr.R + r]);
-  }
+  if (slice != 0) return;
+  int r = 0;
+#pragma unroll
+  for (int g = 0; g < 16; ++g) r += cnt[g][lane];
+  if (q < M) perm[r] = q, sorted[r] = mine;
+  else if (q - M <= rows.n) start[q - M] = r;
 }
 
 // What a wave knows of a tile: lane l < 32 (and l + 32) the row at position 32 tile + l and its adapter.
@@ -161,7 +148,7 @@ struct AdapterTile {
   __device__ AdapterTile(const AdapterRows &r, int first) {
     const int pos = first + (threadIdx.x & 31);
     row = pos < r.M ? r.row(pos) : -1;
-    key = row >= 0 ? r.key(row) : r.n;
+    key = pos < r.M ? r.key_at(pos) : r.n;
   }
   // The adapters of the tile one after the other, in the order of their first rows: the next one behind `left` (lanes not yet
   // dealt with), n when there is none.
@@ -213,7 +200,6 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
     xs[t] = a.x + (ok[t] ? row : 0) * a.ldx;
   }
   f32x4_t acc[RT][2] = {};
-#pragma unroll 2
   for (int k0 = wave * CHUNK; k0 < a.K; k0 += WAVES * CHUNK) {
     const int k = k0 + q * VEC, have = a.K - k;
     slot_t fx[2], fd[RT];
@@ -248,9 +234,8 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
 template <typename T>
 struct OuterArgs {
   AdapterRows rows;
-  const float *inner;  // [M][R], of rows or (by_position) of positions
-  bool by_position;
-  const T *up;         // [n][N][R], or (template ACROSS) [n][R][N]
+  const float *inner;  // [M][R]
+  const T *up;         // [n][N][R]
   const float *scale;  // may be nullptr
   const T *base;       // may be nullptr (zeros), may be out
   T *out;
@@ -260,14 +245,14 @@ struct OuterArgs {
 
 // out = base + f up inner: a wave a tile and 64 columns, `blocks` times; through LDS so that base and out move in whole lines.
 // Bound by HBM.  NF: operand slots of R.  PACKED (bf16, R <= 16): both parts of inner in one product, beside one another.
-template <typename T, int NF, bool PACKED, bool ACROSS>
+template <typename T, int NF, bool PACKED>
 __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, COLS = 64, PITCH = COLS + 4;
   constexpr int PARTS = sizeof(T) == 4 || PACKED ? 1 : 2, LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = TILE / ROWS;
   __shared__ float turn[4][TILE][PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
-  const int first = blockIdx.x * TILE, n = a.rows.n, N = a.N, R = a.R;
-  const AdapterTile tile(a.rows, first);
+  const int n = a.rows.n, N = a.N, R = a.R;
+  const AdapterTile tile(a.rows, blockIdx.x * TILE);
   const int kq = (PACKED ? q & 1 : q) * VEC;
   // inner of the tile's rows (columns of the product), times the adapter's factor
   slot_t fu[2][NF][PARTS];
@@ -278,7 +263,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
     key[t] = __shfl(tile.key, t * 16 + c);
     const bool ok = row >= 0 && key[t] < n;
     const float f = ok && a.scale ? a.scale[key[t]] : 1.0f;
-    const float *u = a.inner + (a.by_position ? (long)first + t * 16 + c : (long)row) * R;
+    const float *u = a.inner + (long)row * R;
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
       union {
@@ -331,19 +316,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
           const int col = v0 + v * 16 + c, k = i * CHUNK + kq;
-          if constexpr (ACROSS) {
-            union {
-              slot_t s;
-              T e[VEC];
-            } o;
-            o.s = slot_t{0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-              if (col < N && k + e < R) o.e[e] = up[(long)(k + e) * N + col];
-            fa[v][i] = o.s;
-          } else {
-            fa[v][i] = load_elems(up + (long)col * R + k, col < N ? R - k : 0, (long)(N - col) * R - k);
-          }
+          fa[v][i] = load_elems(up + (long)col * R + k, col < N ? R - k : 0, (long)(N - col) * R - k);
         }
 #pragma unroll
       for (int v = 0; v < 4; ++v)
@@ -385,193 +358,501 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
   }
 }
 
-// A gradient that is a sum over rows, of all adapters: G[a][v][r] = f_a sum_m d[m][v] w[m][r], w as Transposed; and (template
-// INNER) part[v block][position][r] = sum over the block's v of d[m][v] up[a][v][r].
-// Workgroups: chunks of positions x blocks of columns.  A chunk may hold many adapters and an adapter lie in many chunks: where
-// it has a chunk for itself or shares it whole, G is written, else a part, which adapter_join_kernel sums up.
+// VEC consecutive rows from k0 + (l / 16) VEC on of column c0 + l % 16 of a tile in LDS: an operand whose k are the rows.
+// bf16: the transposing read; of each 16 lanes, lane s points at 4 elements of row s / 4 and gets 4 rows of its column.
+template <typename T>
+__device__ inline slot_t across(const T *tile, int pitch, int k0, int c0) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+  if constexpr (sizeof(T) == 2) {
+    typedef short s16x4_t __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4_t *lds_ptr_t;
+    const T *p = tile + (k0 + q * 8 + (c >> 2)) * pitch + c0 + 4 * (c & 3);
+    union {
+      s16x4_t h[2];
+      slot_t s;
+    } u;
+    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p));
+    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr_t)(p + 4 * pitch));
+    return u.s;
+  } else {
+    const T *p = tile + (k0 + q * 4) * pitch + c0 + c;
+    return slot_t{__builtin_bit_cast(unsigned, p[0]), __builtin_bit_cast(unsigned, p[pitch]), __builtin_bit_cast(unsigned, p[2 * pitch]),
+                  __builtin_bit_cast(unsigned, p[3 * pitch])};
+  }
+}
+// Of two parts (0, 1) of a number packed for bf16 operands, or the number itself.
+template <typename T, int PARTS>
+__device__ inline void operand_parts(const float (&v)[Mma<T>::VEC], slot_t (&s)[PARTS]) {
+  union {
+    slot_t s[PARTS];
+    T e[PARTS][Mma<T>::VEC];
+  } o;
+#pragma unroll
+  for (int e = 0; e < Mma<T>::VEC; ++e) {
+    if constexpr (sizeof(T) == 4) {
+      o.e[0][e] = v[e];
+    } else {
+      bf16_t p[PARTS];
+      bf16_parts<PARTS>(v[e], p);
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) o.e[i][e] = p[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) s[i] = o.s[i];
+}
+
+// A wave's 32 rows x COLS columns of an array, row by row by way of registers (requested early) into LDS.
+template <typename T, int COLS>
+struct WaveTile {
+  static constexpr int VEC = Mma<T>::VEC, LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = ADAPTER_TILE / ROWS, PITCH = COLS + 16 / sizeof(T);
+  slot_t raw[MOVES];
+  int rows;  // of lane l, the row of l % 32 (the last ones may repeat one that is there)
+  // columns v0.. of N; a block that sticks out is fetched element by element (store)
+  __device__ void load(const T *d, long ld, int rows_, int v0, int N) {
+    const int lane = threadIdx.x & 63;
+    rows = rows_;
+    if (v0 + COLS <= N) {
+      const T *at = d + v0 + lane % LANES * VEC;
+#pragma unroll
+      for (int i = 0; i < MOVES; ++i)
+        raw[i] = *reinterpret_cast<const typename SlotOf<T>::type *>(at + __shfl(rows, i * ROWS + lane / LANES) * ld);
+    }
+  }
+  // zeros in place of the rows from `here` on
+  __device__ void store(T (*tile)[PITCH], const T *d, long ld, int here, int v0, int N) const {
+    const int lane = threadIdx.x & 63;
+    if (v0 + COLS <= N) {
+#pragma unroll
+      for (int i = 0; i < MOVES; ++i) {
+        const int m = i * ROWS + lane / LANES;
+        *reinterpret_cast<slot_t *>(&tile[m][lane % LANES * VEC]) = m < here ? raw[i] : slot_t{0u, 0u, 0u, 0u};
+      }
+    } else {
+      for (int i = lane; i < ADAPTER_TILE * COLS; i += 64) {
+        const int m = i / COLS, col = v0 + i % COLS, row = __shfl(rows, m);
+        tile[m][i % COLS] = m < here && col < N ? d[row * ld + col] : from_f32<T>(0.0f);
+      }
+    }
+  }
+};
+
+// Gradients that are sums over rows.  Workgroups: chunks of positions x blocks of columns.  A chunk may hold many adapters and
+// an adapter lie in many chunks: where all of an adapter lies in one, its gradient is written, else a part of it, which
+// adapter_join_kernel sums up.  Part of adapter a in chunk i (in units of a whole gradient): an adapter that starts in front of
+// the chunk has the first, one that goes on behind it the second.
+__device__ inline long adapter_split(int a_start, int chunk, int i) { return 2L * i + (a_start < i * chunk ? 0 : 1); }
+
+constexpr int ADAPTER_GRAD_WAVES = 8;
+
 template <typename T>
 struct GradArgs {
   AdapterRows rows;
   const int32_t *start;
   const T *d;
   long ldd;
-  Transposed<T> w;
+  const float *inner;  // [M][R]
   const T *up;
   const float *scale;  // may be nullptr
-  float *G;            // [n][N][R], or (across) [n][R][N]
+  float *G;            // [n][N][R]
   float *split;        // [2 chunks][N][R]
   float *part;         // [blocks of columns][M][R]
   int N, R, chunk;     // positions of a chunk
-  bool across;
 };
 
-// Part of adapter a in chunk i, in units of N R: an adapter that starts in front of the chunk has the first, one that goes on
-// behind it the second.
-__device__ inline long adapter_split(int a_start, int chunk, int i) { return 2L * i + (a_start < i * chunk ? 0 : 1); }
-
-template <typename T, int JT, int VT, bool INNER>
-__global__ void __launch_bounds__(512) adapter_grad_kernel(const GradArgs<T> a) {
-  constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = 8, COLS = 16 * VT, PARTS = Transposed<T>::PARTS;
-  constexpr int PITCH = COLS + 16 / sizeof(T), LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = TILE / ROWS;
-  constexpr int MK = TILE / CHUNK, VK = COLS / CHUNK;  // slots of the rows, of the columns
-  __shared__ __align__(16) T buf[WAVES][TILE][PITCH];
-  __shared__ float red[INNER ? WAVES : 1][INNER ? TILE : 1][INNER ? JT * 16 + 4 : 1];
+// dup[a][v][r] = f_a sum_m dout[m][v] inner[m][r], and of every block of columns part[position][r] = sum_v dout[m][v] up[a][v][r]:
+// dout is read once, which bounds it.
+template <typename T, int JT, int VT>
+__global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(const GradArgs<T> a) {
+  constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = ADAPTER_GRAD_WAVES, COLS = 16 * VT;
+  constexpr int THREADS = 64 * WAVES, PARTS = GRAD_PARTS<T>, MK = TILE / CHUNK, VK = COLS / CHUNK;  // slots of the rows, of the columns
+  constexpr int REDS = JT <= 2 ? 2 : 1;  // (as many as LDS holds)
+  constexpr int WIDTH = JT == 3 ? 64 : JT * 16, STEP = THREADS / WIDTH, EACH = TILE / STEP;  // a tile's inner numbers over the threads
+  typedef WaveTile<T, COLS> Tile;
+  __shared__ __align__(16) T buf[WAVES][TILE][Tile::PITCH];
+  __shared__ __align__(16) float red[REDS][WAVES][TILE][JT * 16 + 4];
+  __shared__ __align__(16) T turned[2][PARTS][JT * 16][TILE + 16 / sizeof(T)];  // inner of two tiles, its parts, [r][m]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int N = a.N, R = a.R, n = a.rows.n, block = blockIdx.x, ci = blockIdx.y;
   const int v0 = (block * WAVES + wave) * COLS;
-  const int present = a.start[n], end_chunk = min((ci + 1) * a.chunk, present);
-  const int lr = lane / LANES, lc = lane % LANES * VEC, have = N - (v0 + lc);
-  T(*my)[PITCH] = buf[wave];
+  const int end_chunk = min((ci + 1) * a.chunk, a.start[n]);
+  T(*my)[Tile::PITCH] = buf[wave];
+  int turn = 0;
+  const int tr = threadIdx.x % WIDTH, tm = threadIdx.x / WIDTH;  // this thread's r, and first m
   for (int pos = ci * a.chunk; pos < end_chunk;) {
-    const int id = __builtin_amdgcn_readfirstlane(a.rows.key(a.rows.row(pos)));
+    const int id = __builtin_amdgcn_readfirstlane(a.rows.key_at(pos));
+    // rows of a tile: of lane l (and l + 32) that of position l; the last ones may be the last row again
+    const auto rows_at = [&](int at, int end) { return a.rows.row(min(at + (lane & 31), end - 1)); };
     const int a_start = a.start[id], a_end = a.start[id + 1], end = min(a_end, end_chunk);
-    slot_t fup[INNER ? VK : 1][INNER ? JT : 1];
-    if constexpr (INNER) {
-      const T *up = a.up + (long)id * N * R;
+    const T *up = a.up + (long)id * N * R;
+    int rows = rows_at(pos, end), next = rows_at(min(pos + TILE, end - 1), end);
+    Tile tile;
+    tile.load(a.d, a.ldd, rows, v0, N);
+    float in[EACH];
+    const auto inner_load = [&](int rows) {
 #pragma unroll
-      for (int k = 0; k < VK; ++k)
+      for (int i = 0; i < EACH; ++i) {
+        const long row = __shfl(rows, tm + i * STEP);
+        in[i] = tr < R ? a.inner[row * R + tr] : 0.0f;
+      }
+    };
+    const auto inner_store = [&](int here) {
+      if (tr >= JT * 16) return;
 #pragma unroll
-        for (int j = 0; j < JT; ++j) {
-          union {
-            slot_t s;
-            T e[VEC];
-          } o;
-          o.s = slot_t{0u, 0u, 0u, 0u};
+      for (int i = 0; i < EACH; ++i) {
+        const int m = tm + i * STEP;
+        const float v = m < here ? in[i] : 0.0f;
+        if constexpr (PARTS == 1) {
+          turned[turn][0][tr][m] = v;
+        } else {
+          bf16_t p[PARTS];
+          bf16_parts<PARTS>(v, p);
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const int v = v0 + k * CHUNK + q * VEC + e, r = j * 16 + c;
-            if (v < N && r < R) o.e[e] = up[(long)v * R + r];
-          }
-          fup[k][j] = o.s;
+          for (int k = 0; k < PARTS; ++k) turned[turn][k][tr][m] = p[k];
         }
+      }
+    };
+    inner_load(rows);
+    slot_t fup[VK][JT];  // up[v][r]: k = v (r >= R: anything, those rows of the products are dropped)
+    {
+      // a wave's part of up is contiguous: CHUNK R elements at a time, by way of LDS
+      constexpr int PITCH = JT * 16 + 16 / sizeof(T);
+      T *stage = &my[0][0];
+      if (v0 + COLS <= N) {
+#pragma unroll
+        for (int k = 0; k < VK; ++k)
+#pragma unroll
+          for (int j = 0; j < JT; ++j)
+            fup[k][j] = *reinterpret_cast<const typename SlotOf<T>::type *>(up + (unsigned)((v0 + k * CHUNK) * R + min(j * 64 + lane, 4 * R - 1) * VEC));
+      }
+#pragma unroll
+      for (int k = 0; k < VK; ++k) {
+        if (v0 + COLS <= N) {
+#pragma unroll
+          for (int j = 0; j < JT; ++j) {
+            const int i = min(j * 64 + lane, 4 * R - 1) * VEC;
+            int v = i / R, r = i - v * R;
+            if (R % VEC == 0) {
+              *reinterpret_cast<slot_t *>(stage + v * PITCH + r) = fup[k][j];
+            } else {
+              union {
+                slot_t s;
+                T e[VEC];
+              } o;
+              o.s = fup[k][j];
+#pragma unroll
+              for (int e = 0; e < VEC; ++e) {
+                stage[v * PITCH + r] = o.e[e];
+                r = r + 1 == R ? (++v, 0) : r + 1;
+              }
+            }
+          }
+        } else {
+          const int v = v0 + k * CHUNK, there = max(0, min(CHUNK, N - v));
+          for (int i = lane; i < CHUNK * R; i += 64)
+            stage[i / R * PITCH + i % R] = i < there * R ? up[(unsigned)(v * R + i)] : from_f32<T>(0.0f);
+        }
+        wave_sync();
+#pragma unroll
+        for (int j = 0; j < JT; ++j) fup[k][j] = across(stage, PITCH, 0, j * 16);
+        wave_sync();
+      }
     }
+    inner_store(min(TILE, end - pos));
+    __syncthreads();
     f32x4_t g[VT][JT] = {};
     for (; pos < end; pos += TILE) {
       const int here = min(TILE, end - pos);
-      const int row_of = a.rows.row(pos + min(lane & 31, here - 1));
-#pragma unroll
-      for (int i = 0; i < MOVES; ++i) {
-        const int m = i * ROWS + lr, row = __shfl(row_of, m);
-        *reinterpret_cast<slot_t *>(&my[m][lc]) = load_elems(a.d + row * a.ldd + v0 + lc, m < here ? have : 0, have);
-      }
+      const bool more = pos + TILE < end;
+      tile.store(my, a.d, a.ldd, here, v0, N);
       wave_sync();
-      slot_t fw[MK][JT][PARTS];
+      if (more) {
+        tile.load(a.d, a.ldd, next, v0, N);
+        inner_load(next);
+        next = rows_at(min(pos + 2 * TILE, end - 1), end);
+      }
+      f32x4_t acc[JT][2] = {};
+#pragma unroll
+      for (int k = 0; k < VK; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const slot_t fd = *reinterpret_cast<const slot_t *>(&my[t * 16 + c][k * CHUNK + q * VEC]);
+#pragma unroll
+          for (int j = 0; j < JT; ++j) Mma<T>::add(acc[j][t], fup[k][j], fd);
+        }
+      float(*r_of)[TILE][JT * 16 + 4] = red[REDS == 2 ? turn : 0];
+#pragma unroll
+      for (int j = 0; j < JT; ++j)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&r_of[wave][t * 16 + c][j * 16 + q * 4]) = acc[j][t];
+      slot_t fw[MK][JT][PARTS];  // inner[m][r]: k = m
 #pragma unroll
       for (int k = 0; k < MK; ++k)
 #pragma unroll
         for (int j = 0; j < JT; ++j)
 #pragma unroll
-          for (int p = 0; p < PARTS; ++p) {
-            const int r = j * 16 + c, m = k * CHUNK + q * VEC;
-            const T *src = a.w.at + ((long)p * R + (r < R ? r : 0)) * a.w.Mp + pos + m;
-            fw[k][j][p] = load_elems(src, r < R ? here - m : 0, VEC);
-          }
+          for (int p = 0; p < PARTS; ++p) fw[k][j][p] = *reinterpret_cast<const slot_t *>(&turned[turn][p][j * 16 + c][k * CHUNK + q * VEC]);
 #pragma unroll
       for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int k = 0; k < MK; ++k) {
-          union {
-            slot_t s;
-            T e[VEC];
-          } o;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) o.e[e] = my[k * CHUNK + q * VEC + e][v * 16 + c];
+          const slot_t fd = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
 #pragma unroll
           for (int j = 0; j < JT; ++j)
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[k][j][p], o.s);
+            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[k][j][p], fd);
         }
-      if constexpr (INNER) {
-        f32x4_t acc[JT][2] = {};
+      turn ^= 1;
+      if (more) inner_store(min(TILE, end - pos - TILE));
+      __syncthreads();
+      float *part = a.part + ((long)block * a.rows.M + pos) * R;
+      for (int i = threadIdx.x; i < here * R; i += THREADS) {
+        const int m = i / R, r = i - m * R;
+        float s = 0.0f;
 #pragma unroll
-        for (int k = 0; k < VK; ++k)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const slot_t fd = *reinterpret_cast<const slot_t *>(&my[t * 16 + c][k * CHUNK + q * VEC]);
-#pragma unroll
-            for (int j = 0; j < JT; ++j) Mma<T>::add(acc[j][t], fup[k][j], fd);
-          }
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-          for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&red[wave][t * 16 + c][j * 16 + q * 4]) = acc[j][t];
-        __syncthreads();
-        for (int i = threadIdx.x; i < here * R; i += 512) {
-          const int m = i / R, r = i % R;
-          float s = 0.0f;
-#pragma unroll
-          for (int w = 0; w < WAVES; ++w) s += red[w][m][r];
-          a.part[((long)block * a.rows.M + pos + m) * R + r] = s;
-        }
-        __syncthreads();
+        for (int w = 0; w < WAVES; ++w) s += r_of[w][m][r];
+        part[i] = s;
       }
-      wave_sync();
+      if (REDS == 1) __syncthreads();
     }
     pos = end;
     const bool whole = a_start >= ci * a.chunk && a_end == end;
     float *G = whole ? a.G + (long)id * N * R : a.split + adapter_split(a_start, a.chunk, ci) * N * R;
     const float f = whole && a.scale ? a.scale[id] : 1.0f;
-    const bool across = whole && a.across;
 #pragma unroll
     for (int v = 0; v < VT; ++v) {
       const int col = v0 + v * 16 + c;
-      if (col >= N) continue;
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+        const int r = j * 16 + q * 4;
+        float *dst = G + (unsigned)(col * R + r);
+        const f32x4_t x = g[v][j] * f;
+        if (col < N && r + 4 <= R) {
+          *reinterpret_cast<f32x4_t *>(__builtin_assume_aligned(dst, 4)) = x;
+        } else if (col < N) {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (r + e < R) dst[e] = x[e];
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+struct InputGradArgs {
+  AdapterRows rows;
+  const int32_t *start;
+  const T *x, *down;
+  const float *scale;  // may be nullptr
+  const float *part;   // [blocks][M][R]
+  float *G, *split;    // [n][R][K]; [2 chunks][R][K]
+  T *dx;               // may be nullptr
+  long ldx, lddx;
+  int K, R, chunk, blocks;
+};
+
+// dinner of a tile from the blocks' parts, then ddown[a][r][k] = sum_m dinner[m][r] x[m][k] and dx[m][k] = sum_r down[a][r][k]
+// dinner[m][r].  Sums of parts are formed once for every 512 columns of x.
+template <typename T, int JT, int VT>
+__global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_kernel(const InputGradArgs<T> a) {
+  constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = ADAPTER_GRAD_WAVES, COLS = 16 * VT;
+  constexpr int THREADS = 64 * WAVES, PARTS = GRAD_PARTS<T>, PARTS2 = sizeof(T) == 2 ? 2 : 1, MK = TILE / CHUNK;
+  constexpr int JK = (JT * 16 + CHUNK - 1) / CHUNK, RP = JK * CHUNK, DP = RP + 4;
+  typedef WaveTile<T, COLS> Tile;
+  __shared__ __align__(16) T buf[WAVES][TILE][Tile::PITCH];
+  __shared__ __align__(16) float dinner[TILE][DP];
+  __shared__ float sums[THREADS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+  const int K = a.K, R = a.R, n = a.rows.n, ci = blockIdx.y;
+  const int k0 = (blockIdx.x * WAVES + wave) * COLS;
+  const int present = a.start[n], end_chunk = min((ci + 1) * a.chunk, present);
+  T(*my)[Tile::PITCH] = buf[wave];
+  // rows without an adapter
+  if (a.dx)
+    for (int pos = max(ci * a.chunk, present) + wave; pos < min((ci + 1) * a.chunk, a.rows.M); pos += WAVES) {
+      const int row = a.rows.row(pos);
+      const int end = min(K, (int)(blockIdx.x + 1) * WAVES * COLS);
+      for (int k = blockIdx.x * WAVES * COLS + lane; k < end; k += 64) a.dx[row * a.lddx + k] = from_f32<T>(0.0f);
+    }
+  for (int i = threadIdx.x; i < TILE * DP; i += THREADS) dinner[i / DP][i % DP] = 0.0f;  // (behind R as well)
+  __syncthreads();
+  for (int pos = ci * a.chunk; pos < end_chunk;) {
+    const int id = __builtin_amdgcn_readfirstlane(a.rows.key_at(pos));
+    const int a_start = a.start[id], a_end = a.start[id + 1], end = min(a_end, end_chunk);
+    const float f = a.scale ? a.scale[id] : 1.0f;
+    const T *down = a.down + (long)id * R * K;
+    slot_t fdown[VT][JK];  // down[r][k]: k of the product = r
+    if (a.dx) {
+#pragma unroll
+      for (int j = 0; j < JK; j += MK) {
+        const int r0 = j * CHUNK;
+        Tile t;
+        t.load(down, K, min(r0 + (lane & 31), R - 1), k0, K);
+        t.store(my, down, K, R - r0, k0, K);
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < MK && j + i < JK; ++i)
+#pragma unroll
+          for (int v = 0; v < VT; ++v) fdown[v][j + i] = across(&my[0][0], Tile::PITCH, i * CHUNK, v * 16);
+        wave_sync();
+      }
+    }
+    f32x4_t g[VT][JT] = {};
+    for (; pos < end; pos += TILE) {
+      const int here = min(TILE, end - pos);
+      const int rows = a.rows.row(min(pos + (lane & 31), end - 1));
+      Tile tile;
+      tile.load(a.x, a.ldx, rows, k0, K);
+      {  // the tile's part of every block is contiguous: groups of threads share out the blocks where it is short
+        const int size = here * R;
+        int width = 32;
+        while (width < size && width < THREADS) width *= 2;
+        const int groups = THREADS / width, group = threadIdx.x / width, at = threadIdx.x % width;
+        const float *part = a.part + (long)pos * R;
+        const long step = (long)a.rows.M * R;
+        for (int i = at; i < size; i += width) {
+          float s = 0.0f;
+#pragma unroll 8
+          for (int b = group; b < a.blocks; b += groups) s += part[b * step + i];
+          if (groups == 1) dinner[i / R][i % R] = s * f;
+          else sums[threadIdx.x] = s;
+        }
+        if (groups > 1) {
+          __syncthreads();
+          if (threadIdx.x < size) {
+            float s = 0.0f;
+            for (int i = 0; i < groups; ++i) s += sums[i * width + threadIdx.x];
+            dinner[threadIdx.x / R][threadIdx.x % R] = s * f;
+          }
+        }
+        for (int i = size + threadIdx.x; i < TILE * R; i += THREADS) dinner[i / R][i % R] = 0.0f;
+      }
+      tile.store(my, a.x, a.ldx, here, k0, K);
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+        slot_t fw[MK][PARTS];  // dinner[m][r]: k = m
+#pragma unroll
+        for (int k = 0; k < MK; ++k) {
+          float v[VEC];
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[e] = dinner[k * CHUNK + q * VEC + e][j * 16 + c];
+          operand_parts<T>(v, fw[k]);
+        }
+#pragma unroll
+        for (int v = 0; v < VT; ++v)
+#pragma unroll
+          for (int k = 0; k < MK; ++k) {
+            const slot_t fx = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[k][p], fx);
+          }
+      }
+      wave_sync();
+      if (a.dx) {  // by way of this wave's tile, so that rows move in whole lines
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          slot_t fd[JK][PARTS2];  // dinner[m][r]: k = r
+#pragma unroll
+          for (int j = 0; j < JK; ++j) {
+            float v[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[e] = dinner[t * 16 + c][j * CHUNK + q * VEC + e];
+            operand_parts<T>(v, fd[j]);
+          }
+#pragma unroll
+          for (int v = 0; v < VT; ++v) {
+            f32x4_t acc = {};
+#pragma unroll
+            for (int j = 0; j < JK; ++j)
+#pragma unroll
+              for (int p = 0; p < PARTS2; ++p) Mma<T>::add(acc, fdown[v][j], fd[j][p]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) my[t * 16 + c][v * 16 + q * 4 + e] = from_f32<T>(acc[e]);
+          }
+        }
+        wave_sync();
+#pragma unroll
+        for (int i = 0; i < Tile::MOVES; ++i) {
+          const int m = i * Tile::ROWS + lane / Tile::LANES, col = lane % Tile::LANES * VEC, row = __shfl(rows, m);
+          T *dst = a.dx + row * a.lddx + k0 + col;
+          union {
+            slot_t s;
+            T e[VEC];
+          } o;
+          o.s = *reinterpret_cast<const slot_t *>(&my[m][col]);
+          if (m < here && k0 + col + VEC <= K) {
+            *reinterpret_cast<typename SlotOf<T>::type *>(dst) = o.s;
+          } else if (m < here) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+              if (k0 + col + e < K) dst[e] = o.e[e];
+          }
+        }
+      }
+      __syncthreads();
+    }
+    pos = end;
+    const bool whole = a_start >= ci * a.chunk && a_end == end;
+    float *G = whole ? a.G + (long)id * K * R : a.split + adapter_split(a_start, a.chunk, ci) * K * R;
+#pragma unroll
+    for (int v = 0; v < VT; ++v) {
+      const int col = k0 + v * 16 + c;
 #pragma unroll
       for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = j * 16 + q * 4 + e;
-          if (r < R) G[across ? (long)r * N + col : (long)col * R + r] = g[v][j][e] * f;
+          if (col < K && r < R) G[(unsigned)(r * K + col)] = g[v][j][e];
         }
     }
   }
 }
 
-// Sums the parts of the adapters that lie in several chunks; zeros for those without rows.
+// sum[i] of the blocks' parts, in a fixed order: 64 numbers a workgroup, the blocks shared out to 16 groups of its lanes.
+static __global__ void __launch_bounds__(1024) adapter_blocks_kernel(const float *__restrict__ part, int blocks, long size, float *__restrict__ sum) {
+  __shared__ float of[16][64];
+  const int lane = threadIdx.x & 63, group = threadIdx.x >> 6;
+  const long i = (long)blockIdx.x * 64 + lane;
+  float s = 0.0f;
+  if (i < size) {
+#pragma unroll 8
+    for (int b = group; b < blocks; b += 16) s += part[b * size + i];
+  }
+  of[group][lane] = s;
+  __syncthreads();
+  if (group != 0 || i >= size) return;
+  s = 0.0f;
+#pragma unroll
+  for (int g = 0; g < 16; ++g) s += of[g][lane];
+  sum[i] = s;
+}
+
+// Sums the parts of the adapters that lie in several chunks, in order; zeros for those without rows.
 struct JoinArgs {
-  const int32_t *start;
-  const float *split, *scale;
+  const float *split, *scale;  // scale may be nullptr
   float *G;
-  int N, R, chunk, n;
-  bool across;
+  long size;  // of an adapter's gradient
+  int chunk;
 };
-static __global__ void __launch_bounds__(256) adapter_join_kernel(const JoinArgs a) {
-  const long size = (long)a.N * a.R;
-  for (int id = blockIdx.y; id < a.n; id += gridDim.y) {
-    const int start = a.start[id], end = a.start[id + 1];
+static __global__ void __launch_bounds__(256) adapter_join_kernel(const int32_t *__restrict__ begin, int n, const JoinArgs up, const JoinArgs down) {
+  const JoinArgs a = blockIdx.z ? down : up;
+  for (int id = blockIdx.y; id < n; id += gridDim.y) {
+    const int start = begin[id], end = begin[id + 1];
     const int c0 = start / a.chunk, c1 = end > start ? (end - 1) / a.chunk : c0;
     if (end > start && c0 == c1) continue;
     const float f = a.scale ? a.scale[id] : 1.0f;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < size; i += (long)gridDim.x * 256) {
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < a.size; i += (long)gridDim.x * 256) {
       float s = 0.0f;
-      if (end > start)
-        for (int c = c0; c <= c1; ++c) s += a.split[adapter_split(start, a.chunk, c) * size + i];
-      s *= f;
-      a.G[(long)id * size + (a.across ? i % a.R * a.N + i / a.R : i)] = end > start ? s : 0.0f;
+      if (end > start) {
+#pragma unroll 8
+        for (int c = c0; c <= c1; ++c) s += a.split[adapter_split(start, a.chunk, c) * a.size + i];
+        s *= f;
+      }
+      a.G[id * a.size + i] = s;
     }
   }
-}
-
-// dinner [position][R] = f_a sum over the blocks of columns, in order; and transposed.
-template <typename T>
-struct DinnerArgs {
-  AdapterRows rows;
-  const int32_t *start;
-  const float *part, *scale;
-  float *dinner;
-  Transposed<T> tr;
-  int blocks, R;
-};
-template <typename T>
-__global__ void __launch_bounds__(256) adapter_dinner_kernel(const DinnerArgs<T> a) {
-  const long i = (long)blockIdx.x * 256 + threadIdx.x, size = (long)a.rows.M * a.R;
-  const int pos = (int)(i / a.R), r = (int)(i % a.R);
-  if (pos >= a.start[a.rows.n]) return;
-  float s = 0.0f;
-  for (int b = 0; b < a.blocks; ++b) s += a.part[b * size + i];
-  if (a.scale) s *= a.scale[a.rows.key(a.rows.row(pos))];
-  a.dinner[i] = s;
-  a.tr.put(r, pos, s);
 }
 
 }  // namespace rnnlm_dev
