@@ -185,8 +185,8 @@ void launch_inner(const InnerArgs<T> &a, hipStream_t st) {
 template <typename T, int NF, bool PACKED>
 void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
   const int64_t tiles = (a.rows.M + ADAPTER_TILE - 1) / ADAPTER_TILE, cols = (a.N + 255) / 256;
-  // a wave's rows of inner are read once for `blocks` blocks, as long as some 2048 workgroups are left
-  a.blocks = (int)std::max<int64_t>(std::min<int64_t>(4, std::max<int64_t>(1, tiles * cols / 2048)), (tiles * cols * 256 + THREADS_MAX - 1) / THREADS_MAX);
+  // a wave walks over its columns with the next ones requested ahead, as long as every compute unit has three workgroups
+  a.blocks = (int)std::max<int64_t>(1, tiles * cols / 768);
   const dim3 grid((unsigned)tiles, (unsigned)((cols + a.blocks - 1) / a.blocks));
   hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED>), grid, dim3(256), 0, st, a);
 }
@@ -228,7 +228,9 @@ int adapter_forward(const T *x, int64_t ldx, int64_t M, int32_t K, int32_t N, co
   if (!inner) inner = reinterpret_cast<float *>(ws + p.inner);
   launch_inner<T>({rows, x, static_cast<const T *>(a.down), ldx, K, a.R, inner, flag}, st);
   LAUNCHED();
-  launch_outer<T>({rows, inner, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1}, st);
+  launch_outer<T>({rows, inner, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1,
+                   read_once(M, N, sizeof(T) == 4 ? RNNLM_DTYPE_FP32 : RNNLM_DTYPE_BF16)},
+                  st);
   LAUNCHED();
   return RNNLM_OK;
 }

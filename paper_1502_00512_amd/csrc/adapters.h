@@ -63,6 +63,16 @@ __device__ inline slot_t first_elems(slot_t s, int left) {
   }
   return s;
 }
+// Zeros in place of the first `gone` elements of a slot.
+template <typename T>
+__device__ inline slot_t last_elems(slot_t s, int gone) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) s[i] = i < gone ? 0u : s[i];
+    else s[i] = 2 * i + 1 < gone ? 0u : 2 * i < gone ? s[i] & 0xffff0000u : s[i];
+  }
+  return s;
+}
 // Up to `left` elements from p on (zeros behind them), of which `there` may be read.
 template <typename T>
 __device__ inline slot_t load_elems(const T *p, int left, long there) {
@@ -115,20 +125,21 @@ static __global__ void __launch_bounds__(1024) adapter_order_kernel(const Adapte
   int rank = 0;
   for (int base = 0; base < M; base += KEYS) {
     const int n = min(KEYS, M - base);
-    for (int i = threadIdx.x; i < (n + 63) / 64 * 64; i += 1024) keys[i] = i < n ? rows.key(base + i) : 0x7fffffff;
+#pragma unroll
+    for (int j = 0; j < KEYS / 1024; ++j) {
+      const int i = j * 1024 + threadIdx.x;
+      keys[i] = i < n ? rows.key(base + i) : 0x7fffffff;
+    }
     __syncthreads();
     // 64 keys at a time: those in front of this workgroup's own rows count where they are equal, too
     for (int i = slice * 64; i < n; i += 1024) {
       const int4 *k = reinterpret_cast<const int4 *>(keys + i);
-      const bool own = base + i == first;
       const int below = q < M && base + i < first ? mine + 1 : mine;
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
         const int4 v = k[j];
         rank += (v.x < below) + (v.y < below) + (v.z < below) + (v.w < below);
       }
-      if (own && q < M)
-        for (int j = 0; j < lane; ++j) rank += keys[i + j] == mine;
     }
     __syncthreads();
   }
@@ -138,6 +149,10 @@ static __global__ void __launch_bounds__(1024) adapter_order_kernel(const Adapte
   int r = 0;
 #pragma unroll
   for (int g = 0; g < 16; ++g) r += cnt[g][lane];
+  if (q < M) {  // equal ones among this workgroup's own rows
+#pragma unroll 8
+    for (int j = 0; j < 63; ++j) r += __builtin_amdgcn_readlane(mine, j) == mine && j < lane;
+  }
   if (q < M) perm[r] = q, sorted[r] = mine;
   else if (q - M <= rows.n) start[q - M] = r;
 }
@@ -190,30 +205,54 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
     }
   }
   if (id >= n) return;
-  const T *down = a.down + (long)id * a.R * a.K;
-  const T *xs[2];
-  int ok[2];
+  // Rows of other adapters, and r >= R, go along: their products are dropped.
+  const T *xs[2], *ds[RT];
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int row = __shfl(tile.row, t * 16 + c);
-    ok[t] = row >= 0 && __shfl(tile.key, t * 16 + c) == id;
-    xs[t] = a.x + (ok[t] ? row : 0) * a.ldx;
-  }
+  for (int t = 0; t < 2; ++t) xs[t] = a.x + max(0, __shfl(tile.row, t * 16 + c)) * a.ldx + q * VEC;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) ds[r] = a.down + ((long)id * a.R + min(r * 16 + c, a.R - 1)) * a.K + q * VEC;
   f32x4_t acc[RT][2] = {};
-  for (int k0 = wave * CHUNK; k0 < a.K; k0 += WAVES * CHUNK) {
-    const int k = k0 + q * VEC, have = a.K - k;
-    slot_t fx[2], fd[RT];
+  typedef typename SlotOf<T>::type Slot;
+  const int whole = a.K / CHUNK * CHUNK;
+  constexpr int AHEAD = 4;  // chunks whose loads are under way together
+  for (int k0 = wave * CHUNK; k0 < whole; k0 += AHEAD * WAVES * CHUNK) {
+    slot_t fx[AHEAD][2], fd[AHEAD][RT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) fx[t] = load_elems(xs[t] + k, ok[t] ? have : 0, have);
+    for (int u = 0; u < AHEAD; ++u) {
+      const int k = min(k0 + u * WAVES * CHUNK, whole - CHUNK);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int j = r * 16 + c;
-      fd[r] = load_elems(down + (long)j * a.K + k, j < a.R ? have : 0, have);
+      for (int t = 0; t < 2; ++t) fx[u][t] = *reinterpret_cast<const Slot *>(xs[t] + k);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) fd[u][r] = *reinterpret_cast<const Slot *>(ds[r] + k);
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k0 + u * WAVES * CHUNK >= whole) {  // (behind the end: nothing is added)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) Mma<T>::add(acc[r][t], fd[r], fx[t]);
+        for (int t = 0; t < 2; ++t) fx[u][t] = slot_t{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < RT; ++r) fd[u][r] = slot_t{0u, 0u, 0u, 0u};
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) Mma<T>::add(acc[r][t], fd[u][r], fx[u][t]);
+    }
+  }
+  if (whole < a.K && wave == whole / CHUNK % WAVES) {
+    const int have = a.K - whole - q * VEC;
+    slot_t fx[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) fx[t] = load_elems(xs[t] + whole, have, have);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const slot_t fd = load_elems(ds[r] + whole, have, have);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) Mma<T>::add(acc[r][t], fd, fx[t]);
+    }
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r)
@@ -241,6 +280,7 @@ struct OuterArgs {
   T *out;
   long ldb, ldo;
   int N, R, blocks;    // blocks of 64 columns of a wave
+  bool once;           // base and out are read and written past the caches
 };
 
 // out = base + f up inner: a wave a tile and 64 columns, `blocks` times; through LDS so that base and out move in whole lines.
@@ -295,64 +335,97 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
   int rows[MOVES];
 #pragma unroll
   for (int i = 0; i < MOVES; ++i) rows[i] = __shfl(tile.row, i * ROWS + lr);
-  for (int b = 0; b < a.blocks; ++b) {
-    const int v0 = ((blockIdx.y * a.blocks + b) * 4 + wave) * COLS;
-    if (v0 >= N) break;  // (nothing is shared between the waves)
-    slot_t old[MOVES];
+  const bool wide = N >= COLS, slots = R % VEC == 0;
+  typedef typename SlotOf<T>::type Slot;
+  // the last block starts early enough not to stick out; its columns from `from` on are written
+  const int first = (blockIdx.y * 4 * a.blocks + wave) * COLS, end = min(N, first + 4 * a.blocks * COLS);
+  const auto start = [&](int from) { return wide ? min(from, N - COLS) : from; };
+  const auto load_base = [&](int v0, slot_t (&old)[MOVES]) {
 #pragma unroll
     for (int i = 0; i < MOVES; ++i) {
-      const int have = N - (v0 + lc);
-      old[i] = a.base && rows[i] >= 0 ? load_elems(a.base + rows[i] * a.ldb + v0 + lc, have, have) : slot_t{0u, 0u, 0u, 0u};
+      const T *at = a.base + max(rows[i], 0) * a.ldb + v0 + lc;
+      if (!a.base) old[i] = slot_t{0u, 0u, 0u, 0u};
+      else if (!wide) old[i] = load_elems(at, N - (v0 + lc), N - (v0 + lc));
+      else if (a.once) old[i] = __builtin_nontemporal_load(reinterpret_cast<const Slot *>(at));
+      else old[i] = *reinterpret_cast<const Slot *>(at);
     }
-    f32x4_t sum[4][2];
+  };
+  // (columns behind the last one, of narrow arrays: the last one again, dropped)
+  const auto load_up = [&](int v0, int id, slot_t (&fa)[4][NF]) {
+    const T *up = a.up + (long)id * N * R;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) sum[v][0] = sum[v][1] = f32x4_t{-0.0f, -0.0f, -0.0f, -0.0f};  // (x + -0 is x)
-    unsigned left = 0xffffffffu;
-    for (int id = tile.next(left, n); id < n; id = tile.next(left, n)) {
-      const T *up = a.up + (long)id * N * R;
-      slot_t fa[4][NF];
+    for (int v = 0; v < 4; ++v)
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
+      for (int i = 0; i < NF; ++i) {
+        const int col = min(v0 + v * 16 + c, N - 1), k = i * CHUNK + kq;
+        if (slots) fa[v][i] = *reinterpret_cast<const Slot *>(up + (unsigned)(col * R + min(k, R - VEC)));
+        else fa[v][i] = load_elems(up + (unsigned)(col * R + k), R - k, (long)(N - col) * R - k);
+      }
+  };
+  if (first >= N) return;  // (nothing is shared between the waves)
+  unsigned left = 0xffffffffu;
+  const int id0 = tile.next(left, n);
+  const unsigned left0 = left;
+  constexpr bool EARLY = NF == 1 || sizeof(T) == 2;  // up is requested a step ahead, too (where registers are left for it)
+  slot_t old[2][MOVES], fa[EARLY ? 2 : 1][4][NF];
+  load_base(start(first), old[0]);
+  if (EARLY && id0 < n) load_up(start(first), id0, fa[0]);
+  for (int from = first; from < end; from += 4 * COLS) {
+    const int v0 = start(from), after = from + 4 * COLS;
+    if (after < end) load_base(start(after), old[1]);
 #pragma unroll
-        for (int i = 0; i < NF; ++i) {
-          const int col = v0 + v * 16 + c, k = i * CHUNK + kq;
-          fa[v][i] = load_elems(up + (long)col * R + k, col < N ? R - k : 0, (long)(N - col) * R - k);
-        }
+    for (int t = 0; t < 2; ++t)
+      if (key[t] >= n) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)  // (x + -0 is x)
+          *reinterpret_cast<f32x4_t *>(&turn[wave][t * 16 + c][v * 16 + q * 4]) = f32x4_t{-0.0f, -0.0f, -0.0f, -0.0f};
+      }
+    left = left0;
+    for (int id = id0; id < n;) {
+      const int next = tile.next(left, n);
+      if constexpr (!EARLY) load_up(v0, id, fa[0]);
+      else if (next < n) load_up(v0, next, fa[1]);
+      else if (after < end) load_up(start(after), id0, fa[1]);
 #pragma unroll
       for (int v = 0; v < 4; ++v)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           f32x4_t acc = {};
 #pragma unroll
-          for (int i = 0; i < NF; ++i)
+          for (int i = 0; i < NF; ++i) {
+            const slot_t f = slots && i * CHUNK + kq >= R ? slot_t{0u, 0u, 0u, 0u} : fa[0][v][i];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) Mma<T>::add(acc, fa[v][i], fu[t][i][p]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[v][t][e] = key[t] == id ? acc[e] : sum[v][t][e];
+            for (int p = 0; p < PARTS; ++p) Mma<T>::add(acc, f, fu[t][i][p]);
+          }
+          if (key[t] == id) *reinterpret_cast<f32x4_t *>(&turn[wave][t * 16 + c][v * 16 + q * 4]) = acc;
         }
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int i = 0; i < NF; ++i) fa[0][v][i] = fa[EARLY][v][i];
+      id = next;
     }
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&turn[wave][t * 16 + c][v * 16 + q * 4]) = sum[v][t];
     wave_sync();
 #pragma unroll
     for (int i = 0; i < MOVES; ++i) {
-      if (rows[i] < 0) continue;
       union {
         slot_t s;
         T t[VEC];
       } o;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) o.t[e] = from_f32<T>(slot_elem<T>(old[i], e) + turn[wave][i * ROWS + lr][lc + e]);
-      T *dst = a.out + rows[i] * a.ldo + v0 + lc;
-      if (v0 + lc + VEC <= N) {
-        *reinterpret_cast<typename SlotOf<T>::type *>(dst) = o.s;
+      for (int e = 0; e < VEC; ++e) o.t[e] = from_f32<T>(slot_elem<T>(old[0][i], e) + turn[wave][i * ROWS + lr][lc + e]);
+      const int col = v0 + lc;
+      T *dst = a.out + max(rows[i], 0) * a.ldo + col;
+      if (rows[i] < 0) {
+      } else if (col >= from && col + VEC <= N) {
+        if (a.once) __builtin_nontemporal_store(o.s, reinterpret_cast<Slot *>(dst));
+        else *reinterpret_cast<Slot *>(dst) = o.s;
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (v0 + lc + e < N) dst[e] = o.t[e];
+          if (col + e >= from && col + e < N) dst[e] = o.t[e];
       }
+      old[0][i] = old[1][i];
     }
     wave_sync();
   }
@@ -402,13 +475,15 @@ __device__ inline void operand_parts(const float (&v)[Mma<T>::VEC], slot_t (&s)[
   for (int i = 0; i < PARTS; ++i) s[i] = o.s[i];
 }
 
-// A wave's 32 rows x COLS columns of an array, row by row by way of registers (requested early) into LDS.
+// A wave's 32 rows x COLS columns of an array, row by row by way of registers (requested early) into LDS.  The last block of
+// columns starts early enough not to stick out (what it has in common with the one in front is left out where it would count
+// twice); only arrays narrower than a block are fetched element by element.
 template <typename T, int COLS>
 struct WaveTile {
   static constexpr int VEC = Mma<T>::VEC, LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = ADAPTER_TILE / ROWS, PITCH = COLS + 16 / sizeof(T);
   slot_t raw[MOVES];
   int rows;  // of lane l, the row of l % 32 (the last ones may repeat one that is there)
-  // columns v0.. of N; a block that sticks out is fetched element by element (store)
+  __device__ static int start(int v0, int N) { return max(0, min(v0, N - COLS)); }
   __device__ void load(const T *d, long ld, int rows_, int v0, int N) {
     const int lane = threadIdx.x & 63;
     rows = rows_;
@@ -429,9 +504,16 @@ struct WaveTile {
         *reinterpret_cast<slot_t *>(&tile[m][lane % LANES * VEC]) = m < here ? raw[i] : slot_t{0u, 0u, 0u, 0u};
       }
     } else {
-      for (int i = lane; i < ADAPTER_TILE * COLS; i += 64) {
-        const int m = i / COLS, col = v0 + i % COLS, row = __shfl(rows, m);
-        tile[m][i % COLS] = m < here && col < N ? d[row * ld + col] : from_f32<T>(0.0f);
+      for (int i0 = 0; i0 < ADAPTER_TILE * COLS; i0 += 8 * 64) {
+        T v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int i = i0 + j * 64 + lane, m = i / COLS, col = v0 + i % COLS;
+          const long row = __shfl(rows, m);
+          v[j] = m < here && col < N ? d[row * ld + col] : from_f32<T>(0.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) tile[(i0 + j * 64 + lane) / COLS][(i0 + j * 64 + lane) % COLS] = v[j];
       }
     }
   }
@@ -474,7 +556,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
   __shared__ __align__(16) T turned[2][PARTS][JT * 16][TILE + 16 / sizeof(T)];  // inner of two tiles, its parts, [r][m]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int N = a.N, R = a.R, n = a.rows.n, block = blockIdx.x, ci = blockIdx.y;
-  const int v0 = (block * WAVES + wave) * COLS;
+  const int from = (block * WAVES + wave) * COLS, v0 = Tile::start(from, N);  // the columns from `from` on count
   const int end_chunk = min((ci + 1) * a.chunk, a.start[n]);
   T(*my)[Tile::PITCH] = buf[wave];
   int turn = 0;
@@ -554,7 +636,10 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
         }
         wave_sync();
 #pragma unroll
-        for (int j = 0; j < JT; ++j) fup[k][j] = across(stage, PITCH, 0, j * 16);
+        for (int j = 0; j < JT; ++j) {
+          fup[k][j] = across(stage, PITCH, 0, j * 16);
+          if (v0 < from) fup[k][j] = last_elems<T>(fup[k][j], from - (v0 + k * CHUNK + q * VEC));
+        }
         wave_sync();
       }
     }
@@ -627,9 +712,10 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
         const int r = j * 16 + q * 4;
         float *dst = G + (unsigned)(col * R + r);
         const f32x4_t x = g[v][j] * f;
-        if (col < N && r + 4 <= R) {
-          *reinterpret_cast<f32x4_t *>(__builtin_assume_aligned(dst, 4)) = x;
-        } else if (col < N) {
+        if (col < from || col >= N) {
+        } else if (r + 4 <= R) {
+          *reinterpret_cast<slot_fp32_t *>(dst) = __builtin_bit_cast(slot_t, x);
+        } else {
 #pragma unroll
           for (int e = 0; e < 3; ++e)
             if (r + e < R) dst[e] = x[e];
@@ -665,7 +751,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
   __shared__ float sums[THREADS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int K = a.K, R = a.R, n = a.rows.n, ci = blockIdx.y;
-  const int k0 = (blockIdx.x * WAVES + wave) * COLS;
+  const int from = (blockIdx.x * WAVES + wave) * COLS, k0 = Tile::start(from, K);  // the columns from `from` on count
   const int present = a.start[n], end_chunk = min((ci + 1) * a.chunk, present);
   T(*my)[Tile::PITCH] = buf[wave];
   // rows without an adapter
@@ -804,7 +890,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = j * 16 + q * 4 + e;
-          if (col < K && r < R) G[(unsigned)(r * K + col)] = g[v][j][e];
+          if (col >= from && col < K && r < R) G[(unsigned)(r * K + col)] = g[v][j][e];
         }
     }
   }
