@@ -94,29 +94,32 @@ constexpr int64_t ADAPTER_ROWS_MAX = 1 << 17;  // (putting the rows in order com
 
 int adapter_r_tiles(int32_t R) { return (R + 15) / 16; }
 // Columns of a wave of adapter_grad_kernel, in 16s: as many as its accumulators and operands leave registers for.
-constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 ? (bf16 ? 8 : 4) : bf16 ? 4 : 2; }
+constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return bf16 ? (r_tiles == 1 ? 8 : 4) : r_tiles <= 2 ? 4 : 2; }
 constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
-// A sum over rows for W columns, 16 tiles of them a wave: blocks of columns, positions of a chunk.  Chunks of at least `least`
-// tiles (what a chunk writes at its end is as much as several tiles of what it reads) until there are some 512 workgroups.
+// A sum over rows for W columns: blocks of columns, positions of a chunk.  A workgroup takes some 3 us a tile; each chunk may
+// leave 2 W R numbers of parts to be written and read: together least at chunks of sqrt(parts of chunks of one tile / 3 us)
+// tiles.  More than some 512 workgroups gain nothing.
 struct GradPlan {
   int blocks, chunks, chunk;
 };
-GradPlan adapter_grad_plan(int64_t rows, int32_t W, int tiles_of_wave, int least) {
+GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave) {
   GradPlan p;
   const int cols = ADAPTER_GRAD_WAVES * 16 * tiles_of_wave;
   p.blocks = (W + cols - 1) / cols;
   const int64_t tiles = std::max<int64_t>(1, (rows + ADAPTER_TILE - 1) / ADAPTER_TILE);
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(tiles / least, 512 / p.blocks));
-  p.chunk = (int)((tiles + want - 1) / want) * ADAPTER_TILE;
+  const double parts_us = 2.0 * tiles * W * R * 4 * 2 / 5e6;
+  const int64_t most = std::max<int64_t>((tiles * p.blocks + 511) / 512, (int64_t)std::lround(std::sqrt(parts_us / 3.0)));
+  const int64_t each = std::min(tiles, std::max<int64_t>(1, most)), chunks = (tiles + each - 1) / each;
+  p.chunk = (int)((tiles + chunks - 1) / chunks) * ADAPTER_TILE;
   p.chunks = (int)std::max<int64_t>(1, (rows + p.chunk - 1) / p.chunk);
   return p;
 }
 GradPlan adapter_up_plan(int64_t rows, int32_t N, int32_t R, int32_t dtype) {
-  return adapter_grad_plan(rows, N, adapter_grad_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16), 4);
+  return adapter_grad_plan(rows, N, R, adapter_grad_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16));
 }
 GradPlan adapter_down_plan(int64_t rows, int32_t K, int32_t R, int32_t dtype) {
-  return adapter_grad_plan(rows, K, adapter_input_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16), 2);
+  return adapter_grad_plan(rows, K, R, adapter_input_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16));
 }
 
 // Rows in up to this many tiles are taken as they come: an adapter is read once for each tile that has it.

@@ -561,89 +561,102 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
   T(*my)[Tile::PITCH] = buf[wave];
   int turn = 0;
   const int tr = threadIdx.x % WIDTH, tm = threadIdx.x / WIDTH;  // this thread's r, and first m
-  for (int pos = ci * a.chunk; pos < end_chunk;) {
-    const int id = __builtin_amdgcn_readfirstlane(a.rows.key_at(pos));
-    // rows of a tile: of lane l (and l + 32) that of position l; the last ones may be the last row again
-    const auto rows_at = [&](int at, int end) { return a.rows.row(min(at + (lane & 31), end - 1)); };
-    const int a_start = a.start[id], a_end = a.start[id + 1], end = min(a_end, end_chunk);
-    const T *up = a.up + (long)id * N * R;
-    int rows = rows_at(pos, end), next = rows_at(min(pos + TILE, end - 1), end);
-    Tile tile;
-    tile.load(a.d, a.ldd, rows, v0, N);
-    float in[EACH];
-    const auto inner_load = [&](int rows) {
+  int pos = ci * a.chunk;
+  if (pos >= end_chunk) return;
+  // rows of a tile: of lane l (and l + 32) that of position l, as far as there are any
+  const auto rows_at = [&](int at) { return a.rows.row(min(at + (lane & 31), a.rows.M - 1)); };
+  float in[EACH];
+  const auto inner_load = [&](int rows) {
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const long row = __shfl(rows, tm + i * STEP);
-        in[i] = tr < R ? a.inner[row * R + tr] : 0.0f;
-      }
-    };
-    const auto inner_store = [&](int here) {
-      if (tr >= JT * 16) return;
+    for (int i = 0; i < EACH; ++i) {
+      const long row = __shfl(rows, tm + i * STEP);
+      in[i] = tr < R ? a.inner[row * R + tr] : 0.0f;
+    }
+  };
+  const auto inner_store = [&](int here) {
+    if (tr >= JT * 16) return;
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        const int m = tm + i * STEP;
-        const float v = m < here ? in[i] : 0.0f;
-        if constexpr (PARTS == 1) {
-          turned[turn][0][tr][m] = v;
-        } else {
-          bf16_t p[PARTS];
-          bf16_parts<PARTS>(v, p);
+    for (int i = 0; i < EACH; ++i) {
+      const int m = tm + i * STEP;
+      const float v = m < here ? in[i] : 0.0f;
+      if constexpr (PARTS == 1) {
+        turned[turn][0][tr][m] = v;
+      } else {
+        bf16_t p[PARTS];
+        bf16_parts<PARTS>(v, p);
 #pragma unroll
-          for (int k = 0; k < PARTS; ++k) turned[turn][k][tr][m] = p[k];
-        }
-      }
-    };
-    inner_load(rows);
-    slot_t fup[VK][JT];  // up[v][r]: k = v (r >= R: anything, those rows of the products are dropped)
-    {
-      // a wave's part of up is contiguous: CHUNK R elements at a time, by way of LDS
-      constexpr int PITCH = JT * 16 + 16 / sizeof(T);
-      T *stage = &my[0][0];
-      if (v0 + COLS <= N) {
-#pragma unroll
-        for (int k = 0; k < VK; ++k)
-#pragma unroll
-          for (int j = 0; j < JT; ++j)
-            fup[k][j] = *reinterpret_cast<const typename SlotOf<T>::type *>(up + (unsigned)((v0 + k * CHUNK) * R + min(j * 64 + lane, 4 * R - 1) * VEC));
-      }
-#pragma unroll
-      for (int k = 0; k < VK; ++k) {
-        if (v0 + COLS <= N) {
-#pragma unroll
-          for (int j = 0; j < JT; ++j) {
-            const int i = min(j * 64 + lane, 4 * R - 1) * VEC;
-            int v = i / R, r = i - v * R;
-            if (R % VEC == 0) {
-              *reinterpret_cast<slot_t *>(stage + v * PITCH + r) = fup[k][j];
-            } else {
-              union {
-                slot_t s;
-                T e[VEC];
-              } o;
-              o.s = fup[k][j];
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) {
-                stage[v * PITCH + r] = o.e[e];
-                r = r + 1 == R ? (++v, 0) : r + 1;
-              }
-            }
-          }
-        } else {
-          const int v = v0 + k * CHUNK, there = max(0, min(CHUNK, N - v));
-          for (int i = lane; i < CHUNK * R; i += 64)
-            stage[i / R * PITCH + i % R] = i < there * R ? up[(unsigned)(v * R + i)] : from_f32<T>(0.0f);
-        }
-        wave_sync();
-#pragma unroll
-        for (int j = 0; j < JT; ++j) {
-          fup[k][j] = across(stage, PITCH, 0, j * 16);
-          if (v0 < from) fup[k][j] = last_elems<T>(fup[k][j], from - (v0 + k * CHUNK + q * VEC));
-        }
-        wave_sync();
+        for (int k = 0; k < PARTS; ++k) turned[turn][k][tr][m] = p[k];
       }
     }
-    inner_store(min(TILE, end - pos));
+  };
+  slot_t fup[VK][JT];  // up[v][r]: k = v (r >= R: anything, those rows of the products are dropped)
+  // A wave's part of up is contiguous: CHUNK R elements at a time, slot by slot first, then turned by way of LDS.
+  const bool inside = v0 + COLS <= N;
+  const auto up_slot = [&](int j) { return min(j * 64 + lane, 4 * R - 1) * VEC; };
+  const auto up_load = [&](int id) {
+    if (!inside) return;
+    const T *up = a.up + (long)id * N * R;
+#pragma unroll
+    for (int k = 0; k < VK; ++k)
+#pragma unroll
+      for (int j = 0; j < JT; ++j) fup[k][j] = *reinterpret_cast<const typename SlotOf<T>::type *>(up + (unsigned)((v0 + k * CHUNK) * R + up_slot(j)));
+  };
+  const auto up_turn = [&](int id) {
+    constexpr int PITCH = JT * 16 + 16 / sizeof(T);
+    T *stage = &my[0][0];
+#pragma unroll
+    for (int k = 0; k < VK; ++k) {
+      if (inside) {
+#pragma unroll
+        for (int j = 0; j < JT; ++j) {
+          const int i = up_slot(j);
+          int v = i / R, r = i - v * R;
+          if (R % VEC == 0) {
+            *reinterpret_cast<slot_t *>(stage + v * PITCH + r) = fup[k][j];
+          } else {
+            union {
+              slot_t s;
+              T e[VEC];
+            } o;
+            o.s = fup[k][j];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              stage[v * PITCH + r] = o.e[e];
+              r = r + 1 == R ? (++v, 0) : r + 1;
+            }
+          }
+        }
+      } else {
+        const T *up = a.up + (long)id * N * R;
+        const int v = v0 + k * CHUNK, there = max(0, min(CHUNK, N - v));
+        for (int i = lane; i < CHUNK * R; i += 64)
+          stage[i / R * PITCH + i % R] = i < there * R ? up[(unsigned)(v * R + i)] : from_f32<T>(0.0f);
+      }
+      wave_sync();
+#pragma unroll
+      for (int j = 0; j < JT; ++j) {
+        fup[k][j] = across(stage, PITCH, 0, j * 16);
+        if (v0 < from) fup[k][j] = last_elems<T>(fup[k][j], from - (v0 + k * CHUNK + q * VEC));
+      }
+      wave_sync();
+    }
+  };
+  // Segment by segment (an adapter's rows in the chunk), tile by tile; what the next tile needs is requested a tile ahead, also
+  // across segments.
+  int id = __builtin_amdgcn_readfirstlane(a.rows.key_at(pos)), a_start = a.start[id], a_end = a.start[id + 1];
+  int rows = rows_at(pos);
+  Tile tile;
+  tile.load(a.d, a.ldd, rows, v0, N);
+  inner_load(rows);
+  up_load(id);
+  inner_store(min(TILE, min(a_end, end_chunk) - pos));
+  while (true) {
+    const int end = min(a_end, end_chunk);
+    const bool last = end >= end_chunk;
+    const int id2_at = last ? id : a.rows.key_at(end);
+    int next = rows_at(pos + TILE < end ? pos + TILE : end);
+    up_turn(id);
+    const int id2 = __builtin_amdgcn_readfirstlane(id2_at), a_end2 = a.start[id2 + 1];
     __syncthreads();
     f32x4_t g[VT][JT] = {};
     for (; pos < end; pos += TILE) {
@@ -651,10 +664,10 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
       const bool more = pos + TILE < end;
       tile.store(my, a.d, a.ldd, here, v0, N);
       wave_sync();
-      if (more) {
+      if (more || !last) {
         tile.load(a.d, a.ldd, next, v0, N);
         inner_load(next);
-        next = rows_at(min(pos + 2 * TILE, end - 1), end);
+        if (more) next = rows_at(pos + 2 * TILE < end ? pos + 2 * TILE : end);
       }
       f32x4_t acc[JT][2] = {};
 #pragma unroll
@@ -665,30 +678,30 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
 #pragma unroll
           for (int j = 0; j < JT; ++j) Mma<T>::add(acc[j][t], fup[k][j], fd);
         }
+      if (!more && !last) up_load(id2);
       float(*r_of)[TILE][JT * 16 + 4] = red[REDS == 2 ? turn : 0];
 #pragma unroll
       for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&r_of[wave][t * 16 + c][j * 16 + q * 4]) = acc[j][t];
-      slot_t fw[MK][JT][PARTS];  // inner[m][r]: k = m
+      // (an operand of inner at a time: all of them at once, and registers spill)
 #pragma unroll
-      for (int k = 0; k < MK; ++k)
-#pragma unroll
-        for (int j = 0; j < JT; ++j)
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) fw[k][j][p] = *reinterpret_cast<const slot_t *>(&turned[turn][p][j * 16 + c][k * CHUNK + q * VEC]);
-#pragma unroll
-      for (int v = 0; v < VT; ++v)
+      for (int j = 0; j < JT; ++j)
 #pragma unroll
         for (int k = 0; k < MK; ++k) {
-          const slot_t fd = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
+          slot_t fw[PARTS];  // inner[m][r]: k = m
 #pragma unroll
-          for (int j = 0; j < JT; ++j)
+          for (int p = 0; p < PARTS; ++p) fw[p] = *reinterpret_cast<const slot_t *>(&turned[turn][p][j * 16 + c][k * CHUNK + q * VEC]);
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[k][j][p], fd);
+          for (int v = 0; v < VT; ++v) {
+            const slot_t fd = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[p], fd);
+          }
         }
       turn ^= 1;
       if (more) inner_store(min(TILE, end - pos - TILE));
+      else if (!last) inner_store(min(TILE, min(a_end2, end_chunk) - end));
       __syncthreads();
       float *part = a.part + ((long)block * a.rows.M + pos) * R;
       for (int i = threadIdx.x; i < here * R; i += THREADS) {
@@ -700,7 +713,6 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
       }
       if (REDS == 1) __syncthreads();
     }
-    pos = end;
     const bool whole = a_start >= ci * a.chunk && a_end == end;
     float *G = whole ? a.G + (long)id * N * R : a.split + adapter_split(a_start, a.chunk, ci) * N * R;
     const float f = whole && a.scale ? a.scale[id] : 1.0f;
@@ -722,6 +734,11 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
         }
       }
     }
+    if (last) break;
+    pos = end;
+    id = id2;
+    a_start = a_end;
+    a_end = a_end2;
   }
 }
 
