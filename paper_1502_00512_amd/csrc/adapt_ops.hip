@@ -98,7 +98,7 @@ constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return bf16 ? (r_tile
 constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
 // A sum over rows for W columns: blocks of columns, positions of a chunk.  A workgroup takes some 3 us a tile; each chunk may
-// leave 2 W R numbers of parts to be written and read: together least at chunks of sqrt(parts of chunks of one tile / 3 us)
+// leave W R numbers to be written and read once more: together least at chunks of sqrt(that time, chunks of one tile / 3 us)
 // tiles.  More than some 512 workgroups gain nothing.
 struct GradPlan {
   int blocks, chunks, chunk;
@@ -108,9 +108,9 @@ GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave
   const int cols = ADAPTER_GRAD_WAVES * 16 * tiles_of_wave;
   p.blocks = (W + cols - 1) / cols;
   const int64_t tiles = std::max<int64_t>(1, (rows + ADAPTER_TILE - 1) / ADAPTER_TILE);
-  const double parts_us = 2.0 * tiles * W * R * 4 * 2 / 5e6;
+  const double parts_us = (double)tiles * W * R * 4 * 2 / 5e6;
   const int64_t most = std::max<int64_t>((tiles * p.blocks + 511) / 512, (int64_t)std::lround(std::sqrt(parts_us / 3.0)));
-  const int64_t each = std::min(tiles, std::max<int64_t>(1, most)), chunks = (tiles + each - 1) / each;
+  const int64_t each = std::min<int64_t>({tiles, ADAPTER_CHUNK / ADAPTER_TILE, std::max<int64_t>(1, most)}), chunks = (tiles + each - 1) / each;
   p.chunk = (int)((tiles + chunks - 1) / chunks) * ADAPTER_TILE;
   p.chunks = (int)std::max<int64_t>(1, (rows + p.chunk - 1) / p.chunk);
   return p;
@@ -148,8 +148,8 @@ AdapterPlan adapter_plan(int64_t rows, int32_t K, int32_t N, int32_t n, int32_t 
     const GradPlan up = adapter_up_plan(rows, N, R, dtype), down = adapter_down_plan(rows, K, R, dtype);
     p.part = take((size_t)up.blocks * rows * R * 4);
     p.dinner = take((size_t)rows * R * 4);
-    p.split_up = take(up.chunks > 1 ? (size_t)2 * up.chunks * N * R * 4 : 0);
-    p.split_down = take(down.chunks > 1 ? (size_t)2 * down.chunks * K * R * 4 : 0);
+    p.split_up = take(up.chunks > 1 ? (size_t)up.chunks * N * R * 4 : 0);
+    p.split_down = take(down.chunks > 1 ? (size_t)down.chunks * K * R * 4 : 0);
   }
   p.total = std::max<size_t>(o, 256);
   return p;
@@ -203,21 +203,32 @@ void launch_outer(const OuterArgs<T> &a, hipStream_t st) {
     with_r_tiles(a.R, [&](auto r) { launch_outer_as<T, decltype(r)::value, false>(a, st); });
   }
 }
+// (Arrays narrower than a wave's columns: one kernel of each type, whatever R.)
 template <typename T>
 void launch_grad(const GradArgs<T> &a, const GradPlan &p, hipStream_t st) {
-  with_r_tiles(a.R, [&](auto r) {
-    constexpr int JT = decltype(r)::value;
-    hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, sizeof(T) == 2)>), dim3(p.blocks, p.chunks),
-                       dim3(64 * ADAPTER_GRAD_WAVES), 0, st, a);
-  });
+  const dim3 grid(p.blocks, p.chunks), threads(64 * ADAPTER_GRAD_WAVES);
+  constexpr bool BF16 = sizeof(T) == 2;
+  if (a.N < 16 * adapter_grad_tiles(adapter_r_tiles(a.R), BF16)) {
+    hipLaunchKernelGGL((adapter_grad_kernel<T, 4, 2, true>), grid, threads, 0, st, a);
+  } else {
+    with_r_tiles(a.R, [&](auto r) {
+      constexpr int JT = decltype(r)::value;
+      hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, BF16), false>), grid, threads, 0, st, a);
+    });
+  }
 }
 template <typename T>
 void launch_input_grad(const InputGradArgs<T> &a, const GradPlan &p, hipStream_t st) {
-  with_r_tiles(a.R, [&](auto r) {
-    constexpr int JT = decltype(r)::value;
-    hipLaunchKernelGGL((adapter_input_grad_kernel<T, JT, adapter_input_tiles(JT, sizeof(T) == 2)>), dim3(p.blocks, p.chunks),
-                       dim3(64 * ADAPTER_GRAD_WAVES), 0, st, a);
-  });
+  const dim3 grid(p.blocks, p.chunks), threads(64 * ADAPTER_GRAD_WAVES);
+  constexpr bool BF16 = sizeof(T) == 2;
+  if (a.K < 16 * adapter_input_tiles(adapter_r_tiles(a.R), BF16)) {
+    hipLaunchKernelGGL((adapter_input_grad_kernel<T, 4, 2, true>), grid, threads, 0, st, a);
+  } else {
+    with_r_tiles(a.R, [&](auto r) {
+      constexpr int JT = decltype(r)::value;
+      hipLaunchKernelGGL((adapter_input_grad_kernel<T, JT, adapter_input_tiles(JT, BF16), false>), grid, threads, 0, st, a);
+    });
+  }
 }
 
 template <typename T>

@@ -478,16 +478,16 @@ __device__ inline void operand_parts(const float (&v)[Mma<T>::VEC], slot_t (&s)[
 // A wave's 32 rows x COLS columns of an array, row by row by way of registers (requested early) into LDS.  The last block of
 // columns starts early enough not to stick out (what it has in common with the one in front is left out where it would count
 // twice); only arrays narrower than a block are fetched element by element.
-template <typename T, int COLS>
+template <typename T, int COLS, bool NARROW>
 struct WaveTile {
   static constexpr int VEC = Mma<T>::VEC, LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = ADAPTER_TILE / ROWS, PITCH = COLS + 16 / sizeof(T);
   slot_t raw[MOVES];
   int rows;  // of lane l, the row of l % 32 (the last ones may repeat one that is there)
   __device__ static int start(int v0, int N) { return max(0, min(v0, N - COLS)); }
-  __device__ void load(const T *d, long ld, int rows_, int v0, int N) {
+  __device__ void load(const T *d, long ld, int rows_, int v0) {
     const int lane = threadIdx.x & 63;
     rows = rows_;
-    if (v0 + COLS <= N) {
+    if constexpr (!NARROW) {
       const T *at = d + v0 + lane % LANES * VEC;
 #pragma unroll
       for (int i = 0; i < MOVES; ++i)
@@ -497,7 +497,7 @@ struct WaveTile {
   // zeros in place of the rows from `here` on
   __device__ void store(T (*tile)[PITCH], const T *d, long ld, int here, int v0, int N) const {
     const int lane = threadIdx.x & 63;
-    if (v0 + COLS <= N) {
+    if constexpr (!NARROW) {
 #pragma unroll
       for (int i = 0; i < MOVES; ++i) {
         const int m = i * ROWS + lane / LANES;
@@ -520,12 +520,52 @@ struct WaveTile {
 };
 
 // Gradients that are sums over rows.  Workgroups: chunks of positions x blocks of columns.  A chunk may hold many adapters and
-// an adapter lie in many chunks: where all of an adapter lies in one, its gradient is written, else a part of it, which
-// adapter_join_kernel sums up.  Part of adapter a in chunk i (in units of a whole gradient): an adapter that starts in front of
-// the chunk has the first, one that goes on behind it the second.
-__device__ inline long adapter_split(int a_start, int chunk, int i) { return 2L * i + (a_start < i * chunk ? 0 : 1); }
+// an adapter lie in many chunks: the one it starts in writes its gradient (finished, where all of it lies there), any other
+// has one such adapter, its first, and writes a part of its own; adapter_join_kernel sums up.
 
-constexpr int ADAPTER_GRAD_WAVES = 8;
+constexpr int ADAPTER_GRAD_WAVES = 8, ADAPTER_CHUNK = 1024;  // most positions of a chunk
+
+// A chunk's tiles, each of rows of one adapter: first position (in the chunk), rows less one, adapter.
+struct TileList {
+  int row[ADAPTER_CHUNK], tile[ADAPTER_CHUNK], of_wave[2][ADAPTER_GRAD_WAVES];
+  __device__ int first(int i) const { return __builtin_amdgcn_readfirstlane(tile[i]) & 1023; }
+  __device__ int rows(int i) const { return (__builtin_amdgcn_readfirstlane(tile[i]) >> 10 & 31) + 1; }
+  __device__ int adapter(int i) const { return __builtin_amdgcn_readfirstlane(tile[i]) >> 15; }
+};
+// Fills the list for positions begin .. end - 1 (more than none, at most ADAPTER_CHUNK): a workgroup of ADAPTER_GRAD_WAVES waves.
+// Returns the number of tiles.
+__device__ inline int list_tiles(const AdapterRows &rows, const int32_t *start, int begin, int end, TileList &list) {
+  constexpr int THREADS = 64 * ADAPTER_GRAD_WAVES;
+  static_assert(ADAPTER_CHUNK == 2 * THREADS, "two positions a thread");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int entry[2];
+  unsigned long long heads[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int pos = begin + j * THREADS + threadIdx.x;
+    const bool in = pos < end;
+    const int p = in ? pos : end - 1, key = rows.sorted[p], row = rows.perm[p];
+    const int from = max(start[key], begin), to = min(start[key + 1], end);
+    list.row[pos - begin] = row;  // (behind the end: the last row)
+    entry[j] = (pos - begin) | (min(ADAPTER_TILE, to - p) - 1) << 10 | key << 15;
+    heads[j] = __ballot(in && ((p - from) & (ADAPTER_TILE - 1)) == 0);
+    if (lane == 0) list.of_wave[j][wave] = __popcll(heads[j]);
+  }
+  __syncthreads();
+  int at = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    int mine = at;
+#pragma unroll
+    for (int w = 0; w < ADAPTER_GRAD_WAVES; ++w) {
+      mine += w < wave ? list.of_wave[j][w] : 0;
+      at += list.of_wave[j][w];
+    }
+    if (heads[j] >> lane & 1) list.tile[mine + __popcll(heads[j] & ((1ull << lane) - 1))] = entry[j];
+  }
+  __syncthreads();
+  return at;
+}
 
 template <typename T>
 struct GradArgs {
@@ -537,88 +577,97 @@ struct GradArgs {
   const T *up;
   const float *scale;  // may be nullptr
   float *G;            // [n][N][R]
-  float *split;        // [2 chunks][N][R]
+  float *split;        // [chunks][N][R]
   float *part;         // [blocks of columns][M][R]
   int N, R, chunk;     // positions of a chunk
 };
 
 // dup[a][v][r] = f_a sum_m dout[m][v] inner[m][r], and of every block of columns part[position][r] = sum_v dout[m][v] up[a][v][r]:
-// dout is read once, which bounds it.
-template <typename T, int JT, int VT>
+// dout is read once, which bounds it.  NARROW: fewer columns than a wave's.
+template <typename T, int JT, int VT, bool NARROW>
 __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(const GradArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = ADAPTER_GRAD_WAVES, COLS = 16 * VT;
   constexpr int THREADS = 64 * WAVES, PARTS = GRAD_PARTS<T>, MK = TILE / CHUNK, VK = COLS / CHUNK;  // slots of the rows, of the columns
   constexpr int REDS = JT <= 2 ? 2 : 1;  // (as many as LDS holds)
   constexpr int WIDTH = JT == 3 ? 64 : JT * 16, STEP = THREADS / WIDTH, EACH = TILE / STEP;  // a tile's inner numbers over the threads
-  typedef WaveTile<T, COLS> Tile;
+  constexpr bool EARLY = JT <= 2;        // the next adapter's up has registers of its own
+  typedef WaveTile<T, COLS, NARROW> Tile;
   __shared__ __align__(16) T buf[WAVES][TILE][Tile::PITCH];
   __shared__ __align__(16) float red[REDS][WAVES][TILE][JT * 16 + 4];
   __shared__ __align__(16) T turned[2][PARTS][JT * 16][TILE + 16 / sizeof(T)];  // inner of two tiles, its parts, [r][m]
+  __shared__ TileList list;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int N = a.N, R = a.R, n = a.rows.n, block = blockIdx.x, ci = blockIdx.y;
   const int from = (block * WAVES + wave) * COLS, v0 = Tile::start(from, N);  // the columns from `from` on count
   const int end_chunk = min((ci + 1) * a.chunk, a.start[n]);
   T(*my)[Tile::PITCH] = buf[wave];
-  int turn = 0;
   const int tr = threadIdx.x % WIDTH, tm = threadIdx.x / WIDTH;  // this thread's r, and first m
-  int pos = ci * a.chunk;
-  if (pos >= end_chunk) return;
-  // rows of a tile: of lane l (and l + 32) that of position l, as far as there are any
-  const auto rows_at = [&](int at) { return a.rows.row(min(at + (lane & 31), a.rows.M - 1)); };
-  float in[EACH];
-  const auto inner_load = [&](int rows) {
+  const int chunk0 = ci * a.chunk;
+  if (chunk0 >= end_chunk) return;
+  const int count = list_tiles(a.rows, a.start, chunk0, end_chunk, list);
+  // What a tile needs of memory, requested two tiles ahead (behind the last one: that again, so that no branch stands between
+  // the requests and the waits can count them).
+  struct Ahead {
+    Tile tile;
+    float in[EACH];
+  };
+  const auto request = [&](Ahead &x, int i) {
+    const int rows = list.row[min(list.first(min(i, count - 1)) + (lane & 31), ADAPTER_CHUNK - 1)];
+    x.tile.load(a.d, a.ldd, rows, v0);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const long row = __shfl(rows, tm + i * STEP);
-      in[i] = tr < R ? a.inner[row * R + tr] : 0.0f;
+    for (int e = 0; e < EACH; ++e) {
+      const long row = __shfl(rows, tm + e * STEP);
+      x.in[e] = a.inner[row * R + min(tr, R - 1)];
     }
   };
-  const auto inner_store = [&](int here) {
+  const auto inner_store = [&](const Ahead &x, int i) {
     if (tr >= JT * 16) return;
+    const int here = list.rows(min(i, count - 1));
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int m = tm + i * STEP;
-      const float v = m < here ? in[i] : 0.0f;
+    for (int e = 0; e < EACH; ++e) {
+      const int m = tm + e * STEP;
+      const float v = m < here ? x.in[e] : 0.0f;  // (r >= R: those rows of the product are dropped)
       if constexpr (PARTS == 1) {
-        turned[turn][0][tr][m] = v;
+        turned[i & 1][0][tr][m] = v;
       } else {
         bf16_t p[PARTS];
         bf16_parts<PARTS>(v, p);
 #pragma unroll
-        for (int k = 0; k < PARTS; ++k) turned[turn][k][tr][m] = p[k];
+        for (int k = 0; k < PARTS; ++k) turned[i & 1][k][tr][m] = p[k];
       }
     }
   };
-  slot_t fup[VK][JT];  // up[v][r]: k = v (r >= R: anything, those rows of the products are dropped)
-  // A wave's part of up is contiguous: CHUNK R elements at a time, slot by slot first, then turned by way of LDS.
-  const bool inside = v0 + COLS <= N;
+  // up[v][r], k = v (r >= R: anything).  A wave's part of up is contiguous: CHUNK R elements at a time, slot by slot first, then
+  // turned by way of LDS.
+  slot_t fup[VK][JT], fup2[EARLY ? VK : 1][EARLY ? JT : 1];
   const auto up_slot = [&](int j) { return min(j * 64 + lane, 4 * R - 1) * VEC; };
-  const auto up_load = [&](int id) {
-    if (!inside) return;
-    const T *up = a.up + (long)id * N * R;
+  const auto up_load = [&](auto &to, int id) {
+    if constexpr (!NARROW) {
+      const T *up = a.up + (long)id * N * R;
 #pragma unroll
-    for (int k = 0; k < VK; ++k)
+      for (int k = 0; k < VK; ++k)
 #pragma unroll
-      for (int j = 0; j < JT; ++j) fup[k][j] = *reinterpret_cast<const typename SlotOf<T>::type *>(up + (unsigned)((v0 + k * CHUNK) * R + up_slot(j)));
+        for (int j = 0; j < JT; ++j) to[k][j] = *reinterpret_cast<const typename SlotOf<T>::type *>(up + (unsigned)((v0 + k * CHUNK) * R + up_slot(j)));
+    }
   };
-  const auto up_turn = [&](int id) {
+  const auto up_turn = [&](const auto &raw, T *stage, int id) {
     constexpr int PITCH = JT * 16 + 16 / sizeof(T);
-    T *stage = &my[0][0];
+    static_assert(CHUNK * PITCH * sizeof(T) <= sizeof(red[0][0]), "a wave's share of red holds a step");
 #pragma unroll
     for (int k = 0; k < VK; ++k) {
-      if (inside) {
+      if constexpr (!NARROW) {
 #pragma unroll
         for (int j = 0; j < JT; ++j) {
           const int i = up_slot(j);
           int v = i / R, r = i - v * R;
           if (R % VEC == 0) {
-            *reinterpret_cast<slot_t *>(stage + v * PITCH + r) = fup[k][j];
+            *reinterpret_cast<slot_t *>(stage + v * PITCH + r) = raw[k][j];
           } else {
             union {
               slot_t s;
               T e[VEC];
             } o;
-            o.s = fup[k][j];
+            o.s = raw[k][j];
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
               stage[v * PITCH + r] = o.e[e];
@@ -641,80 +690,24 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
       wave_sync();
     }
   };
-  // Segment by segment (an adapter's rows in the chunk), tile by tile; what the next tile needs is requested a tile ahead, also
-  // across segments.
-  int id = __builtin_amdgcn_readfirstlane(a.rows.key_at(pos)), a_start = a.start[id], a_end = a.start[id + 1];
-  int rows = rows_at(pos);
-  Tile tile;
-  tile.load(a.d, a.ldd, rows, v0, N);
-  inner_load(rows);
-  up_load(id);
-  inner_store(min(TILE, min(a_end, end_chunk) - pos));
-  while (true) {
-    const int end = min(a_end, end_chunk);
-    const bool last = end >= end_chunk;
-    const int id2_at = last ? id : a.rows.key_at(end);
-    int next = rows_at(pos + TILE < end ? pos + TILE : end);
-    up_turn(id);
-    const int id2 = __builtin_amdgcn_readfirstlane(id2_at), a_end2 = a.start[id2 + 1];
-    __syncthreads();
-    f32x4_t g[VT][JT] = {};
-    for (; pos < end; pos += TILE) {
-      const int here = min(TILE, end - pos);
-      const bool more = pos + TILE < end;
-      tile.store(my, a.d, a.ldd, here, v0, N);
-      wave_sync();
-      if (more || !last) {
-        tile.load(a.d, a.ldd, next, v0, N);
-        inner_load(next);
-        if (more) next = rows_at(pos + 2 * TILE < end ? pos + 2 * TILE : end);
-      }
-      f32x4_t acc[JT][2] = {};
+  f32x4_t g[VT][JT] = {};
+  // What a tile leaves to be written, after the next one's rows have arrived and before further ones are requested (stores
+  // count with the loads: behind them they would be waited for with them): the sums of `part`, and the gradient of an adapter
+  // whose rows end.
+  float sums[EACH];
+  const auto write_sums = [&](int i) {
+    float *part = a.part + ((long)block * a.rows.M + chunk0 + list.first(i)) * R;
+    const int here = list.rows(i);
 #pragma unroll
-      for (int k = 0; k < VK; ++k)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const slot_t fd = *reinterpret_cast<const slot_t *>(&my[t * 16 + c][k * CHUNK + q * VEC]);
-#pragma unroll
-          for (int j = 0; j < JT; ++j) Mma<T>::add(acc[j][t], fup[k][j], fd);
-        }
-      if (!more && !last) up_load(id2);
-      float(*r_of)[TILE][JT * 16 + 4] = red[REDS == 2 ? turn : 0];
-#pragma unroll
-      for (int j = 0; j < JT; ++j)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&r_of[wave][t * 16 + c][j * 16 + q * 4]) = acc[j][t];
-      // (an operand of inner at a time: all of them at once, and registers spill)
-#pragma unroll
-      for (int j = 0; j < JT; ++j)
-#pragma unroll
-        for (int k = 0; k < MK; ++k) {
-          slot_t fw[PARTS];  // inner[m][r]: k = m
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) fw[p] = *reinterpret_cast<const slot_t *>(&turned[turn][p][j * 16 + c][k * CHUNK + q * VEC]);
-#pragma unroll
-          for (int v = 0; v < VT; ++v) {
-            const slot_t fd = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[p], fd);
-          }
-        }
-      turn ^= 1;
-      if (more) inner_store(min(TILE, end - pos - TILE));
-      else if (!last) inner_store(min(TILE, min(a_end2, end_chunk) - end));
-      __syncthreads();
-      float *part = a.part + ((long)block * a.rows.M + pos) * R;
-      for (int i = threadIdx.x; i < here * R; i += THREADS) {
-        const int m = i / R, r = i - m * R;
-        float s = 0.0f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) s += r_of[w][m][r];
-        part[i] = s;
-      }
-      if (REDS == 1) __syncthreads();
+    for (int e = 0; e < EACH; ++e) {
+      const int m = tm + e * STEP;
+      if (tr < R && m < here) part[m * R + tr] = sums[e];
     }
-    const bool whole = a_start >= ci * a.chunk && a_end == end;
-    float *G = whole ? a.G + (long)id * N * R : a.split + adapter_split(a_start, a.chunk, ci) * N * R;
+  };
+  const auto write_gradient = [&](int id) {
+    const int a_start = a.start[id], a_end = a.start[id + 1];
+    const bool whole = a_start >= chunk0 && a_end <= end_chunk;
+    float *G = a_start >= chunk0 ? a.G + (long)id * N * R : a.split + (long)ci * N * R;
     const float f = whole && a.scale ? a.scale[id] : 1.0f;
 #pragma unroll
     for (int v = 0; v < VT; ++v) {
@@ -724,6 +717,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
         const int r = j * 16 + q * 4;
         float *dst = G + (unsigned)(col * R + r);
         const f32x4_t x = g[v][j] * f;
+        g[v][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if (col < from || col >= N) {
         } else if (r + 4 <= R) {
           *reinterpret_cast<slot_fp32_t *>(dst) = __builtin_bit_cast(slot_t, x);
@@ -734,12 +728,80 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(c
         }
       }
     }
-    if (last) break;
-    pos = end;
-    id = id2;
-    a_start = a_end;
-    a_end = a_end2;
+  };
+  int id = list.adapter(0);
+  const auto step = [&](Ahead &x, const Ahead &y, int i) {
+    const int here = list.rows(i), before = id;
+    id = list.adapter(i);
+    const int after = list.adapter(min(i + 1, count - 1));
+    x.tile.store(my, a.d, a.ldd, here, v0, N);
+    if (i > 0) write_sums(i - 1);
+    if (i > 0 && id != before) write_gradient(before);
+    if (i == 0 || id != before) {
+      T *stage = reinterpret_cast<T *>(&red[REDS == 2 ? i & 1 : 0][wave][0][0]);
+      if constexpr (EARLY) up_turn(fup2, stage, id);
+      else up_turn(fup, stage, id);
+    }
+    if constexpr (EARLY)
+      if (after != id) up_load(fup2, after);
+    request(x, i + 2);
+    wave_sync();
+    f32x4_t acc[JT][2] = {};
+#pragma unroll
+    for (int k = 0; k < VK; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const slot_t fd = *reinterpret_cast<const slot_t *>(&my[t * 16 + c][k * CHUNK + q * VEC]);
+#pragma unroll
+        for (int j = 0; j < JT; ++j) Mma<T>::add(acc[j][t], fup[k][j], fd);
+      }
+    if constexpr (!EARLY)
+      if (after != id) up_load(fup, after);
+    float(*r_of)[TILE][JT * 16 + 4] = red[REDS == 2 ? i & 1 : 0];
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4_t *>(&r_of[wave][t * 16 + c][j * 16 + q * 4]) = acc[j][t];
+    // (an operand of inner at a time: all of them at once, and registers spill)
+#pragma unroll
+    for (int j = 0; j < JT; ++j)
+#pragma unroll
+      for (int k = 0; k < MK; ++k) {
+        slot_t fw[PARTS];  // inner[m][r]: k = m
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) fw[p] = *reinterpret_cast<const slot_t *>(&turned[i & 1][p][j * 16 + c][k * CHUNK + q * VEC]);
+#pragma unroll
+        for (int v = 0; v < VT; ++v) {
+          const slot_t fd = across(&my[0][0], Tile::PITCH, k * CHUNK, v * 16);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) Mma<T>::add(g[v][j], fw[p], fd);
+        }
+      }
+    inner_store(y, i + 1);
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      sums[e] = 0.0f;
+      if (tr < JT * 16) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sums[e] += r_of[w][tm + e * STEP][tr];
+      }
+    }
+    if (REDS == 1) __syncthreads();
+  };
+  Ahead even, odd;
+  if constexpr (EARLY) up_load(fup2, id);
+  else up_load(fup, id);
+  request(even, 0);
+  request(odd, 1);
+  inner_store(even, 0);
+  __syncthreads();
+  for (int i = 0; i < count; i += 2) {
+    step(even, odd, i);
+    if (i + 1 < count) step(odd, even, i + 1);
   }
+  write_sums(count - 1);
+  write_gradient(id);
 }
 
 template <typename T>
@@ -749,7 +811,7 @@ struct InputGradArgs {
   const T *x, *down;
   const float *scale;  // may be nullptr
   const float *part;   // [blocks][M][R]
-  float *G, *split;    // [n][R][K]; [2 chunks][R][K]
+  float *G, *split;    // [n][R][K]; [chunks][R][K]
   T *dx;               // may be nullptr
   long ldx, lddx;
   int K, R, chunk, blocks;
@@ -757,12 +819,12 @@ struct InputGradArgs {
 
 // dinner of a tile from the blocks' parts, then ddown[a][r][k] = sum_m dinner[m][r] x[m][k] and dx[m][k] = sum_r down[a][r][k]
 // dinner[m][r].  Sums of parts are formed once for every 512 columns of x.
-template <typename T, int JT, int VT>
+template <typename T, int JT, int VT, bool NARROW>
 __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_kernel(const InputGradArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = ADAPTER_GRAD_WAVES, COLS = 16 * VT;
   constexpr int THREADS = 64 * WAVES, PARTS = GRAD_PARTS<T>, PARTS2 = sizeof(T) == 2 ? 2 : 1, MK = TILE / CHUNK;
   constexpr int JK = (JT * 16 + CHUNK - 1) / CHUNK, RP = JK * CHUNK, DP = RP + 4;
-  typedef WaveTile<T, COLS> Tile;
+  typedef WaveTile<T, COLS, NARROW> Tile;
   __shared__ __align__(16) T buf[WAVES][TILE][Tile::PITCH];
   __shared__ __align__(16) float dinner[TILE][DP];
   __shared__ float sums[THREADS];
@@ -791,7 +853,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
       for (int j = 0; j < JK; j += MK) {
         const int r0 = j * CHUNK;
         Tile t;
-        t.load(down, K, min(r0 + (lane & 31), R - 1), k0, K);
+        t.load(down, K, min(r0 + (lane & 31), R - 1), k0);
         t.store(my, down, K, R - r0, k0, K);
         wave_sync();
 #pragma unroll
@@ -806,7 +868,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
       const int here = min(TILE, end - pos);
       const int rows = a.rows.row(min(pos + (lane & 31), end - 1));
       Tile tile;
-      tile.load(a.x, a.ldx, rows, k0, K);
+      tile.load(a.x, a.ldx, rows, k0);
       {  // the tile's part of every block is contiguous: groups of threads share out the blocks where it is short
         const int size = here * R;
         int width = 32;
@@ -897,8 +959,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
       __syncthreads();
     }
     pos = end;
-    const bool whole = a_start >= ci * a.chunk && a_end == end;
-    float *G = whole ? a.G + (long)id * K * R : a.split + adapter_split(a_start, a.chunk, ci) * K * R;
+    float *G = a_start >= ci * a.chunk ? a.G + (long)id * K * R : a.split + (long)ci * K * R;
 #pragma unroll
     for (int v = 0; v < VT; ++v) {
       const int col = k0 + v * 16 + c;
@@ -932,7 +993,7 @@ static __global__ void __launch_bounds__(1024) adapter_blocks_kernel(const float
   sum[i] = s;
 }
 
-// Sums the parts of the adapters that lie in several chunks, in order; zeros for those without rows.
+// Sums up what the chunks wrote of adapters that lie in several, in order; zeros for those without rows.
 struct JoinArgs {
   const float *split, *scale;  // scale may be nullptr
   float *G;
@@ -946,14 +1007,16 @@ static __global__ void __launch_bounds__(256) adapter_join_kernel(const int32_t 
     const int c0 = start / a.chunk, c1 = end > start ? (end - 1) / a.chunk : c0;
     if (end > start && c0 == c1) continue;
     const float f = a.scale ? a.scale[id] : 1.0f;
+    float *G = a.G + id * a.size;
     for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < a.size; i += (long)gridDim.x * 256) {
       float s = 0.0f;
       if (end > start) {
+        s = G[i];
 #pragma unroll 8
-        for (int c = c0; c <= c1; ++c) s += a.split[adapter_split(start, a.chunk, c) * a.size + i];
+        for (int c = c0 + 1; c <= c1; ++c) s += a.split[c * a.size + i];
         s *= f;
       }
-      a.G[id * a.size + i] = s;
+      G[i] = s;
     }
   }
 }
