@@ -76,16 +76,30 @@ bool preference_sizes_ok(int32_t T, int32_t pairs) {
 template <typename T>
 int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
   const int64_t rows = (int64_t)a.Tn * a.P * 2;
+  const int slots = a.rows.V / SlotOf<T>::N;
   if (rows > 0) {
-    hipLaunchKernelGGL((preference_words_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, a);
+    // (512 threads have eight slots each under way per round: shorter rows are left to fewer)
+    if (slots <= 256) hipLaunchKernelGGL((preference_words_kernel<T, 64>), dim3((unsigned)rows), dim3(64), 0, st, a);
+    else if (slots <= 1024) hipLaunchKernelGGL((preference_words_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((preference_words_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, a);
     LAUNCHED();
   }
-  hipLaunchKernelGGL(preference_pairs_kernel<T>, dim3((unsigned)a.P), dim3(64), 0, st, a);
+  const bool gradient = rows > 0 && a.rows.dz, held = slots <= HELD_SLOTS, inside = gradient && held && a.Tn <= PREFERENCE_INSIDE;
+  if (!inside) {
+    hipLaunchKernelGGL(preference_pairs_kernel<T>, dim3((unsigned)a.P), dim3(64), 0, st, a);
+    LAUNCHED();
+  }
+  if (!gradient) return RNNLM_OK;
+  if (!held) {
+    hipLaunchKernelGGL((preference_stream_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, a);
+  } else {
+    with_row_shape(rows, slots, [&](auto shape) {
+      constexpr int THREADS = decltype(shape)::threads, NV = decltype(shape)::nv;
+      if (inside) hipLaunchKernelGGL((preference_row_kernel<T, THREADS, NV, true>), dim3((unsigned)rows), dim3(THREADS), 0, st, a);
+      else hipLaunchKernelGGL((preference_row_kernel<T, THREADS, NV, false>), dim3((unsigned)rows), dim3(THREADS), 0, st, a);
+    });
+  }
   LAUNCHED();
-  if (rows > 0 && a.rows.dz) {
-    hipLaunchKernelGGL((preference_gradient_kernel<T, 512>), dim3((unsigned)rows), dim3(512), 0, st, a);
-    LAUNCHED();
-  }
   return RNNLM_OK;
 }
 

@@ -72,51 +72,78 @@ __device__ inline double preference_text(const PreferenceArgs<T> &a, int s, int 
 // ln(1 + e^x)
 __device__ inline double softplus(double x) { return (x > 0.0 ? x : 0.0) + log1p(exp(-fabs(x))); }
 
-// A wave a pair: losses, log-probabilities of the texts, factors of the gradients.
+// A pair's factors of the gradient, by one wave; its loss and its texts' log-probabilities, where asked for.
 template <typename T>
-__global__ void __launch_bounds__(64) preference_pairs_kernel(const PreferenceArgs<T> a) {
-  const int p = blockIdx.x;
+__device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int p, bool write) {
   int nc, no;
   double c = preference_text(a, p, nc), o = preference_text(a, a.P + p, no);
-  if (threadIdx.x != 0) return;
   const double sc = a.mean ? 1.0 / (nc > 0 ? nc : 1) : 1.0, so = a.mean ? 1.0 / (no > 0 ? no : 1) : 1.0;
   c *= sc;
   o *= so;
-  if (a.logp) {
+  write = write && (threadIdx.x & 63) == 0;
+  if (write && a.logp) {
     a.logp[p] = (float)c;
     a.logp[a.P + p] = (float)o;
   }
   const double w = a.weight ? (double)a.weight[p] : 1.0, beta = a.beta, eps = a.eps;
   if (w == 0.0) {
-    a.loss[p] = 0.0f;
-    a.pair[p] = {0.0, 0.0};
-    return;
+    if (write) a.loss[p] = 0.0f;
+    return {0.0, 0.0};
   }
   if (a.ref) {
     c -= (double)a.ref[p];
     o -= (double)a.ref[a.P + p];
   }
   const double r = c - o, x = beta * r;
-  double loss, g;
+  double g;
   if (a.kind == PREFER_LOGISTIC) {
-    loss = (1.0 - eps) * softplus(-x) + (eps == 0.0 ? 0.0 : eps * softplus(x));
-    g = beta * (eps / (1.0 + exp(-x)) - (1.0 - eps) / (1.0 + exp(x)));
+    if (write) a.loss[p] = (float)(w * ((1.0 - eps) * softplus(-x) + (eps == 0.0 ? 0.0 : eps * softplus(x))));
+    const double e = exp(-fabs(x)), small = e / (1.0 + e), large = 1.0 / (1.0 + e);  // sigma(-|x|), sigma(|x|)
+    g = beta * (eps * (x < 0.0 ? small : large) - (1.0 - eps) * (x < 0.0 ? large : small));
   } else if (a.kind == PREFER_SQUARED) {
     const double d = r - 0.5 / beta;
-    loss = d * d;
+    if (write) a.loss[p] = (float)(w * (d * d));
     g = 2.0 * d;
   } else {
-    loss = x >= 1.0 ? 0.0 : 1.0 - x;
+    if (write) a.loss[p] = (float)(w * (x >= 1.0 ? 0.0 : 1.0 - x));
     g = x >= 1.0 ? 0.0 : -beta;
   }
-  a.loss[p] = (float)(w * loss);
   g *= w * (double)a.scale;
-  a.pair[p] = {g * sc, -g * so};
+  return {g * sc, -g * so};
 }
 
-// The gradients, a row a workgroup.
+// Where texts are long, or no gradient is wanted: a wave a pair.
+template <typename T>
+__global__ void __launch_bounds__(64) preference_pairs_kernel(const PreferenceArgs<T> a) {
+  const PreferencePair p = preference_pair(a, blockIdx.x, true);
+  if (threadIdx.x == 0) a.pair[blockIdx.x] = p;
+}
+
+// The gradients, a row a workgroup, the row read again.  INSIDE: each finds its pair's factors itself, from the words of both
+// texts (up to PREFERENCE_INSIDE positions: a load or two of each lane), while its row is on the way.
+constexpr int PREFERENCE_INSIDE = 128;
+template <typename T, int THREADS, int NV, bool INSIDE>
+__global__ void __launch_bounds__(THREADS) preference_row_kernel(const PreferenceArgs<T> a) {
+  const WordRows<T> &w = a.rows;
+  const long m = blockIdx.x;
+  const PreferenceRow r = a.row[m];
+  T *drow = w.dz + m * w.ldd;
+  const T *row = w.z + m * w.ldz;
+  const int p = a.pair_of(m), s = (int)(m % (2 * a.P));
+  WordRow<T, THREADS, NV> held;
+  if (r.y >= 0) held.load(row, w.V, false);
+  __shared__ float g;
+  if (threadIdx.x < 64) {
+    const PreferencePair f = INSIDE ? preference_pair(a, p, m == s && s < a.P) : a.pair[p];
+    if (threadIdx.x == 0) g = (float)(s < a.P ? f.g_chosen : f.g_other);
+  }
+  __syncthreads();
+  if (r.y < 0 || r.l == -INFINITY) return word_no_gradient<T, THREADS>(drow, w.V);
+  held.gradient(r.sum, drow, to_f32(row[r.y]), r.y, w.V, 1.0f, g);
+}
+// Rows that do not fit the registers.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) preference_gradient_kernel(const PreferenceArgs<T> a) {
+__global__ void __launch_bounds__(THREADS) preference_stream_kernel(const PreferenceArgs<T> a) {
   const WordRows<T> &w = a.rows;
   const long m = blockIdx.x;
   const PreferenceRow r = a.row[m];
