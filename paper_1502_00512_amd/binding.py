@@ -218,7 +218,10 @@ def _rows(call, name, t, like=None):
         _refuse(call, f"{name}: float32 or bfloat16 rows on a GPU are wanted")
     if like is not None and (dtype is not like.dtype or t.get_device() != like.get_device()):
         _refuse(call, f"{name}: another type or device than the other logits'")
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
+    if t.is_contiguous() and len(shape) >= 2 and (V := shape[-1]) >= 1:  # (as most are)
+        return t.numel() // V, V, V, RNNLM_DTYPE_FP32 if dtype is torch.float32 else RNNLM_DTYPE_BF16
+    stride = t.stride()
     if len(shape) < 2 or (V := shape[-1]) < 1 or (stride[-1] != 1 and V > 1):
         _refuse(call, f"{name}: rows of neighbouring logits are wanted")
     rows, ld = 1, None
@@ -270,7 +273,9 @@ def _on(call, stream, device, f, *args):
 def _launch(device, f, *args):
     """f(*args, the current stream of that device) with that device current."""
     import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
+    # (the stream's number itself: an object around it takes longer than a launch's arguments)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    stream = torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device)
     if torch.cuda.current_device() == device:
         return f(*args, stream)
     with torch.cuda.device(device):
@@ -438,16 +443,19 @@ def _adapters(call, like, down, up, scale, K):
     """The adapters' description, N."""
     import torch
     dev = like.get_device()
-    if down.dim() != 3 or up.dim() != 3 or down.shape[0] != up.shape[0] or down.shape[1] != up.shape[2] or down.shape[2] != K:
+    if down.dim() != 3 or up.dim() != 3:
         _refuse(call, f"down: [n][R][{K}] and up: [n][N][R] are wanted")
-    (n, R, _), N = down.shape, up.shape[1]
-    return rnnlm_adapters(_at(call, "down", down, like.dtype, n * R * K, dev), _at(call, "up", up, like.dtype, n * N * R, dev),
+    (n, R, k), (n2, N, R2) = down.shape, up.shape
+    if n != n2 or R != R2 or k != K:
+        _refuse(call, f"down: [n][R][{K}] and up: [n][N][R] are wanted")
+    dtype = like.dtype
+    return rnnlm_adapters(_at(call, "down", down, dtype, n * R * K, dev), _at(call, "up", up, dtype, n * N * R, dev),
                           _at(call, "scale", scale, torch.float32, n, dev), n, R), N
 
 
 def _beside(call, name, t, x, width):
     """(address, elements from row to row) of rows of `width` beside the rows of x."""
-    if tuple(t.shape) != (*x.shape[:-1], width):
+    if t.shape[-1] != width or t.shape[:-1] != x.shape[:-1]:
         _refuse(call, f"{name}: a tensor of shape {(*x.shape[:-1], width)} is wanted")
     return t.data_ptr(), _rows(call, name, t, x)[2]
 

@@ -201,10 +201,14 @@ void launch_inner(const InnerArgs<T> &a, hipStream_t st) {
 }
 template <typename T, int NF, bool PACKED>
 void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
-  const int64_t tiles = (a.rows.M + ADAPTER_TILE - 1) / ADAPTER_TILE, cols = (a.N + 255) / 256;
-  // a wave walks over its columns with the next ones requested ahead, as long as every compute unit has three workgroups
-  a.blocks = (int)std::max<int64_t>(1, tiles * cols / 768);
-  const dim3 grid((unsigned)tiles, (unsigned)((cols + a.blocks - 1) / a.blocks));
+  const int64_t cols = (a.N + 255) / 256;
+  // a wave takes the adapters of its tile one after the other: smaller tiles until there is a workgroup for every compute unit
+  const auto tiles = [&]() { return (a.rows.M + a.tile - 1) / a.tile; };
+  a.tile = ADAPTER_TILE;
+  while (a.tile > 4 && tiles() * cols < 256) a.tile /= 2;
+  // and walks over its columns with the next ones requested ahead, as long as every compute unit has three workgroups
+  a.blocks = (int)std::max<int64_t>(1, tiles() * cols / 768);
+  const dim3 grid((unsigned)tiles(), (unsigned)((cols + a.blocks - 1) / a.blocks));
   hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED>), grid, dim3(256), 0, st, a);
 }
 template <typename T>
@@ -256,7 +260,7 @@ int adapter_forward(const T *x, int64_t ldx, int64_t M, int32_t K, int32_t N, co
   if (!inner) inner = reinterpret_cast<float *>(ws + p.inner);
   launch_inner<T>({rows, x, static_cast<const T *>(a.down), ldx, K, a.R, inner, flag}, st);
   LAUNCHED();
-  launch_outer<T>({rows, inner, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1,
+  launch_outer<T>({rows, inner, static_cast<const T *>(a.up), a.scale, base, out, ldb, ldo, N, a.R, 1, ADAPTER_TILE,
                    read_once(M, N, sizeof(T) == 4 ? RNNLM_DTYPE_FP32 : RNNLM_DTYPE_BF16)},
                   st);
   LAUNCHED();

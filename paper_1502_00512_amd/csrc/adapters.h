@@ -157,13 +157,14 @@ static __global__ void __launch_bounds__(1024) adapter_order_kernel(const Adapte
   else if (q - M <= rows.n) start[q - M] = r;
 }
 
-// What a wave knows of a tile: lane l < 32 (and l + 32) the row at position 32 tile + l and its adapter.
+// What a wave knows of a tile of up to 32 rows from position `first` on: lane l < 32 (and l + 32) the l-th row and its adapter.
 struct AdapterTile {
   int row, key;  // -1, n: behind the last row
-  __device__ AdapterTile(const AdapterRows &r, int first) {
-    const int pos = first + (threadIdx.x & 31);
-    row = pos < r.M ? r.row(pos) : -1;
-    key = pos < r.M ? r.key_at(pos) : r.n;
+  __device__ AdapterTile(const AdapterRows &r, int first, int rows) {
+    const int l = threadIdx.x & 31, pos = first + l;
+    const bool in = l < rows && pos < r.M;
+    row = in ? r.row(pos) : -1;
+    key = in ? r.key_at(pos) : r.n;
   }
   // The adapters of the tile one after the other, in the order of their first rows: the next one behind `left` (lanes not yet
   // dealt with), n when there is none.
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, WAVES = 8, TILE = ADAPTER_TILE;
   __shared__ float part[WAVES][RT * 16][TILE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
-  const AdapterTile tile(a.rows, blockIdx.x * TILE);
+  const AdapterTile tile(a.rows, blockIdx.x * TILE, TILE);
   const int n = a.rows.n;
   unsigned left = 0xffffffffu;
   int id = tile.next(left, n);
@@ -280,6 +281,7 @@ struct OuterArgs {
   T *out;
   long ldb, ldo;
   int N, R, blocks;    // blocks of 64 columns of a wave
+  int tile;            // rows of a tile, at most 32
   bool once;           // base and out are read and written past the caches
 };
 
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
   __shared__ float turn[4][TILE][PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int n = a.rows.n, N = a.N, R = a.R;
-  const AdapterTile tile(a.rows, blockIdx.x * TILE);
+  const AdapterTile tile(a.rows, blockIdx.x * a.tile, a.tile);
   const int kq = (PACKED ? q & 1 : q) * VEC;
   // inner of the tile's rows (columns of the product), times the adapter's factor
   slot_t fu[2][NF][PARTS];
