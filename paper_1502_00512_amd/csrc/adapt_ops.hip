@@ -201,7 +201,10 @@ void launch_inner(const InnerArgs<T> &a, hipStream_t st) {
 }
 template <typename T, int NF, bool PACKED>
 void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
-  const int64_t cols = (a.N + 255) / 256;
+  // Columns of a wave: what registers hold of up.  2560 rows of 64000, R = 64: fp32 574 us with 32 columns and 868 with 64 (which
+  // spill), bf16 283 and 267.
+  constexpr int VT = NF == 1 || sizeof(T) == 2 ? 4 : 2;
+  const int64_t cols = (a.N + 64 * VT - 1) / (64 * VT);
   // a wave takes the adapters of its tile one after the other: smaller tiles until there is a workgroup for every compute unit
   const auto tiles = [&]() { return (a.rows.M + a.tile - 1) / a.tile; };
   a.tile = ADAPTER_TILE;
@@ -209,7 +212,7 @@ void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
   // and walks over its columns with the next ones requested ahead, as long as every compute unit has three workgroups
   a.blocks = (int)std::max<int64_t>(1, tiles() * cols / 768);
   const dim3 grid((unsigned)tiles(), (unsigned)((cols + a.blocks - 1) / a.blocks));
-  hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED>), grid, dim3(256), 0, st, a);
+  hipLaunchKernelGGL((adapter_outer_kernel<T, NF, PACKED, VT>), grid, dim3(256), 0, st, a);
 }
 template <typename T>
 void launch_outer(const OuterArgs<T> &a, hipStream_t st) {
@@ -293,7 +296,7 @@ int adapter_backward(const T *dout, int64_t ldd, const T *x, int64_t ldx, const 
     LAUNCHED();
   }
   const int64_t size = (int64_t)std::max(N, K) * a.R;
-  const unsigned ids_y = std::min(a.n, 2048), parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>((size + 1023) / 1024, 4096 / ids_y));
+  const unsigned ids_y = std::min(a.n, 1024), parts = (unsigned)std::max<int64_t>(1, std::min<int64_t>((size + 1023) / 1024, 1024 / ids_y));
   hipLaunchKernelGGL(adapter_join_kernel, dim3(parts, ids_y, 2), dim3(256), 0, st, start, a.n,
                      JoinArgs{floats(p.split_up), a.scale, dup, (int64_t)N * a.R, up.chunk},
                      JoinArgs{floats(p.split_down), nullptr, ddown, (int64_t)K * a.R, down.chunk});

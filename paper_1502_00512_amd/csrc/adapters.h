@@ -280,16 +280,16 @@ struct OuterArgs {
   const T *base;       // may be nullptr (zeros), may be out
   T *out;
   long ldb, ldo;
-  int N, R, blocks;    // blocks of 64 columns of a wave
+  int N, R, blocks;    // blocks of columns of a wave
   int tile;            // rows of a tile, at most 32
   bool once;           // base and out are read and written past the caches
 };
 
-// out = base + f up inner: a wave a tile and 64 columns, `blocks` times; through LDS so that base and out move in whole lines.
+// out = base + f up inner: a wave a tile and 16 VT columns, `blocks` times; through LDS so that base and out move in whole lines.
 // Bound by HBM.  NF: operand slots of R.  PACKED (bf16, R <= 16): both parts of inner in one product, beside one another.
-template <typename T, int NF, bool PACKED>
+template <typename T, int NF, bool PACKED, int VT>
 __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T> a) {
-  constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, COLS = 64, PITCH = COLS + 4;
+  constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, COLS = 16 * VT, PITCH = COLS + 4;
   constexpr int PARTS = sizeof(T) == 4 || PACKED ? 1 : 2, LANES = COLS / VEC, ROWS = 64 / LANES, MOVES = TILE / ROWS;
   __shared__ float turn[4][TILE][PITCH];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
@@ -353,10 +353,10 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
     }
   };
   // (columns behind the last one, of narrow arrays: the last one again, dropped)
-  const auto load_up = [&](int v0, int id, slot_t (&fa)[4][NF]) {
+  const auto load_up = [&](int v0, int id, slot_t (&fa)[VT][NF]) {
     const T *up = a.up + (long)id * N * R;
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
+    for (int v = 0; v < VT; ++v)
 #pragma unroll
       for (int i = 0; i < NF; ++i) {
         const int col = min(v0 + v * 16 + c, N - 1), k = i * CHUNK + kq;
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
   const int id0 = tile.next(left, n);
   const unsigned left0 = left;
   constexpr bool EARLY = NF == 1 || sizeof(T) == 2;  // up is requested a step ahead, too (where registers are left for it)
-  slot_t old[2][MOVES], fa[EARLY ? 2 : 1][4][NF];
+  slot_t old[2][MOVES], fa[EARLY ? 2 : 1][VT][NF];
   load_base(start(first), old[0]);
   if (EARLY && id0 < n) load_up(start(first), id0, fa[0]);
   for (int from = first; from < end; from += 4 * COLS) {
@@ -379,7 +379,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
     for (int t = 0; t < 2; ++t)
       if (key[t] >= n) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v)  // (x + -0 is x)
+        for (int v = 0; v < VT; ++v)  // (x + -0 is x)
           *reinterpret_cast<f32x4_t *>(&turn[wave][t * 16 + c][v * 16 + q * 4]) = f32x4_t{-0.0f, -0.0f, -0.0f, -0.0f};
       }
     left = left0;
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
       else if (next < n) load_up(v0, next, fa[1]);
       else if (after < end) load_up(start(after), id0, fa[1]);
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
+      for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           f32x4_t acc = {};
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
           if (key[t] == id) *reinterpret_cast<f32x4_t *>(&turn[wave][t * 16 + c][v * 16 + q * 4]) = acc;
         }
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
+      for (int v = 0; v < VT; ++v)
 #pragma unroll
         for (int i = 0; i < NF; ++i) fa[0][v][i] = fa[EARLY][v][i];
       id = next;
