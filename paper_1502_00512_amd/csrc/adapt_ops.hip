@@ -126,6 +126,11 @@ GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave
   const int64_t most = std::max<int64_t>((tiles * p.blocks + 511) / 512, (int64_t)std::lround(std::sqrt(parts_us / 3.0)));
   const int64_t each = std::min<int64_t>({tiles, ADAPTER_CHUNK / ADAPTER_TILE, std::max<int64_t>(1, most)}), chunks = (tiles + each - 1) / each;
   p.chunk = (int)((tiles + chunks - 1) / chunks) * ADAPTER_TILE;
+  // Few workgroups: parts of tiles, by the same costs, since a workgroup takes its adapters one after the other (160 rows of 8
+  // adapters, N = 2000: 38 us by whole tiles, 34 so; 64 rows of one adapter, N = 10000, R = 60, lose 13 us by less than the costs).
+  const double rows_least = std::sqrt((double)rows * W * R * 8 / 5e6 * ADAPTER_TILE / 3.0);
+  if (chunks * p.blocks < 128)
+    p.chunk = (int)std::min<int64_t>(p.chunk, round_up(std::max<int64_t>({1, rows * p.blocks / 256, std::lround(rows_least)}), 8));
   p.chunks = (int)std::max<int64_t>(1, (rows + p.chunk - 1) / p.chunk);
   return p;
 }
