@@ -111,9 +111,10 @@ int adapter_r_tiles(int32_t R) { return (R + 15) / 16; }
 constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return bf16 ? (r_tiles == 1 ? 8 : 4) : r_tiles <= 2 ? 4 : 2; }
 constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
-// A sum over rows for W columns: blocks of columns, positions of a chunk.  A workgroup takes some 3 us a tile; each chunk may
-// leave W R numbers to be written and read once more: together least at chunks of sqrt(that time, chunks of one tile / 3 us)
-// tiles.  More than some 512 workgroups gain nothing.
+// A sum over rows for W columns: blocks of columns, positions of a chunk.  A compute unit holds one workgroup, which takes some
+// 6 us and 2.5 a tile; each chunk may leave W R numbers to be written and read once more.  The chunk for which rounds of
+// workgroups and that come out least (900 rows, N = 33278, R = 5, fp32: 85 us by chunks until there were 512 workgroups, which
+// made 520, 3 rounds).
 struct GradPlan {
   int blocks, chunks, chunk;
 };
@@ -122,10 +123,13 @@ GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave
   const int cols = ADAPTER_GRAD_WAVES * 16 * tiles_of_wave;
   p.blocks = (W + cols - 1) / cols;
   const int64_t tiles = std::max<int64_t>(1, (rows + ADAPTER_TILE - 1) / ADAPTER_TILE);
-  const double parts_us = (double)tiles * W * R * 4 * 2 / 5e6;
-  const int64_t most = std::max<int64_t>((tiles * p.blocks + 511) / 512, (int64_t)std::lround(std::sqrt(parts_us / 3.0)));
-  const int64_t each = std::min<int64_t>({tiles, ADAPTER_CHUNK / ADAPTER_TILE, std::max<int64_t>(1, most)}), chunks = (tiles + each - 1) / each;
-  p.chunk = (int)((tiles + chunks - 1) / chunks) * ADAPTER_TILE;
+  int64_t chunks = 1;
+  double least = INFINITY;
+  for (int64_t each = 1; each <= std::min<int64_t>(tiles, ADAPTER_CHUNK / ADAPTER_TILE); ++each) {
+    const int64_t k = (tiles + each - 1) / each, rounds = (k * p.blocks + 255) / 256;
+    const double us = rounds * (2.5 * each + 6.0) + (double)k * W * R * 8 / 5e6;
+    if (us <= least) least = us, chunks = k, p.chunk = (int)each * ADAPTER_TILE;
+  }
   // Few workgroups: parts of tiles, by the same costs, since a workgroup takes its adapters one after the other (160 rows of 8
   // adapters, N = 2000: 38 us by whole tiles, 34 so; 64 rows of one adapter, N = 10000, R = 60, lose 13 us by less than the costs).
   const double rows_least = std::sqrt((double)rows * W * R * 8 / 5e6 * ADAPTER_TILE / 3.0);
