@@ -31,7 +31,7 @@ SYMBOLS = [
     "rnnlm_top_logits_workspace_bytes", "rnnlm_top_logits", "rnnlm_distill_loss", "rnnlm_verify_workspace_bytes",
     "rnnlm_verify_drafts", "rnnlm_forward_logits", "rnnlm_distill_train_chunk", "rnnlm_distill_grad_chunk",
     "rnnlm_distill_grad_chunk_compressed", "rnnlm_verify_chunk",
-    "rnnlm_policy_loss", "rnnlm_preference_workspace_bytes", "rnnlm_preference_loss",
+    "rnnlm_policy_loss", "rnnlm_preference_workspace_bytes", "rnnlm_preference_loss", "rnnlm_set_preference_wait",
     "rnnlm_adapter_workspace_bytes", "rnnlm_adapter_forward", "rnnlm_adapter_backward",
     "rnnlm_policy_train_chunk", "rnnlm_policy_grad_chunk", "rnnlm_policy_grad_chunk_compressed", "rnnlm_preference_train_chunk",
     "rnnlm_preference_grad_chunk", "rnnlm_preference_grad_chunk_compressed", "rnnlm_forward_adapted",
@@ -149,6 +149,7 @@ def load():
     lib.rnnlm_preference_workspace_bytes.argtypes = [i32, i32]
     lib.rnnlm_preference_loss.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, vp, i32, f32, f32, i32, f32, vp, vp, vp, vp, i64, vp,
                                           vp, C.c_size_t, vp]
+    lib.rnnlm_set_preference_wait.argtypes = [i32]
     lib.rnnlm_adapter_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32, i32]
     lib.rnnlm_adapter_forward.argtypes = [vp, i64, i32, i64, i32, i32, C.POINTER(rnnlm_adapters), vp, vp, i64, vp, i64, vp, vp, vp,
                                           C.c_size_t, vp]
@@ -433,6 +434,10 @@ def rnnlm_preference_loss(logits, y, ref=None, weight=None, kind: int = RNNLM_PR
                 _at(call, "sum_loss", sum_loss, torch.float64, 1, dev), dz, ldd, _at(call, "range_flag", range_flag, i32, 1, dev), at,
                 nbytes), call)
     return loss, logp
+
+
+def rnnlm_set_preference_wait(polls: int):
+    _ok(load().rnnlm_set_preference_wait(polls), "rnnlm_set_preference_wait")
 
 
 def rnnlm_adapter_workspace_bytes(rows: int, K: int, N: int, n: int, R: int, dtype: int, backward: bool = False) -> int:

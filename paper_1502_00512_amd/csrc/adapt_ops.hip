@@ -1,5 +1,7 @@
 // Host side of the operators that adapt a trained model (include/rnnlm.h, "Adapting"): checks of arguments, choice of kernel,
 // launches.
+#include <atomic>
+
 #include "adapters.h"
 #include "call_checks.h"
 #include "losses.h"
@@ -69,7 +71,27 @@ int policy_call(const PolicyArgs<T> &a, int64_t rows, hipStream_t st) {
 }
 
 // ---- preference loss ----
-size_t preference_rows_bytes(int64_t rows) { return align256((size_t)rows * sizeof(PreferenceRow)); }
+std::atomic<int32_t> preference_polls{256};  // of about a microsecond
+
+struct PreferencePlan {
+  size_t row, pair, published, done, total;
+};
+PreferencePlan preference_plan(int32_t T, int32_t pairs) {
+  const size_t rows = (size_t)T * pairs * 2;
+  PreferencePlan p;
+  size_t o = 0;
+  auto take = [&](size_t n) {
+    const size_t at = o;
+    o += align256(n);
+    return at;
+  };
+  p.row = take(rows * sizeof(PreferenceRow));
+  p.pair = take((size_t)pairs * sizeof(PreferencePair));
+  p.published = take(rows * sizeof(unsigned long long));
+  p.done = take(rows * sizeof(int));
+  p.total = o;
+  return p;
+}
 bool preference_sizes_ok(int32_t T, int32_t pairs) {
   return T >= 0 && pairs >= 1 && pairs <= (1 << 20) && (int64_t)T * pairs * 2 <= ROWS_MAX;
 }
@@ -77,6 +99,19 @@ template <typename T>
 int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
   const int64_t rows = (int64_t)a.Tn * a.P * 2;
   const int slots = a.rows.V / SlotOf<T>::N;
+  // Rows that meet, where they are more than the caches hold: MEET_MEASURED
+  if (rows > 0 && a.rows.dz && slots <= HELD_SLOTS && a.Tn <= PREFERENCE_MEET && (double)rows * a.rows.V * sizeof(T) > 64e6) {
+    hipLaunchKernelGGL(preference_clear_kernel<T>, dim3((unsigned)std::min<int64_t>(256, (rows + 255) / 256)), dim3(256), 0, st, a, (long)rows);
+    LAUNCHED();
+    with_row_shape(rows, slots, [&](auto shape) {
+      constexpr int THREADS = decltype(shape)::threads, NV = decltype(shape)::nv;
+      hipLaunchKernelGGL((preference_meet_kernel<T, THREADS, NV>), dim3((unsigned)rows), dim3(THREADS), 0, st, a);
+    });
+    LAUNCHED();
+    hipLaunchKernelGGL((preference_rest_kernel<T, 512>), dim3((unsigned)std::min<int64_t>(rows, 256)), dim3(512), 0, st, a, (long)rows);
+    LAUNCHED();
+    return RNNLM_OK;
+  }
   if (rows > 0) {
     // (512 threads have eight slots each under way per round: shorter rows are left to fewer)
     if (slots <= 256) hipLaunchKernelGGL((preference_words_kernel<T, 64>), dim3((unsigned)rows), dim3(64), 0, st, a);
@@ -395,7 +430,13 @@ int rnnlm_policy_loss(const void *logits, int32_t dtype, int64_t rows, int32_t V
 }
 
 size_t rnnlm_preference_workspace_bytes(int32_t T, int32_t pairs) {
-  return preference_sizes_ok(T, pairs) ? preference_rows_bytes((int64_t)T * pairs * 2) + align256((size_t)pairs * sizeof(PreferencePair)) : 0;
+  return preference_sizes_ok(T, pairs) ? preference_plan(T, pairs).total : 0;
+}
+
+int rnnlm_set_preference_wait(int32_t polls) {
+  if (polls < 0) return RNNLM_ERR_ARG;
+  preference_polls = polls;
+  return RNNLM_OK;
 }
 
 int rnnlm_preference_loss(const void *logits, int32_t dtype, int32_t T, int32_t pairs, int32_t V, int64_t ld, const int32_t *y,
@@ -414,11 +455,13 @@ int rnnlm_preference_loss(const void *logits, int32_t dtype, int32_t T, int32_t 
     return RNNLM_ERR_ARG;
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < rnnlm_preference_workspace_bytes(T, pairs)) return RNNLM_ERR_ARG;
   hipStream_t st = (hipStream_t)stream;
+  const PreferencePlan p = preference_plan(T, pairs);
+  char *ws = static_cast<char *>(workspace);
   const auto call = [&](auto rows_of) {
     typedef std::remove_const_t<std::remove_pointer_t<decltype(rows_of.z)>> E;
     return preference_call<E>({rows_of, ref, weight, loss, logp, T, pairs, kind, mean != 0, beta, smoothing, scale,
-                               static_cast<PreferenceRow *>(workspace),
-                               reinterpret_cast<PreferencePair *>(static_cast<char *>(workspace) + preference_rows_bytes(rows))},
+                               reinterpret_cast<PreferenceRow *>(ws + p.row), reinterpret_cast<PreferencePair *>(ws + p.pair),
+                               reinterpret_cast<unsigned long long *>(ws + p.published), reinterpret_cast<int *>(ws + p.done), preference_polls.load()},
                               st);
   };
   const int rc = dtype == RNNLM_DTYPE_FP32 ? call(word_rows<float>(logits, rows, V, ld, y, 1.0f, dlogits, ld_dlogits, range_flag))

@@ -29,6 +29,10 @@ struct PreferenceArgs {
   float beta, eps, scale;
   PreferenceRow *row;
   PreferencePair *pair;
+  // rows that meet (preference_meet_kernel): their words as they are published, whether the gradient is written, polls of a wait
+  unsigned long long *published;
+  int *done;
+  int polls;
   __device__ int pair_of(long m) const {
     const int s = (int)(m % (2 * P));
     return s < P ? s : s - P;
@@ -53,15 +57,22 @@ __global__ void __launch_bounds__(THREADS) preference_words_kernel(const Prefere
   if (threadIdx.x == 0) a.row[m] = out;
 }
 
-// Sum of the log-probabilities of stream s and number of its words: one wave, in a fixed order.
-template <typename T>
-__device__ inline double preference_text(const PreferenceArgs<T> &a, int s, int &count) {
+// A word's log-probability as another workgroup reads it; two NaNs of their own kind: not published yet, and a position that
+// does not count.
+constexpr unsigned long long WORD_EMPTY = ~0ull, WORD_NONE = ~1ull;
+__device__ inline unsigned long long word_published(double l, int y) {
+  return y < 0 ? WORD_NONE : l != l ? 0x7ff8000000000000ull : __builtin_bit_cast(unsigned long long, l);
+}
+
+// Sum of the log-probabilities of a text and number of its words: one wave, in a fixed order.  word(t): as published.
+template <class F>
+__device__ inline double preference_text(int Tn, int &count, F &&word) {
   double l = 0.0;
   count = 0;
-  for (int t = threadIdx.x & 63; t < a.Tn; t += 64) {
-    const PreferenceRow &row = a.row[(long)t * 2 * a.P + s];
-    if (row.y >= 0) {
-      l += row.l;
+  for (int t = threadIdx.x & 63; t < Tn; t += 64) {
+    const unsigned long long w = word(t);
+    if (w != WORD_NONE) {
+      l += __builtin_bit_cast(double, w);
       ++count;
     }
   }
@@ -72,11 +83,12 @@ __device__ inline double preference_text(const PreferenceArgs<T> &a, int s, int 
 // ln(1 + e^x)
 __device__ inline double softplus(double x) { return (x > 0.0 ? x : 0.0) + log1p(exp(-fabs(x))); }
 
-// A pair's factors of the gradient, by one wave; its loss and its texts' log-probabilities, where asked for.
-template <typename T>
-__device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int p, bool write) {
+// A pair's factors of the gradient, by one wave; its loss and its texts' log-probabilities, where asked for.  word(t, other): the
+// words of the preferred text and of the other one.
+template <typename T, class F>
+__device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int p, bool write, F &&word) {
   int nc, no;
-  double c = preference_text(a, p, nc), o = preference_text(a, a.P + p, no);
+  double c = preference_text(a.Tn, nc, [&](int t) { return word(t, 0); }), o = preference_text(a.Tn, no, [&](int t) { return word(t, 1); });
   const double sc = a.mean ? 1.0 / (nc > 0 ? nc : 1) : 1.0, so = a.mean ? 1.0 / (no > 0 ? no : 1) : 1.0;
   c *= sc;
   o *= so;
@@ -111,11 +123,19 @@ __device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int
   g *= w * (double)a.scale;
   return {g * sc, -g * so};
 }
+// The same from the rows of the first pass.
+template <typename T>
+__device__ inline PreferencePair preference_pair_of_rows(const PreferenceArgs<T> &a, int p, bool write) {
+  return preference_pair(a, p, write, [&](int t, int other) {
+    const PreferenceRow &row = a.row[((long)t * 2 + other) * a.P + p];
+    return word_published(row.l, row.y);
+  });
+}
 
 // Where texts are long, or no gradient is wanted: a wave a pair.
 template <typename T>
 __global__ void __launch_bounds__(64) preference_pairs_kernel(const PreferenceArgs<T> a) {
-  const PreferencePair p = preference_pair(a, blockIdx.x, true);
+  const PreferencePair p = preference_pair_of_rows(a, blockIdx.x, true);
   if (threadIdx.x == 0) a.pair[blockIdx.x] = p;
 }
 
@@ -134,7 +154,7 @@ __global__ void __launch_bounds__(THREADS) preference_row_kernel(const Preferenc
   if (r.y >= 0) held.load(row, w.V, false);
   __shared__ float g;
   if (threadIdx.x < 64) {
-    const PreferencePair f = INSIDE ? preference_pair(a, p, m == s && s < a.P) : a.pair[p];
+    const PreferencePair f = INSIDE ? preference_pair_of_rows(a, p, m == s && s < a.P) : a.pair[p];
     if (threadIdx.x == 0) g = (float)(s < a.P ? f.g_chosen : f.g_other);
   }
   __syncthreads();
@@ -153,6 +173,113 @@ __global__ void __launch_bounds__(THREADS) preference_stream_kernel(const Prefer
   const T *row = w.z + m * w.ldz;
   const float g = (float)((int)(m % (2 * a.P)) < a.P ? p.g_chosen : p.g_other);
   word_gradient_by_memory<T, THREADS>(r.sum, row, drow, tail_elem(row, threadIdx.x, w.V), to_f32(row[r.y]), r.y, w.V, 1.0f, g);
+}
+
+// ---- rows that meet ----
+// One pass over the logits where they are many: a workgroup holds its row, publishes its word's log-probability (the word is
+// its own flag) and waits for those of its pair, which were started next to it.  A wait ends after `polls` polls, too (the rest
+// of a pair may not be on the GPU yet, where other work fills it): such a row is taken again by preference_rest_kernel.
+constexpr int PREFERENCE_MEET = 64;  // most positions of a text: the pair's rows are at most half of what the GPU holds
+
+template <typename T>
+__global__ void __launch_bounds__(256) preference_clear_kernel(const PreferenceArgs<T> a, long rows) {
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < rows; i += 256L * gridDim.x) a.published[i] = WORD_EMPTY;
+}
+
+template <typename T, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS, 4) preference_meet_kernel(const PreferenceArgs<T> a) {
+  __shared__ WordShared<THREADS / 64> sh;
+  __shared__ unsigned long long words[2 * PREFERENCE_MEET];
+  __shared__ int met, masked;  // (not in sh: its sums may still be read)
+  const WordRows<T> &w = a.rows;
+  // workgroups in the order of the pairs
+  const int p = blockIdx.x / (2 * a.Tn), k = blockIdx.x % (2 * a.Tn), s = k & 1 ? a.P + p : p;
+  const long m = (long)(k >> 1) * 2 * a.P + s;
+  int y = w.word(m);
+  if (a.weight && a.weight[p] == 0.0f) y = -1;
+  const T *row = w.z + m * w.ldz;
+  T *drow = w.dz + m * w.ldd;
+  WordRow<T, THREADS, NV> held;
+  WordSum r = {};
+  float zy = 0.0f;
+  if (y >= 0) {
+    held.load(row, w.V, w.once);
+    zy = to_f32(row[y]);
+    r = held.sum(row, w.V, 1.0f, sh);
+  }
+  double l = 0.0;
+  if (threadIdx.x == 0) {
+    if (y >= 0) l = r.logp(zy, 1.0f);
+    __hip_atomic_store(a.published + m, word_published(l, y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    masked = l == -INFINITY;
+  }
+  if (y < 0) {
+    word_no_gradient<T, THREADS>(drow, w.V);
+    if (k != 0) {  // (the pair's first row sees to its loss)
+      if (threadIdx.x == 0) a.done[m] = 1;
+      return;
+    }
+  }
+  for (int i = threadIdx.x; i < 2 * a.Tn; i += THREADS) {
+    const unsigned long long *at = a.published + (long)(i >> 1) * 2 * a.P + (i & 1 ? a.P + p : p);
+    unsigned long long v = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int n = 0; v == WORD_EMPTY && n < a.polls; ++n) {
+      __builtin_amdgcn_s_sleep(4);
+      v = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    words[i] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    bool all = true;
+    for (int i = threadIdx.x; i < 2 * a.Tn; i += 64) all = all && words[i] != WORD_EMPTY;
+    all = __all(all);
+    if (all) {
+      const PreferencePair f = preference_pair(a, p, k == 0, [&](int t, int other) { return words[2 * t + other]; });
+      if (threadIdx.x == 0) sh.g = (float)(k & 1 ? f.g_other : f.g_chosen);
+    }
+    if (threadIdx.x == 0) {
+      a.done[m] = all;
+      met = all;
+    }
+  }
+  __syncthreads();
+  if (!met || y < 0) return;
+  if (masked) return word_no_gradient<T, THREADS>(drow, w.V);
+  held.gradient(r, drow, zy, y, w.V, 1.0f, sh.g);
+}
+
+// Rows whose wait ended early, by two passes over memory; every word has been published by now.
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS) preference_rest_kernel(const PreferenceArgs<T> a, long rows) {
+  __shared__ WordShared<THREADS / 64> sh;
+  const WordRows<T> &w = a.rows;
+  for (long first = blockIdx.x; first < rows; first += (long)gridDim.x * 64) {
+    // (each wave looks at the same 64 rows, so that all agree)
+    const long mine = first + (long)(threadIdx.x & 63) * gridDim.x;
+    unsigned long long open = __ballot(mine < rows && !a.done[mine < rows ? mine : 0]);
+    while (open) {
+      const long m = first + (long)(__ffsll(open) - 1) * gridDim.x;
+      open &= open - 1;
+      const int s = (int)(m % (2 * a.P)), p = s < a.P ? s : s - a.P;
+      const unsigned long long word = a.published[m];
+      if (threadIdx.x < 64) {
+        const PreferencePair f = preference_pair(a, p, m == s && s < a.P, [&](int t, int other) { return a.published[((long)t * 2 + other) * a.P + p]; });
+        if (threadIdx.x == 0) sh.g = (float)(s < a.P ? f.g_chosen : f.g_other);
+      }
+      T *drow = w.dz + m * w.ldd;
+      const T *row = w.z + m * w.ldz;
+      if (word != WORD_NONE && __builtin_bit_cast(double, word) != -INFINITY) {
+        const int y = w.y[m];
+        const float zt = tail_elem(row, threadIdx.x, w.V), zy = to_f32(row[y]);
+        const WordSum r = word_sum_by_memory<T, THREADS, 4, false>(row, zt, w.V, 1.0f, sh);  // (barriers)
+        word_gradient_by_memory<T, THREADS>(r, row, drow, zt, zy, y, w.V, 1.0f, sh.g);
+      } else {
+        word_no_gradient<T, THREADS>(drow, w.V);
+      }
+      __syncthreads();
+    }
+  }
 }
 
 }  // namespace rnnlm_dev

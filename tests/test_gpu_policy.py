@@ -360,6 +360,49 @@ def test_preference_loss_alone_agrees(V):
         same(loss.cpu(), L, 0.1 * 18 * row_err(z.reshape(-1), 1.0) + F32 * np.abs(L), "loss")
 
 
+@pytest.mark.parametrize("dtype,T,P,V,in_place", [("fp32", 3, 4, 700001, False), ("bf16", 20, 9, 100003, False), ("bf16", 64, 1, 300001, True), ("fp32", 1, 150, 60000, False),
+                                                  ("bf16", 5, 700, 5001, False), ("fp32", 40, 30, 7001, True), ("bf16", 2, 60, 160001, False)])
+@pytest.mark.parametrize("polls", [256, 0])
+def test_preference_rows_that_meet(dtype, T, P, V, in_place, polls):
+    """Many large rows: workgroups wait for their pair's, or (no polls) leave their gradients to a second pass; the same bits as
+    text by text, where rows are few."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.empty(T, 2 * P, V, dtype=DTYPES[dtype], device="cuda").normal_(0.0, 2.0, generator=gen)
+    y = torch.randint(0, V, (T, 2 * P), generator=gen, device="cuda", dtype=torch.int32)
+    if T > 1:
+        y[torch.rand(T, 2 * P, generator=gen, device="cuda") < 0.2] = -1
+    y[0, 0] = -1
+    z[0, 0] = float("nan")
+    z[-1, 1, int(y[-1, 1])] = -float("inf")  # a masked word (where it counts)
+    ref, w = torch.randn(2 * P, generator=gen, device="cuda"), torch.rand(P, generator=gen, device="cuda")
+    w[P - 1] = 0.0 if P > 2 else 1.0
+    parts = []
+    for p in range(P):  # a pair at a time: too few rows to meet (or, of one pair, read in halves of its words' order)
+        two = z[:, [p, P + p]].contiguous()
+        d = torch.empty_like(two)
+        loss, logp = binding.rnnlm_preference_loss(two, y[:, [p, P + p]].contiguous(), ref[[p, P + p]].contiguous(), w[p: p + 1].contiguous(), beta=0.3, smoothing=0.1,
+                                                   mean=True, scale=0.7, dlogits=d)
+        parts.append((loss, logp, d))
+    try:
+        binding.rnnlm_set_preference_wait(polls)
+        dz = z if in_place else torch.full_like(z, 5.0)
+        total = torch.zeros(1, dtype=torch.float64, device="cuda")
+        loss, logp = binding.rnnlm_preference_loss(z, y, ref, w, beta=0.3, smoothing=0.1, mean=True, scale=0.7, dlogits=dz, sum_loss=total)
+        torch.cuda.synchronize()
+    finally:
+        binding.rnnlm_set_preference_wait(256)
+    # sums of a row's exponentials may be formed in another order: E of the logarithms, as above
+    E = 2 * row_err(np.full(V, 12.0), 1.0)
+    for p, (l, s, d) in enumerate(parts):
+        for got, want, scale in ((loss[p], l[0], 1.0), (logp[p], s[0], 1.0), (logp[P + p], s[1], 1.0)):
+            assert got.item() == want.item() or abs(got.item() - want.item()) <= E * scale + 2 * F32 * abs(want.item()), p
+        got, want = dz[:, [p, P + p]].float(), d.float()
+        top = want.abs().amax(2, keepdim=True)
+        assert bool(((got - want).abs() <= 2 * HALF[dtype] * want.abs() + 4 * E * want.abs() + E * top + 2.0 ** -126).all()), p
+        zero = (y[:, [p, P + p]] < 0) | (w[p] == 0)
+        assert not got[zero].any()
+
+
 def test_preference_of_no_positions():
     d = torch.empty(0, 6, 30, device="cuda")
     y = torch.empty(0, 6, dtype=torch.int32, device="cuda")
