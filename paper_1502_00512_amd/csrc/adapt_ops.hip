@@ -99,8 +99,10 @@ template <typename T>
 int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
   const int64_t rows = (int64_t)a.Tn * a.P * 2;
   const int slots = a.rows.V / SlotOf<T>::N;
-  // Rows that meet, where they are more than the caches hold: MEET_MEASURED
-  if (rows > 0 && a.rows.dz && slots <= HELD_SLOTS && a.Tn <= PREFERENCE_MEET && (double)rows * a.rows.V * sizeof(T) > 64e6) {
+  // Rows that meet, where the logits are many and the rows long: they and two passes, us: 26 x 10 bf16 rows of 64000 (33 MB) 22.0
+  // and 23.8, 128 x 10 of 33000 46 and 48, 128 x 20 of 100000 211 and 297, 32 x 20 fp32 of 33278 42 and 48; but 64 x 10 bf16 of
+  // 10000 15.0 and 13.0, 128 x 10 of them 19.4 and 17.4, and 128 x 64 rows of 4000 57 and 45 (a wave a row: all of them wait).
+  if (rows > 0 && a.rows.dz && slots <= HELD_SLOTS && slots >= 1024 && a.Tn <= PREFERENCE_MEET && (double)rows * a.rows.V * sizeof(T) > 30e6) {
     hipLaunchKernelGGL(preference_clear_kernel<T>, dim3((unsigned)std::min<int64_t>(256, (rows + 255) / 256)), dim3(256), 0, st, a, (long)rows);
     LAUNCHED();
     with_row_shape(rows, slots, [&](auto shape) {
