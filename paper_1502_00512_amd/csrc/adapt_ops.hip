@@ -145,7 +145,13 @@ constexpr int64_t ADAPTER_ROWS_MAX = 1 << 17;  // (putting the rows in order com
 
 int adapter_r_tiles(int32_t R) { return (R + 15) / 16; }
 // Columns of a wave of adapter_grad_kernel, in 16s: as many as its accumulators and operands leave registers for.
-constexpr int adapter_grad_tiles(int r_tiles, bool bf16) { return bf16 ? (r_tiles == 1 ? 8 : 4) : r_tiles <= 2 ? 4 : 2; }
+// small: half of them where that lets two workgroups share a compute unit (R <= 16), for gradients of up to 128 MB: they and the
+// others, us: 160 x 2000 bf16 (R = 16) 27.7 and 31.2, 900 x 33278 fp32 (R = 5) 75 and 80; but 2560 x 64000 bf16 (R = 16, 1 and
+// 128 adapters) 111 and 106, 294 and 271, fp32 209 and 203 (twice the parts of dinner).
+constexpr int adapter_grad_tiles(int r_tiles, bool bf16, bool small) {
+  return r_tiles == 1 ? (bf16 ? 8 : 4) / (small ? 2 : 1) : bf16 || r_tiles == 2 ? 4 : 2;
+}
+bool adapter_grad_small(int64_t rows, int32_t N, int32_t dtype) { return (double)rows * N * (double)elem_bytes(dtype) <= (double)READ_ONCE_BYTES; }
 constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
 // A sum over rows for W columns: blocks of columns, positions of a chunk.  A compute unit holds one workgroup, which takes some
@@ -155,7 +161,7 @@ constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 
 struct GradPlan {
   int blocks, chunks, chunk;
 };
-GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave) {
+GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave, int together) {
   GradPlan p;
   const int cols = ADAPTER_GRAD_WAVES * 16 * tiles_of_wave;
   p.blocks = (W + cols - 1) / cols;
@@ -163,7 +169,7 @@ GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave
   int64_t chunks = 1;
   double least = INFINITY;
   for (int64_t each = 1; each <= std::min<int64_t>(tiles, ADAPTER_CHUNK / ADAPTER_TILE); ++each) {
-    const int64_t k = (tiles + each - 1) / each, rounds = (k * p.blocks + 255) / 256;
+    const int64_t k = (tiles + each - 1) / each, rounds = (k * p.blocks + 256 * together - 1) / (256 * together);
     const double us = rounds * (2.5 * each + 6.0) + (double)k * W * R * 8 / 5e6;
     if (us <= least) least = us, chunks = k, p.chunk = (int)each * ADAPTER_TILE;
   }
@@ -176,10 +182,12 @@ GradPlan adapter_grad_plan(int64_t rows, int32_t W, int32_t R, int tiles_of_wave
   return p;
 }
 GradPlan adapter_up_plan(int64_t rows, int32_t N, int32_t R, int32_t dtype) {
-  return adapter_grad_plan(rows, N, R, adapter_grad_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16));
+  const bool small = adapter_grad_small(rows, N, dtype);
+  const int r_tiles = adapter_r_tiles(R);
+  return adapter_grad_plan(rows, N, R, adapter_grad_tiles(r_tiles, dtype == RNNLM_DTYPE_BF16, small), r_tiles == 1 && small ? 2 : 1);
 }
 GradPlan adapter_down_plan(int64_t rows, int32_t K, int32_t R, int32_t dtype) {
-  return adapter_grad_plan(rows, K, R, adapter_input_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16));
+  return adapter_grad_plan(rows, K, R, adapter_input_tiles(adapter_r_tiles(R), dtype == RNNLM_DTYPE_BF16), 1);
 }
 
 // Rows in up to this many tiles are taken as they come: an adapter is read once for each tile that has it.
@@ -275,12 +283,14 @@ template <typename T>
 void launch_grad(const GradArgs<T> &a, const GradPlan &p, hipStream_t st) {
   const dim3 grid(p.blocks, p.chunks), threads(64 * ADAPTER_GRAD_WAVES);
   constexpr bool BF16 = sizeof(T) == 2;
-  if (a.N < 16 * adapter_grad_tiles(adapter_r_tiles(a.R), BF16)) {
+  const bool small = adapter_grad_small(a.rows.M, a.N, BF16 ? RNNLM_DTYPE_BF16 : RNNLM_DTYPE_FP32);
+  if (a.N < 16 * adapter_grad_tiles(adapter_r_tiles(a.R), BF16, small)) {
     hipLaunchKernelGGL((adapter_grad_kernel<T, 4, 2, true>), grid, threads, 0, st, a);
   } else {
     with_r_tiles(a.R, [&](auto r) {
       constexpr int JT = decltype(r)::value;
-      hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, BF16), false>), grid, threads, 0, st, a);
+      if (small) hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, BF16, true), false>), grid, threads, 0, st, a);
+      else hipLaunchKernelGGL((adapter_grad_kernel<T, JT, adapter_grad_tiles(JT, BF16, false), false>), grid, threads, 0, st, a);
     });
   }
 }

@@ -586,11 +586,15 @@ struct GradArgs {
 
 // dup[a][v][r] = f_a sum_m dout[m][v] inner[m][r], and of every block of columns part[position][r] = sum_v dout[m][v] up[a][v][r]:
 // dout is read once, which bounds it.  NARROW: fewer columns than a wave's.
+// Two workgroups to a compute unit where registers and LDS allow it (VT of half the size, R <= 16): each waits less for the other
+// waves of its own.
+template <typename T>
+constexpr bool grad_by_two(int JT, int VT) { return JT == 1 && VT * sizeof(T) <= 8; }
 template <typename T, int JT, int VT, bool NARROW>
-__global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_grad_kernel(const GradArgs<T> a) {
+__global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES, grad_by_two<T>(JT, VT) ? 4 : 2) adapter_grad_kernel(const GradArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, TILE = ADAPTER_TILE, WAVES = ADAPTER_GRAD_WAVES, COLS = 16 * VT;
   constexpr int THREADS = 64 * WAVES, PARTS = GRAD_PARTS<T>, MK = TILE / CHUNK, VK = COLS / CHUNK;  // slots of the rows, of the columns
-  constexpr int REDS = JT <= 2 ? 2 : 1;  // (as many as LDS holds)
+  constexpr int REDS = JT <= 2 && !grad_by_two<T>(JT, VT) ? 2 : 1;  // (as many as LDS holds)
   constexpr int WIDTH = JT == 3 ? 64 : JT * 16, STEP = THREADS / WIDTH, EACH = TILE / STEP;  // a tile's inner numbers over the threads
   constexpr bool EARLY = JT <= 2;        // the next adapter's up has registers of its own
   typedef WaveTile<T, COLS, NARROW> Tile;
@@ -849,6 +853,9 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
     const int a_start = a.start[id], a_end = a.start[id + 1], end = min(a_end, end_chunk);
     const float f = a.scale ? a.scale[id] : 1.0f;
     const T *down = a.down + (long)id * R * K;
+    const auto rows_at = [&](int at) { return a.rows.row(min(at + (lane & 31), a.rows.M - 1)); };
+    Tile tile;  // of x, requested ahead
+    tile.load(a.x, a.ldx, rows_at(pos), k0);
     slot_t fdown[VT][JK];  // down[r][k]: k of the product = r
     if (a.dx) {
 #pragma unroll
@@ -867,10 +874,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
     }
     f32x4_t g[VT][JT] = {};
     for (; pos < end; pos += TILE) {
-      const int here = min(TILE, end - pos);
-      const int rows = a.rows.row(min(pos + (lane & 31), end - 1));
-      Tile tile;
-      tile.load(a.x, a.ldx, rows, k0);
+      const int here = min(TILE, end - pos), rows = tile.rows;
       {  // the tile's part of every block is contiguous: groups of threads share out the blocks where it is short
         const int size = here * R;
         int width = 32;
@@ -897,6 +901,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
       }
       tile.store(my, a.x, a.ldx, here, k0, K);
       __syncthreads();
+      if (pos + TILE < end) tile.load(a.x, a.ldx, rows_at(pos + TILE), k0);
 #pragma unroll
       for (int j = 0; j < JT; ++j) {
         slot_t fw[MK][PARTS];  // dinner[m][r]: k = m
