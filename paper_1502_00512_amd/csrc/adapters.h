@@ -282,7 +282,6 @@ struct OuterArgs {
   long ldb, ldo;
   int N, R, blocks;    // blocks of columns of a wave
   int tile;            // rows of a tile, at most 32
-  bool once;           // base and out are read and written past the caches
 };
 
 // out = base + f up inner: a wave a tile and 16 VT columns, `blocks` times; through LDS so that base and out move in whole lines.
@@ -348,7 +347,6 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
       const T *at = a.base + max(rows[i], 0) * a.ldb + v0 + lc;
       if (!a.base) old[i] = slot_t{0u, 0u, 0u, 0u};
       else if (!wide) old[i] = load_elems(at, N - (v0 + lc), N - (v0 + lc));
-      else if (a.once) old[i] = __builtin_nontemporal_load(reinterpret_cast<const Slot *>(at));
       else old[i] = *reinterpret_cast<const Slot *>(at);
     }
   };
@@ -420,8 +418,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
       T *dst = a.out + max(rows[i], 0) * a.ldo + col;
       if (rows[i] < 0) {
       } else if (col >= from && col + VEC <= N) {
-        if (a.once) __builtin_nontemporal_store(o.s, reinterpret_cast<Slot *>(dst));
-        else *reinterpret_cast<Slot *>(dst) = o.s;
+        *reinterpret_cast<Slot *>(dst) = o.s;
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
