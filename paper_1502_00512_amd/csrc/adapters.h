@@ -353,14 +353,22 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
   // (columns behind the last one, of narrow arrays: the last one again, dropped)
   const auto load_up = [&](int v0, int id, slot_t (&fa)[VT][NF]) {
     const T *up = a.up + (long)id * N * R;
+    // (whole slots of every lane lie in up, all of the block's at once: no branch stands between the loads)
+    if (slots || (long)(N - v0 - COLS) * R + 1 >= VEC) {
 #pragma unroll
-    for (int v = 0; v < VT; ++v)
+      for (int v = 0; v < VT; ++v)
 #pragma unroll
-      for (int i = 0; i < NF; ++i) {
-        const int col = min(v0 + v * 16 + c, N - 1), k = i * CHUNK + kq;
-        if (slots) fa[v][i] = *reinterpret_cast<const Slot *>(up + (unsigned)(col * R + min(k, R - VEC)));
-        else fa[v][i] = load_elems(up + (unsigned)(col * R + k), R - k, (long)(N - col) * R - k);
-      }
+        for (int i = 0; i < NF; ++i)
+          fa[v][i] = *reinterpret_cast<const Slot *>(up + (unsigned)(min(v0 + v * 16 + c, N - 1) * R + min(i * CHUNK + kq, slots ? R - VEC : R - 1)));
+    } else {
+#pragma unroll
+      for (int v = 0; v < VT; ++v)
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+          const int col = min(v0 + v * 16 + c, N - 1), k = i * CHUNK + kq;
+          fa[v][i] = load_elems(up + (unsigned)(col * R + min(k, R - 1)), R - k, (long)(N - col) * R - k);
+        }
+    }
   };
   if (first >= N) return;  // (nothing is shared between the waves)
   unsigned left = 0xffffffffu;
@@ -393,7 +401,7 @@ __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T
           f32x4_t acc = {};
 #pragma unroll
           for (int i = 0; i < NF; ++i) {
-            const slot_t f = slots && i * CHUNK + kq >= R ? slot_t{0u, 0u, 0u, 0u} : fa[0][v][i];
+            const slot_t f = R % CHUNK == 0 ? fa[0][v][i] : first_elems<T>(fa[0][v][i], R - (i * CHUNK + kq));
 #pragma unroll
             for (int p = 0; p < PARTS; ++p) Mma<T>::add(acc, f, fu[t][i][p]);
           }
