@@ -34,15 +34,8 @@ struct RowShape {
 };
 constexpr int HELD_SLOTS = 1024 * 25;
 template <class F>
-void with_row_shape(int64_t rows, int slots, F &&f) {
-  const bool wave_each = rows >= 1024 && slots <= 64 * 8;
-  if (wave_each && slots <= 64 * 2) f(RowShape<64, 2>());
-  else if (wave_each && slots <= 64 * 4) f(RowShape<64, 4>());
-  else if (wave_each) f(RowShape<64, 8>());
-  else if (slots <= 256) f(RowShape<256, 1>());
-  else if (slots <= 256 * 2) f(RowShape<256, 2>());
-  else if (slots <= 256 * 4) f(RowShape<256, 4>());
-  else if (slots <= 256 * 6) f(RowShape<256, 6>());
+void with_long_row_shape(int slots, F &&f) {  // of more than 1024 slots
+  if (slots <= 256 * 6) f(RowShape<256, 6>());
   else if (slots <= 256 * 8) f(RowShape<256, 8>());
   else if (slots <= 512 * 6) f(RowShape<512, 6>());
   else if (slots <= 512 * 8) f(RowShape<512, 8>());
@@ -52,6 +45,17 @@ void with_row_shape(int64_t rows, int slots, F &&f) {
   else if (slots <= 512 * 25) f(RowShape<512, 25>());
   else if (slots <= 1024 * 18) f(RowShape<1024, 18>());
   else f(RowShape<1024, 25>());
+}
+template <class F>
+void with_row_shape(int64_t rows, int slots, F &&f) {
+  const bool wave_each = rows >= 1024 && slots <= 64 * 8;
+  if (wave_each && slots <= 64 * 2) f(RowShape<64, 2>());
+  else if (wave_each && slots <= 64 * 4) f(RowShape<64, 4>());
+  else if (wave_each) f(RowShape<64, 8>());
+  else if (slots <= 256) f(RowShape<256, 1>());
+  else if (slots <= 256 * 2) f(RowShape<256, 2>());
+  else if (slots <= 256 * 4) f(RowShape<256, 4>());
+  else with_long_row_shape(slots, f);
 }
 
 // ---- policy loss ----
@@ -102,10 +106,10 @@ int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
   // Rows that meet, where the logits are many and the rows long: they and two passes, us: 26 x 10 bf16 rows of 64000 (33 MB) 22.0
   // and 23.8, 128 x 10 of 33000 46 and 48, 128 x 20 of 100000 211 and 297, 32 x 20 fp32 of 33278 42 and 48; but 64 x 10 bf16 of
   // 10000 15.0 and 13.0, 128 x 10 of them 19.4 and 17.4, and 128 x 64 rows of 4000 57 and 45 (a wave a row: all of them wait).
-  if (rows > 0 && a.rows.dz && slots <= HELD_SLOTS && slots >= 1024 && a.Tn <= PREFERENCE_MEET && (double)rows * a.rows.V * sizeof(T) > 30e6) {
+  if (rows > 0 && a.rows.dz && slots <= HELD_SLOTS && slots > 1024 && a.Tn <= PREFERENCE_MEET && (double)rows * a.rows.V * sizeof(T) > 30e6) {
     hipLaunchKernelGGL(preference_clear_kernel<T>, dim3((unsigned)std::min<int64_t>(256, (rows + 255) / 256)), dim3(256), 0, st, a, (long)rows);
     LAUNCHED();
-    with_row_shape(rows, slots, [&](auto shape) {
+    with_long_row_shape(slots, [&](auto shape) {
       constexpr int THREADS = decltype(shape)::threads, NV = decltype(shape)::nv;
       hipLaunchKernelGGL((preference_meet_kernel<T, THREADS, NV>), dim3((unsigned)rows), dim3(THREADS), 0, st, a);
     });
@@ -123,7 +127,8 @@ int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
   }
   const bool gradient = rows > 0 && a.rows.dz, held = slots <= HELD_SLOTS, inside = gradient && held && a.Tn <= PREFERENCE_INSIDE;
   if (!inside) {
-    hipLaunchKernelGGL(preference_pairs_kernel<T>, dim3((unsigned)a.P), dim3(64), 0, st, a);
+    if (a.Tn <= 64) hipLaunchKernelGGL((preference_pairs_kernel<T, 2>), dim3((unsigned)a.P), dim3(128), 0, st, a);
+    else hipLaunchKernelGGL((preference_pairs_kernel<T, 16>), dim3((unsigned)a.P), dim3(1024), 0, st, a);
     LAUNCHED();
   }
   if (!gradient) return RNNLM_OK;
@@ -154,8 +159,8 @@ constexpr int adapter_grad_tiles(int r_tiles, bool bf16, bool small) {
 bool adapter_grad_small(int64_t rows, int32_t N, int32_t dtype) { return (double)rows * N * (double)elem_bytes(dtype) <= (double)READ_ONCE_BYTES; }
 constexpr int adapter_input_tiles(int r_tiles, bool bf16) { return r_tiles <= 2 || bf16 ? 4 : 2; }
 
-// A sum over rows for W columns: blocks of columns, positions of a chunk.  A compute unit holds one workgroup, which takes some
-// 6 us and 2.5 a tile; each chunk may leave W R numbers to be written and read once more.  The chunk for which rounds of
+// A sum over rows for W columns: blocks of columns, positions of a chunk.  A compute unit holds `together` workgroups, each of
+// which takes some 6 us and 2.5 a tile; each chunk may leave W R numbers to be written and read once more.  The chunk for which rounds of
 // workgroups and that come out least (900 rows, N = 33278, R = 5, fp32: 85 us by chunks until there were 512 workgroups, which
 // made 520, 3 rounds).
 struct GradPlan {

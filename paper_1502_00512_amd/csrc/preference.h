@@ -64,31 +64,35 @@ __device__ inline unsigned long long word_published(double l, int y) {
   return y < 0 ? WORD_NONE : l != l ? 0x7ff8000000000000ull : __builtin_bit_cast(unsigned long long, l);
 }
 
-// Sum of the log-probabilities of a text and number of its words: one wave, in a fixed order.  word(t): as published.
+// Sum of the log-probabilities of a text, and number of its words.
+struct PreferenceText {
+  double l;
+  int count;
+};
+// By one wave, in a fixed order, `waves` of them sharing a text 64 positions at a time.  word(t): as published.
 template <class F>
-__device__ inline double preference_text(int Tn, int &count, F &&word) {
-  double l = 0.0;
-  count = 0;
-  for (int t = threadIdx.x & 63; t < Tn; t += 64) {
+__device__ inline PreferenceText preference_text(int Tn, int wave, int waves, F &&word) {
+  PreferenceText s = {0.0, 0};
+  for (int t = wave * 64 + (threadIdx.x & 63); t < Tn; t += 64 * waves) {
     const unsigned long long w = word(t);
     if (w != WORD_NONE) {
-      l += __builtin_bit_cast(double, w);
-      ++count;
+      s.l += __builtin_bit_cast(double, w);
+      ++s.count;
     }
   }
-  count = wave_sum(count);
-  return wave_sum(l);
+  return {wave_sum(s.l), wave_sum(s.count)};
 }
 
 // ln(1 + e^x)
 __device__ inline double softplus(double x) { return (x > 0.0 ? x : 0.0) + log1p(exp(-fabs(x))); }
 
-// A pair's factors of the gradient, by one wave; its loss and its texts' log-probabilities, where asked for.  word(t, other): the
-// words of the preferred text and of the other one.
-template <typename T, class F>
-__device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int p, bool write, F &&word) {
-  int nc, no;
-  double c = preference_text(a.Tn, nc, [&](int t) { return word(t, 0); }), o = preference_text(a.Tn, no, [&](int t) { return word(t, 1); });
+// A pair's factors of the gradient, by one wave, from the sums of its preferred text and of the other one; its loss and its texts'
+// log-probabilities, where asked for.
+template <typename T>
+__device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int p, bool write, const PreferenceText &chosen,
+                                                 const PreferenceText &other) {
+  const int nc = chosen.count, no = other.count;
+  double c = chosen.l, o = other.l;
   const double sc = a.mean ? 1.0 / (nc > 0 ? nc : 1) : 1.0, so = a.mean ? 1.0 / (no > 0 ? no : 1) : 1.0;
   c *= sc;
   o *= so;
@@ -123,20 +127,38 @@ __device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int
   g *= w * (double)a.scale;
   return {g * sc, -g * so};
 }
-// The same from the rows of the first pass.
+// The same by one wave that adds up the words: word(t, other).
+template <typename T, class F>
+__device__ inline PreferencePair preference_pair_of(const PreferenceArgs<T> &a, int p, bool write, F &&word) {
+  return preference_pair(a, p, write, preference_text(a.Tn, 0, 1, [&](int t) { return word(t, 0); }),
+                         preference_text(a.Tn, 0, 1, [&](int t) { return word(t, 1); }));
+}
+// A word of the first pass.
 template <typename T>
-__device__ inline PreferencePair preference_pair_of_rows(const PreferenceArgs<T> &a, int p, bool write) {
-  return preference_pair(a, p, write, [&](int t, int other) {
-    const PreferenceRow &row = a.row[((long)t * 2 + other) * a.P + p];
-    return word_published(row.l, row.y);
-  });
+__device__ inline unsigned long long preference_word(const PreferenceArgs<T> &a, int p, int t, int other) {
+  const PreferenceRow &row = a.row[((long)t * 2 + other) * a.P + p];
+  return word_published(row.l, row.y);
 }
 
-// Where texts are long, or no gradient is wanted: a wave a pair.
-template <typename T>
-__global__ void __launch_bounds__(64) preference_pairs_kernel(const PreferenceArgs<T> a) {
-  const PreferencePair p = preference_pair_of_rows(a, blockIdx.x, true);
-  if (threadIdx.x == 0) a.pair[blockIdx.x] = p;
+// Where texts are long, or no gradient is wanted: a workgroup a pair, half of its waves to a text (a wave alone is a chain of
+// loads: 1 pair of 512 positions 5.2 us, 4 of 2048 28, 1 of 20000 133; so 2.9, 10 and 18.5).
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) preference_pairs_kernel(const PreferenceArgs<T> a) {
+  constexpr int HALF = WAVES / 2;
+  __shared__ PreferenceText text[WAVES];
+  const int wave = threadIdx.x >> 6, other = wave / HALF, p = blockIdx.x;
+  const PreferenceText mine = preference_text(a.Tn, wave % HALF, HALF, [&](int t) { return preference_word(a, p, t, other); });
+  if ((threadIdx.x & 63) == 0) text[wave] = mine;
+  __syncthreads();
+  if (wave != 0) return;
+  PreferenceText sum[2] = {text[0], text[HALF]};
+  for (int i = 1; i < HALF; ++i)
+    for (int j = 0; j < 2; ++j) {
+      sum[j].l += text[j * HALF + i].l;
+      sum[j].count += text[j * HALF + i].count;
+    }
+  const PreferencePair f = preference_pair(a, p, true, sum[0], sum[1]);
+  if (threadIdx.x == 0) a.pair[p] = f;
 }
 
 // The gradients, a row a workgroup, the row read again.  INSIDE: each finds its pair's factors itself, from the words of both
@@ -154,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) preference_row_kernel(const Preferenc
   if (r.y >= 0) held.load(row, w.V, false);
   __shared__ float g;
   if (threadIdx.x < 64) {
-    const PreferencePair f = INSIDE ? preference_pair_of_rows(a, p, m == s && s < a.P) : a.pair[p];
+    const PreferencePair f = INSIDE ? preference_pair_of(a, p, m == s && s < a.P, [&](int t, int other) { return preference_word(a, p, t, other); }) : a.pair[p];
     if (threadIdx.x == 0) g = (float)(s < a.P ? f.g_chosen : f.g_other);
   }
   __syncthreads();
@@ -235,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 4) preference_meet_kernel(const Prefe
     for (int i = threadIdx.x; i < 2 * a.Tn; i += 64) all = all && words[i] != WORD_EMPTY;
     all = __all(all);
     if (all) {
-      const PreferencePair f = preference_pair(a, p, k == 0, [&](int t, int other) { return words[2 * t + other]; });
+      const PreferencePair f = preference_pair_of(a, p, k == 0, [&](int t, int other) { return words[2 * t + other]; });
       if (threadIdx.x == 0) sh.g = (float)(k & 1 ? f.g_other : f.g_chosen);
     }
     if (threadIdx.x == 0) {
@@ -264,7 +286,7 @@ __global__ void __launch_bounds__(THREADS) preference_rest_kernel(const Preferen
       const int s = (int)(m % (2 * a.P)), p = s < a.P ? s : s - a.P;
       const unsigned long long word = a.published[m];
       if (threadIdx.x < 64) {
-        const PreferencePair f = preference_pair(a, p, m == s && s < a.P, [&](int t, int other) { return a.published[((long)t * 2 + other) * a.P + p]; });
+        const PreferencePair f = preference_pair_of(a, p, m == s && s < a.P, [&](int t, int other) { return a.published[((long)t * 2 + other) * a.P + p]; });
         if (threadIdx.x == 0) sh.g = (float)(s < a.P ? f.g_chosen : f.g_other);
       }
       T *drow = w.dz + m * w.ldd;

@@ -323,6 +323,17 @@ def test_preference_rows_of_all_kinds(kind, V, dtype):
     check_preference(d, z, y, ref, None, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,P,mean", [(1025, 2, False), (2500, 1, True)])
+def test_preference_long_texts(T, P, mean, dtype):
+    d, z, y, rng = draw_preference(T, P, 9, dtype, T)
+    ref = (A.preference(z, y, mean=mean)[1] + rng.normal(size=2 * P)).astype(np.float32)
+    check_preference(d, z, y, ref, None, dtype, mean=mean)
+    alone = binding.rnnlm_preference_loss(d, gpu(y, torch.int32), gpu(ref), mean=mean)
+    both = binding.rnnlm_preference_loss(d, gpu(y, torch.int32), gpu(ref), mean=mean, dlogits=torch.empty_like(d))
+    assert all(torch.equal(a, b) for a, b in zip(alone, both))
+
+
 def test_preference_texts_that_do_not_count():
     d, z, y, rng = draw_preference(6, 4, 90, "fp32", 31)
     w = np.array([1.0, 0.0, 0.5, 2.0], np.float32)
