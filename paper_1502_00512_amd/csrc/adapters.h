@@ -6,7 +6,7 @@
 // of several adapters, each of which is multiplied with the whole tile and kept where it belongs (the products are few beside
 // the bytes of base, out and dout, which bound all of this).
 // Products: 16 x 16 tiles of the matrix cores.  bf16: inner and dinner are fp32 and go in as two parts (products that end in a
-// bf16 number; 2^-17) or three (gradients in fp32; 2^-25), everything else is bf16 already; fp32: the fp32 instruction.
+// bf16 number; 2^-17) or three (gradients in fp32; 2^-26), everything else is bf16 already; fp32: the fp32 instruction.
 #pragma once
 #include "rows.h"
 

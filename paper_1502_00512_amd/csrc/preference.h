@@ -202,7 +202,8 @@ __global__ void __launch_bounds__(THREADS) preference_stream_kernel(const Prefer
 // ---- rows that meet ----
 // One pass over the logits where they are many: a workgroup holds its row, publishes its word's log-probability (the word is
 // its own flag) and waits for those of its pair, which were started next to it.  A wait ends after `polls` polls, too (the rest
-// of a pair may not be on the GPU yet, where other work fills it): such a row is taken again by preference_rest_kernel.
+// of a pair may not be on the GPU yet, where other work fills it): such a row leaves its sum to preference_rest_kernel, which
+// writes the same gradient.
 // 2560 x 64000 bf16 (64 pairs of 20 positions) 134-138 us where a row by itself (policy_row_kernel) takes 114: a pair's rows write
 // only when the last of them has been read.  Two passes: 188.
 constexpr int PREFERENCE_MEET = 64;  // most positions of a text: the pair's rows are at most half of what the GPU holds
@@ -266,6 +267,7 @@ __global__ void __launch_bounds__(THREADS, 4) preference_meet_kernel(const Prefe
     }
     if (threadIdx.x == 0) {
       a.done[m] = all;
+      if (!all) a.row[m] = {l, r, y};
       met = all;
     }
   }
@@ -275,10 +277,11 @@ __global__ void __launch_bounds__(THREADS, 4) preference_meet_kernel(const Prefe
   held.gradient(r, drow, zy, y, w.V, 1.0f, sh.g);
 }
 
-// Rows whose wait ended early, by two passes over memory; every word has been published by now.  4 us where there are none.
+// Rows whose wait ended early, read again (every word has been published by now): the same sum, the same steps behind it, the same
+// bits.  4 us where there are none.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) preference_rest_kernel(const PreferenceArgs<T> a, long rows) {
-  __shared__ WordShared<THREADS / 64> sh;
+  __shared__ float g;
   const WordRows<T> &w = a.rows;
   for (long first = blockIdx.x; first < rows; first += (long)gridDim.x * 64) {
     // (each wave looks at the same 64 rows, so that all agree)
@@ -288,21 +291,16 @@ __global__ void __launch_bounds__(THREADS) preference_rest_kernel(const Preferen
       const long m = first + (long)(__ffsll(open) - 1) * gridDim.x;
       open &= open - 1;
       const int s = (int)(m % (2 * a.P)), p = s < a.P ? s : s - a.P;
-      const unsigned long long word = a.published[m];
+      const PreferenceRow r = a.row[m];
       if (threadIdx.x < 64) {
         const PreferencePair f = preference_pair_of(a, p, m == s && s < a.P, [&](int t, int other) { return a.published[((long)t * 2 + other) * a.P + p]; });
-        if (threadIdx.x == 0) sh.g = (float)(s < a.P ? f.g_chosen : f.g_other);
+        if (threadIdx.x == 0) g = (float)(s < a.P ? f.g_chosen : f.g_other);
       }
+      __syncthreads();
       T *drow = w.dz + m * w.ldd;
       const T *row = w.z + m * w.ldz;
-      if (word != WORD_NONE && __builtin_bit_cast(double, word) != -INFINITY) {
-        const int y = w.y[m];
-        const float zt = tail_elem(row, threadIdx.x, w.V), zy = to_f32(row[y]);
-        const WordSum r = word_sum_by_memory<T, THREADS, 4, false>(row, zt, w.V, 1.0f, sh);  // (barriers)
-        word_gradient_by_memory<T, THREADS>(r, row, drow, zt, zy, y, w.V, 1.0f, sh.g);
-      } else {
-        word_no_gradient<T, THREADS>(drow, w.V);
-      }
+      if (r.y < 0 || r.l == -INFINITY) word_no_gradient<T, THREADS>(drow, w.V);
+      else word_gradient_by_memory<T, THREADS>(r.sum, row, drow, tail_elem(row, threadIdx.x, w.V), to_f32(row[r.y]), r.y, w.V, 1.0f, g);
       __syncthreads();
     }
   }

@@ -2,8 +2,10 @@
 
 Tolerances.  A sum of n products in fp32 is off by at most (n + 2) 2^-24 (twice that: the matrix cores' own sums) of the sum of
 the products' magnitudes; where blocks are summed first, n is the longest chain of additions.  bf16: operands are exact, inner
-enters out as two bf16 parts (2^-18 of it is left), dinner and inner enter the gradients as three (2^-26).  What an operand is
-off by goes through the product it enters.  Outputs are rounded once: eps / 2 of their type."""
+enters out, and dinner dx, as two bf16 parts (2^-17 of it is left), dinner and inner enter the gradients as three (2^-26).  (A
+number x of 1 <= x < 2: the first part is off by at most half a step, 2^-8; what is left is below 2^-8, or is it and exact, where half
+a step is 2^-9 2^-8 = 2^-17; what is then left is below 2^-17, where half a step is 2^-18 2^-8 = 2^-26.)  What an operand is off
+by goes through the product it enters.  Outputs are rounded once: eps / 2 of their type."""
 import numpy as np
 import pytest
 import torch
@@ -65,7 +67,7 @@ class Case:
         f = (self.SCALE[self.of] * self.has)[:, None]
         size = f * np.einsum("mr,mnr->mn", np.abs(INNER), np.abs(self.UP[self.of]))
         moved = f * np.einsum("mr,mnr->mn", di, np.abs(self.UP[self.of]))
-        parts = 2.0 ** -18 if self.dtype == "bf16" else 0.0
+        parts = 2.0 ** -17 if self.dtype == "bf16" else 0.0
         b = np.abs(self.BASE) if with_base else 0.0
         tol = (moved + size * (2 * (2 * self.R + 4) * F32 + parts) + F32 * (b + size)) * 1.01
         near(out, want, tol + HALF[self.dtype] * (np.abs(want) + tol) + 1e-38, "out")
@@ -87,7 +89,7 @@ class Case:
         assert got[0] is ddown and got[1] is dup
         DD, DU, DX = A.adapter_backward(self.DOUT, self.X, INNER, self.DOWN, self.UP, self.IDS, self.SCALE)
         a = [np.abs(t) for t in (self.DOUT, self.X, INNER, self.DOWN, self.UP)]
-        rows = np.array([max((self.of[self.has] == i).sum(), 0) for i in range(self.n)])[:, None, None]
+        rows = np.bincount(self.of[self.has], minlength=self.n)[:, None, None]
         parts = 2.0 ** -26 if self.dtype == "bf16" else 0.0
         SD, SU, SX = A.adapter_backward(*a, self.IDS, self.SCALE)  # of the magnitudes
         near(dup, DU, (2 * (rows + 4) * F32 + parts) * SU * 1.01, "dup")
@@ -96,7 +98,7 @@ class Case:
         near(ddown, DD, (2 * (rows + 4 + chain) * F32 + parts) * SD * 1.01, "ddown")
         assert not ddown[torch.as_tensor(rows[:, 0, 0] == 0).cuda()].any()
         if with_dx:
-            own = (2 * (2 * self.R + 4 + chain) * F32 + (2.0 ** -18 if self.dtype == "bf16" else 0.0)) * SX * 1.01
+            own = (2 * (2 * self.R + 4 + chain) * F32 + (2.0 ** -17 if self.dtype == "bf16" else 0.0)) * SX * 1.01
             near(dx, DX, own + HALF[self.dtype] * (np.abs(DX) + own) + 1e-38, "dx")
             assert not dx[torch.as_tensor(~self.has).cuda()].any()
         return ddown, dup, dx
@@ -284,3 +286,57 @@ def test_captured_calls_replay(dtype):
     got = binding.rnnlm_adapter_forward(c.x, c.down, c.up, c.ids, c.scale, base=c.base, stream=stream)
     torch.cuda.current_stream().wait_stream(stream)
     assert torch.equal(got[0], want[0])
+
+
+@BOTH
+@pytest.mark.parametrize("M,K,N,n,R", [(1 << 17, 1, 1, 1 << 16, 1), (3, 1 << 16, 1, 1, 64), (2, 1, 1 << 20, 1, 3)])
+def test_largest_sizes(M, K, N, n, R, dtype):
+    c = Case(M, K, N, n, R, dtype, 16)
+    c.check_forward()
+    c.check_backward()
+
+
+def test_rows_far_apart():
+    """Rows whose distance times their number passes 2^31."""
+    c = Case(40, 24, 90, 3, 5, "bf16", 17)
+    out, inner = binding.rnnlm_adapter_forward(c.x, c.down, c.up, c.ids, c.scale, base=c.base)
+    dx = torch.empty_like(c.x)
+    ddown, dup = binding.rnnlm_adapter_backward(c.dout, c.x, inner, c.down, c.up, c.ids, c.scale, dx=dx)
+
+    def far(t=None, width=0):
+        rows = torch.empty(40, 60_000_000, dtype=torch.bfloat16, device="cuda")
+        assert rows.numel() > 1 << 31
+        rows = rows[:, 17: 17 + (width if t is None else t.shape[1])]
+        return rows if t is None else rows.copy_(t)
+    x, out2 = far(c.x), far(width=90)
+    got = binding.rnnlm_adapter_forward(x, c.down, c.up, c.ids, c.scale, base=far(c.base), out=out2)
+    assert torch.equal(got[0], out) and torch.equal(got[1], inner)
+    dx2 = far(width=24)
+    got = binding.rnnlm_adapter_backward(far(c.dout), x, inner, c.down, c.up, c.ids, c.scale, dx=dx2)
+    assert torch.equal(got[0], ddown) and torch.equal(got[1], dup) and torch.equal(dx2, dx)
+
+
+def test_adapters_of_more_than_two_to_the_31_numbers():
+    """The last of many wide adapters has what it has by itself."""
+    n, N, K, R, M = 36, 1 << 20, 40, 64, 5
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    normal = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)  # noqa: E731
+    x, down, up, base, dout = normal(M, K), normal(n, R, K), normal(n, N, R), normal(M, N), normal(M, N)
+    assert up.numel() > 1 << 31
+    ids = torch.tensor([n - 1, 0, n - 1, -1, n - 1], dtype=torch.int32, device="cuda")
+    out, inner = binding.rnnlm_adapter_forward(x, down, up, ids, base=base)
+    dx = torch.empty_like(x)
+    ddown, dup = binding.rnnlm_adapter_backward(dout, x, inner, down, up, ids, dx=dx)
+    one = torch.where(ids == 0, 0, torch.where(ids < 0, -1, 1)).int()
+    down2, up2 = down[[0, n - 1]].contiguous(), up[[0, n - 1]].contiguous()
+    out2, inner2 = binding.rnnlm_adapter_forward(x, down2, up2, one, base=base)
+    dx2 = torch.empty_like(x)
+    ddown2, dup2 = binding.rnnlm_adapter_backward(dout, x, inner, down2, up2, one, dx=dx2)
+    assert torch.equal(out, out2) and torch.equal(inner, inner2) and torch.equal(dx, dx2)
+    assert torch.equal(ddown[[0, n - 1]], ddown2) and torch.equal(dup[0], dup2[0]) and torch.equal(dup[n - 1], dup2[1])
+    assert not ddown[1: n - 1].any() and not dup[1: n - 1].any()
+    want = base[0].double() + up[n - 1].double() @ inner[0].double()
+    size = base[0].double().abs() + up[n - 1].double().abs() @ inner[0].double().abs()
+    off = (out[0].double() - want).abs()
+    own = size * (2 * (2 * R + 4) * F32 + 2.0 ** -17) * 1.01
+    assert bool((off <= own + HALF["bf16"] * (want.abs() + own)).all())

@@ -414,6 +414,64 @@ def test_preference_rows_that_meet(dtype, T, P, V, in_place, polls):
         assert not got[zero].any()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_preference_waits_leave_no_mark(dtype):
+    """Rows that met and rows that did not wait have the same bits, and so do calls that share the GPU: on two streams at once."""
+    T, P, V = 20, 40, 40000
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    z = [torch.empty(T, 2 * P, V, dtype=DTYPES[dtype], device="cuda").normal_(0.0, 2.0, generator=gen) for _ in range(2)]
+    z[1][3, 5, : V // 2] = -float("inf")  # (a row whose sum is formed by way of memory)
+    y = torch.randint(V // 2, V, (T, 2 * P), generator=gen, device="cuda", dtype=torch.int32)
+    y[torch.rand(T, 2 * P, generator=gen, device="cuda") < 0.2] = -1
+    want = []
+    for a in z:
+        d = torch.empty_like(a)
+        want.append((*binding.rnnlm_preference_loss(a, y, dlogits=d), d))
+    try:
+        binding.rnnlm_set_preference_wait(0)
+        for a, w in zip(z, want):
+            d = torch.empty_like(a)
+            got = (*binding.rnnlm_preference_loss(a, y, dlogits=d), d)
+            assert all(torch.equal(p, q) for p, q in zip(got, w))
+        torch.cuda.synchronize()
+    finally:
+        binding.rnnlm_set_preference_wait(256)
+    streams = [torch.cuda.Stream() for _ in z]
+    nbytes = binding.rnnlm_preference_workspace_bytes(T, P)
+    outs = [(torch.empty(P, device="cuda"), torch.empty(2 * P, device="cuda"), torch.empty_like(a), torch.empty(nbytes, dtype=torch.uint8, device="cuda")) for a in z]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, stream, (loss, logp, d, ws) in zip(z, streams, outs):
+            binding.rnnlm_preference_loss(a, y, loss=loss, logp=logp, dlogits=d, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    for got, w in zip(outs, want):
+        assert all(torch.equal(p, q) for p, q in zip(got, w))
+
+
+def test_more_than_two_to_the_31_logits():
+    """The last rows of calls of 2^22 - 64 rows: the bits of the same rows by themselves, and the words' logarithms."""
+    V, T, P = 600, 32, 65535
+    z = torch.empty(T, 2 * P, V, dtype=torch.bfloat16, device="cuda").normal_(0.0, 2.0, generator=torch.Generator(device="cuda").manual_seed(1))
+    assert z.numel() > 1 << 31 and T * 2 * P == (1 << 22) - 64
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    y = torch.randint(0, V, (T, 2 * P), generator=gen, device="cuda", dtype=torch.int32)
+    adv = torch.randn(T, 2 * P, generator=gen, device="cuda")
+    d = torch.empty_like(z)
+    loss, logp = binding.rnnlm_policy_loss(z, y, adv, dlogits=d)
+    few = [t.view(T * 2 * P, *t.shape[2:])[-2000:] for t in (z, y, adv, d, loss, logp)]
+    d2 = torch.empty_like(few[0])
+    loss2, logp2 = binding.rnnlm_policy_loss(few[0], few[1], few[2], dlogits=d2)
+    assert torch.equal(d2, few[3]) and torch.equal(loss2, few[4]) and torch.equal(logp2, few[5])
+    want = torch.log_softmax(few[0].double(), 1).gather(1, few[1].long()[:, None])[:, 0]
+    E = row_err(np.full(V, few[0].abs().max().item()), 1.0)
+    same(logp2.cpu(), want.cpu().numpy(), E + F32 * want.abs().cpu().numpy(), "logp")
+    pairs, S = binding.rnnlm_preference_loss(z, y, dlogits=d)
+    last = [torch.cat([t[:, P - 100: P], t[:, 2 * P - 100:]], 1).contiguous() for t in (z, y, d)]
+    d2 = torch.empty_like(last[0])
+    pairs2, S2 = binding.rnnlm_preference_loss(last[0], last[1], dlogits=d2)
+    assert torch.equal(d2, last[2]) and torch.equal(pairs2, pairs[-100:]) and torch.equal(S2, torch.cat([S[P - 100: P], S[-100:]]))
+
+
 def test_preference_of_no_positions():
     d = torch.empty(0, 6, 30, device="cuda")
     y = torch.empty(0, 6, dtype=torch.int32, device="cuda")
