@@ -375,8 +375,8 @@ int rnnlm_preference_loss(const void *logits, int32_t dtype, int32_t T, int32_t 
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /* Number of polls, of about a microsecond each, that a row of a large rnnlm_preference_loss waits for the other rows of its pair
- * before it leaves its gradient to a second pass (default 256).  For tests of that path: with polls = 0 rows do not wait.  Holds
- * for the process's later calls. */
+ * before it leaves its gradient to a second pass (default 256, at most 2^20; results are the same).  For tests of that path: with
+ * polls = 0 rows do not wait.  Holds for the process's later calls. */
 int rnnlm_set_preference_wait(int32_t polls);
 
 /* Low-rank adapters of many texts at once beside a shared projection (the output layer, above all): row m of x belongs to

@@ -453,7 +453,7 @@ size_t rnnlm_preference_workspace_bytes(int32_t T, int32_t pairs) {
 }
 
 int rnnlm_set_preference_wait(int32_t polls) {
-  if (polls < 0) return RNNLM_ERR_ARG;
+  if (polls < 0 || polls > (1 << 20)) return RNNLM_ERR_ARG;  // (calls that share the GPU may wait for one another's rows)
   preference_polls = polls;
   return RNNLM_OK;
 }

@@ -65,6 +65,14 @@ def test_preference_workspaces(lib):
     assert ws(-1, 1) == ws(1, 0) == ws(1, -1) == ws(1 << 22, 1) == ws(1, 1 << 21) == 0
 
 
+def test_preference_waits(lib):
+    for polls in (-1, (1 << 20) + 1, (1 << 31) - 1):
+        with pytest.raises(binding.RnnlmError):
+            binding.rnnlm_set_preference_wait(polls)
+    for polls in (1 << 20, 0, 256):  # (the default last)
+        binding.rnnlm_set_preference_wait(polls)
+
+
 FORWARD = dict(x=LOGITS, ldx=40, dtype=1, rows=4, K=40, N=100, a=None, ids=Y, base=A, ldb=100, out=OUT, ldo=100, inner=MORE, flag=None, ws=WS,
                bytes=1 << 20, stream=None)
 BACKWARD = dict(dout=A, ldd=100, x=LOGITS, ldx=40, inner=MORE, dtype=0, rows=4, K=40, N=100, a=None, ids=Y, ddown=B, dup=B + (1 << 30), dx=OUT,
