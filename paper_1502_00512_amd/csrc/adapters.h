@@ -92,6 +92,19 @@ __device__ inline slot_t load_elems(const T *p, int left, long there) {
     if (e < left) o.t[e] = p[e];
   return o.s;
 }
+// Up to `left` elements from p on, zeros behind them; as many in front of them may be read as are missing of a slot (left < 0: p lies
+// behind the end).  One load and no branch: element by element, the last columns were what small calls waited for.
+template <typename T>
+__device__ inline slot_t load_last(const T *p, long left) {
+  constexpr int N = SlotOf<T>::N;
+  const long back = left < N ? N - left : 0;
+  const slot_t s = *reinterpret_cast<const typename SlotOf<T>::type *>(p - back);
+  const int bits = (int)min(back, (long)N) * (128 / N);
+  const unsigned long long lo = s[0] | (unsigned long long)s[1] << 32, hi = s[2] | (unsigned long long)s[3] << 32;
+  const unsigned long long low = bits == 0 ? lo : bits < 64 ? lo >> bits | hi << (64 - bits) : bits < 128 ? hi >> (bits - 64) : 0;
+  const unsigned long long high = bits < 64 ? hi >> bits : 0;
+  return slot_t{(unsigned)low, (unsigned)(low >> 32), (unsigned)high, (unsigned)(high >> 32)};
+}
 // A number in PARTS bf16 parts, each the rest of those in front of it.
 template <int PARTS>
 __device__ inline void bf16_parts(float x, bf16_t (&p)[PARTS]) {
@@ -192,7 +205,7 @@ struct InnerArgs {
 template <typename T, int RT>
 __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, WAVES = 8, TILE = ADAPTER_TILE;
-  __shared__ float part[WAVES][RT * 16][TILE];
+  __shared__ float part[WAVES][RT * 16][TILE + 1];  // (read down its columns)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const AdapterTile tile(a.rows, blockIdx.x * TILE, TILE);
   const int n = a.rows.n;
@@ -246,15 +259,22 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
   }
   if (whole < a.K && wave == whole / CHUNK % WAVES) {
     const int have = a.K - whole - q * VEC;
-    slot_t fx[2];
+    slot_t fx[2], fd[RT];
+    if (a.K >= VEC) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) fx[t] = load_elems(xs[t] + whole, have, have);
+      for (int t = 0; t < 2; ++t) fx[t] = load_last(xs[t] + whole, have);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const slot_t fd = load_elems(ds[r] + whole, have, have);
+      for (int r = 0; r < RT; ++r) fd[r] = load_last(ds[r] + whole, have);
+    } else {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) Mma<T>::add(acc[r][t], fd, fx[t]);
+      for (int t = 0; t < 2; ++t) fx[t] = load_elems(xs[t], have, have);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) fd[r] = load_elems(ds[r], have, have);
     }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) Mma<T>::add(acc[r][t], fd[r], fx[t]);
   }
 #pragma unroll
   for (int r = 0; r < RT; ++r)
