@@ -201,7 +201,8 @@ struct InnerArgs {
 };
 
 // inner: a workgroup a tile and one of its adapters (blockIdx.y-th); K over the waves, joined in LDS in order.  A chain of
-// latencies (a tile has 32 K numbers): 2560 x 1024 bf16, R = 16, 8 adapters 7.6 us, 128 rows of as many adapters 6.7.
+// latencies (a tile has 32 K numbers): 2560 x 1024 bf16, R = 16, 8 adapters 6.6 us, 128 rows of as many adapters 7.0.  Chunks behind the end of short rows are branched around: 164 rows of K = 387,
+// R = 58 9.1 us, 16.4 where the last one was loaded again in their place (bf16 rows of odd length: a load takes its lanes one by one).
 template <typename T, int RT>
 __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, WAVES = 8, TILE = ADAPTER_TILE;
@@ -234,15 +235,13 @@ __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a
     slot_t fx[AHEAD][2], fd[AHEAD][RT];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int k = min(k0 + u * WAVES * CHUNK, whole - CHUNK);
+      const int k = k0 + u * WAVES * CHUNK;
+      if (k < whole) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) fx[u][t] = *reinterpret_cast<const Slot *>(xs[t] + k);
+        for (int t = 0; t < 2; ++t) fx[u][t] = *reinterpret_cast<const Slot *>(xs[t] + k);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) fd[u][r] = *reinterpret_cast<const Slot *>(ds[r] + k);
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (k0 + u * WAVES * CHUNK >= whole) {  // (behind the end: nothing is added)
+        for (int r = 0; r < RT; ++r) fd[u][r] = *reinterpret_cast<const Slot *>(ds[r] + k);
+      } else {  // (behind the end: nothing is added)
 #pragma unroll
         for (int t = 0; t < 2; ++t) fx[u][t] = slot_t{0u, 0u, 0u, 0u};
 #pragma unroll
