@@ -201,8 +201,9 @@ struct InnerArgs {
 };
 
 // inner: a workgroup a tile and one of its adapters (blockIdx.y-th); K over the waves, joined in LDS in order.  A chain of
-// latencies (a tile has 32 K numbers): 2560 x 1024 bf16, R = 16, 8 adapters 6.6 us, 128 rows of as many adapters 7.0.  Chunks behind the end of short rows are branched around: 164 rows of K = 387,
-// R = 58 9.1 us, 16.4 where the last one was loaded again in their place (bf16 rows of odd length: a load takes its lanes one by one).
+// latencies (a tile has 32 K numbers): 2560 x 1024 bf16, R = 16, 8 adapters 6.6 us, 128 rows of as many adapters 7.0.  Chunks
+// behind the end of short rows are branched around: 164 rows of K = 387, R = 58 9.1 us, 16.4 where the last one was loaded again
+// in their place (bf16 rows of odd length: a load takes its lanes one by one).
 template <typename T, int RT>
 __global__ void __launch_bounds__(512) adapter_inner_kernel(const InnerArgs<T> a) {
   constexpr int VEC = Mma<T>::VEC, CHUNK = Mma<T>::CHUNK, WAVES = 8, TILE = ADAPTER_TILE;
