@@ -402,7 +402,10 @@ int rnnlm_adapter_forward(const void *x, int64_t ld_x, int32_t dtype, int64_t ro
 /* Its gradients, from those of out (the gradient of base is dout itself) and the inner of the forward pass:
  *     dinner = scale[i] up[i]^T dout,   dup[i] = scale[i] sum_m dout inner^T,   ddown[i] = sum_m dinner x^T,   dx = down[i]^T dinner
  * dout: dev [rows][N]; ddown: dev float[n][R][K] and dup: dev float[n][N][R], zero for adapters without rows; dx: dev [rows][K]
- * of dtype, zero for rows without an adapter, or NULL.  Sums in fp32 in an order that hangs on the sizes and ids only. */
+ * of dtype, zero for rows without an adapter, or NULL.  Sums in fp32 in an order that hangs on the sizes and ids only.  What is
+ * not finite in a row of dout, x or inner stays with that row's adapter (and dx row).  An infinity of dout makes the infinities of
+ * the formula in ddown and dx; of bf16, an infinity of dout in dup and one of x in ddown may become NaNs instead (the other factor
+ * goes in as several numbers, some of them zero or of the other sign). */
 int rnnlm_adapter_backward(const void *dout, int64_t ld_dout, const void *x, int64_t ld_x, const float *inner, int32_t dtype, int64_t rows,
                            int32_t K, int32_t N, const rnnlm_adapters *a, const int32_t *ids, float *ddown, float *dup, void *dx,
                            int64_t ld_dx, int32_t *range_flag, void *workspace, size_t workspace_bytes, void *stream);

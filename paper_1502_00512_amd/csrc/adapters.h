@@ -525,8 +525,13 @@ struct WaveTile {
         raw[i] = *reinterpret_cast<const typename SlotOf<T>::type *>(at + __shfl(rows, i * ROWS + lane / LANES) * ld);
     }
   }
-  // zeros in place of the rows from `here` on
-  __device__ void store(T (*tile)[PITCH], const T *d, long ld, int here, int v0, int N) const {
+  // kept: of this lane's columns, ones
+  __device__ void keep(const slot_t &kept) {
+#pragma unroll
+    for (int i = 0; i < MOVES; ++i) raw[i] &= kept;
+  }
+  // zeros in place of the rows from `here` on (of narrow arrays: and of the columns in front of `from`)
+  __device__ void store(T (*tile)[PITCH], const T *d, long ld, int here, int v0, int from, int N) const {
     const int lane = threadIdx.x & 63;
     if constexpr (!NARROW) {
 #pragma unroll
@@ -541,7 +546,7 @@ struct WaveTile {
         for (int j = 0; j < 8; ++j) {
           const int i = i0 + j * 64 + lane, m = i / COLS, col = v0 + i % COLS;
           const long row = __shfl(rows, m);
-          v[j] = m < here && col < N ? d[row * ld + col] : from_f32<T>(0.0f);
+          v[j] = m < here && col >= from && col < N ? d[row * ld + col] : from_f32<T>(0.0f);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) tile[(i0 + j * 64 + lane) / COLS][(i0 + j * 64 + lane) % COLS] = v[j];
@@ -633,6 +638,10 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES, grad_by_two<T>(JT, VT
   __shared__ __align__(16) float red[REDS][WAVES][TILE][JT * 16 + 4];
   __shared__ __align__(16) T turned[2][PARTS][JT * 16][TILE + 16 / sizeof(T)];  // inner of two tiles, its parts, [r][m]
   __shared__ TileList list;
+  // Ones where a wave's columns count.  What it has in common with the wave in front is zero in up and in dout: 0 times an infinity
+  // is no number.  Read from here for every tile, without a branch: masks held in registers made the kernels spill, and a branch
+  // for the last waves cost all others 5% (900 x 33278 bf16, R = 16: 59.7 us without zeros in dout, 60.8 so, 62.9 with the branch).
+  __shared__ slot_t counted[WAVES][Tile::LANES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int N = a.N, R = a.R, n = a.rows.n, block = blockIdx.x, ci = blockIdx.y;
   const int from = (block * WAVES + wave) * COLS, v0 = Tile::start(from, N);  // the columns from `from` on count
@@ -641,6 +650,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES, grad_by_two<T>(JT, VT
   const int tr = threadIdx.x % WIDTH, tm = threadIdx.x / WIDTH;  // this thread's r, and first m
   const int chunk0 = ci * a.chunk;
   if (chunk0 >= end_chunk) return;
+  if (lane < Tile::LANES) counted[wave][lane] = last_elems<T>(slot_t{~0u, ~0u, ~0u, ~0u}, from - (v0 + lane * VEC));
   const int count = list_tiles(a.rows, a.start, chunk0, end_chunk, list);
   // What a tile needs of memory, requested two tiles ahead (behind the last one: that again, so that no branch stands between
   // the requests and the waits can count them).
@@ -722,7 +732,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES, grad_by_two<T>(JT, VT
 #pragma unroll
       for (int j = 0; j < JT; ++j) {
         fup[k][j] = across(stage, PITCH, 0, j * 16);
-        if (v0 < from) fup[k][j] = last_elems<T>(fup[k][j], from - (v0 + k * CHUNK + q * VEC));
+        fup[k][j] &= counted[wave][k * (CHUNK / VEC) + q];
       }
       wave_sync();
     }
@@ -771,7 +781,8 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES, grad_by_two<T>(JT, VT
     const int here = list.rows(i), before = id;
     id = list.adapter(i);
     const int after = list.adapter(min(i + 1, count - 1));
-    x.tile.store(my, a.d, a.ldd, here, v0, N);
+    if constexpr (!NARROW) x.tile.keep(counted[wave][lane % Tile::LANES]);
+    x.tile.store(my, a.d, a.ldd, here, v0, from, N);
     if (i > 0) write_sums(i - 1);
     if (i > 0 && id != before) write_gradient(before);
     if (i == 0 || id != before) {
@@ -894,7 +905,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
         const int r0 = j * CHUNK;
         Tile t;
         t.load(down, K, min(r0 + (lane & 31), R - 1), k0);
-        t.store(my, down, K, R - r0, k0, K);
+        t.store(my, down, K, R - r0, k0, k0, K);
         wave_sync();
 #pragma unroll
         for (int i = 0; i < MK && j + i < JK; ++i)
@@ -930,7 +941,7 @@ __global__ void __launch_bounds__(64 * ADAPTER_GRAD_WAVES) adapter_input_grad_ke
         }
         for (int i = size + threadIdx.x; i < TILE * R; i += THREADS) dinner[i / R][i % R] = 0.0f;
       }
-      tile.store(my, a.x, a.ldx, here, k0, K);
+      tile.store(my, a.x, a.ldx, here, k0, k0, K);
       __syncthreads();
       if (pos + TILE < end) tile.load(a.x, a.ldx, rows_at(pos + TILE), k0);
 #pragma unroll

@@ -235,6 +235,37 @@ def test_weights_that_are_not_finite_stay_with_their_adapter(bad, dtype):
 
 
 @BOTH
+@pytest.mark.parametrize("N", [20, 200, 1100])
+@pytest.mark.parametrize("R", [6, 20, 60])
+def test_infinities_of_dout_are_those_of_the_formula(N, R, dtype):
+    """An adapter a row, one element of each row infinite: in the first columns, in the last ones, and where the last blocks of
+    columns and those in front of them share some.  (All other numbers positive, so that every sum has its infinity's sign.)"""
+    M = 40
+    c = Case(M, 30, N, M, R, dtype, N + R, ids=np.arange(M))
+    for t, a in ((c.x, c.X), (c.down, c.DOWN), (c.up, c.UP), (c.dout, c.DOUT)):
+        t.abs_()
+        np.abs(a, out=a)
+    column = np.unique(np.concatenate([np.arange(0, N, max(1, N // 12)), np.arange(N - 12, N), np.arange(max(0, N - 70), N, 5)]))[-M:]
+    for m, v in enumerate(column):
+        c.DOUT[m, v] = np.inf if m % 2 else -np.inf
+        c.dout[m, int(v)] = c.DOUT[m, v]
+    INNER = np.abs(c.rng.normal(size=(M, R))).astype(np.float32)
+    dx = torch.empty_like(c.x)
+    ddown, dup = binding.rnnlm_adapter_backward(c.dout, c.x, torch.as_tensor(INNER).cuda(), c.down, c.up, c.ids, c.scale, dx=dx)
+    DD, DU, DX = A.adapter_backward(c.DOUT, c.X, INNER.astype(np.float64), c.DOWN, c.UP, c.IDS, c.SCALE)
+    some = len(column)
+    assert np.isinf(DD[:some]).all() and np.isinf(DX[:some]).all() and np.isfinite(DD[some:]).all()
+    for got, want in ((ddown, DD), (dx, DX)):
+        got = got.float().cpu().numpy()
+        assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)]) and np.isfinite(got[np.isfinite(want)]).all()
+    got = dup.cpu().numpy()
+    if dtype == "fp32":
+        assert np.array_equal(got[np.isinf(DU)], DU[np.isinf(DU)])
+    assert not np.isfinite(got[np.isinf(DU)]).any()  # (bf16: inner goes in as parts, of which some are zero or negative)
+    assert np.isfinite(got[np.isfinite(DU)]).all()
+
+
+@BOTH
 def test_the_same_call_gives_the_same_bits(dtype):
     c = Case(700, 130, 3000, 11, 20, dtype, 13)
     inner = torch.randn(700, 20, device="cuda")
