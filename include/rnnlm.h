@@ -362,7 +362,8 @@ int rnnlm_policy_loss(const void *logits, int32_t dtype, int64_t rows, int32_t V
  *                                * ([v = y] - softmax(z)(v))
  * Positions with a negative y (prompts, padding) and pairs of weight 0 have a gradient of zeros whatever their rows hold (the
  * texts of such a pair count as empty); y >= V counts as negative and raises *range_flag.  A word that its row masks makes its
- * text's sum -inf (and r infinite or no number); that row's gradient is zero.
+ * text's sum -inf; that row's gradient is zero, the loss and the pair's other rows have what the formulas give for such an r: no
+ * number for any kind of loss where r is none (masked words in both texts).
  * y: dev int32[T][2 pairs]; ref: dev float[2 pairs], a reference's sums (or means), or NULL: 0; weight: dev float[pairs] or NULL;
  * beta > 0; 0 <= smoothing <= 0.5, 0 but for LOGISTIC; T >= 0; loss: dev float[pairs]; logp: dev float[2 pairs] = S, or NULL;
  * sum_loss: of the pairs; dlogits, ld_dlogits, scale (1 / pairs for the mean), range_flag: as in rnnlm_distill_loss; workspace:

@@ -64,13 +64,14 @@ def preference(z, y, ref=None, weight=None, kind="logistic", beta=0.1, smoothing
     with np.errstate(invalid="ignore"):
         r = against[:P] - against[P:]
     if kind == "logistic":
-        up, down = np.logaddexp(0.0, -beta * r), np.logaddexp(0.0, beta * r)
+        with np.errstate(invalid="ignore"):
+            up, down = np.logaddexp(0.0, -beta * r), np.logaddexp(0.0, beta * r)
         loss = (1.0 - smoothing) * up + (smoothing * down if smoothing else 0.0)
         g = beta * (smoothing * np.exp(-up) - (1.0 - smoothing) * np.exp(-down))
     elif kind == "squared":
         loss, g = (r - 0.5 / beta) ** 2, 2.0 * (r - 0.5 / beta)
     else:
-        loss, g = np.maximum(0.0, 1.0 - beta * r), np.where(beta * r >= 1.0, 0.0, -beta)
+        loss, g = np.maximum(0.0, 1.0 - beta * r), np.where(beta * r >= 1.0, 0.0, np.where(np.isnan(r), np.nan, -beta))
     dz = np.zeros((T, B, V))
     for t in range(T):
         for s in range(B):

@@ -123,7 +123,7 @@ __device__ inline PreferencePair preference_pair(const PreferenceArgs<T> &a, int
     g = 2.0 * d;
   } else {
     if (write) a.loss[p] = (float)(w * (x >= 1.0 ? 0.0 : 1.0 - x));
-    g = x >= 1.0 ? 0.0 : -beta;
+    g = x >= 1.0 ? 0.0 : x < 1.0 ? -beta : x;  // (no number: neither)
   }
   g *= w * (double)a.scale;
   return {g * sc, -g * so};

@@ -360,6 +360,28 @@ def test_preference_words_without_probability():
     assert abs(dz[0, 0, y[0, 0]].item() + 0.1 * (1 - A.softmax(z[0, 0])[y[0, 0]])) < 1e-6
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("kind", ["logistic", "squared", "hinge"])
+@pytest.mark.parametrize("T", [3, 140])
+def test_preference_of_two_texts_without_probability(T, kind, dtype):
+    """r is no number where both texts of a pair hold a masked word, or their references are infinite: so are the pair's loss and
+    its gradient, but for the masked words' rows."""
+    d, z, y, _ = draw_preference(T, 3, 40, dtype, 34, ragged=False)
+    for t, s in ((1, 0), (2, 3)):  # pair 0
+        d[t, s, y[t, s]] = -float("inf")
+        z[t, s, y[t, s]] = -np.inf
+    ref = np.array([0.0, np.inf, 1.0, 0.5, np.inf, 0.0], np.float32)  # pair 1
+    which = dict(logistic=binding.RNNLM_PREFERENCE_LOGISTIC, squared=binding.RNNLM_PREFERENCE_SQUARED, hinge=binding.RNNLM_PREFERENCE_HINGE)[kind]
+    dz = torch.full_like(d, 7.0)
+    loss, logp = binding.rnnlm_preference_loss(d, gpu(y, torch.int32), gpu(ref), kind=which, dlogits=dz)
+    L, S, D, _, _ = A.preference(z, y, ref, kind=kind, beta=float(np.float32(0.1)))
+    assert np.isnan(L[:2]).all() and np.isfinite(L[2]) and np.isnan(D[:, [1, 4]]).all()
+    assert loss[:2].isnan().all() and loss[2].isfinite() and torch.equal(logp.isinf().cpu(), torch.as_tensor(np.isinf(S)))
+    got = dz.float().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(D)) and not got[1, 0].any() and not got[2, 3].any()
+    assert np.isfinite(got[:, [2, 5]]).all()
+
+
 @pytest.mark.parametrize("V", [64, 4097])
 def test_preference_loss_alone_agrees(V):
     d, z, y, rng = draw_preference(9, 5, V, "bf16", 8)

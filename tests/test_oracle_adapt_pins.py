@@ -68,6 +68,18 @@ def test_preference_gradient(kind, smoothing, mean):
     assert np.abs(dz - difference(lambda x: 0.5 * A.preference(x, y, **kw)[0].sum(), z)).max() < 1e-7
 
 
+@pytest.mark.parametrize("kind", ["logistic", "squared", "hinge"])
+def test_preference_without_a_number(kind):
+    # both texts of pair 0 hold a masked word: r = -inf + inf; pair 1 is as by itself
+    z, y = np.zeros((2, 4, 3)), np.zeros((2, 4), int)
+    z[0, 0, 0] = z[1, 2, 0] = -np.inf
+    loss, S, dz, r, g = A.preference(z, y, kind=kind)
+    assert S[0] == -np.inf and S[2] == -np.inf and np.isnan(r[0]) and np.isnan(loss[0]) and np.isnan(g[0])
+    assert not dz[0, 0].any() and not dz[1, 2].any() and np.isnan(dz[1, 0]).all() and np.isnan(dz[0, 2]).all()
+    alone = A.preference(z[:, [1, 3]], y[:, [1, 3]], kind=kind)
+    assert loss[1] == alone[0][0] and np.array_equal(dz[:, [1, 3]], alone[2])
+
+
 def test_adapter_gradient():
     rng = np.random.default_rng(3)
     M, K, N, R, n = 5, 4, 6, 2, 3
