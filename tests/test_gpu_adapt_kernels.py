@@ -1,12 +1,14 @@
 """The kernels that large calls of the operators that adapt a model take: the adapters' forward pass and gradients over wide windows and
-long chunks of rows, against 64-bit products.  (That these sizes take these kernels is tested without a GPU:
-test_adapt_kernels_cpu.py.)
+long chunks of rows, the preference loss's rows that meet in every shape, against 64-bit products and softmaxes.  (That these sizes
+take these kernels is tested without a GPU: test_adapt_kernels_cpu.py.)
 
-Tolerances: as in test_gpu_adapters.py, on the GPU."""
+Tolerances: as in test_gpu_adapters.py and test_gpu_policy.py, on the GPU."""
 import pytest
 import torch
 
 import test_gpu_adapters as adapters
+import test_gpu_policy as policy
+from oracle import adapt as A
 from paper_1502_00512_amd import binding
 
 pytestmark = pytest.mark.gpu
@@ -74,3 +76,83 @@ def test_adapters_over_wide_windows(dtype, M, N, n, R, kernel):
         want, size = b + f * (V @ U.T), f * (V.abs() @ U.abs().T)
         own = (f * (dv @ U.abs().T) + size * (2 * (2 * R + 4) * F32 + bf16 * 2.0 ** -17) + F32 * (b.abs() + size)) * 1.01
         near(out[rows], want, own + HALF[dtype] * (want.abs() + own) + 1e-38, ("out", a))
+
+
+# T, pairs, words of bf16 (half as many of fp32), and the shape of the kernel in which they meet (None: two passes)
+MEET = [
+    (64, 15, 8203, (256, 6)), (64, 8, 16383, (256, 8)), (64, 5, 24001, (512, 6)), (64, 4, 32001, (512, 8)), (40, 5, 40009, (512, 12)),
+    (64, 3, 64001, (512, 16)), (64, 2, 80003, (512, 20)), (50, 2, 100003, (512, 25)), (64, 1, 120007, (1024, 18)), (40, 1, 204807, (1024, 25)),
+    (1, 200, 64001, (512, 16)),
+    # next to them: rows of 1024 slots, texts of 65 positions, rows that no shape holds
+    (64, 15, 8199, None), (65, 3, 64001, None), (40, 1, 204811, None),
+]
+
+
+def words(dtype, V):
+    return V if dtype == "bf16" else V // 2
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,P,V,shape", MEET)
+@pytest.mark.parametrize("in_place", [False, True])
+def test_preference_rows_of_every_shape(T, P, V, shape, in_place, dtype):
+    V = words(dtype, V)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    z = torch.empty(T, 2 * P, V, dtype=DTYPES[dtype], device="cuda").normal_(0.0, 2.0, generator=gen)
+    y = torch.randint(0, V, (T, 2 * P), generator=gen, device="cuda", dtype=torch.int32)
+    y[torch.rand(T, 2 * P, generator=gen, device="cuda") < 0.2] = -1
+    y[0, 0] = -1
+    Z = z.double()
+    Z[0, 0] = 0.0
+    z[0, 0] = float("nan")
+    beta, eps, scale = 0.25, 0.125, 0.5
+    has, at = y >= 0, y.long().clamp(min=0)[..., None]
+    l = torch.log_softmax(Z, 2)
+    q = l.exp()
+    l = torch.where(has, l.gather(2, at)[..., 0], 0.0)
+    share = 1.0 / has.sum(0).clamp(min=1).double()
+    S = l.sum(0) * share
+    ref = (S + torch.randn(2 * P, generator=gen, device="cuda")).float()
+    r = S - ref.double()
+    r = r[:P] - r[P:]
+    soft = torch.nn.functional.softplus
+    L = (1 - eps) * soft(-beta * r) + eps * soft(beta * r)
+    f = beta * (torch.sigmoid(beta * r) - (1 - eps))
+    f = torch.cat([f, -f]) * share * scale
+    most = Z.abs().amax(2)
+    terms = 26 * 8 + 1
+    if shape is None:
+        terms = max(terms, V // 512 + 1)
+    E = torch.where(has, (terms * 1.1 + 24) * F32 + F32 * (4 * most + 2), 0.0)
+    dS = E.sum(0) * share + 1e-15 * S.abs()
+    dr = dS[:P] + dS[P:]
+    hit = torch.zeros_like(q).scatter_(2, at, 1.0)
+    want = torch.where(has[..., None], f[:, None] * (hit - q), 0.0)
+    of_value = (E + F32 * (4 * most + 8))[..., None]
+    F = f.abs()[:, None]
+    df = (share * scale * (beta * beta / 4) * torch.cat([dr, dr]) + F32 * f.abs())[:, None]
+    tol = F * (q * of_value + hit * 2 * F32) + df * (hit - q).abs() + HALF[dtype] * want.abs() * (1 + 2 * of_value) + F * 2.0 ** -100 + 2.0 ** -126
+    results = []
+    for polls in (256, 0):
+        try:
+            binding.rnnlm_set_preference_wait(polls)
+            rows = z.clone()
+            dz = rows if in_place else torch.full_like(z, 5.0)
+            loss, logp = binding.rnnlm_preference_loss(rows, y, ref, beta=beta, smoothing=eps, mean=True, scale=scale, dlogits=dz)
+            torch.cuda.synchronize()
+        finally:
+            binding.rnnlm_set_preference_wait(256)
+        results.append((loss, logp, dz))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    loss, logp, dz = results[0]
+    near(logp, S, dS + F32 * S.abs(), "logp")
+    near(loss, L, (beta + beta * beta / 4 * dr) * dr + F32 * L + 1e-14 * (1 + beta * r.abs()), "loss")
+    near(dz, want, tol, "dlogits")
+    assert not dz[~has].any()
+
+
+@pytest.mark.parametrize("dtype,T,P,V", [("bf16", 64, 3, 64001), ("fp32", 64, 1, 60003)])
+def test_preference_rows_that_meet_against_the_oracle(dtype, T, P, V):
+    d, z, y, rng = policy.draw_preference(T, P, V, dtype, 50)
+    ref = (A.preference(z, y)[1] + rng.normal(size=2 * P)).astype("float32")
+    policy.check_preference(d, z, y, ref, None, dtype, "logistic", 0.2, 0.1, in_place=True)
