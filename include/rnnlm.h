@@ -386,8 +386,9 @@ int rnnlm_set_preference_wait(int32_t polls);
  * Rows of one adapter may stand anywhere; an adapter is read once for every 32 of its rows or so.  A row without an adapter has
  * out = base and inner = 0.  Weights that are not finite spoil the rows of their own adapter only.
  * x: dev [rows][K], ld_x apart; base: dev [rows][N] or NULL (zeros); out: dev [rows][N]: may be base (same ld), else it overlaps
- * nothing; inner: dev float[rows][R], what the backward pass wants, or NULL; x, down, up, base and out are of dtype (bf16: sums
- * in fp32, inner not rounded, out rounded once).  down: dev [n][R][K], up: dev [n][N][R], scale: dev float[n] or NULL (1).
+ * nothing; inner: dev float[rows][R], what the backward pass wants, or NULL; x, down, up, base and out are of dtype.  Sums are in
+ * fp32, inner is written so, out is rounded once; in bf16 scale inner enters out, and dinner dx, as two bf16 numbers, which hold it to
+ * 2^-17 (in ddown and dup inner and dinner as three: 2^-26).  down: dev [n][R][K], up: dev [n][N][R], scale: dev float[n] or NULL (1).
  * rows <= 2^17, K <= 65536, N <= 2^20, n <= 65536, 1 <= R <= 64; workspace: 256-byte aligned, at least
  * rnnlm_adapter_workspace_bytes (backward: 0 or 1; 0 bytes: sizes out of range). */
 typedef struct {

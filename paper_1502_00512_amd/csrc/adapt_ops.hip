@@ -27,7 +27,9 @@ bool gradient_rows_ok(const void *logits, int64_t ld, const void *dlogits, int64
 }
 
 // Threads and slots of a thread that hold a row of `slots` whole slots: f(std::integral_constant...).  Many short rows: a wave
-// each, since a row's time is the latency of its steps, not its bytes.
+// each, since a row's time is the latency of its steps, not its bytes.  The shapes of 25 slots keep 36 to 100 bytes of a thread in
+// scratch.  512 threads of 25 and 1024 of 13, us: rows that meet, 2560 x 100000 bf16 214 and 242, x 50000 fp32 200 and 214, but the policy
+// loss, 8192 x 100000 bf16 657 and 623, 2560 x 50000 fp32 220 and 194.
 template <int THREADS, int NV>
 struct RowShape {
   static constexpr int threads = THREADS, nv = NV;
@@ -149,10 +151,12 @@ int preference_call(const PreferenceArgs<T> &a, hipStream_t st) {
 constexpr int64_t ADAPTER_ROWS_MAX = 1 << 17;  // (putting the rows in order compares each with each)
 
 int adapter_r_tiles(int32_t R) { return (R + 15) / 16; }
-// Columns of a wave of adapter_grad_kernel, in 16s: as many as its accumulators and operands leave registers for.
-// small: half of them where that lets two workgroups share a compute unit (R <= 16), for gradients of up to 128 MB: they and the
-// others, us: 160 x 2000 bf16 (R = 16) 27.7 and 31.2, 900 x 33278 fp32 (R = 5) 75 and 80; but 2560 x 64000 bf16 (R = 16, 1 and
-// 128 adapters) 111 and 106, 294 and 271, fp32 209 and 203 (twice the parts of dinner).
+// Columns of a wave of adapter_grad_kernel, in 16s.  Four, even where some registers go to scratch (bf16 of R > 48: 196 bytes of a
+// thread, fp32 of 16 < R <= 32: 116), since half the columns are twice the parts of dinner: four and two, us, 2560 x 64000, 16 adapters:
+// bf16 R = 64 331 and 468, fp32 R = 32 356 and 396 (900 x 33278: 135 and 140, 135 and 135).
+// small: half of what R <= 16 has otherwise, where that lets two workgroups share a compute unit, for gradients of up to 128 MB: they
+// and the others, us: 160 x 2000 bf16 (R = 16) 29 and 32, 900 x 33278 fp32 (R = 5) 75 and 78 (but bf16, R = 16 60 and 57); 2560 x
+// 64000 bf16 (R = 16, 1 and 128 adapters) 113 and 105, 301 and 271, fp32 (1 and 16 adapters) 196 and 194, 218 and 216.
 constexpr int adapter_grad_tiles(int r_tiles, bool bf16, bool small) {
   return r_tiles == 1 ? (bf16 ? 8 : 4) / (small ? 2 : 1) : bf16 || r_tiles == 2 ? 4 : 2;
 }
@@ -260,17 +264,16 @@ void launch_inner(const InnerArgs<T> &a, hipStream_t st) {
 }
 template <typename T, int NF, bool PACKED>
 void launch_outer_as(OuterArgs<T> a, hipStream_t st) {
-  // Columns of a wave: what registers hold of up.  2560 rows of 64000, R = 64: fp32 574 us with 32 columns and 868 with 64 (which
-  // spill), bf16 283 and 267.
+  // Columns of a wave, 32 and 64, us, 2560 rows of 64000, 8 adapters: R = 64 fp32 492 and 723 (64 spill), bf16 270 and 218, R = 40
+  // 262 and 211; fp32 of 16 < R <= 48 would do better with 64 (R = 32 385 and 324, R = 48 437 and 359).
   constexpr int VT = NF == 1 || sizeof(T) == 2 ? 4 : 2;
   const int64_t cols = (a.N + 64 * VT - 1) / (64 * VT);
   // a wave takes the adapters of its tile one after the other: smaller tiles until there is a workgroup for every compute unit
   const auto tiles = [&]() { return (a.rows.M + a.tile - 1) / a.tile; };
   a.tile = ADAPTER_TILE;
   while (a.tile > 4 && tiles() * cols < 256) a.tile /= 2;
-  // and walks over its columns with the next ones requested ahead: one round of as many workgroups as the GPU holds (2560 rows of
-  // 64000 bf16, R = 16: 164 us, 173 with a second round begun and 183 with 1024 workgroups; R = 64 221, fp32 305, and 273 and 342
-  // with 768)
+  // and walks over its columns with the next ones requested ahead: one round of as many workgroups as the GPU holds (512, 768 and
+  // 1024 of them, us, 2560 rows of 64000: bf16 R = 16 165, 163, 183, R = 64 217, 265, 232, fp32 R = 16 298, 336, 305)
   constexpr int64_t WGS = NF == 1 && sizeof(T) == 2 ? 768 : 512;
   const int64_t side = std::max<int64_t>(1, std::min(cols, WGS / tiles()));
   a.blocks = (int)((cols + side - 1) / side);

@@ -306,9 +306,11 @@ struct OuterArgs {
 };
 
 // out = base + f up inner: a wave a tile and 16 VT columns, `blocks` times; through LDS so that base and out move in whole lines.
-// Bound by HBM: 2560 x 64000 bf16, R = 16, 8 adapters 140 us (676 MB, 4.8 TB/s; up is read again by every XCD, out of the
-// memory-side cache: workgroups dealt so that each XCD has its own columns took as long), 128 rows of as many adapters 50 where
-// up stays in that cache, 62 where it does not (295 MB, 4.8 TB/s).
+// Bound by HBM: 2560 x 64000 bf16, R = 16, 8 adapters 140 us (676 MB, 4.8 TB/s; workgroups dealt so that each XCD has its own
+// columns took as long), 128 rows of as many adapters 50 where up stays in the memory-side cache, 62 where it does not (295 MB, 4.8
+// TB/s), fp32 113 (576 MB, 5.1 TB/s).  Every tile reads all of its adapter's up again, mostly out of the memory-side cache, which
+// bounds high ranks: of the 8 adapters above R = 64 (2560 rows) bf16 fetches 841 MB in place of 394, 202 us, fp32 1704 MB in place
+// of 786, 478 us.
 // NF: operand slots of R.  PACKED (bf16, R <= 16): both parts of inner in one product, beside one another.
 template <typename T, int NF, bool PACKED, int VT>
 __global__ void __launch_bounds__(256, 2) adapter_outer_kernel(const OuterArgs<T> a) {
@@ -484,7 +486,7 @@ __device__ inline slot_t across(const T *tile, int pitch, int k0, int c0) {
                   __builtin_bit_cast(unsigned, p[3 * pitch])};
   }
 }
-// Of two parts (0, 1) of a number packed for bf16 operands, or the number itself.
+// VEC numbers as an operand: of bf16 PARTS operands, the numbers' first parts, second ones, ...; of fp32 the numbers themselves.
 template <typename T, int PARTS>
 __device__ inline void operand_parts(const float (&v)[Mma<T>::VEC], slot_t (&s)[PARTS]) {
   union {

@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(THREADS) preference_stream_kernel(const Prefer
 // its own flag) and waits for those of its pair, which were started next to it.  A wait ends after `polls` polls, too (the rest
 // of a pair may not be on the GPU yet, where other work fills it): such a row leaves its sum to preference_rest_kernel, which
 // writes the same gradient.
-// 2560 x 64000 bf16 (64 pairs of 20 positions) 134-138 us where a row by itself (policy_row_kernel) takes 114: a pair's rows write
+// 2560 x 64000 bf16 (64 pairs of 20 positions) 138-141 us where a row by itself (policy_row_kernel) takes 115: a pair's rows write
 // only when the last of them has been read.  Two passes: 188.
 constexpr int PREFERENCE_MEET = 64;  // most positions of a text: the pair's rows are at most half of what the GPU holds
 

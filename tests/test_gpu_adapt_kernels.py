@@ -14,7 +14,7 @@ from paper_1502_00512_amd import binding
 pytestmark = pytest.mark.gpu
 
 DTYPES, HALF, F32 = adapters.DTYPES, adapters.HALF, adapters.F32
-POWER = {"fp32": 0.0, "bf16": 1.0}
+IN_PARTS = {"fp32": 0.0, "bf16": 1.0}  # operands in fp32 go in as bf16 numbers
 
 # dtype, rows, N, n, R, and the kernel that forms dup (columns of a wave / 16, rank / 16).  Up to 2^27 bytes of dout the ranks up to
 # 16 have columns of their own.
@@ -50,7 +50,7 @@ def test_adapters_over_wide_windows(dtype, M, N, n, R, kernel):
     ddown, dup, dx = torch.full((n, R, K), 7.0, device="cuda"), torch.full((n, N, R), 7.0, device="cuda"), torch.full_like(x, 7.0)
     binding.rnnlm_adapter_backward(dout, x, inner, down, up, ids, scale, ddown=ddown, dup=dup, dx=dx)
     out, u = binding.rnnlm_adapter_forward(x, down, up, ids, scale, base=base)
-    bf16 = POWER[dtype]
+    bf16 = IN_PARTS[dtype]
     chain = 140 + 8 + N // 512 + 1  # of dinner: a wave's columns, the waves, the blocks
     for a in range(-1, n):
         rows = (ids == a).nonzero()[:, 0]
