@@ -78,6 +78,32 @@ def test_adapters_over_wide_windows(dtype, M, N, n, R, kernel):
         near(out[rows], want, own + HALF[dtype] * (want.abs() + own) + 1e-38, ("out", a))
 
 
+@pytest.mark.parametrize("dtype,M,N,R", [("bf16", 2017, 33279, 16), ("fp32", 1009, 33279, 16), ("bf16", 2017, 33279, 48), ("fp32", 1009, 33279, 32)])
+def test_infinities_in_the_last_columns_of_wide_windows(dtype, M, N, R):
+    """One infinite element of dout an adapter, in columns that the last wave and the one in front have in common (N = 33279: 1 to 127
+    of them).  (up and down are positive, x is not zero.)"""
+    K, n, dt = 40, 6, DTYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(R)
+    normal = lambda *s, t=dt: torch.empty(*s, dtype=t, device="cuda").normal_(generator=gen)  # noqa: E731
+    x, down, up, inner, dout = normal(M, K), normal(n, R, K).abs_(), normal(n, N, R).abs_(), normal(M, R, t=torch.float32), normal(M, N)
+    x[x == 0], down[down == 0], up[up == 0] = 1.0, 1.0, 1.0
+    ids = torch.arange(M, device="cuda", dtype=torch.int32) % n
+    columns = [N - 1, N - 2, N - 31, N - 33, N - 60, N - 127]
+    for a, v in enumerate(columns):
+        dout[600 + a, v] = float("inf") if a % 2 else -float("inf")  # (600 % n = 0)
+    dx = torch.empty_like(x)
+    ddown, dup = binding.rnnlm_adapter_backward(dout, x, inner, down, up, ids, dx=dx)
+    for a, v in enumerate(columns):
+        d = dout[600 + a, v].float()
+        assert bool((ddown[a] == d * x[600 + a].float()).all()) and bool((dx[600 + a].float() == d).all()), (a, v)
+    spoilt = torch.zeros(n, N, dtype=torch.bool, device="cuda")
+    spoilt[torch.arange(n, device="cuda"), torch.tensor(columns, device="cuda")] = True
+    assert torch.equal(~dup.isfinite(), spoilt[..., None].expand(n, N, R))
+    others = torch.ones(M, dtype=torch.bool, device="cuda")
+    others[600: 600 + n] = False
+    assert bool(dx[others].isfinite().all())
+
+
 # T, pairs, words of bf16 (half as many of fp32), and the shape of the kernel in which they meet (None: two passes)
 MEET = [
     (64, 15, 8203, (256, 6)), (64, 8, 16383, (256, 8)), (64, 5, 24001, (512, 6)), (64, 4, 32001, (512, 8)), (40, 5, 40009, (512, 12)),

@@ -235,7 +235,7 @@ def test_weights_that_are_not_finite_stay_with_their_adapter(bad, dtype):
 
 
 @BOTH
-@pytest.mark.parametrize("N", [20, 200, 1100])
+@pytest.mark.parametrize("N", [20, 50, 100, 200, 1100])
 @pytest.mark.parametrize("R", [6, 20, 60])
 def test_infinities_of_dout_are_those_of_the_formula(N, R, dtype):
     """An adapter a row, one element of each row infinite: in the first columns, in the last ones, and where the last blocks of
